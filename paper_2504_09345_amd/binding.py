@@ -1,4 +1,5 @@
-"""ctypes binding of libpagedattn.so, the C ABI declared in include/pagedattn.h.
+"""ctypes binding of libpagedattn.so, the C ABI declared in include/pagedattn.h
+and, for the cache held in 4 bits, include/pagedattn_q4.h.
 
 Argument marshalling only: every step of the attention runs in the library's
 HIP kernels.  Device buffers are passed as torch tensors (torch provides
@@ -23,7 +24,9 @@ PAGE_SIZE = 16
 EXPORTED = ("pa_workspace_size", "paged_attn", "paged_attn_varlen", "paged_attn_varlen_noalloc",
             "pa_gather_trace",
             "pa_kv_append", "pa_schedule_step", "pa_perf_model", "pa_read_probe", "pa_issue_probe",
-            "pa_strerror")
+            "pa_strerror",
+            "pa_q4_tile_bytes", "pa_kv_append_q4", "pa_kv_read_q4", "pa_workspace_size_q4", "paged_attn_q4",
+            "paged_attn_varlen_q4")
 
 
 class PaDims(ctypes.Structure):
@@ -124,6 +127,15 @@ def load():
     lib.pa_issue_probe.restype = ctypes.c_int
     lib.pa_strerror.argtypes = [ctypes.c_int]
     lib.pa_strerror.restype = ctypes.c_char_p
+    lib.pa_q4_tile_bytes.argtypes = [ctypes.c_int32, ctypes.POINTER(SZ)]
+    lib.pa_kv_append_q4.argtypes = [P, P, P, P, P, P, P, DP, P]
+    lib.pa_kv_read_q4.argtypes = [P, P, P, P, P, P, P, DP, P]
+    lib.pa_workspace_size_q4.argtypes = [DP, ctypes.POINTER(SZ)]
+    lib.paged_attn_q4.argtypes = [P, P, P, P, P, ctypes.c_float, P, DP, P, SZ, P, TP]
+    lib.paged_attn_varlen_q4.argtypes = [P, P, P, P, P, P, ctypes.c_float, P, DP, P, SZ, P, TP]
+    for name in ("pa_q4_tile_bytes", "pa_kv_append_q4", "pa_kv_read_q4", "pa_workspace_size_q4", "paged_attn_q4",
+                 "paged_attn_varlen_q4"):
+        getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -180,13 +192,13 @@ def pa_strerror(code: int) -> str:
     return load().pa_strerror(int(code)).decode()
 
 
-def _workspace(dims, workspace, device, stream=None):
+def _workspace(dims, workspace, device, stream=None, size_of=pa_workspace_size):
     """The caller's workspace, or a temporary one of pa_workspace_size()
-    bytes.  A temporary is allocated on torch's current stream; when the call
+    bytes (size_of: of another call's size).  A temporary is allocated on torch's current stream; when the call
     runs on another stream, the allocation is also recorded on that stream, so
     torch's caching allocator does not hand the memory to other work before
     the call's kernels have finished with it."""
-    need = pa_workspace_size(dims)
+    need = size_of(dims)
     if workspace is None and need > 0:
         import torch
         if isinstance(stream, int) and stream:
@@ -265,6 +277,107 @@ def pa_kv_append(k_new, v_new, block_table, context_lens, k_pages, v_pages, dims
                              ctypes.byref(dims), _stream(stream))
     if check and rc != PA_OK:
         raise PagedAttnError("pa_kv_append", rc)
+    return rc
+
+
+def pa_q4_tile_bytes(head_dim) -> int:
+    """Bytes of a (page, KV head) tile of the 4-bit cache; a pool is uint8
+    [num_pages][num_kv_heads][pa_q4_tile_bytes(head_dim)]."""
+    n = ctypes.c_size_t(0)
+    rc = load().pa_q4_tile_bytes(int(head_dim), ctypes.byref(n))
+    if rc != PA_OK:
+        raise PagedAttnError("pa_q4_tile_bytes", rc)
+    return int(n.value)
+
+
+def make_dims_q4(rows, k_pages, block_table, max_context_len, num_q_rows=0, max_q_len=0, num_seqs=None) -> PaDims:
+    """pa_dims_t of a call on the 4-bit cache from tensor shapes: rows
+    [rows][H][D] (q, or k_new / k_out of the append and the read), k_pages uint8
+    [N][H_kv][tile], block_table [B][max_pages_per_seq]."""
+    _, H, D = rows.shape
+    N, H_kv, tile = k_pages.shape
+    if tile != pa_q4_tile_bytes(D):
+        raise ValueError(f"k_pages holds tiles of {tile} bytes, head_dim {D} takes {pa_q4_tile_bytes(D)}")
+    B = block_table.shape[0] if num_seqs is None else num_seqs
+    return PaDims(num_seqs=B, num_q_heads=H, num_kv_heads=H_kv, head_dim=D, page_size=PAGE_SIZE, num_pages=N,
+                  max_pages_per_seq=block_table.shape[1], max_context_len=int(max_context_len), pages_per_split=0,
+                  dtype=_dtype_code(rows), num_q_rows=int(num_q_rows), max_q_len=int(max_q_len))
+
+
+def pa_workspace_size_q4(dims: PaDims) -> int:
+    n = ctypes.c_size_t(0)
+    rc = load().pa_workspace_size_q4(ctypes.byref(dims), ctypes.byref(n))
+    if rc != PA_OK:
+        raise PagedAttnError("pa_workspace_size_q4", rc)
+    return int(n.value)
+
+
+def _check_q4(dims, dense, pools, ints):
+    """What the 4-bit entries are given where it is a tensor: contiguous, on
+    the current device, of the type that dims and the format say."""
+    import torch
+    dense_type = torch.bfloat16 if dims.dtype == PA_BF16 else torch.float32
+    for kind, tensors in ((dense_type, dense), (torch.uint8, pools), (torch.int32, ints)):
+        for t in tensors:
+            if t is None or isinstance(t, int):
+                continue
+            if t.dtype != kind:
+                raise TypeError(f"{t.dtype} where {kind} is needed")
+            if not t.is_contiguous():
+                raise ValueError("tensors must be contiguous")
+            if not t.is_cuda or t.device.index != torch.cuda.current_device():
+                raise ValueError(f"a tensor on {t.device}, not on the current device")
+
+
+def pa_kv_append_q4(k_new, v_new, block_table, context_lens, k_pages, v_pages, dims: PaDims, query_start_loc=None,
+                    stream=None, check=True) -> int:
+    """int pa_kv_append_q4(...): quantise the new tokens' K/V into the 4-bit pools."""
+    _check_q4(dims, (k_new, v_new), (k_pages, v_pages), (block_table, context_lens, query_start_loc))
+    rc = load().pa_kv_append_q4(_addr(k_new), _addr(v_new), _addr(block_table), _addr(context_lens),
+                                _addr(query_start_loc), _addr(k_pages), _addr(v_pages), ctypes.byref(dims),
+                                _stream(stream))
+    if check and rc != PA_OK:
+        raise PagedAttnError("pa_kv_append_q4", rc)
+    return rc
+
+
+def pa_kv_read_q4(k_pages, v_pages, block_table, context_lens, k_out, v_out, dims: PaDims, query_start_loc=None,
+                  stream=None, check=True) -> int:
+    """int pa_kv_read_q4(...): the values that the 4-bit pools hold of the rows
+    which pa_kv_append_q4 with the same arguments writes."""
+    _check_q4(dims, (k_out, v_out), (k_pages, v_pages), (block_table, context_lens, query_start_loc))
+    rc = load().pa_kv_read_q4(_addr(k_pages), _addr(v_pages), _addr(block_table), _addr(context_lens),
+                              _addr(query_start_loc), _addr(k_out), _addr(v_out), ctypes.byref(dims), _stream(stream))
+    if check and rc != PA_OK:
+        raise PagedAttnError("pa_kv_read_q4", rc)
+    return rc
+
+
+def paged_attn_q4(q, k_pages, v_pages, block_table, context_lens, scale, out, dims: PaDims, workspace=None,
+                  stream=None, timing: PaTiming | None = None, check=True) -> int:
+    """int paged_attn_q4(...): decode attention over the 4-bit cache; out is
+    written in place."""
+    _check_q4(dims, (q, out), (k_pages, v_pages), (block_table, context_lens))
+    ws, ws_bytes = _workspace(dims, workspace, getattr(q, "device", None), stream, pa_workspace_size_q4)
+    rc = load().paged_attn_q4(_addr(q), _addr(k_pages), _addr(v_pages), _addr(block_table), _addr(context_lens),
+                              float(scale), _addr(out), ctypes.byref(dims), _addr(ws), ws_bytes, _stream(stream),
+                              ctypes.byref(timing) if timing is not None else None)
+    if check and rc != PA_OK:
+        raise PagedAttnError("paged_attn_q4", rc)
+    return rc
+
+
+def paged_attn_varlen_q4(q, k_pages, v_pages, block_table, context_lens, query_start_loc, scale, out, dims: PaDims,
+                         workspace=None, stream=None, timing: PaTiming | None = None, check=True) -> int:
+    """int paged_attn_varlen_q4(...): causal chunks plus decode rows over the
+    4-bit cache."""
+    _check_q4(dims, (q, out), (k_pages, v_pages), (block_table, context_lens, query_start_loc))
+    ws, ws_bytes = _workspace(dims, workspace, getattr(q, "device", None), stream, pa_workspace_size_q4)
+    rc = load().paged_attn_varlen_q4(_addr(q), _addr(k_pages), _addr(v_pages), _addr(block_table), _addr(context_lens),
+                                     _addr(query_start_loc), float(scale), _addr(out), ctypes.byref(dims), _addr(ws),
+                                     ws_bytes, _stream(stream), ctypes.byref(timing) if timing is not None else None)
+    if check and rc != PA_OK:
+        raise PagedAttnError("paged_attn_varlen_q4", rc)
     return rc
 
 

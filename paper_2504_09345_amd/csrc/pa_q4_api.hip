@@ -1,0 +1,205 @@
+// C ABI of the 4-bit cache (pagedattn_q4.h): host-side validation, planning and
+// dispatch.  Validation runs before any HIP call; nothing is kept between calls.
+#include <math.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "pa_q4.h"
+#include "pagedattn_q4.h"
+
+namespace {
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// The cache's part of dims.
+int check_cache(const pa_dims_t* d) {
+  if (d == nullptr) return PA_EINVAL;
+  if (d->num_seqs < 0 || d->num_kv_heads <= 0 || d->num_pages < 0 || d->max_pages_per_seq < 0 || d->max_context_len < 0 ||
+      d->pages_per_split != 0)
+    return PA_EINVAL;
+  if (d->dtype != PA_BF16 && d->dtype != PA_FP32) return PA_ENOTSUP;
+  if (d->head_dim != 64 && d->head_dim != 128) return PA_ENOTSUP;
+  if (d->page_size != 16) return PA_ENOTSUP;
+  if (((int64_t)d->max_context_len + 15) / 16 > d->max_pages_per_seq) return PA_EINVAL;
+  return PA_OK;
+}
+
+bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
+
+int rows_call(const void* k_rows, const void* v_rows, const int32_t* block_table, const int32_t* context_lens,
+              const int32_t* query_start_loc, void* k_pages, void* v_pages, const pa_dims_t* d, hipStream_t stream,
+              hipError_t (*launch)(int, int, const pa::Q4RowsArgs&, hipStream_t)) {
+  const int rc = check_cache(d);
+  if (rc != PA_OK) return rc;
+  int rows;
+  if (query_start_loc != nullptr) {
+    if (d->num_q_rows < 0 || (d->num_q_rows > 0 && d->num_seqs == 0)) return PA_EINVAL;
+    rows = d->num_q_rows;
+  } else {
+    if (d->num_q_rows != 0 && d->num_q_rows != d->num_seqs) return PA_EINVAL;
+    rows = d->num_seqs;
+  }
+  if (rows == 0) return PA_OK;
+  if (!k_rows || !v_rows || !block_table || !context_lens || !k_pages || !v_pages) return PA_EINVAL;
+  if (misaligned(k_rows) || misaligned(v_rows) || misaligned(k_pages) || misaligned(v_pages)) return PA_EINVAL;
+  pa::Q4RowsArgs a;
+  a.k_rows = k_rows;
+  a.v_rows = v_rows;
+  a.k_pages = static_cast<uint8_t*>(k_pages);
+  a.v_pages = static_cast<uint8_t*>(v_pages);
+  a.block_table = block_table;
+  a.context_lens = context_lens;
+  a.query_start_loc = query_start_loc;
+  a.bt_stride = d->max_pages_per_seq;
+  a.B = d->num_seqs;
+  a.rows = rows;
+  a.H_kv = d->num_kv_heads;
+  a.num_pages = d->num_pages;
+  a.max_context_len = d->max_context_len;
+  return launch(d->dtype, d->head_dim, a, stream) == hipSuccess ? PA_OK : PA_EHIP;
+}
+
+struct Plan {
+  int s = 0, rows = 0, blocks = 1, n_slots = 0, n_split = 1, split_units = 1;
+  size_t ws_o = 0, ws_ml = 0;
+};
+
+// Parts that a call's items are cut into: as many as give the GPU (256 CUs of 8
+// waves) a wave of work each, of at least kLeastUnits units, at most 64.
+constexpr int kWavesWanted = 2048, kLeastUnits = 4, kMaxSplit = 64;
+
+int plan(const pa_dims_t* d, bool varlen, Plan* p) {
+  const int rc = check_cache(d);
+  if (rc != PA_OK) return rc;
+  if (d->num_q_heads <= 0 || d->num_q_heads % d->num_kv_heads != 0) return PA_EINVAL;
+  const int s = p->s = d->num_q_heads / d->num_kv_heads;
+  if (s != 1 && s != 2 && s != 4 && s != 6 && s != 8) return PA_ENOTSUP;
+  if (varlen) {
+    if (d->num_q_rows < 0 || d->max_q_len < 0) return PA_EINVAL;
+    if (d->num_q_rows > 0 && (d->max_q_len < 1 || d->num_seqs == 0 || d->max_q_len > d->max_context_len)) return PA_EINVAL;
+    p->rows = d->num_q_rows;
+    p->blocks = d->max_q_len * (int64_t)s <= 16 ? 1 : d->max_q_len * (int64_t)s <= 32 ? 2 : 4;
+    p->n_slots = p->rows / pa::q4_positions(p->blocks, s) + d->num_seqs;
+  } else {
+    if ((d->num_q_rows != 0 && d->num_q_rows != d->num_seqs) || d->max_q_len < 0 || d->max_q_len > 1) return PA_EINVAL;
+    p->rows = p->n_slots = d->num_seqs;
+  }
+  if (p->rows == 0) return PA_OK;
+  const int64_t items = (int64_t)p->n_slots * d->num_kv_heads;
+  const int64_t units = ((int64_t)d->max_context_len + pa::kQ4Unit - 1) / pa::kQ4Unit;
+  int64_t split = kWavesWanted / items;
+  if (split > units / kLeastUnits) split = units / kLeastUnits;
+  if (split > kMaxSplit) split = kMaxSplit;
+  if (split < 1) split = 1;
+  p->split_units = (int)((units + split - 1) / split);
+  if (p->split_units < 1) p->split_units = 1;
+  p->n_split = (int)((units + p->split_units - 1) / p->split_units);
+  if (p->n_split < 1) p->n_split = 1;
+  if ((items + 4 * d->num_kv_heads) * p->n_split > INT32_MAX || (int64_t)p->rows * d->num_q_heads > INT32_MAX) return PA_ENOTSUP;
+  if (p->n_split > 1) {
+    const size_t recs = (size_t)p->rows * d->num_q_heads * p->n_split;
+    p->ws_o = align256(recs * d->head_dim * sizeof(float));
+    p->ws_ml = align256(recs * 2 * sizeof(float));
+  }
+  return PA_OK;
+}
+
+int attend(const void* q, const void* k_pages, const void* v_pages, const int32_t* block_table, const int32_t* context_lens,
+           const int32_t* query_start_loc, float scale, void* out, const pa_dims_t* d, void* workspace, size_t workspace_bytes,
+           hipStream_t stream, const pa_timing_t* timing, bool varlen) {
+  Plan p;
+  const int rc = plan(d, varlen, &p);
+  if (rc != PA_OK) return rc;
+  if (!isfinite(scale) || !(scale > 0.0f)) return PA_EINVAL;
+  if (p.rows > 0) {
+    if (!q || !k_pages || !v_pages || !block_table || !context_lens || !out || (varlen && !query_start_loc)) return PA_EINVAL;
+    if (misaligned(q) || misaligned(k_pages) || misaligned(v_pages) || misaligned(out) || misaligned(workspace)) return PA_EINVAL;
+    if (p.ws_o > 0 && (workspace == nullptr || workspace_bytes < p.ws_o + p.ws_ml)) return PA_ENOSPC;
+  }
+  const hipEvent_t begin = timing ? timing->attn_begin : nullptr, end = timing ? timing->attn_end : nullptr;
+  const hipEvent_t joined = timing ? timing->reduce_end : nullptr;
+  if (p.rows == 0) {
+    for (hipEvent_t ev : {begin, end, joined})
+      if (ev != nullptr) (void)hipEventRecord(ev, stream);
+    return PA_OK;
+  }
+  pa::Q4AttnArgs a{};
+  a.q = q;
+  a.k_pages = static_cast<const uint8_t*>(k_pages);
+  a.v_pages = static_cast<const uint8_t*>(v_pages);
+  a.block_table = block_table;
+  a.context_lens = context_lens;
+  a.query_start_loc = varlen ? query_start_loc : nullptr;
+  a.out = out;
+  a.ws_o = static_cast<float*>(workspace);
+  a.ws_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.ws_o);
+  a.bt_stride = d->max_pages_per_seq;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.B = d->num_seqs;
+  a.s = p.s;
+  a.H_q = d->num_q_heads;
+  a.H_kv = d->num_kv_heads;
+  a.rows = p.rows;
+  a.num_pages = d->num_pages;
+  a.max_context_len = d->max_context_len;
+  a.n_slots = p.n_slots;
+  a.n_split = p.n_split;
+  a.split_units = p.split_units;
+  pa::KernelEvents ev;
+  ev.start = begin;
+  ev.stop = end;
+  if (pa::launch_q4_attn(d->dtype, d->head_dim, p.blocks, a, stream, ev) != hipSuccess) return PA_EHIP;
+  if (p.n_split > 1 && pa::launch_q4_merge(d->dtype, d->head_dim, a, stream) != hipSuccess) return PA_EHIP;
+  if (joined != nullptr) (void)hipEventRecord(joined, stream);
+  return PA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pa_q4_tile_bytes(int32_t head_dim, size_t* bytes) {
+  if (bytes == nullptr) return PA_EINVAL;
+  if (head_dim != 64 && head_dim != 128) return PA_ENOTSUP;
+  *bytes = (size_t)pa::q4_tile_bytes(head_dim);
+  return PA_OK;
+}
+
+int pa_kv_append_q4(const void* k_new, const void* v_new, const int32_t* block_table, const int32_t* context_lens,
+                    const int32_t* query_start_loc, void* k_pages, void* v_pages, const pa_dims_t* dims, hipStream_t stream) {
+  return rows_call(k_new, v_new, block_table, context_lens, query_start_loc, k_pages, v_pages, dims, stream,
+                   pa::launch_q4_append);
+}
+
+int pa_kv_read_q4(const void* k_pages, const void* v_pages, const int32_t* block_table, const int32_t* context_lens,
+                  const int32_t* query_start_loc, void* k_out, void* v_out, const pa_dims_t* dims, hipStream_t stream) {
+  return rows_call(k_out, v_out, block_table, context_lens, query_start_loc, const_cast<void*>(k_pages),
+                   const_cast<void*>(v_pages), dims, stream, pa::launch_q4_read);
+}
+
+int pa_workspace_size_q4(const pa_dims_t* dims, size_t* bytes) {
+  if (bytes == nullptr) return PA_EINVAL;
+  Plan p;
+  const bool varlen = dims != nullptr && (dims->max_q_len > 1 || (dims->num_q_rows != 0 && dims->num_q_rows != dims->num_seqs));
+  const int rc = plan(dims, varlen, &p);
+  if (rc != PA_OK) return rc;
+  *bytes = p.ws_o + p.ws_ml;
+  return PA_OK;
+}
+
+int paged_attn_q4(const void* q, const void* k_pages, const void* v_pages, const int32_t* block_table,
+                  const int32_t* context_lens, float scale, void* out, const pa_dims_t* dims, void* workspace,
+                  size_t workspace_bytes, hipStream_t stream, const pa_timing_t* timing) {
+  return attend(q, k_pages, v_pages, block_table, context_lens, nullptr, scale, out, dims, workspace, workspace_bytes, stream,
+                timing, false);
+}
+
+int paged_attn_varlen_q4(const void* q, const void* k_pages, const void* v_pages, const int32_t* block_table,
+                         const int32_t* context_lens, const int32_t* query_start_loc, float scale, void* out,
+                         const pa_dims_t* dims, void* workspace, size_t workspace_bytes, hipStream_t stream,
+                         const pa_timing_t* timing) {
+  return attend(q, k_pages, v_pages, block_table, context_lens, query_start_loc, scale, out, dims, workspace, workspace_bytes,
+                stream, timing, true);
+}
+
+}  // extern "C"

@@ -1,0 +1,199 @@
+// The 4-bit cache's attention kernel and its picker (design in pa_q4_attn.hip).
+// Each (element type, head dim) is instantiated in one translation unit.
+#pragma once
+
+#include "pa_q4_tile.h"
+
+namespace pa {
+
+constexpr int kQ4Waves = 4;  // waves of a workgroup, each with an item of its own
+
+// An item's sequence and rows.
+struct Q4Item {
+  int b, row0, n_pos;  // sequence, first query row, query rows (0: none)
+  int last0;           // last key of the first row
+  bool bad;            // rows are NaN
+};
+
+// Row block `slot` of the call: in a varlen call the blocks of sequence b are the
+// slots from query_start_loc[b] / positions + b on, which no two sequences share.
+__device__ __forceinline__ Q4Item q4_item(const Q4AttnArgs& a, int slot, int positions, int lane) {
+  Q4Item it{slot, slot, 0, 0, false};
+  int L = 1, first = 0;
+  if (a.query_start_loc != nullptr) {
+    const int32_t* qsl = a.query_start_loc;
+    it.b = q4::wave_search(a.B, slot, lane, [&](int b) { return qsl[b] / positions + b; });
+    const int q0 = qsl[it.b];
+    L = qsl[it.b + 1] - q0;
+    first = (slot - (q0 / positions + it.b)) * positions;
+    it.row0 = q0 + first;
+    if (q0 < 0 || first < 0 || it.row0 >= a.rows) return it;
+    it.n_pos = max(0, min(positions, min(L - first, a.rows - it.row0)));
+  } else {
+    it.n_pos = 1;
+  }
+  const int C = a.context_lens[it.b];
+  it.last0 = C - L + first;
+  it.bad = C < 0 || C > a.max_context_len || (C + kPage - 1) / kPage > a.bt_stride || (a.query_start_loc != nullptr && L > C);
+  return it;
+}
+
+template <typename T, int D, int NB>
+__global__ __launch_bounds__(64 * kQ4Waves) void q4_attn_kernel(Q4AttnArgs a) {
+  const int S = a.s;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int slot, split, g;
+  if (a.query_start_loc == nullptr) {  // heads of a page side by side
+    const int f = blockIdx.x * kQ4Waves + wave;
+    g = f % a.H_kv;
+    split = f / a.H_kv % a.n_split;
+    slot = f / a.H_kv / a.n_split;
+  } else {  // row blocks of one head side by side
+    split = blockIdx.x % a.n_split;
+    g = blockIdx.x / a.n_split % a.H_kv;
+    slot = blockIdx.x / a.n_split / a.H_kv * kQ4Waves + wave;
+  }
+  if (slot >= a.n_slots) return;
+  const Q4Item it = q4_item(a, slot, q4_positions(NB, S), lane);
+  if (it.n_pos == 0) return;
+
+  const int n = lane & 15, G = lane >> 4;
+  T* out = reinterpret_cast<T*>(a.out);
+  const int all_last = it.last0 + it.n_pos - 1;
+  if (it.bad || all_last < 0) {  // (a decode row of an empty context: zeros)
+    if (split != 0) return;
+    const float fill = it.bad ? NAN : 0.0f;
+    for (int i = lane; i < it.n_pos * S * D; i += 64)
+      store_out<T>(out + ((int64_t)(it.row0 + i / (S * D)) * a.H_q + (int64_t)g * S) * D + i % (S * D), fill);
+    return;
+  }
+  const int n_units = all_last / kQ4Unit + 1;
+  const int u0 = split * a.split_units, u1 = min(n_units, u0 + a.split_units);
+  if (u0 >= u1) return;
+
+  q4::State<T, D, NB> st;
+  int64_t at[NB];  // of the column's (row, head) vector, among all
+#pragma unroll
+  for (int c = 0; c < NB; ++c) {
+    const int col = 16 * c + n, pos = col / S;
+    const bool there = pos < it.n_pos;  // (columns past the item's positions are none)
+    st.last[c] = there ? it.last0 + pos : -1;
+    at[c] = (int64_t)(it.row0 + (there ? pos : 0)) * a.H_q + (int64_t)g * S + col % S;
+    q4::load_query<T, D>(st.q[c], there ? reinterpret_cast<const T*>(a.q) + at[c] * D : nullptr, lane);
+  }
+  q4::reset(st);
+
+  const int n_pages = all_last / kPage + 1;
+  const int64_t tile = q4_tile_bytes(D), page_bytes = tile * a.H_kv;
+  const uint8_t* kg = a.k_pages + g * tile;
+  const uint8_t* vg = a.v_pages + g * tile;
+  const int32_t* table = a.block_table + (int64_t)it.b * a.bt_stride;
+  // lane i: entry of page 64 (u / 32) + i
+  int ids = 0;
+  auto fetch = [&](q4::Unit<D>& u, int at_unit, int& bad) {
+    if ((at_unit & 31) == 0 || at_unit == u0) {
+      const int p = (at_unit >> 5) * 64 + lane;
+      ids = p < n_pages ? table[p] : 0;
+    }
+    bad = 0;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const bool there = 2 * at_unit + p < n_pages;
+      const int id = __builtin_amdgcn_readlane(ids, (2 * at_unit + p) & 63);
+      const bool ok = there && id >= 0 && id < a.num_pages;
+      bad |= (there && !ok) << p;
+      const int64_t off = ok ? id * page_bytes : 0;
+      q4::load_k<D>(u, p, kg + off, ok, lane);
+      q4::load_v<D>(u, p, vg + off, ok, lane);
+    }
+  };
+  q4::Unit<D> u;
+  int bad;
+  fetch(u, u0, bad);
+  for (int k = u0; k < u1; ++k) {
+    q4::Unit<D> next = u;
+    int next_bad = 0;
+    if (k + 1 < u1) fetch(next, k + 1, next_bad);
+    q4::fold<T, D, NB>(st, u, k * kQ4Unit, it.last0, all_last, bad, a.scale_log2, lane);
+    u = next;
+    bad = next_bad;
+  }
+
+#pragma unroll
+  for (int c = 0; c < NB; ++c) {
+    const float l = rows4_sum(st.l[c]);
+    if (st.last[c] < 0) continue;
+    const float inv = 1.0f / l;
+    const int64_t rec = at[c] * a.n_split + split;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+      float o[8];
+      q4::eight_out(st, c, j, o);
+      const int d = 32 * j + 8 * G;
+      if (a.n_split == 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] *= inv;
+        q4::store_eight(out + at[c] * D + d, o);
+      } else {
+        q4::store_eight(a.ws_o + rec * D + d, o);
+      }
+    }
+    if (a.n_split > 1 && G == 0) {
+      a.ws_ml[rec * 2] = st.m[c];
+      a.ws_ml[rec * 2 + 1] = l;
+    }
+  }
+}
+
+// Join the parts of one (query row, head) per wave.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int f = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = f / a.H_q;
+  if (row >= a.rows) return;
+  int b = row, L = 1, j = 0;
+  if (a.query_start_loc != nullptr) {
+    const int32_t* qsl = a.query_start_loc;
+    b = q4::wave_search(a.B, row, lane, [&](int i) { return qsl[i]; });
+    L = qsl[b + 1] - qsl[b];
+    j = row - qsl[b];
+    if (j < 0 || j >= L) return;
+  }
+  const int C = a.context_lens[b];
+  // (rows without keys or with an error are written already)
+  if (C < L || C > a.max_context_len || (C + kPage - 1) / kPage > a.bt_stride) return;
+  // the parts that have a key of the row: any later ones of its item weigh nothing
+  const int n = min(a.n_split, (C - L + j) / kQ4Unit / a.split_units + 1);
+  const int64_t rec = (int64_t)f * a.n_split;
+  float m = kMInit, l = 0.0f;
+  if (lane < n) {
+    m = a.ws_ml[(rec + lane) * 2];
+    l = a.ws_ml[(rec + lane) * 2 + 1];
+  }
+  const float M = across_groups_max<1>(m);  // (every lane takes part)
+  const float w = lane < n ? fast_exp2(m - M) : 0.0f;
+  const float total = across_groups_sum<1>(l * w);
+  constexpr int E = D / 64;
+  float o[E] = {};
+  for (int i = 0; i < n; ++i) {
+    const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i));
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(a.ws_o[(rec + i) * D + lane * E + e], wi, o[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) store_out<T>(reinterpret_cast<T*>(a.out) + (int64_t)f * D + lane * E + e, o[e] / total);
+}
+
+template <typename T, int D>
+const void* q4_attn_pick(int blocks) {
+  switch (blocks) {
+    case 1: return reinterpret_cast<const void*>(&q4_attn_kernel<T, D, 1>);
+    case 2: return reinterpret_cast<const void*>(&q4_attn_kernel<T, D, 2>);
+    case 4: return reinterpret_cast<const void*>(&q4_attn_kernel<T, D, 4>);
+  }
+  return nullptr;
+}
+
+}  // namespace pa
