@@ -103,7 +103,7 @@ int paged_attn_q4(const void *q, const void *k_pages, const void *v_pages,
  * paged_attn_varlen with 4-bit pools.  Row j of a chunk of length L in a context C
  * attends to positions 0 .. C - L + j; keys that a row does not see never reach
  * it, whatever they hold (NaN blocks included).  Rows of a chunk longer than its
- * context are NaN, rows of no sequence are left as they were.
+ * context or than max_q_len are NaN, rows of no sequence are left as they were.
  * Errors: PA_EINVAL, PA_ENOTSUP, PA_ENOSPC, PA_EHIP. */
 int paged_attn_varlen_q4(const void *q, const void *k_pages, const void *v_pages,
                          const int32_t *block_table, const int32_t *context_lens,

@@ -14,6 +14,7 @@
 
 #include "pa_counter.h"
 #include "pa_kernels.h"
+#include "pa_q4.h"
 #include "pa_route.h"
 #include "pa_sched.h"
 #include "pagedattn.h"
@@ -315,7 +316,7 @@ int run(const void* q, const void* k_pages, const void* v_pages, const int32_t* 
     sa.ws_o = reinterpret_cast<float*>(ws);
     sa.ws_ml = reinterpret_cast<float*>(ws + p.st_o);
     sa.ws_flag = reinterpret_cast<unsigned long long*>(ws + p.st_o + p.st_ml);
-    sa.key = pa::counter_key(next_call());
+    sa.key = pa::new_call_key();
     sa.bt_stride = dims->max_pages_per_seq;
     sa.scale_log2 = scale * 1.4426950408889634f;
     sa.B = dims->num_seqs;
@@ -449,6 +450,10 @@ int run(const void* q, const void* k_pages, const void* v_pages, const int32_t* 
 }
 
 }  // namespace
+
+namespace pa {
+CounterKey new_call_key() { return counter_key(next_call()); }
+}  // namespace pa
 
 extern "C" {
 

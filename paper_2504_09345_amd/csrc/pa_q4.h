@@ -26,7 +26,9 @@ struct Q4RowsArgs {
 hipError_t launch_q4_append(int dtype, int D, const Q4RowsArgs& a, hipStream_t st);
 hipError_t launch_q4_read(int dtype, int D, const Q4RowsArgs& a, hipStream_t st);
 
-// Attention.  A wave takes an item, a KV head's 16 NB columns (query row, head of
+constexpr int kQ4Unit = 2 * 16;  // tokens of a step: two pages
+
+// Chunk rows.  A wave takes an item, a KV head's 16 NB columns (query row, head of
 // the group) of one sequence, over a part of its keys.
 struct Q4AttnArgs {
   const void* q;
@@ -41,16 +43,53 @@ struct Q4AttnArgs {
   int64_t bt_stride;
   float scale_log2;
   int B, s /* heads of a group */, H_q, H_kv, rows, num_pages, max_context_len;
-  int n_slots;  // row blocks, at most (q4_slot)
+  int n_slots;   // row blocks, at most
+  int min_rows;  // sequences of fewer rows are the stream kernel's
+  int max_q_len;
   int n_split, split_units;
 };
-constexpr int kQ4Unit = 2 * 16;  // tokens of a step: two pages
+constexpr int kQ4Waves = 4;  // waves of a workgroup, each with an item of its own
 
 // Column blocks (of 16) that a wave holds.
-constexpr int kQ4BlocksMax = 4;
 constexpr int q4_positions(int blocks, int s) { return 16 * blocks / s; }  // query rows of an item
 
 hipError_t launch_q4_attn(int dtype, int D, int blocks, const Q4AttnArgs& a, hipStream_t st, KernelEvents ev);
 hipError_t launch_q4_merge(int dtype, int D, const Q4AttnArgs& a, hipStream_t st);
+
+// The persistent kernel of decode rows (sequences of one row): (sequence, head
+// block, unit) triples of the whole batch in equal contiguous ranges, one per team
+// of W waves, a wave per KV head of a head block.
+struct Q4StreamArgs {
+  const void* q;
+  const uint8_t* k_pages;
+  const uint8_t* v_pages;
+  const int32_t* block_table;
+  const int32_t* context_lens;
+  const int32_t* query_start_loc;  // nullptr: decode
+  void* out;
+  // of each range, slot (0: the item that its start cuts, 1: that its end cuts) and
+  // wave, as in StreamArgs
+  float* ws_o;
+  float* ws_ml;
+  unsigned long long* ws_flag;  // a counter per range
+  CounterKey key;
+  int64_t bt_stride;
+  float scale_log2;
+  int B, H_q, H_kv, rows, num_pages, max_context_len;
+  int nb;         // head blocks = H_kv / W
+  int max_q_len;  // longer chunks are NaN rows, where write_long
+  int write_long;
+};
+constexpr int kQ4StreamSeqs = 8192;    // sequences of a launch
+constexpr int kQ4StreamWaves = 4096;   // waves of a launch: ranges times W
+constexpr int kQ4StreamThreads = 512;  // of a workgroup: 8 / W teams
+
+constexpr int q4_waves(int H_kv) { return H_kv % 8 == 0 ? 8 : H_kv % 4 == 0 ? 4 : H_kv % 2 == 0 ? 2 : 1; }
+int q4_stream_occupancy(int dtype, int D, int s, int W);  // workgroups per CU, 0 on error
+hipError_t launch_q4_stream(int dtype, int D, int s, int W, const Q4StreamArgs& a, int workgroups, hipStream_t st, KernelEvents ev);
+template <typename T, int D> const void* q4_stream_pick(int s, int W);
+
+// A call's key (pa_counter.h), its own among the process's.
+CounterKey new_call_key();
 
 }  // namespace pa

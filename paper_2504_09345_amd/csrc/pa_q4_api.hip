@@ -1,5 +1,6 @@
 // C ABI of the 4-bit cache (pagedattn_q4.h): host-side validation, planning and
-// dispatch.  Validation runs before any HIP call; nothing is kept between calls.
+// dispatch.  Validation runs before any HIP call; nothing is kept between calls but
+// their number (pa_api.hip), which keys the arrival counters.
 #include <math.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -17,6 +18,7 @@ int check_cache(const pa_dims_t* d) {
   if (d->num_seqs < 0 || d->num_kv_heads <= 0 || d->num_pages < 0 || d->max_pages_per_seq < 0 || d->max_context_len < 0 ||
       d->pages_per_split != 0)
     return PA_EINVAL;
+  if (d->max_context_len > 1 << 30) return PA_ENOTSUP;  // (page counts are 32-bit)
   if (d->dtype != PA_BF16 && d->dtype != PA_FP32) return PA_ENOTSUP;
   if (d->head_dim != 64 && d->head_dim != 128) return PA_ENOTSUP;
   if (d->page_size != 16) return PA_ENOTSUP;
@@ -60,13 +62,24 @@ int rows_call(const void* k_rows, const void* v_rows, const int32_t* block_table
 }
 
 struct Plan {
-  int s = 0, rows = 0, blocks = 1, n_slots = 0, n_split = 1, split_units = 1;
-  size_t ws_o = 0, ws_ml = 0;
+  int s = 0, rows = 0;
+  bool stream = false, chunks = false;  // which kernels the call needs
+  // decode rows
+  int W = 0, per_launch = 0;  // waves of a team; sequences of a launch
+  // chunk rows
+  int blocks = 1, n_slots = 0, n_split = 1, split_units = 1, min_rows = 2;
+  size_t st_o = 0, st_ml = 0, st_flag = 0, ch_o = 0, ch_ml = 0;
+  size_t stream_bytes() const { return st_o + st_ml + st_flag; }
+  size_t chunk_bytes() const { return ch_o + ch_ml; }
+  // (the kernels run one after the other and share the workspace)
+  size_t bytes() const { return stream_bytes() > chunk_bytes() ? stream_bytes() : chunk_bytes(); }
 };
 
-// Parts that a call's items are cut into: as many as give the GPU (256 CUs of 8
-// waves) a wave of work each, of at least kLeastUnits units, at most 64.
+// Parts that chunks are cut into: as many as give the GPU (256 CUs of 8 waves) a
+// wave of work each, of at least kLeastUnits units, at most 64.
 constexpr int kWavesWanted = 2048, kLeastUnits = 4, kMaxSplit = 64;
+// Units of a launch of the stream kernel, at most (its counts are 32-bit).
+constexpr int64_t kStreamUnits = 1 << 30;
 
 int plan(const pa_dims_t* d, bool varlen, Plan* p) {
   const int rc = check_cache(d);
@@ -78,28 +91,48 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
     if (d->num_q_rows < 0 || d->max_q_len < 0) return PA_EINVAL;
     if (d->num_q_rows > 0 && (d->max_q_len < 1 || d->num_seqs == 0 || d->max_q_len > d->max_context_len)) return PA_EINVAL;
     p->rows = d->num_q_rows;
-    p->blocks = d->max_q_len * (int64_t)s <= 16 ? 1 : d->max_q_len * (int64_t)s <= 32 ? 2 : 4;
-    p->n_slots = p->rows / pa::q4_positions(p->blocks, s) + d->num_seqs;
   } else {
     if ((d->num_q_rows != 0 && d->num_q_rows != d->num_seqs) || d->max_q_len < 0 || d->max_q_len > 1) return PA_EINVAL;
-    p->rows = p->n_slots = d->num_seqs;
+    p->rows = d->num_seqs;
   }
   if (p->rows == 0) return PA_OK;
-  const int64_t items = (int64_t)p->n_slots * d->num_kv_heads;
+  if ((int64_t)p->rows * d->num_q_heads > INT32_MAX) return PA_ENOTSUP;
   const int64_t units = ((int64_t)d->max_context_len + pa::kQ4Unit - 1) / pa::kQ4Unit;
-  int64_t split = kWavesWanted / items;
-  if (split > units / kLeastUnits) split = units / kLeastUnits;
-  if (split > kMaxSplit) split = kMaxSplit;
-  if (split < 1) split = 1;
-  p->split_units = (int)((units + split - 1) / split);
-  if (p->split_units < 1) p->split_units = 1;
-  p->n_split = (int)((units + p->split_units - 1) / p->split_units);
-  if (p->n_split < 1) p->n_split = 1;
-  if ((items + 4 * d->num_kv_heads) * p->n_split > INT32_MAX || (int64_t)p->rows * d->num_q_heads > INT32_MAX) return PA_ENOTSUP;
-  if (p->n_split > 1) {
-    const size_t recs = (size_t)p->rows * d->num_q_heads * p->n_split;
-    p->ws_o = align256(recs * d->head_dim * sizeof(float));
-    p->ws_ml = align256(recs * 2 * sizeof(float));
+  p->chunks = varlen && d->max_q_len > 1;
+  // every sequence carrying max_q_len rows leaves no decode row (a single row that
+  // is there all the same is then a chunk of one)
+  p->stream = !(p->chunks && (int64_t)d->max_q_len * d->num_seqs == d->num_q_rows);
+  if (p->stream) {
+    p->W = pa::q4_waves(d->num_kv_heads);
+    const int nb = d->num_kv_heads / p->W;
+    const int64_t most = kStreamUnits / ((units > 0 ? units : 1) * nb);
+    if (most < 1) return PA_ENOTSUP;
+    p->per_launch = most < pa::kQ4StreamSeqs ? (int)most : pa::kQ4StreamSeqs;
+    const size_t recs = (size_t)pa::kQ4StreamWaves * 2 * s;
+    p->st_o = align256(recs * d->head_dim * sizeof(float));
+    p->st_ml = align256(recs * 2 * sizeof(float));
+    p->st_flag = align256((size_t)pa::kQ4StreamWaves / p->W * sizeof(unsigned long long));
+  }
+  if (p->chunks) {
+    p->min_rows = p->stream ? 2 : 1;
+    p->blocks = d->max_q_len * (int64_t)s <= 16 ? 1 : d->max_q_len * (int64_t)s <= 32 ? 2 : 4;
+    const int64_t slots = p->rows / pa::q4_positions(p->blocks, s) + (int64_t)d->num_seqs;
+    // row blocks of the sequences that can be chunks
+    const int64_t chunk_rows = p->stream ? (int64_t)p->rows - d->num_seqs : p->rows;
+    const int64_t items = (chunk_rows / pa::q4_positions(p->blocks, s) + 1) * d->num_kv_heads;
+    int64_t split = kWavesWanted / items;
+    if (split > units / kLeastUnits) split = units / kLeastUnits;
+    if (split > kMaxSplit) split = kMaxSplit;
+    if (split < 1) split = 1;
+    p->split_units = (int)((units + split - 1) / split);
+    p->n_split = (int)((units + p->split_units - 1) / p->split_units);
+    if ((slots + pa::kQ4Waves) * d->num_kv_heads * p->n_split > INT32_MAX) return PA_ENOTSUP;
+    p->n_slots = (int)slots;
+    if (p->n_split > 1) {
+      const size_t recs = (size_t)p->rows * d->num_q_heads * p->n_split;
+      p->ch_o = align256(recs * d->head_dim * sizeof(float));
+      p->ch_ml = align256(recs * 2 * sizeof(float));
+    }
   }
   return PA_OK;
 }
@@ -114,7 +147,7 @@ int attend(const void* q, const void* k_pages, const void* v_pages, const int32_
   if (p.rows > 0) {
     if (!q || !k_pages || !v_pages || !block_table || !context_lens || !out || (varlen && !query_start_loc)) return PA_EINVAL;
     if (misaligned(q) || misaligned(k_pages) || misaligned(v_pages) || misaligned(out) || misaligned(workspace)) return PA_EINVAL;
-    if (p.ws_o > 0 && (workspace == nullptr || workspace_bytes < p.ws_o + p.ws_ml)) return PA_ENOSPC;
+    if (p.bytes() > 0 && (workspace == nullptr || workspace_bytes < p.bytes())) return PA_ENOSPC;
   }
   const hipEvent_t begin = timing ? timing->attn_begin : nullptr, end = timing ? timing->attn_end : nullptr;
   const hipEvent_t joined = timing ? timing->reduce_end : nullptr;
@@ -123,33 +156,80 @@ int attend(const void* q, const void* k_pages, const void* v_pages, const int32_
       if (ev != nullptr) (void)hipEventRecord(ev, stream);
     return PA_OK;
   }
-  pa::Q4AttnArgs a{};
-  a.q = q;
-  a.k_pages = static_cast<const uint8_t*>(k_pages);
-  a.v_pages = static_cast<const uint8_t*>(v_pages);
-  a.block_table = block_table;
-  a.context_lens = context_lens;
-  a.query_start_loc = varlen ? query_start_loc : nullptr;
-  a.out = out;
-  a.ws_o = static_cast<float*>(workspace);
-  a.ws_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.ws_o);
-  a.bt_stride = d->max_pages_per_seq;
-  a.scale_log2 = scale * 1.4426950408889634f;
-  a.B = d->num_seqs;
-  a.s = p.s;
-  a.H_q = d->num_q_heads;
-  a.H_kv = d->num_kv_heads;
-  a.rows = p.rows;
-  a.num_pages = d->num_pages;
-  a.max_context_len = d->max_context_len;
-  a.n_slots = p.n_slots;
-  a.n_split = p.n_split;
-  a.split_units = p.split_units;
-  pa::KernelEvents ev;
-  ev.start = begin;
-  ev.stop = end;
-  if (pa::launch_q4_attn(d->dtype, d->head_dim, p.blocks, a, stream, ev) != hipSuccess) return PA_EHIP;
-  if (p.n_split > 1 && pa::launch_q4_merge(d->dtype, d->head_dim, a, stream) != hipSuccess) return PA_EHIP;
+  char* ws = static_cast<char*>(workspace);
+  const float scale_log2 = scale * 1.4426950408889634f;
+  if (p.chunks) {
+    pa::Q4AttnArgs a{};
+    a.q = q;
+    a.k_pages = static_cast<const uint8_t*>(k_pages);
+    a.v_pages = static_cast<const uint8_t*>(v_pages);
+    a.block_table = block_table;
+    a.context_lens = context_lens;
+    a.query_start_loc = query_start_loc;
+    a.out = out;
+    a.ws_o = reinterpret_cast<float*>(ws);
+    a.ws_ml = reinterpret_cast<float*>(ws + p.ch_o);
+    a.bt_stride = d->max_pages_per_seq;
+    a.scale_log2 = scale_log2;
+    a.B = d->num_seqs;
+    a.s = p.s;
+    a.H_q = d->num_q_heads;
+    a.H_kv = d->num_kv_heads;
+    a.rows = p.rows;
+    a.num_pages = d->num_pages;
+    a.max_context_len = d->max_context_len;
+    a.n_slots = p.n_slots;
+    a.min_rows = p.min_rows;
+    a.max_q_len = d->max_q_len;
+    a.n_split = p.n_split;
+    a.split_units = p.split_units;
+    pa::KernelEvents ev;
+    ev.start = begin;
+    ev.stop = p.stream ? nullptr : end;
+    if (pa::launch_q4_attn(d->dtype, d->head_dim, p.blocks, a, stream, ev) != hipSuccess) return PA_EHIP;
+    if (p.n_split > 1 && pa::launch_q4_merge(d->dtype, d->head_dim, a, stream) != hipSuccess) return PA_EHIP;
+  }
+  if (p.stream) {
+    int dev = 0, cus = 0;
+    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
+      return PA_EHIP;
+    const int per_cu = pa::q4_stream_occupancy(d->dtype, d->head_dim, p.s, p.W);
+    if (per_cu <= 0) return PA_EHIP;
+    int workgroups = cus * per_cu;
+    const int most = pa::kQ4StreamWaves * 64 / pa::kQ4StreamThreads;
+    if (workgroups > most) workgroups = most;
+    pa::Q4StreamArgs a{};
+    a.k_pages = static_cast<const uint8_t*>(k_pages);
+    a.v_pages = static_cast<const uint8_t*>(v_pages);
+    a.ws_o = reinterpret_cast<float*>(ws);
+    a.ws_ml = reinterpret_cast<float*>(ws + p.st_o);
+    a.ws_flag = reinterpret_cast<unsigned long long*>(ws + p.st_o + p.st_ml);
+    a.bt_stride = d->max_pages_per_seq;
+    a.scale_log2 = scale_log2;
+    a.H_q = d->num_q_heads;
+    a.H_kv = d->num_kv_heads;
+    a.num_pages = d->num_pages;
+    a.max_context_len = d->max_context_len;
+    a.nb = d->num_kv_heads / p.W;
+    a.max_q_len = d->max_q_len;
+    a.write_long = !p.chunks;
+    const size_t row_bytes = (size_t)d->num_q_heads * d->head_dim * (d->dtype == PA_BF16 ? 2 : 4);
+    for (int b = 0; b < d->num_seqs; b += p.per_launch) {
+      a.B = d->num_seqs - b < p.per_launch ? d->num_seqs - b : p.per_launch;
+      a.block_table = block_table + (int64_t)b * d->max_pages_per_seq;
+      a.context_lens = context_lens + b;
+      // (query_start_loc counts rows of the call; a decode call's rows are its sequences)
+      a.query_start_loc = varlen ? query_start_loc + b : nullptr;
+      a.rows = varlen ? p.rows : a.B;
+      a.q = static_cast<const char*>(q) + (varlen ? 0 : b * row_bytes);
+      a.out = static_cast<char*>(out) + (varlen ? 0 : b * row_bytes);
+      a.key = pa::new_call_key();
+      pa::KernelEvents ev;
+      ev.start = b == 0 && !p.chunks ? begin : nullptr;
+      ev.stop = b + a.B == d->num_seqs ? end : nullptr;
+      if (pa::launch_q4_stream(d->dtype, d->head_dim, p.s, p.W, a, workgroups, stream, ev) != hipSuccess) return PA_EHIP;
+    }
+  }
   if (joined != nullptr) (void)hipEventRecord(joined, stream);
   return PA_OK;
 }
@@ -183,7 +263,7 @@ int pa_workspace_size_q4(const pa_dims_t* dims, size_t* bytes) {
   const bool varlen = dims != nullptr && (dims->max_q_len > 1 || (dims->num_q_rows != 0 && dims->num_q_rows != dims->num_seqs));
   const int rc = plan(dims, varlen, &p);
   if (rc != PA_OK) return rc;
-  *bytes = p.ws_o + p.ws_ml;
+  *bytes = p.bytes();
   return PA_OK;
 }
 

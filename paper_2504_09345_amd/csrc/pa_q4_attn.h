@@ -6,8 +6,6 @@
 
 namespace pa {
 
-constexpr int kQ4Waves = 4;  // waves of a workgroup, each with an item of its own
-
 // An item's sequence and rows.
 struct Q4Item {
   int b, row0, n_pos;  // sequence, first query row, query rows (0: none)
@@ -28,13 +26,14 @@ __device__ __forceinline__ Q4Item q4_item(const Q4AttnArgs& a, int slot, int pos
     first = (slot - (q0 / positions + it.b)) * positions;
     it.row0 = q0 + first;
     if (q0 < 0 || first < 0 || it.row0 >= a.rows) return it;
+    if (L < a.min_rows) return it;  // (the stream kernel's)
     it.n_pos = max(0, min(positions, min(L - first, a.rows - it.row0)));
   } else {
     it.n_pos = 1;
   }
   const int C = a.context_lens[it.b];
   it.last0 = C - L + first;
-  it.bad = C < 0 || C > a.max_context_len || (C + kPage - 1) / kPage > a.bt_stride || (a.query_start_loc != nullptr && L > C);
+  it.bad = C < 0 || C > a.max_context_len || (C + kPage - 1) / kPage > a.bt_stride || (a.query_start_loc != nullptr && (L > C || L > a.max_q_len));
   return it;
 }
 
@@ -115,7 +114,16 @@ __global__ __launch_bounds__(64 * kQ4Waves) void q4_attn_kernel(Q4AttnArgs a) {
     q4::Unit<D> next = u;
     int next_bad = 0;
     if (k + 1 < u1) fetch(next, k + 1, next_bad);
-    q4::fold<T, D, NB>(st, u, k * kQ4Unit, it.last0, all_last, bad, a.scale_log2, lane);
+    const int key0 = k * kQ4Unit;
+    const bool edge = key0 + kQ4Unit - 1 > it.last0;
+    q4::f32x4_t s[NB][2];
+    u32x4 pt[NB][q4::kPParts<T>];
+    q4::fold_qk<T, D, NB>(st, u, bad, s);
+    q4::fold_softmax<T, D, NB>(st, s, key0, edge, a.scale_log2, lane, pt);
+    if (edge)
+      q4::fold_pv_edge<T, D, NB>(st, u, pt, key0, all_last, lane);
+    else
+      q4::fold_pv<T, D, NB>(st, u, pt);
     u = next;
     bad = next_bad;
   }
@@ -159,7 +167,7 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
     b = q4::wave_search(a.B, row, lane, [&](int i) { return qsl[i]; });
     L = qsl[b + 1] - qsl[b];
     j = row - qsl[b];
-    if (j < 0 || j >= L) return;
+    if (j < 0 || j >= L || L < a.min_rows || L > a.max_q_len) return;
   }
   const int C = a.context_lens[b];
   // (rows without keys or with an error are written already)

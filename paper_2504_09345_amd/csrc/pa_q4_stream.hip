@@ -1,0 +1,48 @@
+// Decode rows over the 4-bit paged cache for gfx950 (format in pagedattn_q4.h): a
+// persistent grid in which every team of waves streams an equal contiguous range of
+// the batch's (sequence, head block, unit) triples, as the stream-K kernel of the
+// 16-bit cache does (pa_stream.hip: equal bytes per workgroup whatever the context
+// lengths, items cut by a range's ends joined by the part that arrives last, one
+// launch), with another inner loop:
+//
+//  * A unit is two pages (32 tokens) of one KV head, 4.3 KiB of K and V at head_dim
+//    128: softmax and the products' bookkeeping are paid once per 32 tokens, and the
+//    PV product's k dimension is filled by them.
+//  * The codes lie in memory as the lanes hold the matrix-core operands, so the
+//    waves share nothing: no LDS tiles, no barrier per unit.  A wave's K registers
+//    are loaded again as soon as the scores are formed and V's after the PV
+//    products, one unit ahead, and four waves per SIMD keep 70 KB per CU in flight.
+#include "pa_q4_stream.h"
+
+namespace pa {
+
+extern template const void* q4_stream_pick<uint16_t, 64>(int, int);
+extern template const void* q4_stream_pick<float, 128>(int, int);
+extern template const void* q4_stream_pick<float, 64>(int, int);
+template const void* q4_stream_pick<uint16_t, 128>(int, int);
+
+static const void* q4_stream_fn(int dtype, int D, int s, int W) {
+  if (dtype == 0 && D == 128) return q4_stream_pick<uint16_t, 128>(s, W);
+  if (dtype == 0 && D == 64) return q4_stream_pick<uint16_t, 64>(s, W);
+  if (dtype == 1 && D == 128) return q4_stream_pick<float, 128>(s, W);
+  if (dtype == 1 && D == 64) return q4_stream_pick<float, 64>(s, W);
+  return nullptr;
+}
+
+int q4_stream_occupancy(int dtype, int D, int s, int W) {
+  const void* fn = q4_stream_fn(dtype, D, s, W);
+  int n = 0;
+  if (fn == nullptr || hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, fn, kQ4StreamThreads, 0) != hipSuccess) return 0;
+  return n;
+}
+
+hipError_t launch_q4_stream(int dtype, int D, int s, int W, const Q4StreamArgs& a, int workgroups, hipStream_t st,
+                            KernelEvents ev) {
+  const void* fn = q4_stream_fn(dtype, D, s, W);
+  if (fn == nullptr || workgroups <= 0) return hipErrorInvalidValue;
+  void* args[] = {const_cast<Q4StreamArgs*>(&a)};
+  hipError_t e = hipExtLaunchKernel(fn, dim3(workgroups), dim3(kQ4StreamThreads), args, 0, st, ev.start, ev.stop, 0);
+  return e != hipSuccess ? e : hipGetLastError();
+}
+
+}  // namespace pa

@@ -171,16 +171,13 @@ __device__ __forceinline__ void load_query(u32x4 (&q)[D / 32][kQParts<T>], const
   }
 }
 
-// Fold the unit of keys key0 .. key0 + 31 into the state.  first_last: the
-// smallest `last` of the wave's columns (units beyond it are masked column by
-// column), all_last: the largest.  bad: bit p, page p's entry lies outside the
-// pool (its scores are NaN).
+// Fold of the unit of keys key0 .. key0 + 31, in three steps, so that K's registers
+// and then V's are free for the next unit's loads as soon as they are read.
+//
+// Scores S^T[token][column] = K . Q^T, the K operand shared by the columns.  bad:
+// bit p, page p's entry lies outside the pool (its scores are NaN).
 template <typename T, int D, int NB>
-__device__ __forceinline__ void fold(State<T, D, NB>& st, Unit<D>& u, int key0, int first_last, int all_last, int bad,
-                                     float scale_log2, int lane) {
-  const int G = lane >> 4;
-  // scores S^T[token][column] = K . Q^T, the K operand shared by the columns
-  f32x4_t s[NB][2];
+__device__ __forceinline__ void fold_qk(const State<T, D, NB>& st, const Unit<D>& u, int bad, f32x4_t (&s)[NB][2]) {
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
     const float ks = __uint_as_float(u.ks[p] << 23);
@@ -203,50 +200,25 @@ __device__ __forceinline__ void fold(State<T, D, NB>& st, Unit<D>& u, int key0, 
       for (int p = 0; p < 2; ++p)
         if (bad >> p & 1) s[c][p] = f32x4_t{NAN, NAN, NAN, NAN};
   }
-  // Keys that some column does not see.  Their weights are 0, but 0 times a NaN
-  // is NaN: the scales of such blocks become 0 here, and columns that do see the
-  // first NaN of a block get it below.
-  const bool edge = key0 + kQ4Unit - 1 > first_last;  // wave-uniform
-  int nan_key[D / 32];
-  bool nans = false;
-  if (edge) {
-#pragma unroll
-    for (int c = 0; c < NB; ++c)
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          s[c][p][i] = key0 + 16 * p + 4 * G + i <= st.last[c] ? s[c][p][i] : -INFINITY;
-    bool any = false;
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) nan_key[j] = INT32_MAX;
-#pragma unroll
-    for (int p = 1; p >= 0; --p)
-#pragma unroll
-      for (int i = 3; i >= 0; --i) {
-        constexpr int n = D / 32;
-        const int key = key0 + 16 * p + 4 * G + i, sh = n == 4 ? 0 : (i & 1) * 16;
-        uint32_t& w = u.vs[p][n == 4 ? i : i >> 1];
-        if (key > all_last) w &= n == 4 ? 0u : 0xffff0000u >> sh;  // (an unused slot may hold anything)
-#pragma unroll
-        for (int j = 0; j < n; ++j) {
-          const uint32_t byte = 0xffu << (sh + 8 * j);
-          if ((w & byte) == byte) {
-            w &= ~byte;
-            nan_key[j] = key;
-            any = true;
-          }
-        }
-      }
-    nans = __builtin_amdgcn_ballot_w64(any) != 0;
-  }
-  // online softmax; the base moves only past the slack
-  u32x4 pt[NB][kPParts<T>];
+}
+
+// Online softmax; the weights' bf16 parts as P^T operands.  edge (wave-uniform):
+// some column does not see every key of the unit.  The base moves only past the
+// slack.
+template <typename T, int D, int NB>
+__device__ __forceinline__ void fold_softmax(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], int key0, bool edge,
+                                             float scale_log2, int lane, u32x4 (&pt)[NB][kPParts<T>]) {
+  const int G = lane >> 4;
 #pragma unroll
   for (int c = 0; c < NB; ++c) {
     float x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = s[c][i >> 2][i & 3];
+    if (edge) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = key0 + 16 * (i >> 2) + 4 * G + (i & 3) <= st.last[c] ? x[i] : -INFINITY;
+    }
+    // (scale > 0, so the largest score is the scaled largest)
     const float mx = rows4_max(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])))) *
                      scale_log2;
     const float mc = fmaxf(st.m[c], mx);
@@ -262,7 +234,23 @@ __device__ __forceinline__ void fold(State<T, D, NB>& st, Unit<D>& u, int key0, 
     st.l[c] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
     split8(x, pt[c]);
   }
-  // O^T += V^T . P^T
+}
+
+// V of keys past all_last, which no column sees: their weights are 0, but an unused
+// slot may hold anything, and 0 times a NaN is NaN.  Their scales become 0.
+template <int D>
+__device__ __forceinline__ void clear_dead(Unit<D>& u, int key0, int all_last, int lane) {
+  constexpr int n = D / 32;
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (key0 + 16 * p + 4 * (lane >> 4) + i > all_last) u.vs[p][n == 4 ? i : i >> 1] &= n == 4 ? 0u : 0xffff0000u >> ((i & 1) * 16);
+}
+
+// O^T += V^T . P^T
+template <typename T, int D, int NB>
+__device__ __forceinline__ void fold_pv(State<T, D, NB>& st, const Unit<D>& u, const u32x4 (&pt)[NB][kPParts<T>]) {
   auto block = [&](auto j_) {
     constexpr int j = decltype(j_)::value;
     u32x4 a[2];
@@ -282,14 +270,44 @@ __device__ __forceinline__ void fold(State<T, D, NB>& st, Unit<D>& u, int key0, 
     block(std::integral_constant<int, 2>{});
     block(std::integral_constant<int, 3>{});
   }
+}
+
+// fold_pv for a unit of which some columns see a part of the keys: a NaN block of
+// V reaches the columns that see its key, and no other (a weight of 0 times NaN
+// would be NaN).  Its scale becomes 0, and the columns that see the first such key
+// of a block get NaN outright.
+template <typename T, int D, int NB>
+__device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, const u32x4 (&pt)[NB][kPParts<T>], int key0,
+                                             int all_last, int lane) {
+  constexpr int n = D / 32;
+  clear_dead(u, key0, all_last, lane);
+  int nan_key[n];
+  bool any = false;
+#pragma unroll
+  for (int j = 0; j < n; ++j) nan_key[j] = INT32_MAX;
+#pragma unroll
+  for (int p = 1; p >= 0; --p)
+#pragma unroll
+    for (int i = 3; i >= 0; --i) {
+      uint32_t& w = u.vs[p][n == 4 ? i : i >> 1];
+#pragma unroll
+      for (int j = 0; j < n; ++j) {
+        const uint32_t byte = 0xffu << ((n == 4 ? 0 : (i & 1) * 16) + 8 * j);
+        if ((w & byte) == byte) {
+          w &= ~byte;
+          nan_key[j] = key0 + 16 * p + 4 * (lane >> 4) + i;
+          any = true;
+        }
+      }
+    }
+  const bool nans = __builtin_amdgcn_ballot_w64(any) != 0;
+  fold_pv<T, D, NB>(st, u, pt);
   if (nans) {
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
+    for (int j = 0; j < n; ++j) {
       int k = nan_key[j];
       k = min(k, __shfl_xor(k, 16));
       k = min(k, __shfl_xor(k, 32));
-#pragma unroll
-      for (int off = 1; off < 16; off <<= 1) k = min(k, __shfl_xor(k, off));
 #pragma unroll
       for (int c = 0; c < NB; ++c)
         if (st.last[c] >= k) st.acc[c][2 * j] = st.acc[c][2 * j + 1] = f32x4_t{NAN, NAN, NAN, NAN};

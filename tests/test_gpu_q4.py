@@ -275,3 +275,94 @@ def test_a_serving_step():
         assert np.array_equal(back[1].float().cpu().numpy(), q4.values(*q4.quantise(vn)))
         ctx = ctx + 1
     assert np.array_equal(d["k"].cpu().numpy(), k) and np.array_equal(d["v"].cpu().numpy(), v)
+
+
+# --- the decode kernel's division of work ------------------------------------
+
+@pytest.mark.parametrize("H_kv", [1, 2, 4, 8])
+@pytest.mark.parametrize("n,lo,hi", [(1, 2000, 2000), (3, 900, 1500), (40, 1, 700), (7, 33, 64)])
+def test_decode_ranges(H_kv, n, lo, hi):
+    """Items cut over several ranges, in one and two levels of joins, for every
+    number of waves per team; the same bits every time."""
+    announce(f"q4 decode ranges H_kv={H_kv} {n} x {lo}-{hi}")
+    rng = np.random.default_rng(H_kv + n)
+    b = Batch([(int(c), 1) for c in rng.integers(lo, hi + 1, n)], 2 * H_kv, H_kv, 64, varlen=False, seed=n)
+    d = b.upload()
+    first = b.attend(d)
+    check(first.float().cpu(), b.expected(), hi, "bf16")
+    ws = torch.full((pb.pa_workspace_size_q4(b.dims(d)),), 0xA5, dtype=torch.uint8, device="cuda")
+    for fill in (0xA5, 0xFF):
+        ws.fill_(fill)
+        assert torch.equal(b.attend(d, workspace=ws), first)
+    for _ in range(3):
+        assert torch.equal(b.attend(d, workspace=ws), first)
+
+
+@pytest.mark.parametrize("B,ctx", [(8192, 4224), (9000, 40)])
+def test_many_sequences_share_their_pages(B, ctx):
+    """More sequences than a launch takes; and ranges of more units than a table
+    holds.  All sequences read the same pages and a few different queries."""
+    announce(f"q4 decode {B} sequences of {ctx}")
+    one = Batch([(ctx, 1)], 1, 1, 64, varlen=False)
+    d = one.upload()
+    q = one.cuda(one.round(np.random.default_rng(1).standard_normal((8, 1, 64)))).to(torch.bfloat16)
+    which = torch.arange(B, device="cuda") * 7 % 8
+    d["q"] = q[which].contiguous()
+    d["bt"] = d["bt"].expand(B, -1).contiguous()
+    d["cl"] = d["cl"].expand(B).contiguous()
+    out = one.attend(d)
+    ref = [q4.attention(q[i:i + 1].float().cpu().numpy(), one.k, one.v, one.bt, one.ctx, one.scale) for i in range(8)]
+    ref = [np.concatenate([r[j] for r in ref]) for j in range(3)]
+    for i in range(8):
+        mine = out[which == i]
+        check(mine[:1].float().cpu(), [r[i:i + 1] for r in ref], ctx, "bf16")
+        # equal up to where the ranges cut them
+        ulp = 2.0 ** -7 * mine[0].float().abs() + 1e-6
+        assert ((mine.float() - mine[0].float()).abs() <= 2 * ulp).all()
+
+
+def test_mixed_call_with_wrong_max_q_len():
+    announce("q4 varlen, chunks longer than max_q_len")
+    b = Batch([(40, 9), (33, 1), (64, 4)], 4, 2, 64)
+    d = b.upload()
+    for most, nan in ((1, (0, 2)), (4, (0,))):
+        ref = b.expected()
+        for i in nan:
+            ref[0][b.qsl[i]:b.qsl[i + 1]] = np.nan
+        check(b.attend(d, b.dims(d, max_q_len=most)).float().cpu(), ref, 64, "bf16")
+
+
+def test_captured_calls_replay():
+    """A step recorded once and replayed on other contents, with eager calls on
+    the same workspace between the replays."""
+    announce("q4 captured step")
+    H_q, H_kv, D = 8, 2, 128
+    b = Batch([(300, 1), (70, 20), (1000, 1)], H_q, H_kv, D, seed=4)
+    d = b.upload()
+    rows = torch.zeros((2, b.T, H_kv, D), dtype=torch.bfloat16, device="cuda")
+    dims = b.dims(d)
+    ws = torch.empty(pb.pa_workspace_size_q4(dims), dtype=torch.uint8, device="cuda")
+    out, back = torch.empty_like(d["q"]), torch.empty_like(rows)
+
+    def step():
+        pb.pa_kv_append_q4(rows[0], rows[1], d["bt"], d["cl"], d["k"], d["v"], dims, query_start_loc=d["qsl"])
+        b.attend(d, dims, out, workspace=ws)
+        pb.pa_kv_read_q4(d["k"], d["v"], d["bt"], d["cl"], back[0], back[1], dims, query_start_loc=d["qsl"])
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in range(4):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rows.copy_(torch.randn(rows.shape, device="cuda", generator=g))
+        d["q"].copy_(torch.randn(d["q"].shape, device="cuda", generator=g))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), back.clone()
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(out, got[0]) and torch.equal(back, got[1])
+        ref = q4.attention(d["q"].float().cpu().numpy(), d["k"].cpu().numpy(), d["v"].cpu().numpy(), b.bt, b.ctx, b.scale, b.qsl)
+        check(got[0].float().cpu(), ref, 1000, "bf16")
