@@ -290,18 +290,20 @@ def pa_q4_tile_bytes(head_dim) -> int:
     return int(n.value)
 
 
+_Q4_TILE = {64: 544, 128: 1088}  # pa_q4_tile_bytes (checked against it by the tests)
+
+
 def make_dims_q4(rows, k_pages, block_table, max_context_len, num_q_rows=0, max_q_len=0, num_seqs=None) -> PaDims:
     """pa_dims_t of a call on the 4-bit cache from tensor shapes: rows
     [rows][H][D] (q, or k_new / k_out of the append and the read), k_pages uint8
     [N][H_kv][tile], block_table [B][max_pages_per_seq]."""
     _, H, D = rows.shape
     N, H_kv, tile = k_pages.shape
-    if tile != pa_q4_tile_bytes(D):
+    B, width = block_table.shape
+    if _Q4_TILE.get(D) != tile:
         raise ValueError(f"k_pages holds tiles of {tile} bytes, head_dim {D} takes {pa_q4_tile_bytes(D)}")
-    B = block_table.shape[0] if num_seqs is None else num_seqs
-    return PaDims(num_seqs=B, num_q_heads=H, num_kv_heads=H_kv, head_dim=D, page_size=PAGE_SIZE, num_pages=N,
-                  max_pages_per_seq=block_table.shape[1], max_context_len=int(max_context_len), pages_per_split=0,
-                  dtype=_dtype_code(rows), num_q_rows=int(num_q_rows), max_q_len=int(max_q_len))
+    return PaDims(B if num_seqs is None else num_seqs, H, H_kv, D, PAGE_SIZE, N, width, int(max_context_len), 0,
+                  _dtype_code(rows), int(num_q_rows), int(max_q_len))
 
 
 def pa_workspace_size_q4(dims: PaDims) -> int:
@@ -312,55 +314,73 @@ def pa_workspace_size_q4(dims: PaDims) -> int:
     return int(n.value)
 
 
-def _check_q4(dims, dense, pools, ints):
-    """What the 4-bit entries are given where it is a tensor: contiguous, on
-    the current device, of the type that dims and the format say."""
+def _check_q4(dims, heads, varlen, dense, pools, block_table, context_lens, query_start_loc):
+    """Refuses a tensor that is not what dims and the format say: of another type
+    or too few elements, not contiguous, not on the current device.  (Addresses
+    are taken as they are.)"""
     import torch
-    dense_type = torch.bfloat16 if dims.dtype == PA_BF16 else torch.float32
-    for kind, tensors in ((dense_type, dense), (torch.uint8, pools), (torch.int32, ints)):
-        for t in tensors:
-            if t is None or isinstance(t, int):
-                continue
-            if t.dtype != kind:
-                raise TypeError(f"{t.dtype} where {kind} is needed")
-            if not t.is_contiguous():
-                raise ValueError("tensors must be contiguous")
-            if not t.is_cuda or t.device.index != torch.cuda.current_device():
-                raise ValueError(f"a tensor on {t.device}, not on the current device")
+    dev = torch.cuda.current_device()
+    B, D = dims.num_seqs, dims.head_dim
+    rows = dims.num_q_rows if varlen else B
+    kind, code = (torch.bfloat16, "bfloat16") if dims.dtype == PA_BF16 else (torch.float32, "float32")
+    tiles = dims.num_pages * dims.num_kv_heads * _Q4_TILE.get(D, 0)
+    for t, want, name, n in ((dense[0], kind, code, rows * heads * D), (dense[1], kind, code, rows * heads * D),
+                             (pools[0], torch.uint8, "uint8", tiles), (pools[1], torch.uint8, "uint8", tiles),
+                             (block_table, torch.int32, "int32", B * dims.max_pages_per_seq),
+                             (context_lens, torch.int32, "int32", B), (query_start_loc, torch.int32, "int32", B + 1)):
+        if t is None or t.__class__ is int:
+            continue
+        if t.dtype is not want:
+            raise TypeError(f"a tensor of {t.dtype} where torch.{name} is needed")
+        if t.get_device() != dev:
+            raise ValueError(f"a tensor on {t.device}, not on the current device")
+        if t.numel() < n or not t.is_contiguous():
+            raise ValueError(f"a tensor of {t.numel()} elements{'' if t.is_contiguous() else ', not contiguous'}, "
+                             f"where {n} in a row are needed")
+
+
+def _workspace_q4(dims, workspace, q, stream):
+    """(address, bytes, owner) of the caller's workspace or of a temporary one."""
+    if workspace is None or workspace.__class__ is int:
+        ws, size = _workspace(dims, workspace, getattr(q, "device", None), stream, pa_workspace_size_q4)
+        return _addr(ws), size, ws
+    return workspace.data_ptr() or None, workspace.numel() * workspace.element_size(), workspace
+
+
+def _rows_q4(name, k_rows, v_rows, first, block_table, context_lens, last, dims, query_start_loc, stream, check):
+    _check_q4(dims, dims.num_kv_heads, query_start_loc is not None, (k_rows, v_rows),
+              last if name == "pa_kv_append_q4" else first, block_table, context_lens, query_start_loc)
+    rc = getattr(load(), name)(_addr(first[0]), _addr(first[1]), _addr(block_table), _addr(context_lens),
+                               _addr(query_start_loc), _addr(last[0]), _addr(last[1]), ctypes.byref(dims),
+                               _stream(stream))
+    if check and rc != PA_OK:
+        raise PagedAttnError(name, rc)
+    return rc
 
 
 def pa_kv_append_q4(k_new, v_new, block_table, context_lens, k_pages, v_pages, dims: PaDims, query_start_loc=None,
                     stream=None, check=True) -> int:
     """int pa_kv_append_q4(...): quantise the new tokens' K/V into the 4-bit pools."""
-    _check_q4(dims, (k_new, v_new), (k_pages, v_pages), (block_table, context_lens, query_start_loc))
-    rc = load().pa_kv_append_q4(_addr(k_new), _addr(v_new), _addr(block_table), _addr(context_lens),
-                                _addr(query_start_loc), _addr(k_pages), _addr(v_pages), ctypes.byref(dims),
-                                _stream(stream))
-    if check and rc != PA_OK:
-        raise PagedAttnError("pa_kv_append_q4", rc)
-    return rc
+    return _rows_q4("pa_kv_append_q4", k_new, v_new, (k_new, v_new), block_table, context_lens, (k_pages, v_pages),
+                    dims, query_start_loc, stream, check)
 
 
 def pa_kv_read_q4(k_pages, v_pages, block_table, context_lens, k_out, v_out, dims: PaDims, query_start_loc=None,
                   stream=None, check=True) -> int:
     """int pa_kv_read_q4(...): the values that the 4-bit pools hold of the rows
     which pa_kv_append_q4 with the same arguments writes."""
-    _check_q4(dims, (k_out, v_out), (k_pages, v_pages), (block_table, context_lens, query_start_loc))
-    rc = load().pa_kv_read_q4(_addr(k_pages), _addr(v_pages), _addr(block_table), _addr(context_lens),
-                              _addr(query_start_loc), _addr(k_out), _addr(v_out), ctypes.byref(dims), _stream(stream))
-    if check and rc != PA_OK:
-        raise PagedAttnError("pa_kv_read_q4", rc)
-    return rc
+    return _rows_q4("pa_kv_read_q4", k_out, v_out, (k_pages, v_pages), block_table, context_lens, (k_out, v_out),
+                    dims, query_start_loc, stream, check)
 
 
 def paged_attn_q4(q, k_pages, v_pages, block_table, context_lens, scale, out, dims: PaDims, workspace=None,
                   stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_q4(...): decode attention over the 4-bit cache; out is
     written in place."""
-    _check_q4(dims, (q, out), (k_pages, v_pages), (block_table, context_lens))
-    ws, ws_bytes = _workspace(dims, workspace, getattr(q, "device", None), stream, pa_workspace_size_q4)
+    _check_q4(dims, dims.num_q_heads, False, (q, out), (k_pages, v_pages), block_table, context_lens, None)
+    ws, ws_bytes, owner = _workspace_q4(dims, workspace, q, stream)
     rc = load().paged_attn_q4(_addr(q), _addr(k_pages), _addr(v_pages), _addr(block_table), _addr(context_lens),
-                              float(scale), _addr(out), ctypes.byref(dims), _addr(ws), ws_bytes, _stream(stream),
+                              scale, _addr(out), ctypes.byref(dims), ws, ws_bytes, _stream(stream),
                               ctypes.byref(timing) if timing is not None else None)
     if check and rc != PA_OK:
         raise PagedAttnError("paged_attn_q4", rc)
@@ -371,11 +391,11 @@ def paged_attn_varlen_q4(q, k_pages, v_pages, block_table, context_lens, query_s
                          workspace=None, stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_varlen_q4(...): causal chunks plus decode rows over the
     4-bit cache."""
-    _check_q4(dims, (q, out), (k_pages, v_pages), (block_table, context_lens, query_start_loc))
-    ws, ws_bytes = _workspace(dims, workspace, getattr(q, "device", None), stream, pa_workspace_size_q4)
+    _check_q4(dims, dims.num_q_heads, True, (q, out), (k_pages, v_pages), block_table, context_lens, query_start_loc)
+    ws, ws_bytes, owner = _workspace_q4(dims, workspace, q, stream)
     rc = load().paged_attn_varlen_q4(_addr(q), _addr(k_pages), _addr(v_pages), _addr(block_table), _addr(context_lens),
-                                     _addr(query_start_loc), float(scale), _addr(out), ctypes.byref(dims), _addr(ws),
-                                     ws_bytes, _stream(stream), ctypes.byref(timing) if timing is not None else None)
+                                     _addr(query_start_loc), scale, _addr(out), ctypes.byref(dims), ws, ws_bytes,
+                                     _stream(stream), ctypes.byref(timing) if timing is not None else None)
     if check and rc != PA_OK:
         raise PagedAttnError("paged_attn_varlen_q4", rc)
     return rc

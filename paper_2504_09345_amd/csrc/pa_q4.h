@@ -85,7 +85,9 @@ constexpr int kQ4StreamWaves = 4096;   // waves of a launch: ranges times W
 constexpr int kQ4StreamThreads = 512;  // of a workgroup: 8 / W teams
 
 constexpr int q4_waves(int H_kv) { return H_kv % 8 == 0 ? 8 : H_kv % 4 == 0 ? 4 : H_kv % 2 == 0 ? 2 : 1; }
-int q4_stream_occupancy(int dtype, int D, int s, int W);  // workgroups per CU, 0 on error
+// Workgroups that the current device holds at once, at most as many as a launch may
+// have; 0 on error.
+int q4_stream_workgroups(int dtype, int D, int s, int W);
 hipError_t launch_q4_stream(int dtype, int D, int s, int W, const Q4StreamArgs& a, int workgroups, hipStream_t st, KernelEvents ev);
 template <typename T, int D> const void* q4_stream_pick(int s, int W);
 

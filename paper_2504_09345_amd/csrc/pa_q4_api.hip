@@ -190,14 +190,8 @@ int attend(const void* q, const void* k_pages, const void* v_pages, const int32_
     if (p.n_split > 1 && pa::launch_q4_merge(d->dtype, d->head_dim, a, stream) != hipSuccess) return PA_EHIP;
   }
   if (p.stream) {
-    int dev = 0, cus = 0;
-    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
-      return PA_EHIP;
-    const int per_cu = pa::q4_stream_occupancy(d->dtype, d->head_dim, p.s, p.W);
-    if (per_cu <= 0) return PA_EHIP;
-    int workgroups = cus * per_cu;
-    const int most = pa::kQ4StreamWaves * 64 / pa::kQ4StreamThreads;
-    if (workgroups > most) workgroups = most;
+    const int workgroups = pa::q4_stream_workgroups(d->dtype, d->head_dim, p.s, p.W);
+    if (workgroups <= 0) return PA_EHIP;
     pa::Q4StreamArgs a{};
     a.k_pages = static_cast<const uint8_t*>(k_pages);
     a.v_pages = static_cast<const uint8_t*>(v_pages);

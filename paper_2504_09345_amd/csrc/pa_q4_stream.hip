@@ -14,6 +14,9 @@
 //    products, one unit ahead, and four waves per SIMD keep 70 KB per CU in flight.
 #include "pa_q4_stream.h"
 
+#include <algorithm>
+#include <atomic>
+
 namespace pa {
 
 extern template const void* q4_stream_pick<uint16_t, 64>(int, int);
@@ -29,10 +32,22 @@ static const void* q4_stream_fn(int dtype, int D, int s, int W) {
   return nullptr;
 }
 
-int q4_stream_occupancy(int dtype, int D, int s, int W) {
+// (a property of the kernel and the device, so it is asked for once: the two
+// queries take as long as the rest of a small call on the host)
+int q4_stream_workgroups(int dtype, int D, int s, int W) {
+  constexpr int kDevices = 64;
+  static std::atomic<int> known[kDevices][2][2][9][9];
+  int dev = 0, cus = 0, per_cu = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return 0;
+  std::atomic<int>* at = dev >= 0 && dev < kDevices && dtype >= 0 && dtype < 2 && s <= 8 && W <= 8 ? &known[dev][dtype][D / 128][s][W] : nullptr;
+  int n = at != nullptr ? at->load(std::memory_order_relaxed) : 0;
+  if (n > 0) return n;
   const void* fn = q4_stream_fn(dtype, D, s, W);
-  int n = 0;
-  if (fn == nullptr || hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, fn, kQ4StreamThreads, 0) != hipSuccess) return 0;
+  if (fn == nullptr || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
+      hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, fn, kQ4StreamThreads, 0) != hipSuccess)
+    return 0;
+  n = std::min(cus * per_cu, kQ4StreamWaves * 64 / kQ4StreamThreads);
+  if (at != nullptr) at->store(n, std::memory_order_relaxed);
   return n;
 }
 
