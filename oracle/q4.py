@@ -112,13 +112,15 @@ def dense(which, pool, block_table, b, C, D):
 
 
 def attention(q, k_pages, v_pages, block_table, context_lens, scale, query_start_loc=None):
-    """(out, spread, size) in float64 [rows][H_q][D]: the attention, sum_t w_t
-    |v_t|, and per (row, head) the largest scale * sum_d |q_d k_d| of its keys.
-    Rows of no sequence are NaN; of an empty decode context 0."""
+    """(out, spread, mass, size, reach) in float64: the attention [rows][H_q][D],
+    sum_t w_t |v_t|, sum_t |v_t|, and per (row, head) the largest scale * sum_d |q_d k_d| and scale *
+    max_d |q_d| * sum_d |k_d| of its keys.  Rows of no sequence are NaN; of an empty
+    decode context 0."""
     rows, H_q, D = q.shape
     H_kv = k_pages.shape[1]
     s = H_q // H_kv
     out, spread, size = np.full(q.shape, np.nan), np.full(q.shape, np.nan), np.zeros((rows, H_q))
+    mass, reach = np.zeros(q.shape), np.zeros((rows, H_q))
     for b, C in enumerate(int(c) for c in context_lens):
         r0, r1 = (b, b + 1) if query_start_loc is None else (int(query_start_loc[b]), int(query_start_loc[b + 1]))
         if C == 0:
@@ -137,5 +139,7 @@ def attention(q, k_pages, v_pages, block_table, context_lens, scale, query_start
                     w = np.exp(x - x.max())
                     w /= w.sum()
                     out[r, h], spread[r, h] = w @ v[g, :n], w @ np.abs(v[g, :n])
+                mass[r, h] = np.abs(v[g, :n]).sum(0)
                 size[r, h] = scale * np.abs(qk).sum(-1).max()
-    return out, spread, size
+                reach[r, h] = scale * np.abs(q[r, h]).max() * np.abs(k[g, :n]).sum(-1).max()
+    return out, spread, mass, size, reach

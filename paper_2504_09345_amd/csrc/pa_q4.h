@@ -71,7 +71,7 @@ struct Q4StreamArgs {
   // wave, as in StreamArgs
   float* ws_o;
   float* ws_ml;
-  unsigned long long* ws_flag;  // a counter per range
+  unsigned long long* ws_flag;  // a counter per range and wave, kQ4CounterStride apart
   CounterKey key;
   int64_t bt_stride;
   float scale_log2;
@@ -83,6 +83,7 @@ struct Q4StreamArgs {
 constexpr int kQ4StreamSeqs = 8192;    // sequences of a launch
 constexpr int kQ4StreamWaves = 4096;   // waves of a launch: ranges times W
 constexpr int kQ4StreamThreads = 512;  // of a workgroup: 8 / W teams
+constexpr int kQ4CounterStride = 16;   // 128 bytes: atomics on one line follow each other 30 ns apart
 
 constexpr int q4_waves(int H_kv) { return H_kv % 8 == 0 ? 8 : H_kv % 4 == 0 ? 4 : H_kv % 2 == 0 ? 2 : 1; }
 // Workgroups that the current device holds at once, at most as many as a launch may

@@ -111,7 +111,7 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
     const size_t recs = (size_t)pa::kQ4StreamWaves * 2 * s;
     p->st_o = align256(recs * d->head_dim * sizeof(float));
     p->st_ml = align256(recs * 2 * sizeof(float));
-    p->st_flag = align256((size_t)pa::kQ4StreamWaves / p->W * sizeof(unsigned long long));
+    p->st_flag = align256((size_t)pa::kQ4StreamWaves * pa::kQ4CounterStride * sizeof(unsigned long long));
   }
   if (p->chunks) {
     p->min_rows = p->stream ? 2 : 1;

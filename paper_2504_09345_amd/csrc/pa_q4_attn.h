@@ -38,7 +38,8 @@ __device__ __forceinline__ Q4Item q4_item(const Q4AttnArgs& a, int slot, int pos
 }
 
 template <typename T, int D, int NB>
-__global__ __launch_bounds__(64 * kQ4Waves) void q4_attn_kernel(Q4AttnArgs a) {
+__global__ __launch_bounds__(64 * kQ4Waves) __attribute__((amdgpu_waves_per_eu(NB <= 2 ? 2 : 1)))
+void q4_attn_kernel(Q4AttnArgs a) {
   const int S = a.s;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -51,7 +52,8 @@ __global__ __launch_bounds__(64 * kQ4Waves) void q4_attn_kernel(Q4AttnArgs a) {
   } else {  // row blocks of one head side by side
     split = blockIdx.x % a.n_split;
     g = blockIdx.x / a.n_split % a.H_kv;
-    slot = blockIdx.x / a.n_split / a.H_kv * kQ4Waves + wave;
+    // (the last blocks of a sequence see the most keys: they start first)
+    slot = (gridDim.x / a.n_split / a.H_kv - 1 - blockIdx.x / a.n_split / a.H_kv) * kQ4Waves + wave;
   }
   if (slot >= a.n_slots) return;
   const Q4Item it = q4_item(a, slot, q4_positions(NB, S), lane);
@@ -85,47 +87,84 @@ __global__ __launch_bounds__(64 * kQ4Waves) void q4_attn_kernel(Q4AttnArgs a) {
 
   const int n_pages = all_last / kPage + 1;
   const int64_t tile = q4_tile_bytes(D), page_bytes = tile * a.H_kv;
+  const int tile_size = a.num_pages > 0 ? q4_tile_bytes(D) : 0;
   const uint8_t* kg = a.k_pages + g * tile;
   const uint8_t* vg = a.v_pages + g * tile;
   const int32_t* table = a.block_table + (int64_t)it.b * a.bt_stride;
-  // lane i: entry of page 64 (u / 32) + i
-  int ids = 0;
-  auto fetch = [&](q4::Unit<D>& u, int at_unit, int& bad) {
-    if ((at_unit & 31) == 0 || at_unit == u0) {
-      const int p = (at_unit >> 5) * 64 + lane;
-      ids = p < n_pages ? table[p] : 0;
+  // lane i: entries of page 64 (k / 32) + i of the present unit k and of the 64 after
+  auto entries = [&](int k) {
+    const int p = (k >> 5) * 64 + lane;
+    return p < n_pages ? table[p] : 0;
+  };
+  int ids = entries(u0), ids_after = entries(u0 + 32);
+  struct Pages {
+    int64_t at[2];
+    int bad;  // bit p: page p's entry lies outside the pool
+  };
+  auto pages = [&](int k) {  // (wave-uniform; k goes up by one from call to call)
+    if ((k & 31) == 0 && k != u0) {
+      ids = ids_after;
+      ids_after = entries(k + 32);
     }
-    bad = 0;
+    Pages t{{0, 0}, 0};
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const bool there = 2 * at_unit + p < n_pages;
-      const int id = __builtin_amdgcn_readlane(ids, (2 * at_unit + p) & 63);
-      const bool ok = there && id >= 0 && id < a.num_pages;
-      bad |= (there && !ok) << p;
-      const int64_t off = ok ? id * page_bytes : 0;
-      q4::load_k<D>(u, p, kg + off, ok, lane);
-      q4::load_v<D>(u, p, vg + off, ok, lane);
+      const int id = __builtin_amdgcn_readlane(ids, (2 * k + p) & 63);
+      const bool ok = id >= 0 && id < a.num_pages;
+      t.at[p] = ok ? id * page_bytes : 0;
+      t.bad |= (ok ? 0 : 1) << p;
     }
+    return t;
   };
   q4::Unit<D> u;
-  int bad;
-  fetch(u, u0, bad);
-  for (int k = u0; k < u1; ++k) {
-    q4::Unit<D> next = u;
-    int next_bad = 0;
-    if (k + 1 < u1) fetch(next, k + 1, next_bad);
-    const int key0 = k * kQ4Unit;
-    const bool edge = key0 + kQ4Unit - 1 > it.last0;
+  auto fetch_k = [&](const Pages& t, bool any) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) q4::load_k<D>(u, p, kg + t.at[p], any ? tile_size : 0, lane);
+  };
+  auto fetch_v = [&](const Pages& t, bool any) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) q4::load_v<D>(u, p, vg + t.at[p], any ? tile_size : 0, lane);
+  };
+  Pages t = pages(u0);
+  fetch_k(t, true);
+  fetch_v(t, true);
+  constexpr bool kF16 = q4::kF16<T>;
+  const int u_full = min(u1, (it.last0 + 1) / kQ4Unit);  // units before are seen whole by every column
+  for (int k = u0; k < u1;) {
     q4::f32x4_t s[NB][2];
-    u32x4 pt[NB][q4::kPParts<T>];
-    q4::fold_qk<T, D, NB>(st, u, bad, s);
-    q4::fold_softmax<T, D, NB>(st, s, key0, edge, a.scale_log2, lane, pt);
-    if (edge)
-      q4::fold_pv_edge<T, D, NB>(st, u, pt, key0, all_last, lane);
-    else
-      q4::fold_pv<T, D, NB>(st, u, pt);
-    u = next;
-    bad = next_bad;
+    float x[NB][8];
+    Pages next = t;
+    bool formed = false;  // the unit's weights are there, but V is beyond fp16
+#pragma unroll 1
+    for (; k < u_full && t.bad == 0; ++k) {  // (nothing but the usual unit, so that the sums stay in place)
+      const bool more = k + 1 < u1;
+      if (more) next = pages(k + 1);
+      q4::fold_qk<T, D, NB>(st, u, s);
+      fetch_k(next, more);
+      q4::fold_softmax<T, D, NB>(st, s, a.scale_log2, x);
+      if (kF16 && q4::beyond_fp16<D>(u)) {
+        formed = true;
+        break;
+      }
+      q4::fold_pv<kF16, T, D, NB>(st, u, x);
+      fetch_v(next, more);
+      t = next;
+    }
+    if (k >= u1) break;
+    const bool more = k + 1 < u1;
+    if (more && !formed) next = pages(k + 1);
+    if (formed) {
+      q4::fold_pv<false, T, D, NB>(st, u, x);
+    } else {
+      q4::fold_qk<T, D, NB>(st, u, s);
+      fetch_k(next, more);
+      q4::mask_scores<T, D, NB>(st, k * kQ4Unit, t.bad, lane, s);
+      q4::fold_softmax<T, D, NB>(st, s, a.scale_log2, x);
+      q4::fold_pv_edge<T, D, NB>(st, u, x, k * kQ4Unit, all_last, lane);
+    }
+    fetch_v(next, more);
+    t = next;
+    ++k;
   }
 
 #pragma unroll

@@ -35,21 +35,24 @@ struct Q4Record {
 };
 
 struct Q4UnitEntry {
-  int32_t page[2];  // -1: outside the pool, or no page
-  int32_t info;     // tokens (6 bits) | item start | item end | head block
+  int64_t at[2];  // the pages' first byte of the head block (0: outside the pool, or no page)
+  int32_t info;   // tokens (6 bits) | page 0, 1 outside the pool | anything but 32 tokens of the pool | head block
+  int32_t left;   // units to the item's end, this one included
   int32_t row;
+  int32_t first;  // whether it is the item's first
 };
 
 template <int W>
 struct Q4StreamSmem {
   static constexpr int kTeams = kQ4StreamThreads / 64 / W;
-  static constexpr int kUnits = 2048 / kTeams;  // of a table
+  static constexpr int kUnits = 1024 / kTeams;  // of a table
   int32_t cum[kQ4StreamSeqs + 1];               // units of the sequences before, per head block
   int32_t scan[kQ4StreamThreads / 64];
   struct Team {
     Q4UnitEntry unit[kUnits];
-    Q4Cut cut[2];
-    int32_t last[2];
+    Q4Cut cut[2];          // the items cut by the range's start and by its end (x0 = -1: none)
+    int32_t job[W][2][2];  // their row and KV head
+    int32_t last_row, last_hb;  // of the range's last unit
   } team[kTeams];
 };
 
@@ -70,8 +73,96 @@ __device__ __forceinline__ int q4_decode_row(const Q4StreamArgs& a, int b, int& 
   return nv == 0 ? 2 : 1;
 }
 
+// Join n <= 64 records of an item, those of ranges xs, xs + step, .. (record slot 1
+// of the item's first range x0, slot 0 of the others), in range order, by one wave;
+// lane l takes the records' 16-byte chunks l, l + 64, ..  final: normalise and write
+// the output; otherwise the joined record takes the first one's place.  Records
+// bypass the L2 (a round trip of 1 to 2 us), so all (m, l), record i by lane i, and
+// the first kBatch records' outputs are loaded at once.
 template <typename T, int D, int S, int W>
-__global__ __launch_bounds__(kQ4StreamThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 4 : 2)))
+__device__ __forceinline__ void q4_join(const Q4StreamArgs& a, int x0, int xs, int step, int n, bool final, int w, int lane, T* out) {
+  using Rec = Q4Record<D, S>;
+  constexpr int kChunks = S * D / 4, C = (kChunks + 63) / 64;  // chunks per lane
+  constexpr int kBatch = 4;  // (8 are no faster)
+  asm volatile("" ::: "memory");  // (the loads stay below the arrival)
+  auto slot = [&](int i) {
+    const int x = xs + i * step;
+    return ((int64_t)x * 2 + (x == x0 ? 1 : 0)) * W + w;
+  };
+  f32x4_dev_t v[kBatch][C];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {  // (past the last record: that one again, unused)
+      const __amdgpu_buffer_rsrc_t r = record_rsrc(a.ws_o + slot(min(i0 + b, n - 1)) * S * D, S * D);
+#pragma unroll
+      for (int u = 0; u < C; ++u) v[b][u] = load_dev4(r, (u * 64 + lane) * 4);
+    }
+  };
+  // lane i: record i's bases and sums, then its weight for each head
+  float c[S], l[S], M[S], L[S];
+  {
+    const float* ml = a.ws_ml + slot(min(lane, n - 1)) * S * 2;
+#pragma unroll
+    for (int j = 0; j < S; ++j) load_dev2(ml + j * 2, c[j], l[j]);
+  }
+  load(0);
+#pragma unroll
+  for (int j = 0; j < S; ++j) {
+    M[j] = across_groups_max<1>(c[j]);
+    c[j] = fast_exp2(c[j] - M[j]);
+    L[j] = 0.0f;
+  }
+  auto bcast = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
+  // value of head h among the S wave-uniform ones (chosen between as values: an array
+  // indexed at run time would move to memory)
+  auto pick = [&](const float (&x)[S], int h) {
+    float y = x[0];
+#pragma unroll
+    for (int j = 1; j < S; ++j) {
+      const float xj = x[j];
+      y = h == j ? xj : y;
+    }
+    return y;
+  };
+  f32x4_dev_t acc[C];
+#pragma unroll
+  for (int u = 0; u < C; ++u) acc[u] = f32x4_dev_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += kBatch) {
+    if (i0 > 0) load(i0);
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      if (i0 + b < n) {  // wave-uniform
+        float ci[S];
+#pragma unroll
+        for (int j = 0; j < S; ++j) {
+          ci[j] = bcast(c[j], i0 + b);
+          L[j] = fmaf(bcast(l[j], i0 + b), ci[j], L[j]);
+        }
+#pragma unroll
+        for (int u = 0; u < C; ++u) acc[u] = v[b][u] * pick(ci, Rec::head(u * 64 + lane)) + acc[u];
+      }
+    }
+  }
+  const __amdgpu_buffer_rsrc_t r = record_rsrc(a.ws_o + slot(0) * S * D, S * D);
+#pragma unroll
+  for (int u = 0; u < C; ++u) {
+    const int ch = u * 64 + lane;
+    if (final) {
+      const f32x4_dev_t o = acc[u] * (1.0f / pick(L, Rec::head(ch)));
+      if (kChunks % 64 == 0 || ch < kChunks) q4::store_four(out + Rec::head(ch) * D + Rec::dim(ch), o);
+    } else {
+      store_dev4(r, ch * 4, acc[u]);  // (a chunk past the record is out of the descriptor's range)
+    }
+  }
+  if (!final && lane == 0) {
+#pragma unroll
+    for (int j = 0; j < S; ++j) store_dev(a.ws_ml + slot(0) * S * 2 + j * 2, M[j], L[j]);
+  }
+}
+
+template <typename T, int D, int S, int W>
+__global__ __launch_bounds__(kQ4StreamThreads) __attribute__((amdgpu_waves_per_eu(2)))
 void q4_stream_kernel(Q4StreamArgs a) {
   using Sm = Q4StreamSmem<W>;
   using Rec = Q4Record<D, S>;
@@ -114,8 +205,13 @@ void q4_stream_kernel(Q4StreamArgs a) {
   const int U = a.nb * sm.cum[R];
   const int G = max(1, min(n_wg * kTeams, U));  // ranges
   if (wg >= G || U == 0) return;
-  auto begin_of = [&](int x) { return (int)((uint64_t)U * (uint32_t)min(x, G) / (uint32_t)G); };
-  auto range_of = [&](int e) { return (int)(((uint64_t)(e + 1) * (uint32_t)G - 1) / (uint32_t)U); };
+  // ranges of each or each + 1 units, the longer ones first
+  const int each = U / G, longer = U % G;
+  auto begin_of = [&](int x) { return min(x, G) * each + min(x, longer); };
+  auto range_of = [&](int e) {
+    const int split = longer * (each + 1);
+    return e < split ? e / (each + 1) : longer + (e - split) / each;
+  };
   auto units_of = [&](int x) { return begin_of(x + 1) - begin_of(x); };
   const int u0 = begin_of(bid);
   const int n_units = units_of(bid);
@@ -128,24 +224,74 @@ void q4_stream_kernel(Q4StreamArgs a) {
   const int n = lane & 15, Gl = lane >> 4;
   const int64_t tile = q4_tile_bytes(D);
   T* out = reinterpret_cast<T*>(a.out);
-  bool head_partial = false;
-  bool stored[2] = {false, false};  // this team's part of the item cut by the range's start, by its end
-  int job_row[2] = {0, 0}, job_g[2] = {0, 0};
-  auto entry = [&](int i) {
+  const uint8_t* kw = a.k_pages + w * tile;
+  const uint8_t* vw = a.v_pages + w * tile;
+  struct Tiles {
+    int64_t at[2];
+    int info;
+  };
+  auto tiles = [&](int i) {  // (wave-uniform)
     const Q4UnitEntry& e = tm.unit[i];
-    return Q4UnitEntry{{__builtin_amdgcn_readfirstlane(e.page[0]), __builtin_amdgcn_readfirstlane(e.page[1])},
-                       __builtin_amdgcn_readfirstlane(e.info), __builtin_amdgcn_readfirstlane(e.row)};
-  };
-  auto tile_at = [&](const Q4UnitEntry& e, int p) {
-    return ((int64_t)max(e.page[p], 0) * a.H_kv + (e.info >> 8) * W + w) * tile;
-  };
-  auto fetch_k = [&](const Q4UnitEntry& e) {
+    Tiles t;
 #pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_k<D>(u, p, a.k_pages + tile_at(e, p), e.page[p] >= 0, lane);
+    for (int p = 0; p < 2; ++p)
+      t.at[p] = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(e.at[p] >> 32)) << 32 |
+                          (uint32_t)__builtin_amdgcn_readfirstlane((int)e.at[p]));
+    t.info = __builtin_amdgcn_readfirstlane(e.info);
+    return t;
   };
-  auto fetch_v = [&](const Q4UnitEntry& e) {
+  const int tile_size = a.num_pages > 0 ? q4_tile_bytes(D) : 0;
+  auto fetch_k = [&](const Tiles& e, bool any) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_v<D>(u, p, a.v_pages + tile_at(e, p), e.page[p] >= 0, lane);
+    for (int p = 0; p < 2; ++p) q4::load_k<D>(u, p, kw + e.at[p], any ? tile_size : 0, lane);
+  };
+  auto fetch_v = [&](const Tiles& e, bool any) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) q4::load_v<D>(u, p, vw + e.at[p], any ? tile_size : 0, lane);
+  };
+
+  // Items cut by the range's ends.  Each wave is alone: a part is its record in the
+  // workspace and one count of the item's counter for this wave's head.  Whichever
+  // part counts last joins all of them in range order; nothing waits on another
+  // workgroup.  The item that the start cuts (job 0), its record stored at the end of
+  // unit k, counts when unit k + 3 starts: the vector-memory counter retires in issue
+  // order, and unit k + 2, whose loads went out after the record, has been folded.
+  // It looks at the answer when the range has streamed.  The item that the end cuts
+  // (job 1) has usually one other part, which was the first thing of the next range:
+  // its count is looked at before the last unit, and if it is there the wave joins
+  // its record from registers and stores none of its own.
+  auto counter_at = [&](int x) {
+    unsigned long long* p = a.ws_flag + ((int64_t)x * W + w) * kQ4CounterStride;
+    asm("" : "+v"(p));  // (an address of lanes: one atomic, not a wave's reduction)
+    return DeviceCounter{p};
+  };
+  auto level_of = [&](const Q4Cut& cut) { return cut.grouped() && !cut.group_of_one(bid) ? 0 : 1; };
+  bool stored[2] = {false, false};
+  int counted_at = INT32_MAX;  // job 0 counts before this unit
+  bool counted = false;
+  uint64_t counted_old = 0;    // the counter before
+  uint64_t seen = 0;           // the last item's counter
+  bool look = false;           // whether it has been read
+  bool head_partial = false, open = false;  // of the present item: it began before the range; it has not ended
+  auto store_part = [&](int which, float l, int row, int g) {
+    const int64_t slot = ((int64_t)bid * 2 + which) * W + w;
+    const __amdgpu_buffer_rsrc_t r = record_rsrc(a.ws_o + slot * S * D, S * D);
+    if (n < S) {
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        float o[8];
+        q4::eight_out(st, 0, j, o);
+        store_dev4(r, Rec::chunk(n, 2 * j, Gl) * 4, f32x4_dev_t{o[0], o[1], o[2], o[3]});
+        store_dev4(r, Rec::chunk(n, 2 * j + 1, Gl) * 4, f32x4_dev_t{o[4], o[5], o[6], o[7]});
+      }
+      if (Gl == 0) store_dev(a.ws_ml + (slot * S + n) * 2, st.m[0], l);
+    }
+    if (lane == 0) {
+      tm.job[w][which][0] = row;
+      tm.job[w][which][1] = g;
+    }
+    stored[0] |= which == 0;
+    stored[1] |= which == 1;
   };
 
   for (int base = 0; base < n_steps; base += Sm::kUnits) {
@@ -160,120 +306,175 @@ void q4_stream_kernel(Q4StreamArgs a) {
       const int hb = rem / np, p = rem - hb * np;
       const int left = a.context_lens[r] - p * kQ4Unit;  // tokens from the unit on
       Q4UnitEntry e;
+      int odd = 0;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        e.page[h] = left > kPage * h ? a.block_table[(int64_t)r * a.bt_stride + 2 * p + h] : -1;
-        if (e.page[h] < 0 || e.page[h] >= a.num_pages) e.page[h] = -1;
+        const int page = left > kPage * h ? a.block_table[(int64_t)r * a.bt_stride + 2 * p + h] : 0;
+        const bool ok = page >= 0 && page < a.num_pages;
+        odd |= (ok || left <= kPage * h ? 0 : 1) << h;
+        e.at[h] = ok ? ((int64_t)page * a.H_kv + hb * W) * tile : 0;
       }
-      e.info = min(left, kQ4Unit) | (p == 0) << 6 | (p == np - 1) << 7 | hb << 8;
+      e.info = min(left, kQ4Unit) | odd << 6 | (odd != 0 || left < kQ4Unit) << 8 | hb << 9;
+      e.left = np - p;
       e.row = a.query_start_loc != nullptr ? a.query_start_loc[r] : r;
+      e.first = p == 0;
       tm.unit[i] = e;
-      const Q4Cut cut{range_of(x - p), range_of(x - p + np - 1)};
-      if (base + i == 0) tm.cut[0] = p == 0 ? Q4Cut{-1, -1} : cut;
-      if (base + i == n_units - 1) tm.cut[1] = p == np - 1 ? Q4Cut{-1, -1} : cut;
+      if (base + i == 0) tm.cut[0] = p == 0 ? Q4Cut{-1, -1} : Q4Cut{range_of(x - p), range_of(x - p + np - 1)};
+      if (base + i == n_units - 1) tm.last_row = e.row, tm.last_hb = hb;
+      if (base + i == n_units - 1) tm.cut[1] = p == np - 1 ? Q4Cut{-1, -1} : Q4Cut{range_of(x - p), range_of(x - p + np - 1)};
     }
     __syncthreads();
     if (m <= 0) continue;
+    const bool has_next = base + m == n_units && tm.cut[1].x0 == bid && tm.cut[1].x1 == bid + 1;
 
-    // 3. stream the units: wave w handles KV head hb * W + w of every unit
-    Q4UnitEntry e = entry(0);
-    fetch_k(e);
-    fetch_v(e);
-    for (int i = 0; i < m; ++i) {
-      const int k = base + i, tokens = e.info & 63;
-      const int64_t at = (int64_t)e.row * a.H_q + (int64_t)((e.info >> 8) * W + w) * S + n;
-      if ((e.info >> 6 & 1) || k == 0) {
-        head_partial = !(e.info >> 6 & 1);
-        q4::load_query<T, D>(st.q[0], n < S ? reinterpret_cast<const T*>(a.q) + at * D : nullptr, lane);
+    // 3. stream the units: wave w handles KV head hb * W + w of every unit, the next
+    // unit's K loaded as soon as the scores are formed, its V after the products
+    Tiles t = tiles(0);
+    fetch_k(t, true);
+    fetch_v(t, true);
+    for (int i = 0; i < m;) {
+      const Q4UnitEntry& e = tm.unit[i];
+      const int left = __builtin_amdgcn_readfirstlane(e.left);
+      const int g = (__builtin_amdgcn_readfirstlane(e.info) >> 9) * W + w;
+      const int row = __builtin_amdgcn_readfirstlane(e.row);
+      const int64_t at = ((int64_t)row * a.H_q + (int64_t)g * S + n) * D;
+      if (__builtin_amdgcn_readfirstlane(e.first) || base + i == 0) {
+        head_partial = !__builtin_amdgcn_readfirstlane(e.first);
+        q4::load_query<T, D>(st.q[0], n < S ? reinterpret_cast<const T*>(a.q) + at : nullptr, lane);
         q4::reset(st);
+        open = true;
       }
-      const Q4UnitEntry next = entry(min(i + 1, m - 1));
-      const int bad = (e.page[0] < 0 ? 1 : 0) | (e.page[1] < 0 && tokens > kPage ? 2 : 0);
-      q4::f32x4_t s[1][2];
-      u32x4 pt[1][q4::kPParts<T>];
-      q4::fold_qk<T, D, 1>(st, u, bad, s);
-      if (i + 1 < m) fetch_k(next);
-      st.last[0] = tokens - 1;
-      q4::fold_softmax<T, D, 1>(st, s, 0, tokens < kQ4Unit, a.scale_log2, lane, pt);
-      if (tokens < kQ4Unit) q4::clear_dead(u, 0, tokens - 1, lane);
-      q4::fold_pv<T, D, 1>(st, u, pt);
-      if (i + 1 < m) fetch_v(next);
-      if ((e.info >> 7 & 1) || k == n_units - 1) {
-        const bool tail_partial = !(e.info >> 7 & 1);
-        const float l = rows4_sum(st.l[0]);
-        if (!head_partial && !tail_partial) {  // the whole item in this range
-          const float inv = 1.0f / l;
-          if (n < S) {
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j) {
-              float o[8];
-              q4::eight_out(st, 0, j, o);
-#pragma unroll
-              for (int x = 0; x < 8; ++x) o[x] *= inv;
-              q4::store_eight(out + at * D + 32 * j + 8 * Gl, o);
-            }
+      // units without anything else to do between them
+      int stop = min(m, i + left);
+      if (base + i == counted_at) {
+        asm volatile("" ::: "memory");
+        const Q4Cut cut = tm.cut[0];
+        if (lane == 0) counted_old = counter_at(cut.counter(level_of(cut), bid)).fetch_add(a.key.step);
+        counted = true;
+      }
+      if (counted_at > base + i) stop = min(stop, counted_at - base);
+      if (has_next) {
+        if (i < m - 1) stop = min(stop, m - 1);
+        else seen = __hip_atomic_load(counter_at(bid).p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), look = true;
+      }
+      const bool ends = stop == i + left;
+      while (i < stop) {
+        constexpr bool kF16 = q4::kF16<T>;
+        q4::f32x4_t s[1][2];
+        float x[1][8];
+        bool formed = false;  // the unit's weights are there, but V is beyond fp16
+#pragma unroll 1
+        for (; i < stop && !(t.info & 256); ++i) {  // (nothing but the usual unit, so that the sums stay in place)
+          const bool more = i + 1 < m;
+          const Tiles next = tiles(more ? i + 1 : i);
+          q4::fold_qk<T, D, 1>(st, u, s);
+          fetch_k(next, more);
+          q4::fold_softmax<T, D, 1>(st, s, a.scale_log2, x);
+          if (kF16 && q4::beyond_fp16<D>(u)) {
+            formed = true;
+            break;
           }
-        } else {
-          const int which = head_partial ? 0 : 1;
-          const int64_t slot = ((int64_t)bid * 2 + which) * W + w;
-          const __amdgpu_buffer_rsrc_t r = record_rsrc(a.ws_o + slot * S * D, S * D);
-          if (n < S) {
+          q4::fold_pv<kF16, T, D, 1>(st, u, x);
+          fetch_v(next, more);
+          t = next;
+        }
+        if (i >= stop) break;
+        const bool more = i + 1 < m;
+        const Tiles next = tiles(more ? i + 1 : i);
+        if (!formed) {
+          const int tokens = t.info & 63;
+          q4::fold_qk<T, D, 1>(st, u, s);
+          fetch_k(next, more);
+          st.last[0] = tokens - 1;
+          q4::mask_scores<T, D, 1>(st, 0, t.info >> 6 & 3, lane, s);
+          q4::fold_softmax<T, D, 1>(st, s, a.scale_log2, x);
+          q4::clear_dead(u, 0, tokens - 1, lane);
+        }
+        q4::fold_pv<false, T, D, 1>(st, u, x);
+        fetch_v(next, more);
+        t = next;
+        ++i;
+      }
+      if (!ends) continue;
+      // the item ends: its output, or the record of this range's part of it
+      const float l = rows4_sum(st.l[0]);
+      if (!head_partial) {
+        const float inv = 1.0f / l;
+        if (n < S) {
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) {
-              float o[8];
-              q4::eight_out(st, 0, j, o);
-              store_dev4(r, Rec::chunk(n, 2 * j, Gl) * 4, f32x4_dev_t{o[0], o[1], o[2], o[3]});
-              store_dev4(r, Rec::chunk(n, 2 * j + 1, Gl) * 4, f32x4_dev_t{o[4], o[5], o[6], o[7]});
-            }
-            if (Gl == 0) store_dev(a.ws_ml + (slot * S + n) * 2, st.m[0], l);
+          for (int j = 0; j < D / 32; ++j) {
+            float o[8];
+            q4::eight_out(st, 0, j, o);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) o[x] *= inv;
+            q4::store_eight(out + at + 32 * j + 8 * Gl, o);
           }
-          const int g = (e.info >> 8) * W + w;
-          stored[0] |= which == 0;
-          stored[1] |= which == 1;
-          job_row[0] = which == 0 ? e.row : job_row[0];
-          job_row[1] = which == 1 ? e.row : job_row[1];
-          job_g[0] = which == 0 ? g : job_g[0];
-          job_g[1] = which == 1 ? g : job_g[1];
+        }
+      } else {
+        store_part(0, l, row, g);
+        counted_at = base + i + 2;  // (i: the unit after)
+      }
+      open = false;
+    }
+  }
+  if (open) {  // the range ends inside an item
+    const float l = rows4_sum(st.l[0]);
+    const int row = __builtin_amdgcn_readfirstlane(tm.last_row), g = __builtin_amdgcn_readfirstlane(tm.last_hb) * W + w;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)seen), hi = __builtin_amdgcn_readfirstlane((uint32_t)(seen >> 32));
+    if (look && ((uint64_t)hi << 32 | lo) == a.key.step) {  // its other part has counted: join it from registers
+      asm volatile("" ::: "memory");  // (the record's loads stay below the look at the counter)
+      const int64_t slot = ((int64_t)(bid + 1) * 2) * W + w;
+      const __amdgpu_buffer_rsrc_t r = record_rsrc(a.ws_o + slot * S * D, S * D);
+      const int nn = min(n, S - 1);
+      float m1, l1;
+      f32x4_dev_t o1[D / 16];
+      load_dev2(a.ws_ml + (slot * S + nn) * 2, m1, l1);
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) o1[j] = load_dev4(r, Rec::chunk(nn, j, Gl) * 4);
+      // (q4_join's operations in its order, so the bits do not depend on who joins)
+      const float M = fmaxf(st.m[0], m1);
+      const float c0 = fast_exp2(st.m[0] - M), c1 = fast_exp2(m1 - M);
+      const float inv = 1.0f / fmaf(l1, c1, l * c0);
+      if (n < S) {
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+          float o[8];
+          q4::eight_out(st, 0, j, o);
+#pragma unroll
+          for (int x = 0; x < 8; ++x) o[x] = fmaf(o1[2 * j + x / 4][x % 4], c1, o[x] * c0) * inv;
+          q4::store_eight(out + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D + 32 * j + 8 * Gl, o);
         }
       }
-      e = next;
+      if (lane == 0) counter_at(bid).store(0);
+    } else {
+      store_part(head_partial ? 0 : 1, l, row, g);
     }
   }
 
-  // 4. join the cut items: once a part's record is stored it counts its arrival, and
-  // the part that arrives last joins all of them in range order (in two levels
-  // beyond 16 parts).  Nothing waits on another workgroup.
-  int level[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) level[j] = stored[j] && tm.cut[j].grouped() && !tm.cut[j].group_of_one(bid) ? 0 : 1;
-  StreamArgs sa{};
-  sa.ws_o = a.ws_o;
-  sa.ws_ml = a.ws_ml;
+  // 4. join the cut items
 #pragma unroll 1
-  for (int step = 0; step < 2; ++step) {
-    if (kTeams == 1 && !stored[0] && !stored[1]) break;
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0);  // the records are stored, in every wave
-    __syncthreads();
-    if (w == 0 && lane < 2 && (lane == 0 ? stored[0] : stored[1])) {
-      const Q4Cut cut = tm.cut[lane];
-      const int lv = lane == 0 ? level[0] : level[1];
-      DeviceCounter ctr{a.ws_flag + cut.counter(lv, bid)};
-      tm.last[lane] = counter_arrive(ctr, a.key, cut.parts(lv, bid));
-    }
-    __syncthreads();
+  for (int j = 0; j < 2; ++j) {
+    if (!(j == 0 ? stored[0] : stored[1])) continue;
+    const Q4Cut cut = tm.cut[j];
+    const int row = __builtin_amdgcn_readfirstlane(tm.job[w][j][0]), g = __builtin_amdgcn_readfirstlane(tm.job[w][j][1]);
+    T* o = out + ((int64_t)row * a.H_q + (int64_t)g * S) * D;
+    bool early = j == 0 && counted;
 #pragma unroll 1
-    for (int j = 0; j < 2; ++j) {
-      const bool mine = (j == 0 ? stored[0] : stored[1]) && tm.last[j];
-      const int lv = j == 0 ? level[0] : level[1];
-      if (mine) {
-        const Q4Cut cut = tm.cut[j];
-        T* o = out + ((int64_t)(j == 0 ? job_row[0] : job_row[1]) * a.H_q + (int64_t)(j == 0 ? job_g[0] : job_g[1]) * S) * D;
-        merge_records<T, D, S, W, Rec>(sa, cut.x0, cut.first(lv, bid), cut.step(lv), cut.parts(lv, bid), lv == 1, w, lane, o);
+    for (int lv = level_of(cut); lv < 2; ++lv) {
+      const int parts = cut.parts(lv, bid);
+      int last = 0;
+      if (!early) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0);  // the record is stored
       }
+      if (lane == 0) {
+        DeviceCounter ctr = counter_at(cut.counter(lv, bid));
+        last = early ? counter_answer(ctr, a.key, parts, counted_old) : counter_arrive(ctr, a.key, parts);
+      }
+      early = false;
+      if (!__builtin_amdgcn_readfirstlane(last)) break;
       // (a group's record counts in the item next)
-      if (j == 0) stored[0] = mine && lv == 0, level[0] = 1;
-      else stored[1] = mine && lv == 0, level[1] = 1;
+      q4_join<T, D, S, W>(a, cut.x0, cut.first(lv, bid), cut.step(lv), parts, lv == 1, w, lane, o);
     }
   }
 }

@@ -33,17 +33,24 @@ __device__ __forceinline__ int wave_search(int n, int x, int lane, Key key) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// The value 2^(byte - 127) of byte B of w.
+// The value 2^(byte - 127) of byte B of w: the byte as a float's exponent, in one
+// instruction (the compiler takes two for three of the four bytes).
 template <int B>
 __device__ __forceinline__ float scale_of(uint32_t w) {
-  return __uint_as_float(((w >> (8 * B)) & 0xffu) << 23);
+  uint32_t r;
+  if constexpr (B == 0) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(r) : "v"(23u), "v"(w));
+  if constexpr (B == 1) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(r) : "v"(23u), "v"(w));
+  if constexpr (B == 2) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(r) : "v"(23u), "v"(w));
+  if constexpr (B == 3) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(r) : "v"(23u), "v"(w));
+  return __uint_as_float(r);
 }
 
 // Byte B of w (two codes) times scale, as two bf16: exact for scale bytes 0 ..
-// 252, NaN for 255 (v_cvt_scalef32_pk_bf16_fp4).
-template <int B>
+// 252, NaN for 255 (v_cvt_scalef32_pk_bf16_fp4); or as two fp16, exact for 104 .. 140.
+template <int B, bool F16 = false>
 __device__ __forceinline__ uint32_t pair_of(uint32_t w, float scale) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B));
+  if constexpr (F16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, B));
+  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B));
 }
 __device__ __forceinline__ u32x4 eight_of(uint32_t w, float scale) {
   return u32x4{pair_of<0>(w, scale), pair_of<1>(w, scale), pair_of<2>(w, scale), pair_of<3>(w, scale)};
@@ -68,20 +75,18 @@ __device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int off, ui
     x[0] = w.x; x[1] = w.y;
   }
 }
-// Loads of page p (0 or 1) of a unit from the tiles at k and v; where !there,
-// nothing is read and every code and scale is 0.
+// Loads of page p (0 or 1) of a unit from the tiles at k and v; with bytes = 0 instead
+// of the tile's nothing is read, and every code and scale is 0.
 template <int D>
-__device__ __forceinline__ void load_k(Unit<D>& u, int p, const uint8_t* k, bool there, int lane) {
-  const __amdgpu_buffer_rsrc_t r =
-      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(k), (short)0, there ? q4_tile_bytes(D) : 0, 0x00020000);
+__device__ __forceinline__ void load_k(Unit<D>& u, int p, const uint8_t* k, int bytes, int lane) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(k), (short)0, bytes, 0x00020000);
   load_words<D>(r, lane * (D / 8), u.k[p]);
   u.ks[p] = __builtin_amdgcn_raw_buffer_load_b8(r, kScales<D> + (lane & 15) * (D / 32) + (lane >> 4) * D / 128, 0,
                                                 kKvLoadPolicy);
 }
 template <int D>
-__device__ __forceinline__ void load_v(Unit<D>& u, int p, const uint8_t* v, bool there, int lane) {
-  const __amdgpu_buffer_rsrc_t r =
-      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(v), (short)0, there ? q4_tile_bytes(D) : 0, 0x00020000);
+__device__ __forceinline__ void load_v(Unit<D>& u, int p, const uint8_t* v, int bytes, int lane) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(v), (short)0, bytes, 0x00020000);
   load_words<D>(r, lane * (D / 8), u.v[p]);
   load_words<D>(r, kScales<D> + (lane >> 4) * (D / 8), u.vs[p]);
 }
@@ -97,13 +102,13 @@ __device__ __forceinline__ float v_scale(const uint32_t (&vs)[kWords<D>]) {
 // (a[1]), k slots 8 G + 4 p + i the token 4 G + i of page p.  A byte holds the two
 // dims of a token, so each pair of tokens is two conversions and two byte
 // permutations.
-template <int D, int J>
+template <int D, int J, bool F16>
 __device__ __forceinline__ void v_operands(const Unit<D>& u, u32x4 (&a)[2]) {
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
     const uint32_t w = u.v[p][J];
-    const uint32_t t0 = pair_of<0>(w, v_scale<D, J, 0>(u.vs[p])), t1 = pair_of<1>(w, v_scale<D, J, 1>(u.vs[p]));
-    const uint32_t t2 = pair_of<2>(w, v_scale<D, J, 2>(u.vs[p])), t3 = pair_of<3>(w, v_scale<D, J, 3>(u.vs[p]));
+    const uint32_t t0 = pair_of<0, F16>(w, v_scale<D, J, 0>(u.vs[p])), t1 = pair_of<1, F16>(w, v_scale<D, J, 1>(u.vs[p]));
+    const uint32_t t2 = pair_of<2, F16>(w, v_scale<D, J, 2>(u.vs[p])), t3 = pair_of<3, F16>(w, v_scale<D, J, 3>(u.vs[p]));
     a[0][2 * p] = __builtin_amdgcn_perm(t1, t0, 0x05040100u);
     a[0][2 * p + 1] = __builtin_amdgcn_perm(t3, t2, 0x05040100u);
     a[1][2 * p] = __builtin_amdgcn_perm(t1, t0, 0x07060302u);
@@ -111,10 +116,41 @@ __device__ __forceinline__ void v_operands(const Unit<D>& u, u32x4 (&a)[2]) {
   }
 }
 
-// bf16 parts of a query (its type's own bits for bf16, three parts for fp32, which
-// carry its 24) and of a softmax weight.
+// How products are formed.
+//
+// Scores.  bf16 queries at head_dim 128 meet K's codes as they lie in memory: one
+// v_mfma_scale_f32_16x16x128_f8f6f4 takes a token's 128 codes and its four scales,
+// so K costs no conversion, and the queries as e4m3 in two parts.  With a column's
+// queries scaled so that the largest lies in [128, 256), the first part holds four
+// significant bits of a value and the second the four that a bf16 has left, times
+// 32: exact for values down to 2^-14 of the column's largest, and within 2^-22 of
+// that largest below.  (33 cycles per product against four of 19 for bf16 operands
+// and 16 conversions of 4.)  At head_dim 64 half of such a product would be zeros,
+// and fp32 queries would take six parts: there K becomes bf16, exactly, and the
+// queries their own bits or three bf16 parts, which carry the 24 of an fp32.
+//
+// Outputs.  For bf16 outputs the weights are rounded once, to fp16 (2^-11 of each, as
+// the chunk kernel of the 16-bit cache rounds them), and V becomes fp16, exactly where
+// its scales lie in 2^-23 .. 2^8; a unit with another scale takes V as bf16 and the
+// weights in two bf16 parts.  For fp32 outputs always bf16, in three parts.
+template <typename T, int D> constexpr bool kCodeScores = sizeof(T) == 2 && D == 128;
 template <typename T> constexpr int kQParts = sizeof(T) == 2 ? 1 : 3;
 template <typename T> constexpr int kPParts = sizeof(T) == 2 ? 2 : 3;
+template <typename T> constexpr bool kF16 = sizeof(T) == 2;
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+
+// A column's queries: the Q^T operands of its lanes.
+template <typename T, int D, bool CODES = kCodeScores<T, D>>
+struct Query {
+  u32x4 x[D / 32][kQParts<T>];  // of step s: dims D/4 (lane / 16) + 8 s .. +8
+};
+template <typename T, int D>
+struct Query<T, D, true> {
+  i32x8_t x[2];   // dims 16 (lane / 16) .. +15, then 64 more
+  uint32_t s[2];  // the parts' scale bytes
+};
 
 // x as a sum of N bf16 parts, each the rest of those before it to nearest even;
 // part i of the eight values as one operand.
@@ -137,7 +173,7 @@ __device__ __forceinline__ void split8(const float (&x)[8], u32x4 (&part)[N]) {
 // equal lane % 16.
 template <typename T, int D, int NB>
 struct State {
-  u32x4 q[NB][D / 32][kQParts<T>];  // Q^T operand of step s: dims D/4 (lane / 16) + 8 s .. +8
+  Query<T, D> q[NB];
   f32x4_t acc[NB][D / 16];          // O^T: block 2 j + h, entry i: dim 32 j + 8 (lane / 16) + 2 i + h
   float m[NB], l[NB];               // base (log2 units, one per column), the lane's part of the sum
   int last[NB];                     // last key that the column sees, -1: no column
@@ -154,19 +190,55 @@ __device__ __forceinline__ void reset(State<T, D, NB>& st) {
   }
 }
 
-// A column's queries; row: its D elements (nullptr: zeros).
+// row: the column's D elements (nullptr: zeros).  (All lanes active.)
 template <typename T, int D>
-__device__ __forceinline__ void load_query(u32x4 (&q)[D / 32][kQParts<T>], const T* row, int lane) {
+__device__ __forceinline__ void load_query(Query<T, D>& q, const T* row, int lane) {
   const int G = lane >> 4;
+  if constexpr (kCodeScores<T, D>) {
+    uint32_t f[16];
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) {
-    if constexpr (sizeof(T) == 2) {
-      q[s][0] = row != nullptr ? *reinterpret_cast<const u32x4*>(row + G * (D / 4) + 8 * s) : u32x4{0, 0, 0, 0};
-    } else {
-      float x[8];
+    for (int h = 0; h < 4; ++h) {  // 16-byte pieces: two of dims 16 G, two of 64 + 16 G
+      const u32x4 w = row != nullptr ? *reinterpret_cast<const u32x4*>(row + h / 2 * 64 + G * 16 + h % 2 * 8) : u32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = row != nullptr ? row[G * (D / 4) + 8 * s + e] : 0.0f;
-      split8(x, q[s]);
+      for (int i = 0; i < 4; ++i) f[4 * h + i] = w[i];
+    }
+    // the column's largest magnitude, as bits (those of infinities and NaN are larger)
+    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+    u16x2_t m2 = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m2 = __builtin_elementwise_max(m2, __builtin_bit_cast(u16x2_t, f[i] & 0x7fff7fffu));
+    const uint32_t most = __float_as_uint(rows4_max(__uint_as_float((uint32_t)max(m2[0], m2[1]) << 16)));
+    const bool odd = rows4_max((uint32_t)max(m2[0], m2[1]) >= 0x7f80u ? 1.0f : 0.0f) != 0.0f;
+    // 2^E: the largest over it lies in [128, 256)
+    const int byte = min(max((int)(most >> 23) - 7, 6), 250);
+    const float sc = __uint_as_float((uint32_t)byte << 23), sc_lo = __uint_as_float((uint32_t)(byte - 5) << 23);
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      typedef short s16x2_t __attribute__((ext_vector_type(2)));
+      s16x2_t hi = {0, 0}, lo = {0, 0};
+      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2_t, f[2 * w]), sc, false);
+      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2_t, f[2 * w + 1]), sc, true);
+      const uint32_t hw = __builtin_bit_cast(uint32_t, hi);
+      const f32x2_t ab = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hw, sc, false), cd = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hw, sc, true);
+      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, bf16_lo(f[2 * w]) - ab[0], bf16_hi(f[2 * w]) - ab[1], sc_lo, false);
+      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, bf16_lo(f[2 * w + 1]) - cd[0], bf16_hi(f[2 * w + 1]) - cd[1], sc_lo, true);
+      q.x[0][w] = odd ? 0 : (int)hw;
+      q.x[1][w] = odd ? 0 : __builtin_bit_cast(int, lo);
+    }
+    // (a query that is infinite or NaN: the scale of NaN, which makes every score NaN)
+    q.s[0] = odd ? 255u : (uint32_t)byte;
+    q.s[1] = (uint32_t)byte - 5u;
+  } else {
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+      if constexpr (sizeof(T) == 2) {
+        q.x[s][0] = row != nullptr ? *reinterpret_cast<const u32x4*>(row + G * (D / 4) + 8 * s) : u32x4{0, 0, 0, 0};
+      } else {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = row != nullptr ? row[G * (D / 4) + 8 * s + e] : 0.0f;
+        split8(x, q.x[s]);
+      }
     }
   }
 }
@@ -174,70 +246,95 @@ __device__ __forceinline__ void load_query(u32x4 (&q)[D / 32][kQParts<T>], const
 // Fold of the unit of keys key0 .. key0 + 31, in three steps, so that K's registers
 // and then V's are free for the next unit's loads as soon as they are read.
 //
-// Scores S^T[token][column] = K . Q^T, the K operand shared by the columns.  bad:
-// bit p, page p's entry lies outside the pool (its scores are NaN).
+// Scores S^T[token][column] = K . Q^T, the K operand shared by the columns.
 template <typename T, int D, int NB>
-__device__ __forceinline__ void fold_qk(const State<T, D, NB>& st, const Unit<D>& u, int bad, f32x4_t (&s)[NB][2]) {
+__device__ __forceinline__ void fold_qk(const State<T, D, NB>& st, const Unit<D>& u, f32x4_t (&s)[NB][2]) {
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
-    const float ks = __uint_as_float(u.ks[p] << 23);
 #pragma unroll
     for (int c = 0; c < NB; ++c) s[c][p] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if constexpr (kCodeScores<T, D>) {
+      const i32x8_t a = {(int)u.k[p][0], (int)u.k[p][1], (int)u.k[p][2], (int)u.k[p][3], 0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < D / 32; ++w) {
-      const bf16x8_t a = __builtin_bit_cast(bf16x8_t, eight_of(u.k[p][w], ks));
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int c = 0; c < NB; ++c)
+        for (int c = 0; c < NB; ++c)  // (formats: 4 the codes, 0 e4m3)
+          s[c][p] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, st.q[c].x[i], s[c][p], 4, 0, 0, (int)u.ks[p], 0, (int)st.q[c].s[i]);
+    } else {
+      const float ks = __uint_as_float(u.ks[p] << 23);
 #pragma unroll
-        for (int i = 0; i < kQParts<T>; ++i)
-          s[c][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8_t, st.q[c][w][i]), s[c][p], 0, 0, 0);
+      for (int w = 0; w < D / 32; ++w) {
+        const bf16x8_t a = __builtin_bit_cast(bf16x8_t, eight_of(u.k[p][w], ks));
+#pragma unroll
+        for (int c = 0; c < NB; ++c)
+#pragma unroll
+          for (int i = 0; i < kQParts<T>; ++i)
+            s[c][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8_t, st.q[c].x[w][i]), s[c][p], 0, 0, 0);
+      }
     }
-  }
-  if (bad != 0) {
-#pragma unroll
-    for (int c = 0; c < NB; ++c)
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-        if (bad >> p & 1) s[c][p] = f32x4_t{NAN, NAN, NAN, NAN};
   }
 }
 
-// Online softmax; the weights' bf16 parts as P^T operands.  edge (wave-uniform):
-// some column does not see every key of the unit.  The base moves only past the
-// slack.
+// Scores of a unit that some columns see in part, or of which a page's entry lies
+// outside the pool (bit p of bad): those of the latter are NaN, and of keys that a
+// column does not see -inf.
 template <typename T, int D, int NB>
-__device__ __forceinline__ void fold_softmax(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], int key0, bool edge,
-                                             float scale_log2, int lane, u32x4 (&pt)[NB][kPParts<T>]) {
-  const int G = lane >> 4;
+__device__ __forceinline__ void mask_scores(const State<T, D, NB>& st, int key0, int bad, int lane, f32x4_t (&s)[NB][2]) {
 #pragma unroll
-  for (int c = 0; c < NB; ++c) {
-    float x[8];
+  for (int c = 0; c < NB; ++c)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = s[c][i >> 2][i & 3];
-    if (edge) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = key0 + 16 * (i >> 2) + 4 * G + (i & 3) <= st.last[c] ? x[i] : -INFINITY;
+    for (int i = 0; i < 8; ++i) {
+      if (bad >> (i >> 2) & 1) s[c][i >> 2][i & 3] = NAN;
+      if (key0 + 16 * (i >> 2) + 4 * (lane >> 4) + (i & 3) > st.last[c]) s[c][i >> 2][i & 3] = -INFINITY;
     }
-    // (scale > 0, so the largest score is the scaled largest)
-    const float mx = rows4_max(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])))) *
-                     scale_log2;
-    const float mc = fmaxf(st.m[c], mx);
-    if (__builtin_amdgcn_ballot_w64(mc > st.m[c] + kRescaleSlack) != 0) {
+}
+
+// The base of a column's weights is kHeadroom log2 units below its largest score:
+// weights lie between 2^7 (the largest so far, when the base moves) and the 2^15
+// that moves it again, so that in fp16 all from 2^-21 of the largest on are normal
+// numbers, and what is rounded of a smaller one is 2^-32 of the largest at most.
+constexpr float kHeadroom = 7.0f;
+constexpr float kWeightLimit = 32768.0f;
+
+// Online softmax: the weights.  They are formed with the base of the units before,
+// and only where one exceeds the limit (as a column's first does, whose base is
+// kMInit) the bases of the wave move, so a unit needs no maximum across lanes.
+template <typename T, int D, int NB>
+__device__ __forceinline__ void fold_softmax(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, float (&x)[NB][8]) {
+  auto weights = [&]() {
+    float most = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NB; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[c][i] = fast_exp2(fmaf(s[c][i >> 2][i & 3], scale_log2, -st.m[c]));
+        most = fmaxf(most, x[c][i]);
+      }
+    return most > kWeightLimit;
+  };
+  if (__builtin_amdgcn_ballot_w64(weights()) != 0) {
+#pragma unroll
+    for (int c = 0; c < NB; ++c) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx = fmaxf(mx, s[c][i >> 2][i & 3]);
+      // (scale > 0, so the largest score is the scaled largest)
+      const float mc = fmaxf(st.m[c], rows4_max(mx) * scale_log2 - kHeadroom);
       const float alpha = fast_exp2(st.m[c] - mc);
       st.m[c] = mc;
       st.l[c] *= alpha;
 #pragma unroll
       for (int mb = 0; mb < D / 16; ++mb) st.acc[c][mb] *= alpha;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = fast_exp2(fmaf(x[i], scale_log2, -st.m[c]));
-    st.l[c] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-    split8(x, pt[c]);
+    weights();
   }
+#pragma unroll
+  for (int c = 0; c < NB; ++c)
+    st.l[c] += ((x[c][0] + x[c][1]) + (x[c][2] + x[c][3])) + ((x[c][4] + x[c][5]) + (x[c][6] + x[c][7]));
 }
 
 // V of keys past all_last, which no column sees: their weights are 0, but an unused
-// slot may hold anything, and 0 times a NaN is NaN.  Their scales become 0.
+// slot may hold anything, and 0 times a NaN is NaN.  Their scales become 1.
 template <int D>
 __device__ __forceinline__ void clear_dead(Unit<D>& u, int key0, int all_last, int lane) {
   constexpr int n = D / 32;
@@ -245,24 +342,57 @@ __device__ __forceinline__ void clear_dead(Unit<D>& u, int key0, int all_last, i
   for (int p = 0; p < 2; ++p)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (key0 + 16 * p + 4 * (lane >> 4) + i > all_last) u.vs[p][n == 4 ? i : i >> 1] &= n == 4 ? 0u : 0xffff0000u >> ((i & 1) * 16);
+      if (key0 + 16 * p + 4 * (lane >> 4) + i > all_last) {
+        uint32_t& w = u.vs[p][n == 4 ? i : i >> 1];
+        w = n == 4 ? 0x7f7f7f7fu : (i & 1) != 0 ? (w & 0xffffu) | 0x7f7f0000u : (w & 0xffff0000u) | 0x7f7fu;
+      }
 }
 
-// O^T += V^T . P^T
-template <typename T, int D, int NB>
-__device__ __forceinline__ void fold_pv(State<T, D, NB>& st, const Unit<D>& u, const u32x4 (&pt)[NB][kPParts<T>]) {
+// Whether fp16 does not hold the unit's V exactly: scale bytes within 104 .. 135 do,
+// the 32 from 2^-23 on (a byte below borrows, which leaves high bits set all the
+// same).  Wave-uniform.
+template <int D>
+__device__ __forceinline__ bool beyond_fp16(const Unit<D>& u) {
+  uint32_t off = 0;
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int w = 0; w < kWords<D>; ++w) off |= u.vs[p][w] - 0x68686868u;
+  return __builtin_amdgcn_ballot_w64((off & 0xe0e0e0e0u) != 0) != 0;
+}
+
+// O^T += V^T . P^T, in fp16 or in bf16 parts.
+template <bool F16, typename T, int D, int NB>
+__device__ __forceinline__ void fold_pv(State<T, D, NB>& st, const Unit<D>& u, const float (&x)[NB][8]) {
+  constexpr int N = F16 ? 1 : kPParts<T>;
+  u32x4 pt[NB][N];
+#pragma unroll
+  for (int c = 0; c < NB; ++c) {
+    if constexpr (F16) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h)
+        pt[c][0][h] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{x[c][2 * h], x[c][2 * h + 1]}), f16x2_t));
+    } else {
+      split8(x[c], pt[c]);
+    }
+  }
   auto block = [&](auto j_) {
     constexpr int j = decltype(j_)::value;
     u32x4 a[2];
-    v_operands<D, j>(u, a);
+    v_operands<D, j, F16>(u, a);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int c = 0; c < NB; ++c)
+      for (int c = 0; c < NB; ++c) {
+        f32x4_t& acc = st.acc[c][2 * j + h];
 #pragma unroll
-        for (int i = 0; i < kPParts<T>; ++i)
-          st.acc[c][2 * j + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              __builtin_bit_cast(bf16x8_t, a[h]), __builtin_bit_cast(bf16x8_t, pt[c][i]), st.acc[c][2 * j + h], 0, 0, 0);
+        for (int i = 0; i < N; ++i) {
+          if constexpr (F16)
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a[h]), __builtin_bit_cast(f16x8_t, pt[c][i]), acc, 0, 0, 0);
+          else
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a[h]), __builtin_bit_cast(bf16x8_t, pt[c][i]), acc, 0, 0, 0);
+        }
+      }
   };
   block(std::integral_constant<int, 0>{});
   block(std::integral_constant<int, 1>{});
@@ -272,12 +402,12 @@ __device__ __forceinline__ void fold_pv(State<T, D, NB>& st, const Unit<D>& u, c
   }
 }
 
-// fold_pv for a unit of which some columns see a part of the keys: a NaN block of
+// The same (in bf16) for a unit of which some columns see a part: a NaN block of
 // V reaches the columns that see its key, and no other (a weight of 0 times NaN
-// would be NaN).  Its scale becomes 0, and the columns that see the first such key
+// would be NaN; its codes are 0 already).  Its scale becomes 1, and the columns that see the first such key
 // of a block get NaN outright.
 template <typename T, int D, int NB>
-__device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, const u32x4 (&pt)[NB][kPParts<T>], int key0,
+__device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, const float (&x)[NB][8], int key0,
                                              int all_last, int lane) {
   constexpr int n = D / 32;
   clear_dead(u, key0, all_last, lane);
@@ -294,14 +424,14 @@ __device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, co
       for (int j = 0; j < n; ++j) {
         const uint32_t byte = 0xffu << ((n == 4 ? 0 : (i & 1) * 16) + 8 * j);
         if ((w & byte) == byte) {
-          w &= ~byte;
+          w ^= byte & 0x80808080u;  // (255 becomes 127, the scale 1)
           nan_key[j] = key0 + 16 * p + 4 * (lane >> 4) + i;
           any = true;
         }
       }
     }
   const bool nans = __builtin_amdgcn_ballot_w64(any) != 0;
-  fold_pv<T, D, NB>(st, u, pt);
+  fold_pv<false, T, D, NB>(st, u, x);
   if (nans) {
 #pragma unroll
     for (int j = 0; j < n; ++j) {
@@ -325,10 +455,20 @@ __device__ __forceinline__ void eight_out(const State<T, D, NB>& st, int c, int 
   }
 }
 
+// Values to the output's type (bf16 to nearest even, v_cvt_pk_bf16_f32).
+typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t to_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2v_t));
+}
+template <typename T>
+__device__ __forceinline__ void store_four(T* p, f32x4_t o) {
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_t*>(p) = u32x2_t{to_bf16(o[0], o[1]), to_bf16(o[2], o[3])};
+  else *reinterpret_cast<f32x4_t*>(p) = o;
+}
 template <typename T>
 __device__ __forceinline__ void store_eight(T* p, const float (&o)[8]) {
   if constexpr (sizeof(T) == 2) {
-    store_vec(reinterpret_cast<uint16_t*>(p), o);
+    *reinterpret_cast<u32x4*>(p) = u32x4{to_bf16(o[0], o[1]), to_bf16(o[2], o[3]), to_bf16(o[4], o[5]), to_bf16(o[6], o[7])};
   } else {
     *reinterpret_cast<f32x4_t*>(p) = f32x4_t{o[0], o[1], o[2], o[3]};
     *reinterpret_cast<f32x4_t*>(p + 4) = f32x4_t{o[4], o[5], o[6], o[7]};

@@ -88,26 +88,30 @@ class Batch:
         return q4.attention(self.q, self.k, self.v, self.bt, self.ctx, self.scale, self.qsl)
 
 
-def bound(ref, spread, size, keys, dtype, D):
+def bound(ref, spread, mass, size, reach, keys, dtype, D):
     """How far an output may be from the float64 one.
 
     The output's rounding, half a step: 2^-8 (bf16) or 2^-24 of it.  A weight is
-    off by its score's error, at most (3 D + 2) 2^-24 of sum |q k| in whatever
-    order (fp32's queries are three parts, so up to 3 D products), and by
-    2^-22 for the exponential and its argument's rounding (relative to 1 + |x|);
-    by its split into bf16 parts, 2^-16 (two: each leaves at most half a step of a
-    bf16, 2^-8) or 2^-24.  Sums over n keys in 32 bits: n 2^-24.  Numerator and
-    denominator carry both, hence twice, of sum w |v|.  A normalisation: 2^-22."""
-    w = 1.5 * (3 * D + 2) * 2.0 ** -24 * size + 2.0 ** -22 * (1 + 1.5 * size) + (2.0 ** -16 if dtype == "bf16" else 2.0 ** -24) + keys * 2.0 ** -24
-    return (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(ref) + (2 * w[..., None] + 2.0 ** -22) * spread + 1e-37
+    off by its score's error: the accumulation, at most (3 D + 2) 2^-24 of sum |q k|
+    in whatever order (fp32's queries are three parts, so up to 3 D products), and
+    bf16 queries at head_dim 128 as two e4m3 parts, 2^-22 of max |q| sum |k| (half of
+    the last step that both parts hold, 2^-15, beside a largest value of 2^7 at
+    least); by 2^-22 for the exponential and its argument's rounding (relative to 1 +
+    |x|); by its own rounding, 2^-11 (fp16) for bf16 outputs, of small
+    ones half of fp16's last step, 2^-25, beside a largest of 2^7 or more: 2^-32 of
+    sum |v|; or 2^-24 (three bf16 parts).  Sums over n keys in 32 bits: n 2^-24.  Numerator and denominator carry
+    these, hence twice, of sum w |v|.  A normalisation: 2^-22."""
+    w = 1.5 * ((3 * D + 2) * 2.0 ** -24 * size + 2.0 ** -22 * reach) + 2.0 ** -22 * (1 + 1.5 * size)
+    w = w + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -24) + keys * 2.0 ** -24
+    return (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(ref) + (2 * w[..., None] + 2.0 ** -22) * spread + 2.0 ** -32 * mass + 1e-37
 
 
 def check(out, expected, keys, dtype, what=""):
     """Every output within its bound, and NaN only where the reference is."""
-    ref, spread, size = expected
+    ref, spread, mass, size, reach = expected
     x = np.asarray(out, np.float64)
     assert np.array_equal(np.isnan(x), np.isnan(ref)), f"{what}: NaN at other places"
     fine = ~np.isnan(ref)
-    off = np.abs(x - ref)[fine] / bound(ref, spread, size, keys, dtype, ref.shape[-1])[fine]
+    off = np.abs(x - ref)[fine] / bound(ref, spread, mass, size, reach, keys, dtype, ref.shape[-1])[fine]
     assert off.size == 0 or off.max() <= 1.0, f"{what}: {off.max():.3g} times the bound"
     return 0.0 if off.size == 0 else float(off.max())

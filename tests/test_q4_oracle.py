@@ -68,9 +68,9 @@ def test_attention_of_equal_keys_is_the_mean():
     D = 64
     k = q4.pack("k", np.ones((2, 1, 16, D)))
     v = np.arange(32.0).reshape(2, 1, 16, 1) // 8 * np.ones(D)  # 0, 1, 2, 3: all of them codes
-    out, spread, size = q4.attention(np.ones((3, 2, D)), k, q4.pack("v", v), np.array([[1, 0]]), [20], 0.5,
+    out, spread, mass, size, reach = q4.attention(np.ones((3, 2, D)), k, q4.pack("v", v), np.array([[1, 0]]), [20], 0.5,
                                      query_start_loc=[0, 3])
     order = np.concatenate([v[1, 0, :, 0], v[0, 0, :, 0]])
     for j in range(3):
         assert np.allclose(out[j], order[:18 + j].mean())
-    assert np.allclose(spread, out) and np.allclose(size, 32.0)
+    assert np.allclose(spread, out) and np.allclose(size, 32.0) and np.allclose(reach, 32.0)
