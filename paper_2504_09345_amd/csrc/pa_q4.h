@@ -36,7 +36,7 @@ struct Q4AttnArgs {
   const uint8_t* v_pages;
   const int32_t* block_table;
   const int32_t* context_lens;
-  const int32_t* query_start_loc;  // nullptr: decode
+  const int32_t* query_start_loc;
   void* out;
   float* ws_o;   // [rows][H_q][n_split][D] unnormalised outputs of parts
   float* ws_ml;  // [rows][H_q][n_split][2] (base in log2 units, sum)
@@ -52,8 +52,10 @@ constexpr int kQ4Waves = 4;  // waves of a workgroup, each with an item of its o
 
 // Column blocks (of 16) that a wave holds.
 constexpr int q4_positions(int blocks, int s) { return 16 * blocks / s; }  // query rows of an item
+constexpr int kQ4ChunkBlocks = 2 * kQ4Waves;  // of a workgroup that shares V's operands (launch_q4_chunk)
 
 hipError_t launch_q4_attn(int dtype, int D, int blocks, const Q4AttnArgs& a, hipStream_t st, KernelEvents ev);
+hipError_t launch_q4_chunk(int D, const Q4AttnArgs& a, hipStream_t st, KernelEvents ev);  // bf16
 hipError_t launch_q4_merge(int dtype, int D, const Q4AttnArgs& a, hipStream_t st);
 
 // The persistent kernel of decode rows (sequences of one row): (sequence, head

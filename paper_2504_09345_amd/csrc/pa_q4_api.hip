@@ -67,6 +67,7 @@ struct Plan {
   // decode rows
   int W = 0, per_launch = 0;  // waves of a team; sequences of a launch
   // chunk rows
+  bool shared = false;  // V's operands shared by a workgroup
   int blocks = 1, n_slots = 0, n_split = 1, split_units = 1, min_rows = 2;
   size_t st_o = 0, st_ml = 0, st_flag = 0, ch_o = 0, ch_ml = 0;
   size_t stream_bytes() const { return st_o + st_ml + st_flag; }
@@ -115,7 +116,8 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
   }
   if (p->chunks) {
     p->min_rows = p->stream ? 2 : 1;
-    p->blocks = d->max_q_len * (int64_t)s <= 16 ? 1 : d->max_q_len * (int64_t)s <= 32 ? 2 : 4;
+    p->blocks = d->max_q_len * (int64_t)s <= 16 ? 1 : d->dtype == PA_BF16 ? pa::kQ4ChunkBlocks : 2;
+    p->shared = p->blocks == pa::kQ4ChunkBlocks;
     const int64_t slots = p->rows / pa::q4_positions(p->blocks, s) + (int64_t)d->num_seqs;
     // row blocks of the sequences that can be chunks
     const int64_t chunk_rows = p->stream ? (int64_t)p->rows - d->num_seqs : p->rows;
@@ -186,7 +188,9 @@ int attend(const void* q, const void* k_pages, const void* v_pages, const int32_
     pa::KernelEvents ev;
     ev.start = begin;
     ev.stop = p.stream ? nullptr : end;
-    if (pa::launch_q4_attn(d->dtype, d->head_dim, p.blocks, a, stream, ev) != hipSuccess) return PA_EHIP;
+    if ((p.shared ? pa::launch_q4_chunk(d->head_dim, a, stream, ev)
+                  : pa::launch_q4_attn(d->dtype, d->head_dim, p.blocks, a, stream, ev)) != hipSuccess)
+      return PA_EHIP;
     if (p.n_split > 1 && pa::launch_q4_merge(d->dtype, d->head_dim, a, stream) != hipSuccess) return PA_EHIP;
   }
   if (p.stream) {

@@ -13,60 +13,76 @@ struct Q4Item {
   bool bad;            // rows are NaN
 };
 
-// Row block `slot` of the call: in a varlen call the blocks of sequence b are the
-// slots from query_start_loc[b] / positions + b on, which no two sequences share.
+// Row block `slot` of the call: the blocks of sequence b are the slots from query_start_loc[b] / positions + b on, which no two sequences share.
 __device__ __forceinline__ Q4Item q4_item(const Q4AttnArgs& a, int slot, int positions, int lane) {
-  Q4Item it{slot, slot, 0, 0, false};
-  int L = 1, first = 0;
-  if (a.query_start_loc != nullptr) {
-    const int32_t* qsl = a.query_start_loc;
-    it.b = q4::wave_search(a.B, slot, lane, [&](int b) { return qsl[b] / positions + b; });
-    const int q0 = qsl[it.b];
-    L = qsl[it.b + 1] - q0;
-    first = (slot - (q0 / positions + it.b)) * positions;
-    it.row0 = q0 + first;
-    if (q0 < 0 || first < 0 || it.row0 >= a.rows) return it;
-    if (L < a.min_rows) return it;  // (the stream kernel's)
-    it.n_pos = max(0, min(positions, min(L - first, a.rows - it.row0)));
-  } else {
-    it.n_pos = 1;
-  }
+  Q4Item it{0, 0, 0, 0, false};
+  const int32_t* qsl = a.query_start_loc;
+  it.b = q4::wave_search(a.B, slot, lane, [&](int b) { return qsl[b] / positions + b; });
+  const int q0 = qsl[it.b], L = qsl[it.b + 1] - q0;
+  const int first = (slot - (q0 / positions + it.b)) * positions;
+  it.row0 = q0 + first;
+  if (q0 < 0 || first < 0 || it.row0 >= a.rows || L < a.min_rows) return it;  // (fewer rows: the stream kernel's)
+  it.n_pos = max(0, min(positions, min(L - first, a.rows - it.row0)));
   const int C = a.context_lens[it.b];
   it.last0 = C - L + first;
-  it.bad = C < 0 || C > a.max_context_len || (C + kPage - 1) / kPage > a.bt_stride || (a.query_start_loc != nullptr && (L > C || L > a.max_q_len));
+  it.bad = C < 0 || C > a.max_context_len || (C + kPage - 1) / kPage > a.bt_stride || L > C || L > a.max_q_len;
   return it;
 }
 
+// The outputs of a wave's columns, or the records of part `split` of them; at: the
+// column's (row, head) vector among all.
 template <typename T, int D, int NB>
-__global__ __launch_bounds__(64 * kQ4Waves) __attribute__((amdgpu_waves_per_eu(NB <= 2 ? 2 : 1)))
+__device__ __forceinline__ void q4_finish(const Q4AttnArgs& a, const q4::State<T, D, NB>& st, const int64_t (&at)[NB], int split,
+                                          int lane) {
+  const int G = lane >> 4;
+  T* out = reinterpret_cast<T*>(a.out);
+#pragma unroll
+  for (int c = 0; c < NB; ++c) {
+    const float l = rows4_sum(st.l[c]);
+    if (st.last[c] < 0) continue;
+    const float inv = 1.0f / l;
+    const int64_t rec = at[c] * a.n_split + split;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+      float o[8];
+      q4::eight_out(st, c, j, o);
+      const int d = 32 * j + 8 * G;
+      if (a.n_split == 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] *= inv;
+        q4::store_eight(out + at[c] * D + d, o);
+      } else {
+        q4::store_eight(a.ws_o + rec * D + d, o);
+      }
+    }
+    if (a.n_split > 1 && G == 0) {
+      a.ws_ml[rec * 2] = st.m[c];
+      a.ws_ml[rec * 2 + 1] = l;
+    }
+  }
+}
+
+template <typename T, int D, int NB>
+__global__ __launch_bounds__(64 * kQ4Waves) __attribute__((amdgpu_waves_per_eu(2)))
 void q4_attn_kernel(Q4AttnArgs a) {
   const int S = a.s;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int slot, split, g;
-  if (a.query_start_loc == nullptr) {  // heads of a page side by side
-    const int f = blockIdx.x * kQ4Waves + wave;
-    g = f % a.H_kv;
-    split = f / a.H_kv % a.n_split;
-    slot = f / a.H_kv / a.n_split;
-  } else {  // row blocks of one head side by side
-    split = blockIdx.x % a.n_split;
-    g = blockIdx.x / a.n_split % a.H_kv;
-    // (the last blocks of a sequence see the most keys: they start first)
-    slot = (gridDim.x / a.n_split / a.H_kv - 1 - blockIdx.x / a.n_split / a.H_kv) * kQ4Waves + wave;
-  }
+  // row blocks of one head side by side
+  const int split = blockIdx.x % a.n_split, g = blockIdx.x / a.n_split % a.H_kv;
+  // (the last blocks of a sequence see the most keys: they start first)
+  const int slot = (gridDim.x / a.n_split / a.H_kv - 1 - blockIdx.x / a.n_split / a.H_kv) * kQ4Waves + wave;
   if (slot >= a.n_slots) return;
   const Q4Item it = q4_item(a, slot, q4_positions(NB, S), lane);
   if (it.n_pos == 0) return;
 
-  const int n = lane & 15, G = lane >> 4;
+  const int n = lane & 15;
   T* out = reinterpret_cast<T*>(a.out);
   const int all_last = it.last0 + it.n_pos - 1;
-  if (it.bad || all_last < 0) {  // (a decode row of an empty context: zeros)
+  if (it.bad) {
     if (split != 0) return;
-    const float fill = it.bad ? NAN : 0.0f;
     for (int i = lane; i < it.n_pos * S * D; i += 64)
-      store_out<T>(out + ((int64_t)(it.row0 + i / (S * D)) * a.H_q + (int64_t)g * S) * D + i % (S * D), fill);
+      store_out<T>(out + ((int64_t)(it.row0 + i / (S * D)) * a.H_q + (int64_t)g * S) * D + i % (S * D), NAN);
     return;
   }
   const int n_units = all_last / kQ4Unit + 1;
@@ -119,11 +135,11 @@ void q4_attn_kernel(Q4AttnArgs a) {
   q4::Unit<D> u;
   auto fetch_k = [&](const Pages& t, bool any) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_k<D>(u, p, kg + t.at[p], any ? tile_size : 0, lane);
+    for (int p = 0; p < 2; ++p) q4::load_k<D, 0>(u, p, kg + t.at[p], any ? tile_size : 0, lane);
   };
   auto fetch_v = [&](const Pages& t, bool any) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_v<D>(u, p, vg + t.at[p], any ? tile_size : 0, lane);
+    for (int p = 0; p < 2; ++p) q4::load_v<D, 0>(u, p, vg + t.at[p], any ? tile_size : 0, lane);
   };
   Pages t = pages(u0);
   fetch_k(t, true);
@@ -167,30 +183,7 @@ void q4_attn_kernel(Q4AttnArgs a) {
     ++k;
   }
 
-#pragma unroll
-  for (int c = 0; c < NB; ++c) {
-    const float l = rows4_sum(st.l[c]);
-    if (st.last[c] < 0) continue;
-    const float inv = 1.0f / l;
-    const int64_t rec = at[c] * a.n_split + split;
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-      float o[8];
-      q4::eight_out(st, c, j, o);
-      const int d = 32 * j + 8 * G;
-      if (a.n_split == 1) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] *= inv;
-        q4::store_eight(out + at[c] * D + d, o);
-      } else {
-        q4::store_eight(a.ws_o + rec * D + d, o);
-      }
-    }
-    if (a.n_split > 1 && G == 0) {
-      a.ws_ml[rec * 2] = st.m[c];
-      a.ws_ml[rec * 2 + 1] = l;
-    }
-  }
+  q4_finish<T, D, NB>(a, st, at, split, lane);
 }
 
 // Join the parts of one (query row, head) per wave.
@@ -200,14 +193,10 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
   const int f = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = f / a.H_q;
   if (row >= a.rows) return;
-  int b = row, L = 1, j = 0;
-  if (a.query_start_loc != nullptr) {
-    const int32_t* qsl = a.query_start_loc;
-    b = q4::wave_search(a.B, row, lane, [&](int i) { return qsl[i]; });
-    L = qsl[b + 1] - qsl[b];
-    j = row - qsl[b];
-    if (j < 0 || j >= L || L < a.min_rows || L > a.max_q_len) return;
-  }
+  const int32_t* qsl = a.query_start_loc;
+  const int b = q4::wave_search(a.B, row, lane, [&](int i) { return qsl[i]; });
+  const int L = qsl[b + 1] - qsl[b], j = row - qsl[b];
+  if (j < 0 || j >= L || L < a.min_rows || L > a.max_q_len) return;
   const int C = a.context_lens[b];
   // (rows without keys or with an error are written already)
   if (C < L || C > a.max_context_len || (C + kPage - 1) / kPage > a.bt_stride) return;
@@ -238,7 +227,6 @@ const void* q4_attn_pick(int blocks) {
   switch (blocks) {
     case 1: return reinterpret_cast<const void*>(&q4_attn_kernel<T, D, 1>);
     case 2: return reinterpret_cast<const void*>(&q4_attn_kernel<T, D, 2>);
-    case 4: return reinterpret_cast<const void*>(&q4_attn_kernel<T, D, 4>);
   }
   return nullptr;
 }

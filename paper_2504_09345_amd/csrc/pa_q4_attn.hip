@@ -32,8 +32,7 @@ hipError_t launch_q4_attn(int dtype, int D, int blocks, const Q4AttnArgs& a, hip
   const void* fn = q4_attn_fn(dtype, D, blocks);
   if (fn == nullptr) return hipErrorInvalidValue;
   const int64_t parts = (int64_t)a.H_kv * a.n_split;
-  const int64_t grid = a.query_start_loc == nullptr ? (a.n_slots * parts + kQ4Waves - 1) / kQ4Waves
-                                                    : (a.n_slots + kQ4Waves - 1) / kQ4Waves * parts;
+  const int64_t grid = (a.n_slots + kQ4Waves - 1) / kQ4Waves * parts;
   void* args[] = {const_cast<Q4AttnArgs*>(&a)};
   hipError_t e = hipExtLaunchKernel(fn, dim3((uint32_t)grid), dim3(64 * kQ4Waves), args, 0, st, ev.start, ev.stop, 0);
   return e != hipSuccess ? e : hipGetLastError();

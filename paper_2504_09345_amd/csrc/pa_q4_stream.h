@@ -243,11 +243,11 @@ void q4_stream_kernel(Q4StreamArgs a) {
   const int tile_size = a.num_pages > 0 ? q4_tile_bytes(D) : 0;
   auto fetch_k = [&](const Tiles& e, bool any) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_k<D>(u, p, kw + e.at[p], any ? tile_size : 0, lane);
+    for (int p = 0; p < 2; ++p) q4::load_k<D, kKvLoadPolicy>(u, p, kw + e.at[p], any ? tile_size : 0, lane);
   };
   auto fetch_v = [&](const Tiles& e, bool any) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_v<D>(u, p, vw + e.at[p], any ? tile_size : 0, lane);
+    for (int p = 0; p < 2; ++p) q4::load_v<D, kKvLoadPolicy>(u, p, vw + e.at[p], any ? tile_size : 0, lane);
   };
 
   // Items cut by the range's ends.  Each wave is alone: a part is its record in the

@@ -65,30 +65,31 @@ struct Unit {
   uint32_t vs[2][kWords<D>];  // scales of those four tokens, token-major
 };
 
-template <int D>
+// Loads of a unit are non-temporal in the decode kernel (as its 16-bit sibling's:
+// each byte is read once), and cached where other workgroups read them again.
+template <int D, int Policy>
 __device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int off, uint32_t (&x)[kWords<D>]) {
   if constexpr (D == 128) {
-    const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kKvLoadPolicy);
+    const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, Policy);
     x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
   } else {
-    const u32x2_t w = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, kKvLoadPolicy);
+    const u32x2_t w = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, Policy);
     x[0] = w.x; x[1] = w.y;
   }
 }
 // Loads of page p (0 or 1) of a unit from the tiles at k and v; with bytes = 0 instead
 // of the tile's nothing is read, and every code and scale is 0.
-template <int D>
+template <int D, int Policy>
 __device__ __forceinline__ void load_k(Unit<D>& u, int p, const uint8_t* k, int bytes, int lane) {
   const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(k), (short)0, bytes, 0x00020000);
-  load_words<D>(r, lane * (D / 8), u.k[p]);
-  u.ks[p] = __builtin_amdgcn_raw_buffer_load_b8(r, kScales<D> + (lane & 15) * (D / 32) + (lane >> 4) * D / 128, 0,
-                                                kKvLoadPolicy);
+  load_words<D, Policy>(r, lane * (D / 8), u.k[p]);
+  u.ks[p] = __builtin_amdgcn_raw_buffer_load_b8(r, kScales<D> + (lane & 15) * (D / 32) + (lane >> 4) * D / 128, 0, Policy);
 }
-template <int D>
+template <int D, int Policy>
 __device__ __forceinline__ void load_v(Unit<D>& u, int p, const uint8_t* v, int bytes, int lane) {
   const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(v), (short)0, bytes, 0x00020000);
-  load_words<D>(r, lane * (D / 8), u.v[p]);
-  load_words<D>(r, kScales<D> + (lane >> 4) * (D / 8), u.vs[p]);
+  load_words<D, Policy>(r, lane * (D / 8), u.v[p]);
+  load_words<D, Policy>(r, kScales<D> + (lane >> 4) * (D / 8), u.vs[p]);
 }
 
 // Scale of block j of the lane's token i (of four).
@@ -296,23 +297,26 @@ __device__ __forceinline__ void mask_scores(const State<T, D, NB>& st, int key0,
 constexpr float kHeadroom = 7.0f;
 constexpr float kWeightLimit = 32768.0f;
 
-// Online softmax: the weights.  They are formed with the base of the units before,
-// and only where one exceeds the limit (as a column's first does, whose base is
-// kMInit) the bases of the wave move, so a unit needs no maximum across lanes.
+// Online softmax: the weights, formed with the base of the units before; whether
+// one exceeds the limit (as a column's first does, whose base is kMInit).
 template <typename T, int D, int NB>
-__device__ __forceinline__ void fold_softmax(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, float (&x)[NB][8]) {
-  auto weights = [&]() {
-    float most = 0.0f;
+__device__ __forceinline__ bool form_weights(const State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, float (&x)[NB][8]) {
+  float most = 0.0f;
 #pragma unroll
-    for (int c = 0; c < NB; ++c)
+  for (int c = 0; c < NB; ++c)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[c][i] = fast_exp2(fmaf(s[c][i >> 2][i & 3], scale_log2, -st.m[c]));
-        most = fmaxf(most, x[c][i]);
-      }
-    return most > kWeightLimit;
-  };
-  if (__builtin_amdgcn_ballot_w64(weights()) != 0) {
+    for (int i = 0; i < 8; ++i) {
+      x[c][i] = fast_exp2(fmaf(s[c][i >> 2][i & 3], scale_log2, -st.m[c]));
+      most = fmaxf(most, x[c][i]);
+    }
+  return most > kWeightLimit;
+}
+// Only where one does the bases of the wave move (so a unit needs no maximum across
+// lanes); then the columns' sums.
+template <typename T, int D, int NB>
+__device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, bool big,
+                                               float (&x)[NB][8]) {
+  if (__builtin_amdgcn_ballot_w64(big) != 0) {
 #pragma unroll
     for (int c = 0; c < NB; ++c) {
       float mx = -INFINITY;
@@ -326,11 +330,16 @@ __device__ __forceinline__ void fold_softmax(State<T, D, NB>& st, const f32x4_t 
 #pragma unroll
       for (int mb = 0; mb < D / 16; ++mb) st.acc[c][mb] *= alpha;
     }
-    weights();
+    form_weights<T, D, NB>(st, s, scale_log2, x);
   }
 #pragma unroll
   for (int c = 0; c < NB; ++c)
     st.l[c] += ((x[c][0] + x[c][1]) + (x[c][2] + x[c][3])) + ((x[c][4] + x[c][5]) + (x[c][6] + x[c][7]));
+}
+template <typename T, int D, int NB>
+__device__ __forceinline__ void fold_softmax(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, float (&x)[NB][8]) {
+  const bool big = form_weights<T, D, NB>(st, s, scale_log2, x);
+  settle_weights<T, D, NB>(st, s, scale_log2, big, x);
 }
 
 // V of keys past all_last, which no column sees: their weights are 0, but an unused
