@@ -54,7 +54,7 @@ constexpr int kQ4Waves = 4;  // waves of a workgroup, each with an item of its o
 constexpr int q4_positions(int blocks, int s) { return 16 * blocks / s; }  // query rows of an item
 constexpr int kQ4ChunkBlocks = 2 * kQ4Waves;  // of a workgroup that shares V's operands (launch_q4_chunk)
 
-hipError_t launch_q4_attn(int dtype, int D, int blocks, const Q4AttnArgs& a, hipStream_t st, KernelEvents ev);
+hipError_t launch_q4_attn(int dtype, int D, const Q4AttnArgs& a, hipStream_t st, KernelEvents ev);
 hipError_t launch_q4_chunk(int D, const Q4AttnArgs& a, hipStream_t st, KernelEvents ev);  // bf16
 hipError_t launch_q4_merge(int dtype, int D, const Q4AttnArgs& a, hipStream_t st);
 

@@ -77,8 +77,22 @@ struct Plan {
 };
 
 // Parts that chunks are cut into: as many as give the GPU (256 CUs of 8 waves) a
-// wave of work each, of at least kLeastUnits units, at most 64.
-constexpr int kWavesWanted = 2048, kLeastUnits = 4, kMaxSplit = 64;
+// wave of work each, of at least kLeastUnits units, at most 64.  (Parts of 4 units cost
+// one chunk of 300 rows 15 us instead of 11, parts of 32 one of 64 rows on 1,500 tokens
+// 38 instead of 18; 8 or 16 are one as good as the other.)
+constexpr int kWavesWanted = 2048, kLeastUnits = 8, kMaxSplit = 64;
+// Which kernel takes a call's chunks (bf16): waves of 16 columns, each alone, or
+// workgroups of 128 columns that share V's operands.  The latter spend a third less
+// per column and unit, but need the columns (a chunk of at most 32 leaves three of
+// four waves without) and enough work: a wave alone is through its units sooner, and
+// there are more of them.  The line is 32 units for each of 2,048 waves, by the
+// longest context that the call declares.  Alone and together, 32 query heads over 8:
+// one chunk of 700 rows 20 and 35 us, of 1,400 36 and 46, of 2,000 62 and 61, of
+// 4,000 194 and 149; 8 of 205-256 rows on 500 tokens 57 and 47; 4 of 240-300 on
+// 1,000 64 and 59; 4 of 48-60 on 3,000 41 and 55; 2 of 102-128 on 20,000 171 and 128;
+// 16 of 8 rows on 2,000 35 and 45.
+constexpr int64_t kAloneUnits = 32 * 2048;
+constexpr int kAloneColumns = 32;
 // Units of a launch of the stream kernel, at most (its counts are 32-bit).
 constexpr int64_t kStreamUnits = 1 << 30;
 
@@ -116,13 +130,15 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
   }
   if (p->chunks) {
     p->min_rows = p->stream ? 2 : 1;
-    p->blocks = d->max_q_len * (int64_t)s <= 16 ? 1 : d->dtype == PA_BF16 ? pa::kQ4ChunkBlocks : 2;
-    p->shared = p->blocks == pa::kQ4ChunkBlocks;
+    // rows of the sequences that can be chunks
+    const int64_t chunk_rows = p->stream ? (int64_t)p->rows - d->num_seqs + 1 : p->rows;
+    const int64_t alone_units = (chunk_rows / pa::q4_positions(1, s) + 1) * d->num_kv_heads *
+                                ((d->max_context_len - d->max_q_len / 2) / pa::kQ4Unit + 1);
+    p->shared = d->dtype == PA_BF16 && d->max_q_len * (int64_t)s > kAloneColumns && alone_units > kAloneUnits;
+    p->blocks = p->shared ? pa::kQ4ChunkBlocks : 1;
     const int64_t slots = p->rows / pa::q4_positions(p->blocks, s) + (int64_t)d->num_seqs;
-    // row blocks of the sequences that can be chunks
-    const int64_t chunk_rows = p->stream ? (int64_t)p->rows - d->num_seqs : p->rows;
     const int64_t items = (chunk_rows / pa::q4_positions(p->blocks, s) + 1) * d->num_kv_heads;
-    int64_t split = kWavesWanted / items;
+    int64_t split = kWavesWanted / (items * (p->shared ? pa::kQ4Waves : 1));
     if (split > units / kLeastUnits) split = units / kLeastUnits;
     if (split > kMaxSplit) split = kMaxSplit;
     if (split < 1) split = 1;
@@ -189,7 +205,7 @@ int attend(const void* q, const void* k_pages, const void* v_pages, const int32_
     ev.start = begin;
     ev.stop = p.stream ? nullptr : end;
     if ((p.shared ? pa::launch_q4_chunk(d->head_dim, a, stream, ev)
-                  : pa::launch_q4_attn(d->dtype, d->head_dim, p.blocks, a, stream, ev)) != hipSuccess)
+                  : pa::launch_q4_attn(d->dtype, d->head_dim, a, stream, ev)) != hipSuccess)
       return PA_EHIP;
     if (p.n_split > 1 && pa::launch_q4_merge(d->dtype, d->head_dim, a, stream) != hipSuccess) return PA_EHIP;
   }

@@ -62,9 +62,10 @@ __device__ __forceinline__ void q4_finish(const Q4AttnArgs& a, const q4::State<T
   }
 }
 
-template <typename T, int D, int NB>
+template <typename T, int D>
 __global__ __launch_bounds__(64 * kQ4Waves) __attribute__((amdgpu_waves_per_eu(2)))
 void q4_attn_kernel(Q4AttnArgs a) {
+  constexpr int NB = 1;  // column blocks of the wave
   const int S = a.s;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -223,12 +224,8 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
 }
 
 template <typename T, int D>
-const void* q4_attn_pick(int blocks) {
-  switch (blocks) {
-    case 1: return reinterpret_cast<const void*>(&q4_attn_kernel<T, D, 1>);
-    case 2: return reinterpret_cast<const void*>(&q4_attn_kernel<T, D, 2>);
-  }
-  return nullptr;
+const void* q4_attn_pick() {
+  return reinterpret_cast<const void*>(&q4_attn_kernel<T, D>);
 }
 
 }  // namespace pa

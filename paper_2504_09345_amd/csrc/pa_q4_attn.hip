@@ -15,21 +15,21 @@
 
 namespace pa {
 
-extern template const void* q4_attn_pick<uint16_t, 64>(int);
-extern template const void* q4_attn_pick<float, 128>(int);
-extern template const void* q4_attn_pick<float, 64>(int);
-template const void* q4_attn_pick<uint16_t, 128>(int);
+extern template const void* q4_attn_pick<uint16_t, 64>();
+extern template const void* q4_attn_pick<float, 128>();
+extern template const void* q4_attn_pick<float, 64>();
+template const void* q4_attn_pick<uint16_t, 128>();
 
-static const void* q4_attn_fn(int dtype, int D, int blocks) {
-  if (dtype == 0 && D == 128) return q4_attn_pick<uint16_t, 128>(blocks);
-  if (dtype == 0 && D == 64) return q4_attn_pick<uint16_t, 64>(blocks);
-  if (dtype == 1 && D == 128) return q4_attn_pick<float, 128>(blocks);
-  if (dtype == 1 && D == 64) return q4_attn_pick<float, 64>(blocks);
+static const void* q4_attn_fn(int dtype, int D) {
+  if (dtype == 0 && D == 128) return q4_attn_pick<uint16_t, 128>();
+  if (dtype == 0 && D == 64) return q4_attn_pick<uint16_t, 64>();
+  if (dtype == 1 && D == 128) return q4_attn_pick<float, 128>();
+  if (dtype == 1 && D == 64) return q4_attn_pick<float, 64>();
   return nullptr;
 }
 
-hipError_t launch_q4_attn(int dtype, int D, int blocks, const Q4AttnArgs& a, hipStream_t st, KernelEvents ev) {
-  const void* fn = q4_attn_fn(dtype, D, blocks);
+hipError_t launch_q4_attn(int dtype, int D, const Q4AttnArgs& a, hipStream_t st, KernelEvents ev) {
+  const void* fn = q4_attn_fn(dtype, D);
   if (fn == nullptr) return hipErrorInvalidValue;
   const int64_t parts = (int64_t)a.H_kv * a.n_split;
   const int64_t grid = (a.n_slots + kQ4Waves - 1) / kQ4Waves * parts;

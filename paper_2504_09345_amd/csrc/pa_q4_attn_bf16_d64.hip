@@ -3,6 +3,6 @@
 
 namespace pa {
 
-template const void* q4_attn_pick<uint16_t, 64>(int);
+template const void* q4_attn_pick<uint16_t, 64>();
 
 }  // namespace pa

@@ -3,6 +3,6 @@
 
 namespace pa {
 
-template const void* q4_attn_pick<float, 128>(int);
+template const void* q4_attn_pick<float, 128>();
 
 }  // namespace pa

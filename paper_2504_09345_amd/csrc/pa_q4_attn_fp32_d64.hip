@@ -3,6 +3,6 @@
 
 namespace pa {
 
-template const void* q4_attn_pick<float, 64>(int);
+template const void* q4_attn_pick<float, 64>();
 
 }  // namespace pa

@@ -84,8 +84,37 @@ class Batch:
             pb.paged_attn_varlen_q4(d["q"], d["k"], d["v"], d["bt"], d["cl"], d["qsl"], self.scale, out, dims, **kw)
         return out
 
+    def widen(self, d, tokens):
+        """The block table with room for contexts of `tokens` (its further entries name
+        no page)."""
+        import torch
+        more = -(-tokens // 16) - d["bt"].shape[1]
+        d["bt"] = torch.cat([d["bt"], torch.full((d["bt"].shape[0], more), -1, dtype=torch.int32, device="cuda")], 1)
+
     def expected(self):
         return q4.attention(self.q, self.k, self.v, self.bt, self.ctx, self.scale, self.qsl)
+
+    def expected_gpu(self):
+        """The same, a sequence's rows and keys at once."""
+        import torch
+        s = self.H_q // self.H_kv
+        res = [np.zeros(self.q.shape) for _ in range(3)] + [np.zeros(self.q.shape[:2]) for _ in range(2)]
+        for b, C in enumerate(int(c) for c in self.ctx):
+            r0, L = (b, 1) if self.qsl is None else (int(self.qsl[b]), self.n_rows[b])
+            if L == 0 or C == 0:
+                continue
+            k, v = (torch.from_numpy(q4.dense(w, p, self.bt, b, C, self.D)).cuda() for w, p in (("k", self.k), ("v", self.v)))
+            q = torch.from_numpy(self.q[r0:r0 + L].astype(np.float64)).cuda()
+            seen = torch.arange(C, device="cuda")[None, :] <= torch.arange(C - L, C, device="cuda")[:, None]
+            for h in range(self.H_q):
+                kt, vh = k[h // s].t().contiguous(), v[h // s].contiguous()
+                x = (self.scale * torch.matmul(q[:, h].contiguous(), kt)).masked_fill(~seen, -torch.inf)
+                w = torch.softmax(x, -1)
+                size = (self.scale * torch.matmul(q[:, h].abs().contiguous(), kt.abs())).masked_fill(~seen, 0).amax(-1)
+                reach = self.scale * q[:, h].abs().amax(-1) * (seen * kt.abs().sum(0)).amax(-1)
+                for to, what in zip(res, (torch.matmul(w, vh), torch.matmul(w, vh.abs()), torch.matmul(seen.double(), vh.abs()), size, reach)):
+                    to[r0:r0 + L, h] = what.cpu().numpy()
+        return res
 
 
 def bound(ref, spread, mass, size, reach, keys, dtype, D):

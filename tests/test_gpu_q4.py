@@ -388,3 +388,60 @@ def test_queries_of_any_size(D):
     b.q[7, :, ::2] *= 2.0 ** -20
     b.q = b.round(b.q)
     check(b.attend(b.upload()).float().cpu(), b.expected(), 100, "bf16")
+
+
+# --- workgroups that share V (large calls) -----------------------------------
+
+FAR = 1 << 20  # a declared context that makes a call's work large enough for them
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H_q,H_kv", [(34, 34), (68, 34), (8, 2), (6, 1), (16, 2)])
+@pytest.mark.parametrize("lens", [
+    [(100, 7), (64, 64), (16, 1), (90, 33), (1, 1), (0, 0), (200, 50)],
+    [(130, 130), (150, 65)],
+    [(300, 40)],
+], ids=["mixed", "chunks", "one"])
+def test_shared(D, H_q, H_kv, lens):
+    """The sizes where such a workgroup can go wrong, its kernel chosen by a declared
+    context far above the real ones."""
+    announce(f"q4 shared D={D} heads={H_q}/{H_kv} {lens}")
+    b = Batch(lens, H_q, H_kv, D, seed=len(lens))
+    d = b.upload()
+    b.widen(d, FAR)
+    check(b.attend(d, b.dims(d, max_context_len=FAR)).float().cpu(), b.expected_gpu(), max(c for c, _ in lens), "bf16")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H_q,H_kv", [(32, 8), (48, 8), (8, 1)])
+@pytest.mark.parametrize("lens", [
+    [(1000, 256)] * 9 + [(300, 1), (1, 1)],      # whole items
+    [(5000, 100), (4700, 120), (33, 2)],          # items in parts
+    [(2600, 2600)],
+], ids=["items", "parts", "prompt"])
+def test_shared_at_size(D, H_q, H_kv, lens):
+    announce(f"q4 shared at size D={D} heads={H_q}/{H_kv} {lens[0]}")
+    b = Batch(lens, H_q, H_kv, D, seed=9)
+    check(b.attend(b.upload()).float().cpu(), b.expected_gpu(), max(c for c, _ in lens), "bf16")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_shared_nan_blocks_and_any_size(D):
+    """A NaN block reaches the rows that see it, units outside fp16's window are exact
+    beside it, and a page outside the pool reaches the rows that see it."""
+    announce(f"q4 shared, NaN blocks and V of any size D={D}")
+    b = Batch([(170, 140), (64, 1), (100, 90)], 8, 2, D, seed=3)
+    d = b.upload()
+    b.v[b.bt[0, 2], 1, q4.scale_byte_of(D, 13, 1)] = 255   # token 45: rows from 15 on
+    b.k[b.bt[2, 1], 0, q4.scale_byte_of(D, 4, 0)] = 255    # token 20: rows from 10 on
+    for page, e in ((b.bt[0, 5], 60), (b.bt[2, 0], -40), (b.bt[1, 1], 20)):
+        at = [q4.scale_byte_of(D, t, j) for t in range(16) for j in range(D // 32)]
+        b.v[page][:, at] = np.clip(b.v[page][:, at].astype(int) + e, 2, 252)
+    ref = b.expected()
+    assert np.isnan(ref[0]).any() and not np.isnan(ref[0][:15]).any()
+    bt = b.bt.copy()
+    bt[2, 4] = b.num_pages  # tokens 64 .. 79: rows from 54 on
+    ref[0][141 + 54:] = np.nan
+    d.update(k=b.cuda(b.k), v=b.cuda(b.v), bt=b.cuda(bt))
+    b.widen(d, FAR)
+    check(b.attend(d, b.dims(d, max_context_len=FAR)).float().cpu(), ref, 170, "bf16")
