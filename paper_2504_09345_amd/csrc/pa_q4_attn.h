@@ -144,44 +144,42 @@ void q4_attn_kernel(Q4AttnArgs a) {
   };
   Pages t = pages(u0);
   fetch_k(t, true);
+  __builtin_amdgcn_sched_barrier(0);  // (K before V, as the loop's waits expect)
   fetch_v(t, true);
   constexpr bool kF16 = q4::kF16<T>;
   const int u_full = min(u1, (it.last0 + 1) / kQ4Unit);  // units before are seen whole by every column
-  for (int k = u0; k < u1;) {
+  for (int k = u0; k < u1; ++k) {
     q4::f32x4_t s[NB][2];
     float x[NB][8];
     Pages next = t;
-    bool formed = false;  // the unit's weights are there, but V is beyond fp16
+    bool big = false;
+    auto weights = [&](bool usual) {  // the weights of unit k, and the next K; whether its base moves or V is beyond fp16
+      if (k + 1 < u1) next = pages(k + 1);
+      q4::fold_qk<T, D, NB>(st, u, lane, s);
+      fetch_k(next, k + 1 < u1);
+      if (!usual) q4::mask_scores<T, D, NB>(st, k * kQ4Unit, t.bad, lane, s);
+      big = q4::form_weights<T, D, NB>(st, s, a.scale_log2, x);
+      __builtin_amdgcn_sched_barrier(0);  // (V is not waited for before the weights are formed)
+      return __builtin_amdgcn_ballot_w64(big | (kF16 && q4::beyond_fp16<D>(u))) != 0;
+    };
+    bool rare = weights(k < u_full && t.bad == 0);
+    if (k < u_full) {
+      // (one way out, and nothing but the usual unit: the sums stay in place, and the
+      // loads under way are known)
 #pragma unroll 1
-    for (; k < u_full && t.bad == 0; ++k) {  // (nothing but the usual unit, so that the sums stay in place)
-      const bool more = k + 1 < u1;
-      if (more) next = pages(k + 1);
-      q4::fold_qk<T, D, NB>(st, u, s);
-      fetch_k(next, more);
-      q4::fold_softmax<T, D, NB>(st, s, a.scale_log2, x);
-      if (kF16 && q4::beyond_fp16<D>(u)) {
-        formed = true;
-        break;
+      while (!rare & (k + 1 < u_full) & (next.bad == 0)) {
+        q4::add_weights(st, x);
+        q4::fold_pv<kF16, T, D, NB>(st, u, x);
+        fetch_v(next, true);
+        t = next;
+        ++k;
+        rare = weights(true);
       }
-      q4::fold_pv<kF16, T, D, NB>(st, u, x);
-      fetch_v(next, more);
-      t = next;
     }
-    if (k >= u1) break;
-    const bool more = k + 1 < u1;
-    if (more && !formed) next = pages(k + 1);
-    if (formed) {
-      q4::fold_pv<false, T, D, NB>(st, u, x);
-    } else {
-      q4::fold_qk<T, D, NB>(st, u, s);
-      fetch_k(next, more);
-      q4::mask_scores<T, D, NB>(st, k * kQ4Unit, t.bad, lane, s);
-      q4::fold_softmax<T, D, NB>(st, s, a.scale_log2, x);
-      q4::fold_pv_edge<T, D, NB>(st, u, x, k * kQ4Unit, all_last, lane);
-    }
-    fetch_v(next, more);
+    q4::settle_weights<T, D, NB>(st, s, a.scale_log2, big, x);
+    q4::fold_pv_edge<T, D, NB>(st, u, x, k * kQ4Unit, all_last, lane);
+    fetch_v(next, k + 1 < u1);
     t = next;
-    ++k;
   }
 
   q4_finish<T, D, NB>(a, st, at, split, lane);

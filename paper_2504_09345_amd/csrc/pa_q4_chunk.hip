@@ -175,7 +175,7 @@ void q4_chunk_kernel(Q4AttnArgs a) {
   fetch_part(t, true);
   if (u0 + 1 < u1) t1 = pages(u0 + 1);
   q4::f32x4_t s[kNB][2], sn[kNB][2];
-  q4::fold_qk<T, D, kNB>(st, u, s);
+  q4::fold_qk<T, D, kNB>(st, u, lane, s);
   fetch_k(t1, u0 + 1 < w1);
   convert(u0);
   fetch_part(t1, u0 + 1 < u1);
@@ -191,7 +191,7 @@ void q4_chunk_kernel(Q4AttnArgs a) {
         break;
       }
       t2 = k + 2 < u1 ? pages(k + 2) : t1;
-      q4::fold_qk<T, D, kNB>(st, u, sn);
+      q4::fold_qk<T, D, kNB>(st, u, lane, sn);
       const bool big = q4::form_weights<T, D, kNB>(st, s, a.scale_log2, x);
       fetch_k(t2, k + 2 < w1);
       q4::settle_weights<T, D, kNB>(st, s, a.scale_log2, big, x);
@@ -209,7 +209,7 @@ void q4_chunk_kernel(Q4AttnArgs a) {
     if (!entered) __syncthreads();
     const bool active = k < w1;
     t2 = k + 2 < u1 ? pages(k + 2) : t1;
-    if (k + 1 < w1) q4::fold_qk<T, D, kNB>(st, u, sn);
+    if (k + 1 < w1) q4::fold_qk<T, D, kNB>(st, u, lane, sn);
     fetch_k(t2, k + 2 < w1);
     if (active) {
       q4::mask_scores<T, D, kNB>(st, k * kQ4Unit, t.bad, lane, s);

@@ -261,9 +261,11 @@ void q4_stream_kernel(Q4StreamArgs a) {
   // its count is looked at before the last unit, and if it is there the wave joins
   // its record from registers and stores none of its own.
   auto counter_at = [&](int x) {
-    unsigned long long* p = a.ws_flag + ((int64_t)x * W + w) * kQ4CounterStride;
+    // (global memory for certain: while a generic access is under way, every wait is for all)
+    using Global = __attribute__((address_space(1))) unsigned long long;
+    Global* p = (Global*)(a.ws_flag + ((int64_t)x * W + w) * kQ4CounterStride);
     asm("" : "+v"(p));  // (an address of lanes: one atomic, not a wave's reduction)
-    return DeviceCounter{p};
+    return DeviceCounter{(unsigned long long*)p};
   };
   auto level_of = [&](const Q4Cut& cut) { return cut.grouped() && !cut.group_of_one(bid) ? 0 : 1; };
   bool stored[2] = {false, false};
@@ -304,15 +306,17 @@ void q4_stream_kernel(Q4StreamArgs a) {
       const int np = sm.cum[r + 1] - sm.cum[r];
       const int rem = x - a.nb * sm.cum[r];
       const int hb = rem / np, p = rem - hb * np;
+      int page[2];  // (past the context's pages: any entry, unused; read without waiting for the length)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) page[h] = a.block_table[(int64_t)r * a.bt_stride + min((int64_t)2 * p + h, a.bt_stride - 1)];
       const int left = a.context_lens[r] - p * kQ4Unit;  // tokens from the unit on
       Q4UnitEntry e;
       int odd = 0;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int page = left > kPage * h ? a.block_table[(int64_t)r * a.bt_stride + 2 * p + h] : 0;
-        const bool ok = page >= 0 && page < a.num_pages;
-        odd |= (ok || left <= kPage * h ? 0 : 1) << h;
-        e.at[h] = ok ? ((int64_t)page * a.H_kv + hb * W) * tile : 0;
+        const bool used = left > kPage * h, ok = used && page[h] >= 0 && page[h] < a.num_pages;
+        odd |= (ok || !used ? 0 : 1) << h;
+        e.at[h] = ok ? ((int64_t)page[h] * a.H_kv + hb * W) * tile : 0;
       }
       e.info = min(left, kQ4Unit) | odd << 6 | (odd != 0 || left < kQ4Unit) << 8 | hb << 9;
       e.left = np - p;
@@ -331,6 +335,7 @@ void q4_stream_kernel(Q4StreamArgs a) {
     // unit's K loaded as soon as the scores are formed, its V after the products
     Tiles t = tiles(0);
     fetch_k(t, true);
+    __builtin_amdgcn_sched_barrier(0);  // (K before V, as the loop's waits expect)
     fetch_v(t, true);
     for (int i = 0; i < m;) {
       const Q4UnitEntry& e = tm.unit[i];
@@ -358,42 +363,49 @@ void q4_stream_kernel(Q4StreamArgs a) {
         else seen = __hip_atomic_load(counter_at(bid).p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), look = true;
       }
       const bool ends = stop == i + left;
-      while (i < stop) {
+      for (; i < stop; ++i) {
         constexpr bool kF16 = q4::kF16<T>;
         q4::f32x4_t s[1][2];
         float x[1][8];
-        bool formed = false;  // the unit's weights are there, but V is beyond fp16
-#pragma unroll 1
-        for (; i < stop && !(t.info & 256); ++i) {  // (nothing but the usual unit, so that the sums stay in place)
+        Tiles next;
+        bool big;  // the base moves
+        auto weights = [&](bool usual) {  // the weights of unit i, and the next K; whether a base moves or V is beyond fp16
           const bool more = i + 1 < m;
-          const Tiles next = tiles(more ? i + 1 : i);
-          q4::fold_qk<T, D, 1>(st, u, s);
+          next = tiles(more ? i + 1 : i);
+          q4::fold_qk<T, D, 1>(st, u, lane, s);
           fetch_k(next, more);
-          q4::fold_softmax<T, D, 1>(st, s, a.scale_log2, x);
-          if (kF16 && q4::beyond_fp16<D>(u)) {
-            formed = true;
-            break;
+          if (!usual) {
+            const int tokens = t.info & 63;
+            st.last[0] = tokens - 1;
+            q4::mask_scores<T, D, 1>(st, 0, t.info >> 6 & 3, lane, s);
+            q4::clear_dead(u, 0, tokens - 1, lane);
           }
+          big = q4::form_weights<T, D, 1>(st, s, a.scale_log2, x);
+          __builtin_amdgcn_sched_barrier(0);  // (V is not waited for before the weights are formed)
+          return __builtin_amdgcn_ballot_w64(big | (kF16 && q4::beyond_fp16<D>(u))) != 0;
+        };
+        bool rare = weights(!(t.info & 256));
+        // (one way out, and nothing but the usual unit: the sums stay in place, and the
+        // loads under way are known)
+#pragma unroll 1
+        while (!rare & (i + 1 < stop) & !(next.info & 256)) {
+          q4::add_weights(st, x);
           q4::fold_pv<kF16, T, D, 1>(st, u, x);
-          fetch_v(next, more);
+          fetch_v(next, true);
           t = next;
+          ++i;
+          // (of a SIMD's waves the oldest issues first: in turn, so that they end together)
+          if ((i ^ (wave >> 2)) & 1) {
+            __builtin_amdgcn_s_setprio(1);
+          } else {
+            __builtin_amdgcn_s_setprio(0);
+          }
+          rare = weights(true);
         }
-        if (i >= stop) break;
-        const bool more = i + 1 < m;
-        const Tiles next = tiles(more ? i + 1 : i);
-        if (!formed) {
-          const int tokens = t.info & 63;
-          q4::fold_qk<T, D, 1>(st, u, s);
-          fetch_k(next, more);
-          st.last[0] = tokens - 1;
-          q4::mask_scores<T, D, 1>(st, 0, t.info >> 6 & 3, lane, s);
-          q4::fold_softmax<T, D, 1>(st, s, a.scale_log2, x);
-          q4::clear_dead(u, 0, tokens - 1, lane);
-        }
+        q4::settle_weights<T, D, 1>(st, s, a.scale_log2, big, x);
         q4::fold_pv<false, T, D, 1>(st, u, x);
-        fetch_v(next, more);
+        fetch_v(next, i + 1 < m);
         t = next;
-        ++i;
       }
       if (!ends) continue;
       // the item ends: its output, or the record of this range's part of it

@@ -60,7 +60,7 @@ __device__ __forceinline__ u32x4 eight_of(uint32_t w, float scale) {
 template <int D>
 struct Unit {
   uint32_t k[2][kWords<D>];  // codes of token lane % 16, dims D/4 (lane / 16) .. +D/4
-  uint32_t ks[2];            // scale byte of those dims
+  uint32_t ks[2];            // the word that holds the scale of those dims (k_scale)
   uint32_t v[2][kWords<D>];  // word j: tokens 4 (lane / 16) .. +3, dims 32 j + 2 (lane % 16), +1
   uint32_t vs[2][kWords<D>];  // scales of those four tokens, token-major
 };
@@ -83,7 +83,13 @@ template <int D, int Policy>
 __device__ __forceinline__ void load_k(Unit<D>& u, int p, const uint8_t* k, int bytes, int lane) {
   const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(k), (short)0, bytes, 0x00020000);
   load_words<D, Policy>(r, lane * (D / 8), u.k[p]);
-  u.ks[p] = __builtin_amdgcn_raw_buffer_load_b8(r, kScales<D> + (lane & 15) * (D / 32) + (lane >> 4) * D / 128, 0, Policy);
+  u.ks[p] = __builtin_amdgcn_raw_buffer_load_b32(r, kScales<D> + ((lane & 15) * (D / 32) & ~3), 0, Policy);
+}
+// The scale byte of the lane's K codes, with others above it.  (A load of the byte
+// alone is extended where it is loaded, which waits for it there.)
+template <int D>
+__device__ __forceinline__ uint32_t k_scale(const Unit<D>& u, int p, int lane) {
+  return u.ks[p] >> (D == 128 ? (lane >> 4) * 8 : (lane & 1) * 16 + (lane >> 5) * 8);
 }
 template <int D, int Policy>
 __device__ __forceinline__ void load_v(Unit<D>& u, int p, const uint8_t* v, int bytes, int lane) {
@@ -249,20 +255,21 @@ __device__ __forceinline__ void load_query(Query<T, D>& q, const T* row, int lan
 //
 // Scores S^T[token][column] = K . Q^T, the K operand shared by the columns.
 template <typename T, int D, int NB>
-__device__ __forceinline__ void fold_qk(const State<T, D, NB>& st, const Unit<D>& u, f32x4_t (&s)[NB][2]) {
+__device__ __forceinline__ void fold_qk(const State<T, D, NB>& st, const Unit<D>& u, int lane, f32x4_t (&s)[NB][2]) {
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
 #pragma unroll
     for (int c = 0; c < NB; ++c) s[c][p] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if constexpr (kCodeScores<T, D>) {
+      const int ks = (int)k_scale<D>(u, p, lane);  // (the product reads the lowest byte)
       const i32x8_t a = {(int)u.k[p][0], (int)u.k[p][1], (int)u.k[p][2], (int)u.k[p][3], 0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int c = 0; c < NB; ++c)  // (formats: 4 the codes, 0 e4m3)
-          s[c][p] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, st.q[c].x[i], s[c][p], 4, 0, 0, (int)u.ks[p], 0, (int)st.q[c].s[i]);
+          s[c][p] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, st.q[c].x[i], s[c][p], 4, 0, 0, ks, 0, (int)st.q[c].s[i]);
     } else {
-      const float ks = __uint_as_float(u.ks[p] << 23);
+      const float ks = scale_of<0>(k_scale<D>(u, p, lane));
 #pragma unroll
       for (int w = 0; w < D / 32; ++w) {
         const bf16x8_t a = __builtin_bit_cast(bf16x8_t, eight_of(u.k[p][w], ks));
@@ -311,8 +318,15 @@ __device__ __forceinline__ bool form_weights(const State<T, D, NB>& st, const f3
     }
   return most > kWeightLimit;
 }
+template <typename T, int D, int NB>
+__device__ __forceinline__ void add_weights(State<T, D, NB>& st, const float (&x)[NB][8]) {
+#pragma unroll
+  for (int c = 0; c < NB; ++c)
+    st.l[c] += ((x[c][0] + x[c][1]) + (x[c][2] + x[c][3])) + ((x[c][4] + x[c][5]) + (x[c][6] + x[c][7]));
+}
 // Only where one does the bases of the wave move (so a unit needs no maximum across
-// lanes); then the columns' sums.
+// lanes); then the columns' sums.  The kernels' inner loops leave for this: a loop
+// that scales the outputs in one of its branches copies them in the others.
 template <typename T, int D, int NB>
 __device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, bool big,
                                                float (&x)[NB][8]) {
@@ -332,10 +346,9 @@ __device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_
     }
     form_weights<T, D, NB>(st, s, scale_log2, x);
   }
-#pragma unroll
-  for (int c = 0; c < NB; ++c)
-    st.l[c] += ((x[c][0] + x[c][1]) + (x[c][2] + x[c][3])) + ((x[c][4] + x[c][5]) + (x[c][6] + x[c][7]));
+  add_weights(st, x);
 }
+
 template <typename T, int D, int NB>
 __device__ __forceinline__ void fold_softmax(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, float (&x)[NB][8]) {
   const bool big = form_weights<T, D, NB>(st, s, scale_log2, x);
@@ -359,7 +372,7 @@ __device__ __forceinline__ void clear_dead(Unit<D>& u, int key0, int all_last, i
 
 // Whether fp16 does not hold the unit's V exactly: scale bytes within 104 .. 135 do,
 // the 32 from 2^-23 on (a byte below borrows, which leaves high bits set all the
-// same).  Wave-uniform.
+// same), as this lane sees it.
 template <int D>
 __device__ __forceinline__ bool beyond_fp16(const Unit<D>& u) {
   uint32_t off = 0;
@@ -367,7 +380,7 @@ __device__ __forceinline__ bool beyond_fp16(const Unit<D>& u) {
   for (int p = 0; p < 2; ++p)
 #pragma unroll
     for (int w = 0; w < kWords<D>; ++w) off |= u.vs[p][w] - 0x68686868u;
-  return __builtin_amdgcn_ballot_w64((off & 0xe0e0e0e0u) != 0) != 0;
+  return (off & 0xe0e0e0e0u) != 0;
 }
 
 // O^T += V^T . P^T, in fp16 or in bf16 parts.
