@@ -41,15 +41,8 @@ constexpr bool counter_valid(uint64_t v, const CounterKey& key, int n) { return 
 // Word: fetch_add(x) -> old value; swap(expected, x): compare-and-swap, which
 // puts the present value into expected where it fails; store(x).
 template <typename Word>
-constexpr bool counter_answer(Word& word, const CounterKey& key, int n, uint64_t old);
-template <typename Word>
 constexpr bool counter_arrive(Word& word, const CounterKey& key, int n) {
-  return counter_answer(word, key, n, word.fetch_add(key.step));
-}
-// The rest of an arrival whose fetch-and-add gave old (it may have been made
-// earlier: parts that arrive in between count as they would after it).
-template <typename Word>
-constexpr bool counter_answer(Word& word, const CounterKey& key, int n, uint64_t old) {
+  uint64_t old = word.fetch_add(key.step);
   while (!counter_valid(old, key, n)) {
     // (a failed swap met another part's change; each part changes the word a
     // bounded number of times, and once valid it stays so)

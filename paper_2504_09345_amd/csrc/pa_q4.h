@@ -58,9 +58,8 @@ hipError_t launch_q4_attn(int dtype, int D, const Q4AttnArgs& a, hipStream_t st,
 hipError_t launch_q4_chunk(int D, const Q4AttnArgs& a, hipStream_t st, KernelEvents ev);  // bf16
 hipError_t launch_q4_merge(int dtype, int D, const Q4AttnArgs& a, hipStream_t st);
 
-// The persistent kernel of decode rows (sequences of one row): (sequence, head
-// block, unit) triples of the whole batch in equal contiguous ranges, one per team
-// of W waves, a wave per KV head of a head block.
+// The persistent kernel of decode rows (sequences of one row): (sequence, KV head,
+// unit) triples of the whole batch in equal contiguous ranges, one per wave.
 struct Q4StreamArgs {
   const void* q;
   const uint8_t* k_pages;
@@ -69,30 +68,28 @@ struct Q4StreamArgs {
   const int32_t* context_lens;
   const int32_t* query_start_loc;  // nullptr: decode
   void* out;
-  // of each range, slot (0: the item that its start cuts, 1: that its end cuts) and
-  // wave, as in StreamArgs
-  float* ws_o;
-  float* ws_ml;
-  unsigned long long* ws_flag;  // a counter per range and wave, kQ4CounterStride apart
+  // of each workgroup and slot (0: the item that its start cuts, 1: that its end cuts)
+  float* ws_o;   // S * D floats (Q4Record's order)
+  float* ws_ml;  // (base in log2 units, sum) of the S heads
+  unsigned long long* ws_flag;  // a counter per workgroup, kQ4CounterStride apart
   CounterKey key;
   int64_t bt_stride;
   float scale_log2;
   int B, H_q, H_kv, rows, num_pages, max_context_len;
-  int nb;         // head blocks = H_kv / W
   int max_q_len;  // longer chunks are NaN rows, where write_long
   int write_long;
 };
-constexpr int kQ4StreamSeqs = 8192;    // sequences of a launch
-constexpr int kQ4StreamWaves = 4096;   // waves of a launch: ranges times W
-constexpr int kQ4StreamThreads = 512;  // of a workgroup: 8 / W teams
+constexpr int kQ4StreamSeqs = 4096;    // sequences of a launch
+constexpr int kQ4StreamGroups = 512;   // workgroups of a launch
+constexpr int kQ4StreamThreads = 512;  // of a workgroup
 constexpr int kQ4CounterStride = 16;   // 128 bytes: atomics on one line follow each other 30 ns apart
+static_assert(kQ4StreamGroups <= kStreamMaxGrid, "a cut item's groups of records");
 
-constexpr int q4_waves(int H_kv) { return H_kv % 8 == 0 ? 8 : H_kv % 4 == 0 ? 4 : H_kv % 2 == 0 ? 2 : 1; }
 // Workgroups that the current device holds at once, at most as many as a launch may
 // have; 0 on error.
-int q4_stream_workgroups(int dtype, int D, int s, int W);
-hipError_t launch_q4_stream(int dtype, int D, int s, int W, const Q4StreamArgs& a, int workgroups, hipStream_t st, KernelEvents ev);
-template <typename T, int D> const void* q4_stream_pick(int s, int W);
+int q4_stream_workgroups(int dtype, int D, int s);
+hipError_t launch_q4_stream(int dtype, int D, int s, const Q4StreamArgs& a, int workgroups, hipStream_t st, KernelEvents ev);
+template <typename T, int D> const void* q4_stream_pick(int s);
 
 // A call's key (pa_counter.h), its own among the process's.
 CounterKey new_call_key();

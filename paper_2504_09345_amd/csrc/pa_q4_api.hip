@@ -65,7 +65,7 @@ struct Plan {
   int s = 0, rows = 0;
   bool stream = false, chunks = false;  // which kernels the call needs
   // decode rows
-  int W = 0, per_launch = 0;  // waves of a team; sequences of a launch
+  int per_launch = 0;  // sequences of a launch
   // chunk rows
   bool shared = false;  // V's operands shared by a workgroup
   int blocks = 1, n_slots = 0, n_split = 1, split_units = 1, min_rows = 2;
@@ -118,15 +118,13 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
   // is there all the same is then a chunk of one)
   p->stream = !(p->chunks && (int64_t)d->max_q_len * d->num_seqs == d->num_q_rows);
   if (p->stream) {
-    p->W = pa::q4_waves(d->num_kv_heads);
-    const int nb = d->num_kv_heads / p->W;
-    const int64_t most = kStreamUnits / ((units > 0 ? units : 1) * nb);
+    const int64_t most = kStreamUnits / ((units > 0 ? units : 1) * d->num_kv_heads);
     if (most < 1) return PA_ENOTSUP;
     p->per_launch = most < pa::kQ4StreamSeqs ? (int)most : pa::kQ4StreamSeqs;
-    const size_t recs = (size_t)pa::kQ4StreamWaves * 2 * s;
+    const size_t recs = (size_t)pa::kQ4StreamGroups * 2 * s;
     p->st_o = align256(recs * d->head_dim * sizeof(float));
     p->st_ml = align256(recs * 2 * sizeof(float));
-    p->st_flag = align256((size_t)pa::kQ4StreamWaves * pa::kQ4CounterStride * sizeof(unsigned long long));
+    p->st_flag = align256((size_t)pa::kQ4StreamGroups * pa::kQ4CounterStride * sizeof(unsigned long long));
   }
   if (p->chunks) {
     p->min_rows = p->stream ? 2 : 1;
@@ -210,7 +208,7 @@ int attend(const void* q, const void* k_pages, const void* v_pages, const int32_
     if (p.n_split > 1 && pa::launch_q4_merge(d->dtype, d->head_dim, a, stream) != hipSuccess) return PA_EHIP;
   }
   if (p.stream) {
-    const int workgroups = pa::q4_stream_workgroups(d->dtype, d->head_dim, p.s, p.W);
+    const int workgroups = pa::q4_stream_workgroups(d->dtype, d->head_dim, p.s);
     if (workgroups <= 0) return PA_EHIP;
     pa::Q4StreamArgs a{};
     a.k_pages = static_cast<const uint8_t*>(k_pages);
@@ -224,7 +222,6 @@ int attend(const void* q, const void* k_pages, const void* v_pages, const int32_
     a.H_kv = d->num_kv_heads;
     a.num_pages = d->num_pages;
     a.max_context_len = d->max_context_len;
-    a.nb = d->num_kv_heads / p.W;
     a.max_q_len = d->max_q_len;
     a.write_long = !p.chunks;
     const size_t row_bytes = (size_t)d->num_q_heads * d->head_dim * (d->dtype == PA_BF16 ? 2 : 4);
@@ -241,7 +238,7 @@ int attend(const void* q, const void* k_pages, const void* v_pages, const int32_
       pa::KernelEvents ev;
       ev.start = b == 0 && !p.chunks ? begin : nullptr;
       ev.stop = b + a.B == d->num_seqs ? end : nullptr;
-      if (pa::launch_q4_stream(d->dtype, d->head_dim, p.s, p.W, a, workgroups, stream, ev) != hipSuccess) return PA_EHIP;
+      if (pa::launch_q4_stream(d->dtype, d->head_dim, p.s, a, workgroups, stream, ev) != hipSuccess) return PA_EHIP;
     }
   }
   if (joined != nullptr) (void)hipEventRecord(joined, stream);

@@ -134,6 +134,7 @@ void q4_attn_kernel(Q4AttnArgs a) {
     return t;
   };
   q4::Unit<D> u;
+  const int k_shift = q4::k_shift<D>(lane);
   auto fetch_k = [&](const Pages& t, bool any) {
 #pragma unroll
     for (int p = 0; p < 2; ++p) q4::load_k<D, 0>(u, p, kg + t.at[p], any ? tile_size : 0, lane);
@@ -155,7 +156,7 @@ void q4_attn_kernel(Q4AttnArgs a) {
     bool big = false;
     auto weights = [&](bool usual) {  // the weights of unit k, and the next K; whether its base moves or V is beyond fp16
       if (k + 1 < u1) next = pages(k + 1);
-      q4::fold_qk<T, D, NB>(st, u, lane, s);
+      q4::fold_qk<T, D, NB>(st, u, k_shift, s);
       fetch_k(next, k + 1 < u1);
       if (!usual) q4::mask_scores<T, D, NB>(st, k * kQ4Unit, t.bad, lane, s);
       big = q4::form_weights<T, D, NB>(st, s, a.scale_log2, x);

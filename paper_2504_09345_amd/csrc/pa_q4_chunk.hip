@@ -137,9 +137,16 @@ void q4_chunk_kernel(Q4AttnArgs a) {
     if constexpr (kPart == 2) block(std::integral_constant<int, 1>{});
   };
   q4::Unit<D> u;  // K of the unit; V only of a flagged one
+  // (The scale bytes alone, although that waits for K here, behind the present unit's
+  // softmax: 698 us instead of 715 for eight chunks of 2,048 rows on 0-2,048 tokens.)
   auto fetch_k = [&](const Pages& t, bool any) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_k<D, 0>(u, p, kg + t.at[p], any ? tile_size : 0, lane);
+    for (int p = 0; p < 2; ++p) {
+      const __amdgpu_buffer_rsrc_t r =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(kg + t.at[p]), (short)0, any ? tile_size : 0, 0x00020000);
+      q4::load_words<D, 0>(r, lane * (D / 8), u.k[p]);
+      u.ks[p] = __builtin_amdgcn_raw_buffer_load_b8(r, q4::kScales<D> + n * (D / 32) + G * D / 128, 0, 0);
+    }
   };
 
   auto flagged = [&](int k) {
@@ -175,7 +182,7 @@ void q4_chunk_kernel(Q4AttnArgs a) {
   fetch_part(t, true);
   if (u0 + 1 < u1) t1 = pages(u0 + 1);
   q4::f32x4_t s[kNB][2], sn[kNB][2];
-  q4::fold_qk<T, D, kNB>(st, u, lane, s);
+  q4::fold_qk<T, D, kNB>(st, u, 0, s);
   fetch_k(t1, u0 + 1 < w1);
   convert(u0);
   fetch_part(t1, u0 + 1 < u1);
@@ -191,7 +198,7 @@ void q4_chunk_kernel(Q4AttnArgs a) {
         break;
       }
       t2 = k + 2 < u1 ? pages(k + 2) : t1;
-      q4::fold_qk<T, D, kNB>(st, u, lane, sn);
+      q4::fold_qk<T, D, kNB>(st, u, 0, sn);
       const bool big = q4::form_weights<T, D, kNB>(st, s, a.scale_log2, x);
       fetch_k(t2, k + 2 < w1);
       q4::settle_weights<T, D, kNB>(st, s, a.scale_log2, big, x);
@@ -209,7 +216,7 @@ void q4_chunk_kernel(Q4AttnArgs a) {
     if (!entered) __syncthreads();
     const bool active = k < w1;
     t2 = k + 2 < u1 ? pages(k + 2) : t1;
-    if (k + 1 < w1) q4::fold_qk<T, D, kNB>(st, u, lane, sn);
+    if (k + 1 < w1) q4::fold_qk<T, D, kNB>(st, u, 0, sn);
     fetch_k(t2, k + 2 < w1);
     if (active) {
       q4::mask_scores<T, D, kNB>(st, k * kQ4Unit, t.bad, lane, s);

@@ -7,24 +7,6 @@
 
 namespace pa {
 
-// An item cut over ranges x0 .. x1, as CutItem, with groups of 64 for the more
-// ranges that this kernel has.
-struct Q4Cut {
-  int x0, x1;
-  __device__ int n() const { return x1 - x0 + 1; }
-  __device__ bool grouped() const { return n() > 16; }
-  __device__ int shift() const { return n() <= 64 ? 3 : n() <= 256 ? 4 : n() <= 1024 ? 5 : 6; }
-  __device__ int group_first(int x) const { return x0 + ((x - x0) >> shift() << shift()); }
-  __device__ bool group_of_one(int x) const { return group_first(x) == x1; }
-  __device__ int first(int level, int x) const { return level == 0 ? group_first(x) : x0; }
-  __device__ int step(int level) const { return level == 1 && grouped() ? 1 << shift() : 1; }
-  __device__ int parts(int level, int x) const {
-    return level == 0 ? min(1 << shift(), x1 - group_first(x) + 1) : grouped() ? ((n() - 1) >> shift()) + 1 : n();
-  }
-  __device__ int counter(int level, int x) const { return first(level, x) + (level == 0 && group_first(x) == x0 ? 1 : 0); }
-};
-static_assert(kQ4StreamWaves <= 64 * 64, "one record per lane at either level");
-
 // A record's 16-byte chunks: chunk c holds head c / 4 mod S, dims 32 j + 8 (c mod 4)
 // + 4 h .. +3 with 2 j + h = c / 4 S (the accumulators' order, a lane's own pairs).
 template <int D, int S>
@@ -34,26 +16,15 @@ struct Q4Record {
   static __device__ __forceinline__ int chunk(int n, int jh, int G) { return (jh * S + n) * 4 + G; }
 };
 
-struct Q4UnitEntry {
-  int64_t at[2];  // the pages' first byte of the head block (0: outside the pool, or no page)
-  int32_t info;   // tokens (6 bits) | page 0, 1 outside the pool | anything but 32 tokens of the pool | head block
-  int32_t left;   // units to the item's end, this one included
-  int32_t row;
-  int32_t first;  // whether it is the item's first
-};
-
-template <int W>
+template <int D, int S>
 struct Q4StreamSmem {
-  static constexpr int kTeams = kQ4StreamThreads / 64 / W;
-  static constexpr int kUnits = 1024 / kTeams;  // of a table
-  int32_t cum[kQ4StreamSeqs + 1];               // units of the sequences before, per head block
+  int32_t cum[kQ4StreamSeqs + 1];  // units of the sequences before, per KV head
   int32_t scan[kQ4StreamThreads / 64];
-  struct Team {
-    Q4UnitEntry unit[kUnits];
-    Q4Cut cut[2];          // the items cut by the range's start and by its end (x0 = -1: none)
-    int32_t job[W][2][2];  // their row and KV head
-    int32_t last_row, last_hb;  // of the range's last unit
-  } team[kTeams];
+  // of each wave, its parts of the items cut by its range's start (0) and end (1)
+  struct Part {
+    float ml[S][2];
+    alignas(16) float o[S * D];
+  } part[kQ4StreamThreads / 64][2];
 };
 
 // What the kernel does with sequence b: 1 (its row sees nv > 0 keys), 0 (nothing),
@@ -73,21 +44,21 @@ __device__ __forceinline__ int q4_decode_row(const Q4StreamArgs& a, int b, int& 
   return nv == 0 ? 2 : 1;
 }
 
-// Join n <= 64 records of an item, those of ranges xs, xs + step, .. (record slot 1
-// of the item's first range x0, slot 0 of the others), in range order, by one wave;
+// Join n <= 64 records of an item, those of workgroups xs, xs + step, .. (record slot
+// 1 of the item's first workgroup x0, slot 0 of the others), in order, by one wave;
 // lane l takes the records' 16-byte chunks l, l + 64, ..  final: normalise and write
 // the output; otherwise the joined record takes the first one's place.  Records
 // bypass the L2 (a round trip of 1 to 2 us), so all (m, l), record i by lane i, and
 // the first kBatch records' outputs are loaded at once.
-template <typename T, int D, int S, int W>
-__device__ __forceinline__ void q4_join(const Q4StreamArgs& a, int x0, int xs, int step, int n, bool final, int w, int lane, T* out) {
+template <typename T, int D, int S>
+__device__ __forceinline__ void q4_join(const Q4StreamArgs& a, int x0, int xs, int step, int n, bool final, int lane, T* out) {
   using Rec = Q4Record<D, S>;
   constexpr int kChunks = S * D / 4, C = (kChunks + 63) / 64;  // chunks per lane
   constexpr int kBatch = 4;  // (8 are no faster)
   asm volatile("" ::: "memory");  // (the loads stay below the arrival)
   auto slot = [&](int i) {
     const int x = xs + i * step;
-    return ((int64_t)x * 2 + (x == x0 ? 1 : 0)) * W + w;
+    return (int64_t)x * 2 + (x == x0 ? 1 : 0);
   };
   f32x4_dev_t v[kBatch][C];
   auto load = [&](int i0) {
@@ -161,20 +132,17 @@ __device__ __forceinline__ void q4_join(const Q4StreamArgs& a, int x0, int xs, i
   }
 }
 
-template <typename T, int D, int S, int W>
+template <typename T, int D, int S>
 __global__ __launch_bounds__(kQ4StreamThreads) __attribute__((amdgpu_waves_per_eu(2)))
 void q4_stream_kernel(Q4StreamArgs a) {
-  using Sm = Q4StreamSmem<W>;
   using Rec = Q4Record<D, S>;
-  constexpr int kTeams = Sm::kTeams, NT = kQ4StreamThreads;
-  __shared__ Sm sm;
+  constexpr int NT = kQ4StreamThreads, kWaves = NT / 64;
+  __shared__ Q4StreamSmem<D, S> sm;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int team = wave / W, w = wave % W;
   const int wg = blockIdx.x, n_wg = gridDim.x;
-  const int bid = team * n_wg + wg;  // the team's range
-  auto& tm = sm.team[team];
-  const int R = a.B;
+  const int bid = wg * kWaves + wave;  // the wave's range
+  const int R = a.B, H = a.H_kv;
 
   // 1. units per sequence and their prefix sums (every workgroup, redundantly);
   // the rows without units are written by the workgroups in turn
@@ -202,9 +170,9 @@ void q4_stream_kernel(Q4StreamArgs a) {
     T* o = reinterpret_cast<T*>(a.out);
     for (int64_t i = from * a.H_q * D + tid; i < to * a.H_q * D; i += NT) store_out<T>(o + i, what == 2 ? 0.0f : NAN);
   }
-  const int U = a.nb * sm.cum[R];
-  const int G = max(1, min(n_wg * kTeams, U));  // ranges
-  if (wg >= G || U == 0) return;
+  const int U = H * sm.cum[R];
+  const int G = max(1, min(n_wg * kWaves, U));  // ranges
+  if (wg * kWaves >= G || U == 0) return;
   // ranges of each or each + 1 units, the longer ones first
   const int each = U / G, longer = U % G;
   auto begin_of = [&](int x) { return min(x, G) * each + min(x, longer); };
@@ -212,155 +180,135 @@ void q4_stream_kernel(Q4StreamArgs a) {
     const int split = longer * (each + 1);
     return e < split ? e / (each + 1) : longer + (e - split) / each;
   };
-  auto units_of = [&](int x) { return begin_of(x + 1) - begin_of(x); };
   const int u0 = begin_of(bid);
-  const int n_units = units_of(bid);
-  int n_steps = 0;  // units of the longest range of the workgroup's teams
+  const int m = begin_of(bid + 1) - u0;  // units of the range
+
+  // 2. The range's units, 64 at a time, one per lane: the words that their lengths and
+  // pages come from are loaded when the 64 before begin.
+  struct Words {
+    int hb, p, np;  // KV head; unit of the item and the item's units
+    int row, len, page[2];
+  };
+  auto load_entries = [&](int i0) {
+    Words e;
+    const int x = u0 + min(i0 + lane, m - 1);
+    const int r = info_row_seq(sm.cum, R, H, x);
+    const int rem = x - H * sm.cum[r];
+    e.np = sm.cum[r + 1] - sm.cum[r];
+    e.hb = rem / e.np;
+    e.p = rem - e.hb * e.np;
+    e.len = a.context_lens[r];
+    e.row = a.query_start_loc != nullptr ? a.query_start_loc[r] : r;
 #pragma unroll
-  for (int t = 0; t < kTeams; ++t) n_steps = max(n_steps, units_of(t * n_wg + wg));
+    for (int h = 0; h < 2; ++h)  // (past the context's pages: any entry, unused)
+      e.page[h] = a.block_table[(int64_t)r * a.bt_stride + min((int64_t)2 * e.p + h, a.bt_stride - 1)];
+    return e;
+  };
+  struct Entries {
+    int64_t at[2];  // the tiles' first byte (0: outside the pool, or no page)
+    int info;       // tokens (6 bits) | page 0, 1 outside the pool | anything but 32 tokens of the pool
+    int hb, p, np, row;
+  };
+  const int64_t tile = q4_tile_bytes(D);
+  auto make_entries = [&](const Words& w) {
+    Entries e;
+    const int left = w.len - w.p * kQ4Unit;  // tokens from the unit on
+    int odd = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool used = left > kPage * h, ok = used && w.page[h] >= 0 && w.page[h] < a.num_pages;
+      odd |= (ok || !used ? 0 : 1) << h;
+      e.at[h] = ok ? ((int64_t)w.page[h] * H + w.hb) * tile : 0;
+    }
+    e.info = min(left, kQ4Unit) | odd << 6 | (odd != 0 || left < kQ4Unit) << 8;
+    e.hb = w.hb;
+    e.p = w.p;
+    e.np = w.np;
+    e.row = w.row;
+    return e;
+  };
 
   q4::State<T, D, 1> st;
   q4::Unit<D> u;
+  const int k_shift = q4::k_shift<D>(lane);
   const int n = lane & 15, Gl = lane >> 4;
-  const int64_t tile = q4_tile_bytes(D);
   T* out = reinterpret_cast<T*>(a.out);
-  const uint8_t* kw = a.k_pages + w * tile;
-  const uint8_t* vw = a.v_pages + w * tile;
+  const int tile_size = a.num_pages > 0 ? q4_tile_bytes(D) : 0;
   struct Tiles {
     int64_t at[2];
     int info;
   };
-  auto tiles = [&](int i) {  // (wave-uniform)
-    const Q4UnitEntry& e = tm.unit[i];
-    Tiles t;
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-      t.at[p] = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(e.at[p] >> 32)) << 32 |
-                          (uint32_t)__builtin_amdgcn_readfirstlane((int)e.at[p]));
-    t.info = __builtin_amdgcn_readfirstlane(e.info);
-    return t;
-  };
-  const int tile_size = a.num_pages > 0 ? q4_tile_bytes(D) : 0;
   auto fetch_k = [&](const Tiles& e, bool any) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_k<D, kKvLoadPolicy>(u, p, kw + e.at[p], any ? tile_size : 0, lane);
+    for (int p = 0; p < 2; ++p) q4::load_k<D, kKvLoadPolicy>(u, p, a.k_pages + e.at[p], any ? tile_size : 0, lane);
   };
   auto fetch_v = [&](const Tiles& e, bool any) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_v<D, kKvLoadPolicy>(u, p, vw + e.at[p], any ? tile_size : 0, lane);
+    for (int p = 0; p < 2; ++p) q4::load_v<D, kKvLoadPolicy>(u, p, a.v_pages + e.at[p], any ? tile_size : 0, lane);
   };
-
-  // Items cut by the range's ends.  Each wave is alone: a part is its record in the
-  // workspace and one count of the item's counter for this wave's head.  Whichever
-  // part counts last joins all of them in range order; nothing waits on another
-  // workgroup.  The item that the start cuts (job 0), its record stored at the end of
-  // unit k, counts when unit k + 3 starts: the vector-memory counter retires in issue
-  // order, and unit k + 2, whose loads went out after the record, has been folded.
-  // It looks at the answer when the range has streamed.  The item that the end cuts
-  // (job 1) has usually one other part, which was the first thing of the next range:
-  // its count is looked at before the last unit, and if it is there the wave joins
-  // its record from registers and stores none of its own.
-  auto counter_at = [&](int x) {
-    // (global memory for certain: while a generic access is under way, every wait is for all)
-    using Global = __attribute__((address_space(1))) unsigned long long;
-    Global* p = (Global*)(a.ws_flag + ((int64_t)x * W + w) * kQ4CounterStride);
-    asm("" : "+v"(p));  // (an address of lanes: one atomic, not a wave's reduction)
-    return DeviceCounter{(unsigned long long*)p};
-  };
-  auto level_of = [&](const Q4Cut& cut) { return cut.grouped() && !cut.group_of_one(bid) ? 0 : 1; };
-  bool stored[2] = {false, false};
-  int counted_at = INT32_MAX;  // job 0 counts before this unit
-  bool counted = false;
-  uint64_t counted_old = 0;    // the counter before
-  uint64_t seen = 0;           // the last item's counter
-  bool look = false;           // whether it has been read
-  bool head_partial = false, open = false;  // of the present item: it began before the range; it has not ended
-  auto store_part = [&](int which, float l, int row, int g) {
-    const int64_t slot = ((int64_t)bid * 2 + which) * W + w;
-    const __amdgpu_buffer_rsrc_t r = record_rsrc(a.ws_o + slot * S * D, S * D);
+  auto put_part = [&](int which, float l) {
+    auto& part = sm.part[wave][which];
     if (n < S) {
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) {
         float o[8];
         q4::eight_out(st, 0, j, o);
-        store_dev4(r, Rec::chunk(n, 2 * j, Gl) * 4, f32x4_dev_t{o[0], o[1], o[2], o[3]});
-        store_dev4(r, Rec::chunk(n, 2 * j + 1, Gl) * 4, f32x4_dev_t{o[4], o[5], o[6], o[7]});
+        *reinterpret_cast<f32x4_dev_t*>(&part.o[Rec::chunk(n, 2 * j, Gl) * 4]) = f32x4_dev_t{o[0], o[1], o[2], o[3]};
+        *reinterpret_cast<f32x4_dev_t*>(&part.o[Rec::chunk(n, 2 * j + 1, Gl) * 4]) = f32x4_dev_t{o[4], o[5], o[6], o[7]};
       }
-      if (Gl == 0) store_dev(a.ws_ml + (slot * S + n) * 2, st.m[0], l);
+      if (Gl == 0) {
+        part.ml[n][0] = st.m[0];
+        part.ml[n][1] = l;
+      }
     }
-    if (lane == 0) {
-      tm.job[w][which][0] = row;
-      tm.job[w][which][1] = g;
-    }
-    stored[0] |= which == 0;
-    stored[1] |= which == 1;
   };
 
-  for (int base = 0; base < n_steps; base += Sm::kUnits) {
-    // 2. unit table of this part of the range, and the items cut by its ends
-    const int m = min(n_units - base, Sm::kUnits);
-    if (base > 0) __syncthreads();
-    for (int i = w * 64 + lane; i < m; i += 64 * W) {
-      const int x = u0 + base + i;
-      const int r = info_row_seq(sm.cum, R, a.nb, x);
-      const int np = sm.cum[r + 1] - sm.cum[r];
-      const int rem = x - a.nb * sm.cum[r];
-      const int hb = rem / np, p = rem - hb * np;
-      int page[2];  // (past the context's pages: any entry, unused; read without waiting for the length)
+  // 3. Stream the units, the next one's K loaded as soon as the scores are formed, its
+  // V after the products.
+  struct Job {  // an item cut by the range's start (0) or end (1): its ranges, row and KV head
+    int from = -1, to = -1, row = 0, g = 0;
+  } job[2];
+  if (m > 0) {
+    Entries es = make_entries(load_entries(0));
+    Words coming = load_entries(64);
+    int i0 = 0;  // unit of es's first lane
+    auto of = [&](int x, int i) { return __builtin_amdgcn_readlane(x, i - i0); };
+    auto tiles = [&](int i) {  // (wave-uniform)
+      Tiles t;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) page[h] = a.block_table[(int64_t)r * a.bt_stride + min((int64_t)2 * p + h, a.bt_stride - 1)];
-      const int left = a.context_lens[r] - p * kQ4Unit;  // tokens from the unit on
-      Q4UnitEntry e;
-      int odd = 0;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bool used = left > kPage * h, ok = used && page[h] >= 0 && page[h] < a.num_pages;
-        odd |= (ok || !used ? 0 : 1) << h;
-        e.at[h] = ok ? ((int64_t)page[h] * a.H_kv + hb * W) * tile : 0;
-      }
-      e.info = min(left, kQ4Unit) | odd << 6 | (odd != 0 || left < kQ4Unit) << 8 | hb << 9;
-      e.left = np - p;
-      e.row = a.query_start_loc != nullptr ? a.query_start_loc[r] : r;
-      e.first = p == 0;
-      tm.unit[i] = e;
-      if (base + i == 0) tm.cut[0] = p == 0 ? Q4Cut{-1, -1} : Q4Cut{range_of(x - p), range_of(x - p + np - 1)};
-      if (base + i == n_units - 1) tm.last_row = e.row, tm.last_hb = hb;
-      if (base + i == n_units - 1) tm.cut[1] = p == np - 1 ? Q4Cut{-1, -1} : Q4Cut{range_of(x - p), range_of(x - p + np - 1)};
-    }
-    __syncthreads();
-    if (m <= 0) continue;
-    const bool has_next = base + m == n_units && tm.cut[1].x0 == bid && tm.cut[1].x1 == bid + 1;
-
-    // 3. stream the units: wave w handles KV head hb * W + w of every unit, the next
-    // unit's K loaded as soon as the scores are formed, its V after the products
+      for (int p = 0; p < 2; ++p)
+        t.at[p] = (int64_t)((uint64_t)(uint32_t)of((int)(es.at[p] >> 32), i) << 32 | (uint32_t)of((int)es.at[p], i));
+      t.info = of(es.info, i);
+      return t;
+    };
     Tiles t = tiles(0);
     fetch_k(t, true);
     __builtin_amdgcn_sched_barrier(0);  // (K before V, as the loop's waits expect)
     fetch_v(t, true);
+    bool open = false, head = false;  // the present item has begun; it began before the range
+    int from = 0, to = 0, row = 0, g = 0;
     for (int i = 0; i < m;) {
-      const Q4UnitEntry& e = tm.unit[i];
-      const int left = __builtin_amdgcn_readfirstlane(e.left);
-      const int g = (__builtin_amdgcn_readfirstlane(e.info) >> 9) * W + w;
-      const int row = __builtin_amdgcn_readfirstlane(e.row);
-      const int64_t at = ((int64_t)row * a.H_q + (int64_t)g * S + n) * D;
-      if (__builtin_amdgcn_readfirstlane(e.first) || base + i == 0) {
-        head_partial = !__builtin_amdgcn_readfirstlane(e.first);
-        q4::load_query<T, D>(st.q[0], n < S ? reinterpret_cast<const T*>(a.q) + at : nullptr, lane);
+      const int p = of(es.p, i), left = of(es.np, i) - p;
+      if (!open) {
+        row = of(es.row, i);
+        g = of(es.hb, i);
+        head = p > 0;
+        from = range_of(u0 + i - p);
+        to = range_of(u0 + i + left - 1);
+        q4::load_query<T, D>(st.q[0], n < S ? reinterpret_cast<const T*>(a.q) + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D : nullptr, lane);
         q4::reset(st);
         open = true;
       }
-      // units without anything else to do between them
-      int stop = min(m, i + left);
-      if (base + i == counted_at) {
-        asm volatile("" ::: "memory");
-        const Q4Cut cut = tm.cut[0];
-        if (lane == 0) counted_old = counter_at(cut.counter(level_of(cut), bid)).fetch_add(a.key.step);
-        counted = true;
-      }
-      if (counted_at > base + i) stop = min(stop, counted_at - base);
-      if (has_next) {
-        if (i < m - 1) stop = min(stop, m - 1);
-        else seen = __hip_atomic_load(counter_at(bid).p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), look = true;
+      // units without anything else to do between them: the last of the 64 is alone,
+      // the next one's entry is among those coming
+      int stop = min(min(m, i + left), i0 + 63);
+      if (i + 1 - i0 == 64) {
+        stop = i + 1;
+        if (stop < m) {
+          es = make_entries(coming);
+          i0 += 64;
+          coming = load_entries(i0 + 64);
+        }
       }
       const bool ends = stop == i + left;
       for (; i < stop; ++i) {
@@ -372,7 +320,7 @@ void q4_stream_kernel(Q4StreamArgs a) {
         auto weights = [&](bool usual) {  // the weights of unit i, and the next K; whether a base moves or V is beyond fp16
           const bool more = i + 1 < m;
           next = tiles(more ? i + 1 : i);
-          q4::fold_qk<T, D, 1>(st, u, lane, s);
+          q4::fold_qk<T, D, 1>(st, u, k_shift, s);
           fetch_k(next, more);
           if (!usual) {
             const int tokens = t.info & 63;
@@ -408,9 +356,9 @@ void q4_stream_kernel(Q4StreamArgs a) {
         t = next;
       }
       if (!ends) continue;
-      // the item ends: its output, or the record of this range's part of it
+      // the item ends: its output, or this range's part of it
       const float l = rows4_sum(st.l[0]);
-      if (!head_partial) {
+      if (!head) {
         const float inv = 1.0f / l;
         if (n < S) {
 #pragma unroll
@@ -418,97 +366,96 @@ void q4_stream_kernel(Q4StreamArgs a) {
             float o[8];
             q4::eight_out(st, 0, j, o);
 #pragma unroll
-            for (int x = 0; x < 8; ++x) o[x] *= inv;
-            q4::store_eight(out + at + 32 * j + 8 * Gl, o);
+            for (int e = 0; e < 8; ++e) o[e] *= inv;
+            q4::store_eight(out + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D + 32 * j + 8 * Gl, o);
           }
         }
       } else {
-        store_part(0, l, row, g);
-        counted_at = base + i + 2;  // (i: the unit after)
+        put_part(0, l);
+        job[0] = Job{from, to, row, g};
       }
       open = false;
     }
-  }
-  if (open) {  // the range ends inside an item
-    const float l = rows4_sum(st.l[0]);
-    const int row = __builtin_amdgcn_readfirstlane(tm.last_row), g = __builtin_amdgcn_readfirstlane(tm.last_hb) * W + w;
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)seen), hi = __builtin_amdgcn_readfirstlane((uint32_t)(seen >> 32));
-    if (look && ((uint64_t)hi << 32 | lo) == a.key.step) {  // its other part has counted: join it from registers
-      asm volatile("" ::: "memory");  // (the record's loads stay below the look at the counter)
-      const int64_t slot = ((int64_t)(bid + 1) * 2) * W + w;
-      const __amdgpu_buffer_rsrc_t r = record_rsrc(a.ws_o + slot * S * D, S * D);
-      const int nn = min(n, S - 1);
-      float m1, l1;
-      f32x4_dev_t o1[D / 16];
-      load_dev2(a.ws_ml + (slot * S + nn) * 2, m1, l1);
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j) o1[j] = load_dev4(r, Rec::chunk(nn, j, Gl) * 4);
-      // (q4_join's operations in its order, so the bits do not depend on who joins)
-      const float M = fmaxf(st.m[0], m1);
-      const float c0 = fast_exp2(st.m[0] - M), c1 = fast_exp2(m1 - M);
-      const float inv = 1.0f / fmaf(l1, c1, l * c0);
-      if (n < S) {
-#pragma unroll
-        for (int j = 0; j < D / 32; ++j) {
-          float o[8];
-          q4::eight_out(st, 0, j, o);
-#pragma unroll
-          for (int x = 0; x < 8; ++x) o[x] = fmaf(o1[2 * j + x / 4][x % 4], c1, o[x] * c0) * inv;
-          q4::store_eight(out + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D + 32 * j + 8 * Gl, o);
-        }
+    if (open) {  // the range ends inside an item
+      const float l = rows4_sum(st.l[0]);
+      if (head) {
+        put_part(0, l);
+        job[0] = Job{from, to, row, g};
+      } else {
+        put_part(1, l);
+        job[1] = Job{from, to, row, g};
       }
-      if (lane == 0) counter_at(bid).store(0);
-    } else {
-      store_part(head_partial ? 0 : 1, l, row, g);
     }
   }
 
-  // 4. join the cut items
+  // 4. Join the cut items: the parts of the workgroup's waves in LDS, by the wave that
+  // has the first.  An item cut by the workgroup's ends too: that wave stores the joined
+  // part as the workgroup's record (slot 0: of the item that the workgroup's start cuts,
+  // 1: of that which its end cuts) and counts it, and whichever part counts last joins
+  // all of them in order; nothing waits on another workgroup.
+  __syncthreads();
+  auto counter_at = [&](int x) {
+    // (global memory for certain: while a generic access is under way, every wait is for all)
+    using Global = __attribute__((address_space(1))) unsigned long long;
+    Global* p = (Global*)(a.ws_flag + (int64_t)x * kQ4CounterStride);
+    asm("" : "+v"(p));  // (an address of lanes: one atomic, not a wave's reduction)
+    return DeviceCounter{(unsigned long long*)p};
+  };
 #pragma unroll 1
   for (int j = 0; j < 2; ++j) {
-    if (!(j == 0 ? stored[0] : stored[1])) continue;
-    const Q4Cut cut = tm.cut[j];
-    const int row = __builtin_amdgcn_readfirstlane(tm.job[w][j][0]), g = __builtin_amdgcn_readfirstlane(tm.job[w][j][1]);
-    T* o = out + ((int64_t)row * a.H_q + (int64_t)g * S) * D;
-    bool early = j == 0 && counted;
+    const Job it = j == 0 ? job[0] : job[1];
+    if (it.from < 0 || (j == 0 && wave > 0)) continue;  // (else an earlier wave has the item's first part)
+    // parts: slot j of this wave, slot 0 of those up to the item's last
+    const int parts = min(it.to - wg * kWaves, kWaves - 1) - wave + 1;
+    const CutItem cut{it.from / kWaves, it.to / kWaves};
+    const bool whole = cut.x0 == cut.x1;
+    T* o = out + ((int64_t)it.row * a.H_q + (int64_t)it.g * S) * D;
+    const int64_t slot = (int64_t)wg * 2 + j;
+    const __amdgpu_buffer_rsrc_t r = record_rsrc(a.ws_o + slot * S * D, S * D);
+    for (int c = lane; c < S * D / 4; c += 64) {
+      const int h = Rec::head(c);
+      float M = kMInit, L = 0.0f;
+      for (int i = 0; i < parts; ++i) M = fmaxf(M, sm.part[wave + i][i == 0 ? j : 0].ml[h][0]);
+      f32x4_dev_t acc = {0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < parts; ++i) {
+        const auto& part = sm.part[wave + i][i == 0 ? j : 0];
+        const float ci = fast_exp2(part.ml[h][0] - M);
+        L = fmaf(part.ml[h][1], ci, L);
+        acc = *reinterpret_cast<const f32x4_dev_t*>(&part.o[c * 4]) * ci + acc;
+      }
+      if (whole) {
+        q4::store_four(o + h * D + Rec::dim(c), acc * (1.0f / L));
+      } else {
+        store_dev4(r, c * 4, acc);
+        if (Rec::dim(c) == 0) store_dev(a.ws_ml + (slot * S + h) * 2, M, L);
+      }
+    }
+    if (whole) continue;
 #pragma unroll 1
-    for (int lv = level_of(cut); lv < 2; ++lv) {
-      const int parts = cut.parts(lv, bid);
+    for (int lv = cut.grouped() && !cut.group_of_one(wg) ? 0 : 1; lv < 2; ++lv) {
+      const int records = cut.parts(lv, wg);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0);  // the record is stored
       int last = 0;
-      if (!early) {
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0);  // the record is stored
-      }
       if (lane == 0) {
-        DeviceCounter ctr = counter_at(cut.counter(lv, bid));
-        last = early ? counter_answer(ctr, a.key, parts, counted_old) : counter_arrive(ctr, a.key, parts);
+        DeviceCounter ctr = counter_at(cut.counter(lv, wg));
+        last = counter_arrive(ctr, a.key, records);
       }
-      early = false;
       if (!__builtin_amdgcn_readfirstlane(last)) break;
       // (a group's record counts in the item next)
-      q4_join<T, D, S, W>(a, cut.x0, cut.first(lv, bid), cut.step(lv), parts, lv == 1, w, lane, o);
+      q4_join<T, D, S>(a, cut.x0, cut.first(lv, wg), cut.step(lv), records, lv == 1, lane, o);
     }
   }
 }
 
-template <typename T, int D, int S>
-const void* q4_stream_pick_w(int W) {
-  switch (W) {
-    case 1: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, S, 1>);
-    case 2: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, S, 2>);
-    case 4: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, S, 4>);
-    case 8: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, S, 8>);
-  }
-  return nullptr;
-}
 template <typename T, int D>
-const void* q4_stream_pick(int s, int W) {
+const void* q4_stream_pick(int s) {
   switch (s) {
-    case 1: return q4_stream_pick_w<T, D, 1>(W);
-    case 2: return q4_stream_pick_w<T, D, 2>(W);
-    case 4: return q4_stream_pick_w<T, D, 4>(W);
-    case 6: return q4_stream_pick_w<T, D, 6>(W);
-    case 8: return q4_stream_pick_w<T, D, 8>(W);
+    case 1: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, 1>);
+    case 2: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, 2>);
+    case 4: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, 4>);
+    case 6: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, 6>);
+    case 8: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, 8>);
   }
   return nullptr;
 }

@@ -19,41 +19,41 @@
 
 namespace pa {
 
-extern template const void* q4_stream_pick<uint16_t, 64>(int, int);
-extern template const void* q4_stream_pick<float, 128>(int, int);
-extern template const void* q4_stream_pick<float, 64>(int, int);
-template const void* q4_stream_pick<uint16_t, 128>(int, int);
+extern template const void* q4_stream_pick<uint16_t, 64>(int);
+extern template const void* q4_stream_pick<float, 128>(int);
+extern template const void* q4_stream_pick<float, 64>(int);
+template const void* q4_stream_pick<uint16_t, 128>(int);
 
-static const void* q4_stream_fn(int dtype, int D, int s, int W) {
-  if (dtype == 0 && D == 128) return q4_stream_pick<uint16_t, 128>(s, W);
-  if (dtype == 0 && D == 64) return q4_stream_pick<uint16_t, 64>(s, W);
-  if (dtype == 1 && D == 128) return q4_stream_pick<float, 128>(s, W);
-  if (dtype == 1 && D == 64) return q4_stream_pick<float, 64>(s, W);
+static const void* q4_stream_fn(int dtype, int D, int s) {
+  if (dtype == 0 && D == 128) return q4_stream_pick<uint16_t, 128>(s);
+  if (dtype == 0 && D == 64) return q4_stream_pick<uint16_t, 64>(s);
+  if (dtype == 1 && D == 128) return q4_stream_pick<float, 128>(s);
+  if (dtype == 1 && D == 64) return q4_stream_pick<float, 64>(s);
   return nullptr;
 }
 
 // (a property of the kernel and the device, so it is asked for once: the two
 // queries take as long as the rest of a small call on the host)
-int q4_stream_workgroups(int dtype, int D, int s, int W) {
+int q4_stream_workgroups(int dtype, int D, int s) {
   constexpr int kDevices = 64;
-  static std::atomic<int> known[kDevices][2][2][9][9];
+  static std::atomic<int> known[kDevices][2][2][9];
   int dev = 0, cus = 0, per_cu = 0;
   if (hipGetDevice(&dev) != hipSuccess) return 0;
-  std::atomic<int>* at = dev >= 0 && dev < kDevices && dtype >= 0 && dtype < 2 && s <= 8 && W <= 8 ? &known[dev][dtype][D / 128][s][W] : nullptr;
+  std::atomic<int>* at = dev >= 0 && dev < kDevices && dtype >= 0 && dtype < 2 && s <= 8 ? &known[dev][dtype][D / 128][s] : nullptr;
   int n = at != nullptr ? at->load(std::memory_order_relaxed) : 0;
   if (n > 0) return n;
-  const void* fn = q4_stream_fn(dtype, D, s, W);
+  const void* fn = q4_stream_fn(dtype, D, s);
   if (fn == nullptr || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
       hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, fn, kQ4StreamThreads, 0) != hipSuccess)
     return 0;
-  n = std::min(cus * per_cu, kQ4StreamWaves * 64 / kQ4StreamThreads);
+  n = std::min(cus * per_cu, kQ4StreamGroups);
   if (at != nullptr) at->store(n, std::memory_order_relaxed);
   return n;
 }
 
-hipError_t launch_q4_stream(int dtype, int D, int s, int W, const Q4StreamArgs& a, int workgroups, hipStream_t st,
+hipError_t launch_q4_stream(int dtype, int D, int s, const Q4StreamArgs& a, int workgroups, hipStream_t st,
                             KernelEvents ev) {
-  const void* fn = q4_stream_fn(dtype, D, s, W);
+  const void* fn = q4_stream_fn(dtype, D, s);
   if (fn == nullptr || workgroups <= 0) return hipErrorInvalidValue;
   void* args[] = {const_cast<Q4StreamArgs*>(&a)};
   hipError_t e = hipExtLaunchKernel(fn, dim3(workgroups), dim3(kQ4StreamThreads), args, 0, st, ev.start, ev.stop, 0);

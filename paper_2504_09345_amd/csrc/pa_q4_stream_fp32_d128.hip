@@ -3,6 +3,6 @@
 
 namespace pa {
 
-template const void* q4_stream_pick<float, 128>(int, int);
+template const void* q4_stream_pick<float, 128>(int);
 
 }  // namespace pa

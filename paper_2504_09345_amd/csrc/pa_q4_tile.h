@@ -60,7 +60,7 @@ __device__ __forceinline__ u32x4 eight_of(uint32_t w, float scale) {
 template <int D>
 struct Unit {
   uint32_t k[2][kWords<D>];  // codes of token lane % 16, dims D/4 (lane / 16) .. +D/4
-  uint32_t ks[2];            // the word that holds the scale of those dims (k_scale)
+  uint32_t ks[2];            // the word that holds the scale byte of those dims (k_shift)
   uint32_t v[2][kWords<D>];  // word j: tokens 4 (lane / 16) .. +3, dims 32 j + 2 (lane % 16), +1
   uint32_t vs[2][kWords<D>];  // scales of those four tokens, token-major
 };
@@ -85,11 +85,11 @@ __device__ __forceinline__ void load_k(Unit<D>& u, int p, const uint8_t* k, int 
   load_words<D, Policy>(r, lane * (D / 8), u.k[p]);
   u.ks[p] = __builtin_amdgcn_raw_buffer_load_b32(r, kScales<D> + ((lane & 15) * (D / 32) & ~3), 0, Policy);
 }
-// The scale byte of the lane's K codes, with others above it.  (A load of the byte
-// alone is extended where it is loaded, which waits for it there.)
+// The shift that brings the scale byte of the lane's K codes down, with others above it.
+// (A load of the byte alone is extended where it is loaded, which waits for it there.)
 template <int D>
-__device__ __forceinline__ uint32_t k_scale(const Unit<D>& u, int p, int lane) {
-  return u.ks[p] >> (D == 128 ? (lane >> 4) * 8 : (lane & 1) * 16 + (lane >> 5) * 8);
+__device__ __forceinline__ int k_shift(int lane) {
+  return D == 128 ? (lane >> 4) * 8 : (lane & 1) * 16 + (lane >> 5) * 8;
 }
 template <int D, int Policy>
 __device__ __forceinline__ void load_v(Unit<D>& u, int p, const uint8_t* v, int bytes, int lane) {
@@ -253,15 +253,16 @@ __device__ __forceinline__ void load_query(Query<T, D>& q, const T* row, int lan
 // Fold of the unit of keys key0 .. key0 + 31, in three steps, so that K's registers
 // and then V's are free for the next unit's loads as soon as they are read.
 //
-// Scores S^T[token][column] = K . Q^T, the K operand shared by the columns.
+// Scores S^T[token][column] = K . Q^T, the K operand shared by the columns.  shift: of
+// the scale words.
 template <typename T, int D, int NB>
-__device__ __forceinline__ void fold_qk(const State<T, D, NB>& st, const Unit<D>& u, int lane, f32x4_t (&s)[NB][2]) {
+__device__ __forceinline__ void fold_qk(const State<T, D, NB>& st, const Unit<D>& u, int shift, f32x4_t (&s)[NB][2]) {
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
 #pragma unroll
     for (int c = 0; c < NB; ++c) s[c][p] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if constexpr (kCodeScores<T, D>) {
-      const int ks = (int)k_scale<D>(u, p, lane);  // (the product reads the lowest byte)
+      const int ks = (int)(u.ks[p] >> shift);  // (the product reads the lowest byte)
       const i32x8_t a = {(int)u.k[p][0], (int)u.k[p][1], (int)u.k[p][2], (int)u.k[p][3], 0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -269,7 +270,7 @@ __device__ __forceinline__ void fold_qk(const State<T, D, NB>& st, const Unit<D>
         for (int c = 0; c < NB; ++c)  // (formats: 4 the codes, 0 e4m3)
           s[c][p] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, st.q[c].x[i], s[c][p], 4, 0, 0, ks, 0, (int)st.q[c].s[i]);
     } else {
-      const float ks = scale_of<0>(k_scale<D>(u, p, lane));
+      const float ks = scale_of<0>(u.ks[p] >> shift);
 #pragma unroll
       for (int w = 0; w < D / 32; ++w) {
         const bf16x8_t a = __builtin_bit_cast(bf16x8_t, eight_of(u.k[p][w], ks));
