@@ -265,7 +265,7 @@ void q4_stream_kernel(Q4StreamArgs a) {
 
   // 3. Stream the units, the next one's K loaded as soon as the scores are formed, its
   // V after the products.
-  struct Job {  // an item cut by the range's start (0) or end (1): its ranges, row and KV head
+  struct Job {  // an item cut by the range's start (0) or end (1): its first and last unit, row and KV head
     int from = -1, to = -1, row = 0, g = 0;
   } job[2];
   if (m > 0) {
@@ -293,8 +293,8 @@ void q4_stream_kernel(Q4StreamArgs a) {
         row = of(es.row, i);
         g = of(es.hb, i);
         head = p > 0;
-        from = range_of(u0 + i - p);
-        to = range_of(u0 + i + left - 1);
+        from = u0 + i - p;
+        to = u0 + i + left - 1;
         q4::load_query<T, D>(st.q[0], n < S ? reinterpret_cast<const T*>(a.q) + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D : nullptr, lane);
         q4::reset(st);
         open = true;
@@ -406,17 +406,20 @@ void q4_stream_kernel(Q4StreamArgs a) {
     const Job it = j == 0 ? job[0] : job[1];
     if (it.from < 0 || (j == 0 && wave > 0)) continue;  // (else an earlier wave has the item's first part)
     // parts: slot j of this wave, slot 0 of those up to the item's last
-    const int parts = min(it.to - wg * kWaves, kWaves - 1) - wave + 1;
-    const CutItem cut{it.from / kWaves, it.to / kWaves};
+    const int to = range_of(it.to), parts = min(to - wg * kWaves, kWaves - 1) - wave + 1;
+    const CutItem cut{range_of(it.from) / kWaves, to / kWaves};
     const bool whole = cut.x0 == cut.x1;
     T* o = out + ((int64_t)it.row * a.H_q + (int64_t)it.g * S) * D;
     const int64_t slot = (int64_t)wg * 2 + j;
     const __amdgpu_buffer_rsrc_t r = record_rsrc(a.ws_o + slot * S * D, S * D);
+#pragma unroll 1
     for (int c = lane; c < S * D / 4; c += 64) {
       const int h = Rec::head(c);
       float M = kMInit, L = 0.0f;
+#pragma unroll 4
       for (int i = 0; i < parts; ++i) M = fmaxf(M, sm.part[wave + i][i == 0 ? j : 0].ml[h][0]);
       f32x4_dev_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
       for (int i = 0; i < parts; ++i) {
         const auto& part = sm.part[wave + i][i == 0 ? j : 0];
         const float ci = fast_exp2(part.ml[h][0] - M);
