@@ -47,6 +47,7 @@ struct Q4AttnArgs {
   int min_rows;  // sequences of fewer rows are the stream kernel's
   int max_q_len;
   int n_split, split_units;
+  int wave_parts;  // waves (1, 2 or 4) that share an item's units, where a wave has 16 columns
 };
 constexpr int kQ4Waves = 4;  // waves of a workgroup, each with an item of its own
 

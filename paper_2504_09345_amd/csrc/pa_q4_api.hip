@@ -68,7 +68,7 @@ struct Plan {
   int per_launch = 0;  // sequences of a launch
   // chunk rows
   bool shared = false;  // V's operands shared by a workgroup
-  int blocks = 1, n_slots = 0, n_split = 1, split_units = 1, min_rows = 2;
+  int blocks = 1, n_slots = 0, n_split = 1, split_units = 1, min_rows = 2, wave_parts = 1;
   size_t st_o = 0, st_ml = 0, st_flag = 0, ch_o = 0, ch_ml = 0;
   size_t stream_bytes() const { return st_o + st_ml + st_flag; }
   size_t chunk_bytes() const { return ch_o + ch_ml; }
@@ -76,10 +76,17 @@ struct Plan {
   size_t bytes() const { return stream_bytes() > chunk_bytes() ? stream_bytes() : chunk_bytes(); }
 };
 
-// Parts that chunks are cut into: as many as give the GPU (256 CUs of 8 waves) a
-// wave of work each, of at least kLeastUnits units, at most 64.  (Parts of 4 units cost
-// one chunk of 300 rows 15 us instead of 11, parts of 32 one of 64 rows on 1,500 tokens
-// 38 instead of 18; 8 or 16 are one as good as the other.)
+// Waves of a workgroup that share an item's units and join their parts in LDS: 2 or 4
+// while the GPU still holds all of them at once (256 CUs of 12 waves).  Shared and
+// alone, 32 query heads over 8: a chunk of 16 rows on 200 tokens 7 and 10 us, of 300 9
+// and 11, of 64 on 1,500 14 and 18, 4 of 60 on 3,000 34 and 41, 16 of 8 on 2,000 25
+// and 31; with twice the waves that the GPU holds, 8 of 200 rows on 500 tokens take
+// 47 us instead of 41.
+constexpr int kPartWaves = 3072;
+// Parts beyond those, through the workspace and a second launch: as many as give the
+// GPU 2,048 waves of at least kLeastUnits units, at most 64.  (Parts of 4 units cost one
+// chunk of 64 rows on 1,500 tokens 17 us instead of 14; 8 or 16 are one as good as the
+// other.  Twice the waves: one chunk of 700 rows 31 us instead of 19.)
 constexpr int kWavesWanted = 2048, kLeastUnits = 8, kMaxSplit = 64;
 // Which kernel takes a call's chunks (bf16): waves of 16 columns, each alone, or
 // workgroups of 128 columns that share V's operands.  The latter spend a third less
@@ -136,8 +143,11 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
     p->blocks = p->shared ? pa::kQ4ChunkBlocks : 1;
     const int64_t slots = p->rows / pa::q4_positions(p->blocks, s) + (int64_t)d->num_seqs;
     const int64_t items = (chunk_rows / pa::q4_positions(p->blocks, s) + 1) * d->num_kv_heads;
-    int64_t split = kWavesWanted / (items * (p->shared ? pa::kQ4Waves : 1));
-    if (split > units / kLeastUnits) split = units / kLeastUnits;
+    if (!p->shared)
+      while (p->wave_parts < pa::kQ4Waves && items * p->wave_parts * 2 <= kPartWaves && units >= p->wave_parts * 2) p->wave_parts *= 2;
+    const int waves = p->shared ? pa::kQ4Waves : p->wave_parts;  // of an item
+    int64_t split = kWavesWanted / (items * waves);
+    if (split > units / (kLeastUnits * p->wave_parts)) split = units / (kLeastUnits * p->wave_parts);
     if (split > kMaxSplit) split = kMaxSplit;
     if (split < 1) split = 1;
     p->split_units = (int)((units + split - 1) / split);
@@ -199,6 +209,7 @@ int attend(const void* q, const void* k_pages, const void* v_pages, const int32_
     a.max_q_len = d->max_q_len;
     a.n_split = p.n_split;
     a.split_units = p.split_units;
+    a.wave_parts = p.wave_parts;
     pa::KernelEvents ev;
     ev.start = begin;
     ev.stop = p.stream ? nullptr : end;

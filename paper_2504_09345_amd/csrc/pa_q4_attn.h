@@ -13,7 +13,8 @@ struct Q4Item {
   bool bad;            // rows are NaN
 };
 
-// Row block `slot` of the call: the blocks of sequence b are the slots from query_start_loc[b] / positions + b on, which no two sequences share.
+// Row block `slot` of the call: the blocks of sequence b are the slots from
+// query_start_loc[b] / positions + b on, which no two sequences share.
 __device__ __forceinline__ Q4Item q4_item(const Q4AttnArgs& a, int slot, int positions, int lane) {
   Q4Item it{0, 0, 0, 0, false};
   const int32_t* qsl = a.query_start_loc;
@@ -62,6 +63,13 @@ __device__ __forceinline__ void q4_finish(const Q4AttnArgs& a, const q4::State<T
   }
 }
 
+// What a wave hands to the one that joins an item's parts.
+template <int D>
+struct Q4Part {
+  q4::f32x4_t o[D / 16][64];
+  float m[64], l[64];
+};
+
 template <typename T, int D>
 __global__ __launch_bounds__(64 * kQ4Waves) __attribute__((amdgpu_waves_per_eu(2)))
 void q4_attn_kernel(Q4AttnArgs a) {
@@ -72,117 +80,146 @@ void q4_attn_kernel(Q4AttnArgs a) {
   // row blocks of one head side by side
   const int split = blockIdx.x % a.n_split, g = blockIdx.x / a.n_split % a.H_kv;
   // (the last blocks of a sequence see the most keys: they start first)
-  const int slot = (gridDim.x / a.n_split / a.H_kv - 1 - blockIdx.x / a.n_split / a.H_kv) * kQ4Waves + wave;
-  if (slot >= a.n_slots) return;
-  const Q4Item it = q4_item(a, slot, q4_positions(NB, S), lane);
-  if (it.n_pos == 0) return;
+  // (a workgroup's waves have items of their own, or 2 or 4 share one)
+  const int sharers = a.wave_parts, part = wave & (sharers - 1);
+  const int slot = ((gridDim.x / a.n_split / a.H_kv - 1 - blockIdx.x / a.n_split / a.H_kv) * kQ4Waves + wave) / sharers;
+  Q4Item it{0, 0, 0, 0, false};
+  if (slot < a.n_slots) it = q4_item(a, slot, q4_positions(NB, S), lane);
 
   const int n = lane & 15;
   T* out = reinterpret_cast<T*>(a.out);
   const int all_last = it.last0 + it.n_pos - 1;
-  if (it.bad) {
-    if (split != 0) return;
+  if (it.bad && split == 0 && part == 0) {
     for (int i = lane; i < it.n_pos * S * D; i += 64)
       store_out<T>(out + ((int64_t)(it.row0 + i / (S * D)) * a.H_q + (int64_t)g * S) * D + i % (S * D), NAN);
-    return;
   }
-  const int n_units = all_last / kQ4Unit + 1;
-  const int u0 = split * a.split_units, u1 = min(n_units, u0 + a.split_units);
-  if (u0 >= u1) return;
+  // units of the item that the workgroup takes, and the wave's of them
+  const int n_units = it.n_pos == 0 || it.bad ? 0 : all_last / kQ4Unit + 1;
+  const int s0 = split * a.split_units, s1 = min(n_units, s0 + a.split_units);
+  const int per = (max(s1 - s0, 0) + sharers - 1) / sharers;
+  const int u0 = s0 + part * per, u1 = min(s1, u0 + per);
+  if (u0 >= u1 && sharers == 1) return;
 
   q4::State<T, D, NB> st;
   int64_t at[NB];  // of the column's (row, head) vector, among all
-#pragma unroll
-  for (int c = 0; c < NB; ++c) {
-    const int col = 16 * c + n, pos = col / S;
-    const bool there = pos < it.n_pos;  // (columns past the item's positions are none)
-    st.last[c] = there ? it.last0 + pos : -1;
-    at[c] = (int64_t)(it.row0 + (there ? pos : 0)) * a.H_q + (int64_t)g * S + col % S;
-    q4::load_query<T, D>(st.q[c], there ? reinterpret_cast<const T*>(a.q) + at[c] * D : nullptr, lane);
-  }
   q4::reset(st);
+  if (u0 < u1) {
+#pragma unroll
+    for (int c = 0; c < NB; ++c) {
+      const int col = 16 * c + n, pos = col / S;
+      const bool there = pos < it.n_pos;  // (columns past the item's positions are none)
+      st.last[c] = there ? it.last0 + pos : -1;
+      at[c] = (int64_t)(it.row0 + (there ? pos : 0)) * a.H_q + (int64_t)g * S + col % S;
+      q4::load_query<T, D>(st.q[c], there ? reinterpret_cast<const T*>(a.q) + at[c] * D : nullptr, lane);
+    }
 
-  const int n_pages = all_last / kPage + 1;
-  const int64_t tile = q4_tile_bytes(D), page_bytes = tile * a.H_kv;
-  const int tile_size = a.num_pages > 0 ? q4_tile_bytes(D) : 0;
-  const uint8_t* kg = a.k_pages + g * tile;
-  const uint8_t* vg = a.v_pages + g * tile;
-  const int32_t* table = a.block_table + (int64_t)it.b * a.bt_stride;
-  // lane i: entries of page 64 (k / 32) + i of the present unit k and of the 64 after
-  auto entries = [&](int k) {
-    const int p = (k >> 5) * 64 + lane;
-    return p < n_pages ? table[p] : 0;
-  };
-  int ids = entries(u0), ids_after = entries(u0 + 32);
-  struct Pages {
-    int64_t at[2];
-    int bad;  // bit p: page p's entry lies outside the pool
-  };
-  auto pages = [&](int k) {  // (wave-uniform; k goes up by one from call to call)
-    if ((k & 31) == 0 && k != u0) {
-      ids = ids_after;
-      ids_after = entries(k + 32);
-    }
-    Pages t{{0, 0}, 0};
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const int id = __builtin_amdgcn_readlane(ids, (2 * k + p) & 63);
-      const bool ok = id >= 0 && id < a.num_pages;
-      t.at[p] = ok ? id * page_bytes : 0;
-      t.bad |= (ok ? 0 : 1) << p;
-    }
-    return t;
-  };
-  q4::Unit<D> u;
-  const int k_shift = q4::k_shift<D>(lane);
-  auto fetch_k = [&](const Pages& t, bool any) {
-#pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_k<D, 0>(u, p, kg + t.at[p], any ? tile_size : 0, lane);
-  };
-  auto fetch_v = [&](const Pages& t, bool any) {
-#pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_v<D, 0>(u, p, vg + t.at[p], any ? tile_size : 0, lane);
-  };
-  Pages t = pages(u0);
-  fetch_k(t, true);
-  __builtin_amdgcn_sched_barrier(0);  // (K before V, as the loop's waits expect)
-  fetch_v(t, true);
-  constexpr bool kF16 = q4::kF16<T>;
-  const int u_full = min(u1, (it.last0 + 1) / kQ4Unit);  // units before are seen whole by every column
-  for (int k = u0; k < u1; ++k) {
-    q4::f32x4_t s[NB][2];
-    float x[NB][8];
-    Pages next = t;
-    bool big = false;
-    auto weights = [&](bool usual) {  // the weights of unit k, and the next K; whether its base moves or V is beyond fp16
-      if (k + 1 < u1) next = pages(k + 1);
-      q4::fold_qk<T, D, NB>(st, u, k_shift, s);
-      fetch_k(next, k + 1 < u1);
-      if (!usual) q4::mask_scores<T, D, NB>(st, k * kQ4Unit, t.bad, lane, s);
-      big = q4::form_weights<T, D, NB>(st, s, a.scale_log2, x);
-      __builtin_amdgcn_sched_barrier(0);  // (V is not waited for before the weights are formed)
-      return __builtin_amdgcn_ballot_w64(big | (kF16 && q4::beyond_fp16<D>(u))) != 0;
+    const int n_pages = all_last / kPage + 1;
+    const int64_t tile = q4_tile_bytes(D), page_bytes = tile * a.H_kv;
+    const int tile_size = a.num_pages > 0 ? q4_tile_bytes(D) : 0;
+    const uint8_t* kg = a.k_pages + g * tile;
+    const uint8_t* vg = a.v_pages + g * tile;
+    const int32_t* table = a.block_table + (int64_t)it.b * a.bt_stride;
+    // lane i: entries of page 64 (k / 32) + i of the present unit k and of the 64 after
+    auto entries = [&](int k) {
+      const int p = (k >> 5) * 64 + lane;
+      return p < n_pages ? table[p] : 0;
     };
-    bool rare = weights(k < u_full && t.bad == 0);
-    if (k < u_full) {
-      // (one way out, and nothing but the usual unit: the sums stay in place, and the
-      // loads under way are known)
-#pragma unroll 1
-      while (!rare & (k + 1 < u_full) & (next.bad == 0)) {
-        q4::add_weights(st, x);
-        q4::fold_pv<kF16, T, D, NB>(st, u, x);
-        fetch_v(next, true);
-        t = next;
-        ++k;
-        rare = weights(true);
+    int ids = entries(u0), ids_after = entries(u0 + 32);
+    struct Pages {
+      int64_t at[2];
+      int bad;  // bit p: page p's entry lies outside the pool
+    };
+    auto pages = [&](int k) {  // (wave-uniform; k goes up by one from call to call)
+      if ((k & 31) == 0 && k != u0) {
+        ids = ids_after;
+        ids_after = entries(k + 32);
       }
+      Pages t{{0, 0}, 0};
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int id = __builtin_amdgcn_readlane(ids, (2 * k + p) & 63);
+        const bool ok = id >= 0 && id < a.num_pages;
+        t.at[p] = ok ? id * page_bytes : 0;
+        t.bad |= (ok ? 0 : 1) << p;
+      }
+      return t;
+    };
+    q4::Unit<D> u;
+    const int k_shift = q4::k_shift<D>(lane);
+    auto fetch_k = [&](const Pages& t, bool any) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) q4::load_k<D, 0>(u, p, kg + t.at[p], any ? tile_size : 0, lane);
+    };
+    auto fetch_v = [&](const Pages& t, bool any) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) q4::load_v<D, 0>(u, p, vg + t.at[p], any ? tile_size : 0, lane);
+    };
+    Pages t = pages(u0);
+    fetch_k(t, true);
+    __builtin_amdgcn_sched_barrier(0);  // (K before V, as the loop's waits expect)
+    fetch_v(t, true);
+    constexpr bool kF16 = q4::kF16<T>;
+    const int u_full = min(u1, (it.last0 + 1) / kQ4Unit);  // units before are seen whole by every column
+    for (int k = u0; k < u1; ++k) {
+      q4::f32x4_t s[NB][2];
+      float x[NB][8];
+      Pages next = t;
+      bool big = false;
+      auto weights = [&](bool usual) {  // the weights of unit k, and the next K; whether its base moves or V is beyond fp16
+        if (k + 1 < u1) next = pages(k + 1);
+        q4::fold_qk<T, D, NB>(st, u, k_shift, s);
+        fetch_k(next, k + 1 < u1);
+        if (!usual) q4::mask_scores<T, D, NB>(st, k * kQ4Unit, t.bad, lane, s);
+        big = q4::form_weights<T, D, NB>(st, s, a.scale_log2, x);
+        __builtin_amdgcn_sched_barrier(0);  // (V is not waited for before the weights are formed)
+        return __builtin_amdgcn_ballot_w64(big | (kF16 && q4::beyond_fp16<D>(u))) != 0;
+      };
+      bool rare = weights(k < u_full && t.bad == 0);
+      if (k < u_full) {
+        // (one way out, and nothing but the usual unit: the sums stay in place, and the
+        // loads under way are known)
+#pragma unroll 1
+        while (!rare & (k + 1 < u_full) & (next.bad == 0)) {
+          q4::add_weights(st, x);
+          q4::fold_pv<kF16, T, D, NB>(st, u, x);
+          fetch_v(next, true);
+          t = next;
+          ++k;
+          rare = weights(true);
+        }
+      }
+      q4::settle_weights<T, D, NB>(st, s, a.scale_log2, big, x);
+      q4::fold_pv_edge<T, D, NB>(st, u, x, k * kQ4Unit, all_last, lane);
+      fetch_v(next, k + 1 < u1);
+      t = next;
     }
-    q4::settle_weights<T, D, NB>(st, s, a.scale_log2, big, x);
-    q4::fold_pv_edge<T, D, NB>(st, u, x, k * kQ4Unit, all_last, lane);
-    fetch_v(next, k + 1 < u1);
-    t = next;
   }
-
+  if (sharers > 1) {  // join the parts that have units: the first one's wave takes the others'
+    __shared__ Q4Part<D> parts[kQ4Waves];
+    if (part > 0 && u0 < u1) {
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) parts[wave].o[j][lane] = st.acc[0][j];
+      parts[wave].m[lane] = st.m[0];
+      parts[wave].l[lane] = st.l[0];
+    }
+    __syncthreads();
+    if (part > 0 || u0 >= u1) return;
+    const int n_parts = (s1 - s0 + per - 1) / per;
+    float M = st.m[0];
+    for (int i = 1; i < n_parts; ++i) M = fmaxf(M, parts[wave + i].m[lane]);
+    const float c0 = fast_exp2(st.m[0] - M);
+    st.m[0] = M;
+    st.l[0] *= c0;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) st.acc[0][j] *= c0;
+    for (int i = 1; i < n_parts; ++i) {
+      const auto& other = parts[wave + i];
+      const float ci = fast_exp2(other.m[lane] - M);
+      st.l[0] = fmaf(other.l[lane], ci, st.l[0]);
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) st.acc[0][j] = other.o[j][lane] * ci + st.acc[0][j];
+    }
+  }
   q4_finish<T, D, NB>(a, st, at, split, lane);
 }
 

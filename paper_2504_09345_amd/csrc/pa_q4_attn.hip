@@ -32,7 +32,8 @@ hipError_t launch_q4_attn(int dtype, int D, const Q4AttnArgs& a, hipStream_t st,
   const void* fn = q4_attn_fn(dtype, D);
   if (fn == nullptr) return hipErrorInvalidValue;
   const int64_t parts = (int64_t)a.H_kv * a.n_split;
-  const int64_t grid = (a.n_slots + kQ4Waves - 1) / kQ4Waves * parts;
+  const int items = kQ4Waves / a.wave_parts;  // of a workgroup
+  const int64_t grid = (a.n_slots + items - 1) / items * parts;
   void* args[] = {const_cast<Q4AttnArgs*>(&a)};
   hipError_t e = hipExtLaunchKernel(fn, dim3((uint32_t)grid), dim3(64 * kQ4Waves), args, 0, st, ev.start, ev.stop, 0);
   return e != hipSuccess ? e : hipGetLastError();
