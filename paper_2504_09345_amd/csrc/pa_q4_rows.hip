@@ -3,8 +3,9 @@
 // A (row, KV head) vector of D elements is D / 8 lanes of 8 consecutive ones, four
 // lanes to a block of 32.  Writing: the block's largest magnitude over its lanes
 // (DPP), the scale from that value's bits, v_cvt_scalef32_pk_fp4_f32 to codes (its
-// rounding is the format's).  A lane's four bytes are one word of the K tile and
-// four bytes, one in every fourth word, of the V tile.  Reading mirrors it.
+// rounding is the format's).  A lane's four bytes are one word of the K tile and four
+// bytes of the V tile, each in a word with those of three neighbouring tokens: a wave
+// takes four tokens and swaps the bytes in registers.  Reading mirrors it.
 #include "pa_device.h"
 #include "pa_q4_tile.h"
 
@@ -13,25 +14,38 @@ namespace pa {
 namespace {
 
 constexpr int kRowsWaves = 4;
+constexpr int kGroup = 4;  // tokens whose V bytes are a word
 
-// The place of a row in the cache: its slot's token and page, or why it has none.
-struct Place {
-  bool skip, bad;  // a row of no sequence; a row that the contract does not allow
-  int page, token;
+// A wave's rows: those of one sequence that lie in four slots of a page from a multiple
+// of four on (a decode call's: one).
+struct Group {
+  int row, n;   // the first row, rows (0: none)
+  bool bad;     // rows that the contract does not allow
+  int page, token;  // token: of the first row
 };
-__device__ __forceinline__ Place place_of(const Q4RowsArgs& a, int row, int lane) {
-  Place p{true, false, 0, 0};
-  int b = row, L = 1, j = 0;
+template <bool kOne, int kSpan>
+__device__ __forceinline__ Group group_of(const Q4RowsArgs& a, int slot, int lane) {
+  Group p{slot, 1, false, 0, 0};
+  int b = slot, L = 1, j = 0;
   const int32_t* qsl = a.query_start_loc;
-  if (qsl != nullptr) {
-    b = q4::wave_search(a.B, row, lane, [&](int i) { return qsl[i]; });
-    L = qsl[b + 1] - qsl[b];
-    j = row - qsl[b];
-    if (j < 0 || j >= L) return p;
+  int C;
+  if constexpr (!kOne) {
+    // (a sequence of L rows has at most (L + 2 kSpan - 2) / kSpan groups, which is what lies between
+    // its first slot and the next one's)
+    b = q4::wave_search(a.B, slot, lane, [&](int i) { return qsl[i] / kSpan + 2 * i; });
+    const int q0 = qsl[b];
+    L = qsl[b + 1] - q0;
+    C = a.context_lens[b];
+    const int before = C > L ? (C - L) % kSpan : 0;  // slots of the first group that are not the call's
+    const int at = (slot - q0 / kSpan - 2 * b) * kSpan - before;
+    j = max(max(at, 0), -q0);
+    p.row = q0 + j;
+    p.n = at < -before ? 0 : min(min(at + kSpan, L) - j, a.rows - p.row);
+  } else {
+    C = a.context_lens[b];
+    if (C == 0) p.n = 0;
   }
-  const int C = a.context_lens[b];
-  if (qsl == nullptr && C == 0) return p;
-  p.skip = false;
+  if (p.n <= 0) return p;
   const int pos = C - L + j;
   p.bad = C < 0 || L > C || C > a.max_context_len || pos / kPage >= a.bt_stride;
   if (p.bad) return p;
@@ -39,6 +53,16 @@ __device__ __forceinline__ Place place_of(const Q4RowsArgs& a, int row, int lane
   p.token = pos % kPage;
   p.bad = p.page < 0 || p.page >= a.num_pages;
   return p;
+}
+
+// x[t] with bytes m -> x[m] with bytes t.
+__device__ __forceinline__ void transpose4(uint32_t (&x)[4]) {
+  const uint32_t a = __builtin_amdgcn_perm(x[1], x[0], 0x05010400u), b = __builtin_amdgcn_perm(x[1], x[0], 0x07030602u);
+  const uint32_t c = __builtin_amdgcn_perm(x[3], x[2], 0x05010400u), d = __builtin_amdgcn_perm(x[3], x[2], 0x07030602u);
+  x[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+  x[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+  x[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+  x[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 
 template <typename T>
@@ -94,29 +118,62 @@ struct Where {  // a lane's place in a tile: chunk c of eight dims of a token
   static __device__ __forceinline__ int scale(int token, int c) { return q4::kScales<D> + token * (D / 32) + (c >> 2); }
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(Q4RowsArgs a) {
+// kOne: a decode call, whose groups are one row each (7.2 us for 256 rows of 8 heads with
+// the code of both, 6.6 without).
+template <typename T, int D, bool kOne>
+__global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(Q4RowsArgs a, int slots) {
   constexpr int CH = D / 8;
   const int lane = threadIdx.x & 63;
-  const int row = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (row >= a.rows) return;
-  const Place p = place_of(a, row, lane);
-  if (p.skip || p.bad) return;
+  const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (slot >= slots) return;
+  const Group p = group_of<kOne, kGroup>(a, slot, lane);
+  if (p.n <= 0 || p.bad) return;
   for (int i = lane; i < a.H_kv * CH; i += 64) {
     const int g = i / CH, c = i % CH;
-    const int64_t from = ((int64_t)row * a.H_kv + g) * D + c * 8;
+    const int64_t from = ((int64_t)p.row * a.H_kv + g) * D + c * 8, step = (int64_t)a.H_kv * D;
     const int64_t tile = ((int64_t)p.page * a.H_kv + g) * q4_tile_bytes(D);
-    float x[8];
-    uint32_t scale;
-    load_eight(reinterpret_cast<const T*>(a.k_rows) + from, x);
-    const uint32_t k = quantise(x, scale);
-    *reinterpret_cast<uint32_t*>(a.k_pages + tile + Where<D>::k(p.token, c)) = k;
-    if ((c & 3) == 0) a.k_pages[tile + Where<D>::scale(p.token, c)] = (uint8_t)scale;
-    load_eight(reinterpret_cast<const T*>(a.v_rows) + from, x);
-    const uint32_t v = quantise(x, scale);
+    uint8_t* kt = a.k_pages + tile;
+    uint8_t* vt = a.v_pages + tile;
+    auto k_row = [&](int t, const float (&x)[8]) {
+      uint32_t scale;
+      const uint32_t k = quantise(x, scale);
+      *reinterpret_cast<uint32_t*>(kt + Where<D>::k(p.token + t, c)) = k;
+      if ((c & 3) == 0) kt[Where<D>::scale(p.token + t, c)] = (uint8_t)scale;
+    };
+    auto v_row = [&](int t, const float (&x)[8]) {
+      uint32_t scale;
+      const uint32_t v = quantise(x, scale);
+      if ((c & 3) == 0) vt[Where<D>::scale(p.token + t, c)] = (uint8_t)scale;
+      return v;
+    };
+    if (!kOne && p.n == kGroup) {
+      float x[kGroup][8], y[kGroup][8];
 #pragma unroll
-    for (int m = 0; m < 4; ++m) a.v_pages[tile + Where<D>::v(p.token, c, m)] = (uint8_t)(v >> (8 * m));
-    if ((c & 3) == 0) a.v_pages[tile + Where<D>::scale(p.token, c)] = (uint8_t)scale;
+      for (int t = 0; t < kGroup; ++t) {
+        load_eight(reinterpret_cast<const T*>(a.k_rows) + from + t * step, x[t]);
+        load_eight(reinterpret_cast<const T*>(a.v_rows) + from + t * step, y[t]);
+      }
+      uint32_t v[4];
+#pragma unroll
+      for (int t = 0; t < kGroup; ++t) {
+        k_row(t, x[t]);
+        v[t] = v_row(t, y[t]);
+      }
+      transpose4(v);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) *reinterpret_cast<uint32_t*>(vt + Where<D>::v(p.token, c, m)) = v[m];
+    } else {
+#pragma unroll 1
+      for (int t = 0; t < (kOne ? 1 : p.n); ++t) {
+        float x[8], y[8];
+        load_eight(reinterpret_cast<const T*>(a.k_rows) + from + t * step, x);
+        load_eight(reinterpret_cast<const T*>(a.v_rows) + from + t * step, y);
+        k_row(t, x);
+        const uint32_t v = v_row(t, y);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) vt[Where<D>::v(p.token + t, c, m)] = (uint8_t)(v >> (8 * m));
+      }
+    }
   }
 }
 
@@ -134,56 +191,87 @@ __device__ __forceinline__ void put_eight(T* p, uint32_t w, uint32_t scale) {
   }
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(64 * kRowsWaves) void q4_read_kernel(Q4RowsArgs a) {
-  constexpr int CH = D / 8;
+// A wave reads kGroups groups of tokens for 64 (KV head, eight dims): all loads are under
+// way before the first store, since loads after it would wait for it.
+template <typename T, int D, int kGroups>
+__global__ __launch_bounds__(64 * kRowsWaves) void q4_read_kernel(Q4RowsArgs a, int slots) {
+  constexpr int CH = D / 8, kSpan = kGroups * kGroup;
   const int lane = threadIdx.x & 63;
-  const int row = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (row >= a.rows) return;
-  const Place p = place_of(a, row, lane);
-  if (p.skip) return;
-  T* k_out = reinterpret_cast<T*>(const_cast<void*>(a.k_rows));
-  T* v_out = reinterpret_cast<T*>(const_cast<void*>(a.v_rows));
-  for (int i = lane; i < a.H_kv * CH; i += 64) {
-    const int g = i / CH, c = i % CH;
-    const int64_t to = ((int64_t)row * a.H_kv + g) * D + c * 8;
-    uint32_t k = 0, v = 0, ks = 255, vs = 255;
-    if (!p.bad) {
-      const int64_t tile = ((int64_t)p.page * a.H_kv + g) * q4_tile_bytes(D);
-      k = *reinterpret_cast<const uint32_t*>(a.k_pages + tile + Where<D>::k(p.token, c));
-      ks = a.k_pages[tile + Where<D>::scale(p.token, c)];
+  const int slot = blockIdx.x * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = blockIdx.y * 64 + lane;
+  if (slot >= slots) return;
+  const Group p = a.query_start_loc == nullptr ? group_of<true, kSpan>(a, slot, lane) : group_of<false, kSpan>(a, slot, lane);
+  if (p.n <= 0 || i >= a.H_kv * CH) return;
+  const int g = i / CH, c = i % CH, first = p.token & ~(kSpan - 1);
+  // (all tokens of the groups, whichever are asked for)
+  uint32_t k[kSpan] = {}, v[kGroups][kGroup] = {}, ks[kSpan], vs[kSpan];
+  if (!p.bad) {
+    const int64_t tile = ((int64_t)p.page * a.H_kv + g) * q4_tile_bytes(D);
 #pragma unroll
-      for (int m = 0; m < 4; ++m) v |= (uint32_t)a.v_pages[tile + Where<D>::v(p.token, c, m)] << (8 * m);
-      vs = a.v_pages[tile + Where<D>::scale(p.token, c)];
+    for (int t = 0; t < kSpan; ++t) {
+      k[t] = *reinterpret_cast<const uint32_t*>(a.k_pages + tile + Where<D>::k(first + t, c));
+      v[t / kGroup][t % kGroup] =
+          *reinterpret_cast<const uint32_t*>(a.v_pages + tile + Where<D>::v(first + t / kGroup * kGroup, c, t % kGroup));
+      ks[t] = a.k_pages[tile + Where<D>::scale(first + t, c)];
+      vs[t] = a.v_pages[tile + Where<D>::scale(first + t, c)];
     }
-    put_eight(k_out + to, k, ks);
-    put_eight(v_out + to, v, vs);
+  } else {
+#pragma unroll
+    for (int t = 0; t < kSpan; ++t) ks[t] = vs[t] = 255;
+  }
+#pragma unroll
+  for (int t = 0; t < kGroups; ++t) transpose4(v[t]);
+  const int64_t to = ((int64_t)p.row * a.H_kv + g) * D + c * 8, step = (int64_t)a.H_kv * D;
+  T* k_out = reinterpret_cast<T*>(const_cast<void*>(a.k_rows)) + to;
+  T* v_out = reinterpret_cast<T*>(const_cast<void*>(a.v_rows)) + to;
+#pragma unroll
+  for (int t = 0; t < kSpan; ++t) {
+    const int r = first + t - p.token;  // (wave-uniform)
+    if (r < 0 || r >= p.n) continue;
+    put_eight(k_out + r * step, k[t], ks[t]);
+    put_eight(v_out + r * step, v[t / kGroup][t % kGroup], vs[t]);
   }
 }
 
+// fn(element, head dim), by type.
 template <typename Fn>
 hipError_t by_type(int dtype, int D, const Q4RowsArgs& a, Fn fn) {
   if (a.rows == 0) return hipSuccess;
-  const int grid = (a.rows + kRowsWaves - 1) / kRowsWaves;
-  if (dtype == 0 && D == 128) fn(uint16_t(), std::integral_constant<int, 128>{}, grid);
-  else if (dtype == 0 && D == 64) fn(uint16_t(), std::integral_constant<int, 64>{}, grid);
-  else if (dtype == 1 && D == 128) fn(float(), std::integral_constant<int, 128>{}, grid);
-  else if (dtype == 1 && D == 64) fn(float(), std::integral_constant<int, 64>{}, grid);
+  if (dtype == 0 && D == 128) fn(uint16_t(), std::integral_constant<int, 128>{});
+  else if (dtype == 0 && D == 64) fn(uint16_t(), std::integral_constant<int, 64>{});
+  else if (dtype == 1 && D == 128) fn(float(), std::integral_constant<int, 128>{});
+  else if (dtype == 1 && D == 64) fn(float(), std::integral_constant<int, 64>{});
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
 
+// Slots of a call in spans of so many tokens (group_of).
+int slots_of(const Q4RowsArgs& a, int span) { return a.query_start_loc != nullptr ? a.rows / span + 2 * a.B : a.rows; }
+
+// Waves that read a whole page's 16 tokens rather than 4: those of calls that have so
+// many.  (64 contexts of 512-2,048 tokens, 8 heads of 64 dims in fp32, 5,300 such
+// waves: 92 us and 104; one of 4,001 tokens, 8 heads of 128 in bf16, 500: 6.7 and 5.9.)
+constexpr int64_t kWholePages = 4096;
+
 }  // namespace
 
 hipError_t launch_q4_append(int dtype, int D, const Q4RowsArgs& a, hipStream_t st) {
-  return by_type(dtype, D, a, [&](auto t, auto d, int grid) {
-    q4_append_kernel<decltype(t), decltype(d)::value><<<grid, 64 * kRowsWaves, 0, st>>>(a);
+  return by_type(dtype, D, a, [&](auto t, auto d) {
+    constexpr int D = decltype(d)::value;
+    const int slots = slots_of(a, kGroup);
+    const auto fn = a.query_start_loc == nullptr ? &q4_append_kernel<decltype(t), D, true> : &q4_append_kernel<decltype(t), D, false>;
+    fn<<<(slots + kRowsWaves - 1) / kRowsWaves, 64 * kRowsWaves, 0, st>>>(a, slots);
   });
 }
 
 hipError_t launch_q4_read(int dtype, int D, const Q4RowsArgs& a, hipStream_t st) {
-  return by_type(dtype, D, a, [&](auto t, auto d, int grid) {
-    q4_read_kernel<decltype(t), decltype(d)::value><<<grid, 64 * kRowsWaves, 0, st>>>(a);
+  return by_type(dtype, D, a, [&](auto t, auto d) {
+    constexpr int D = decltype(d)::value;
+    const int parts = (a.H_kv * (D / 8) + 63) / 64;
+    const bool pages = a.query_start_loc != nullptr && (int64_t)(a.rows / kPage) * parts >= kWholePages;
+    const int slots = slots_of(a, pages ? kPage : kGroup), waves = pages ? 1 : kRowsWaves;
+    const auto fn = pages ? &q4_read_kernel<decltype(t), D, kPage / kGroup> : &q4_read_kernel<decltype(t), D, 1>;
+    fn<<<dim3((slots + waves - 1) / waves, parts), 64 * waves, 0, st>>>(a, slots);
   });
 }
 
