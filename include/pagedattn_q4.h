@@ -85,10 +85,14 @@ int pa_kv_read_q4(const void *k_pages, const void *v_pages, const int32_t *block
  * num_q_rows != num_seqs) is sized as varlen.  Host only; no HIP call. */
 int pa_workspace_size_q4(const pa_dims_t *dims, size_t *bytes);
 
-/* Decode attention over the 4-bit cache: paged_attn with 4-bit pools.  Every
- * product is formed from the values that the cache stands for (exact in bf16) on
- * the matrix cores with fp32 accumulation; queries in fp32 as sums of three bf16
- * parts, softmax weights of two (bf16 out) or three (fp32 out).
+/* Decode attention over the 4-bit cache: paged_attn with 4-bit pools.  Products are
+ * formed from the values that the cache stands for, without rounding those, on the
+ * matrix cores with fp32 accumulation; softmax bases and sums are fp32.  Queries:
+ * bf16 ones as they are, except at head_dim 128, where a query is two e4m3 parts of
+ * its row's scale (an error of at most 2^-22 of the row's largest); fp32 ones as
+ * sums of three bf16 parts.  Softmax weights: for bf16 outputs in fp16 where every V
+ * of the step is exact in fp16 (scales 2^-23 .. 2^8) and as two bf16 parts elsewhere,
+ * for fp32 outputs as three bf16 parts.  The same inputs give the same bits.
  * GQA group size num_q_heads / num_kv_heads in {1, 2, 4, 6, 8}.  A row that sees
  * no key (context 0) is zeros; a row of a context above max_context_len, or that
  * sees a page entry outside [0, num_pages), is NaN.  q and out are 16-byte

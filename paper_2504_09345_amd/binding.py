@@ -320,7 +320,7 @@ def _check_q4(dims, heads, varlen, dense, pools, block_table, context_lens, quer
     or too few elements, not contiguous, not on the current device.  (Addresses
     are taken as they are.)"""
     import torch
-    dev = torch.cuda.current_device()
+    dev = None
     B, D = dims.num_seqs, dims.head_dim
     rows = dims.num_q_rows if varlen else B
     kind, code = (torch.bfloat16, "bfloat16") if dims.dtype == PA_BF16 else (torch.float32, "float32")
@@ -333,6 +333,8 @@ def _check_q4(dims, heads, varlen, dense, pools, block_table, context_lens, quer
             continue
         if t.dtype is not want:
             raise TypeError(f"a tensor of {t.dtype} where torch.{name} is needed")
+        if dev is None:
+            dev = torch.cuda.current_device()
         if t.get_device() != dev:
             raise ValueError(f"a tensor on {t.device}, not on the current device")
         if t.numel() < n or not t.is_contiguous():
