@@ -23,24 +23,24 @@ struct Group {
   bool bad;     // rows that the contract does not allow
   int page, token;  // token: of the first row
 };
-template <bool kOne, int kSpan>
+template <bool kOne>
 __device__ __forceinline__ Group group_of(const Q4RowsArgs& a, int slot, int lane) {
   Group p{slot, 1, false, 0, 0};
   int b = slot, L = 1, j = 0;
   const int32_t* qsl = a.query_start_loc;
   int C;
   if constexpr (!kOne) {
-    // (a sequence of L rows has at most (L + 2 kSpan - 2) / kSpan groups, which is what lies between
+    // (a sequence of L rows has at most (L + 6) / 4 groups, which is what lies between
     // its first slot and the next one's)
-    b = q4::wave_search(a.B, slot, lane, [&](int i) { return qsl[i] / kSpan + 2 * i; });
+    b = q4::wave_search(a.B, slot, lane, [&](int i) { return qsl[i] / kGroup + 2 * i; });
     const int q0 = qsl[b];
     L = qsl[b + 1] - q0;
     C = a.context_lens[b];
-    const int before = C > L ? (C - L) % kSpan : 0;  // slots of the first group that are not the call's
-    const int at = (slot - q0 / kSpan - 2 * b) * kSpan - before;
+    const int before = C > L ? (C - L) % kGroup : 0;  // slots of the first group that are not the call's
+    const int at = (slot - q0 / kGroup - 2 * b) * kGroup - before;
     j = max(max(at, 0), -q0);
     p.row = q0 + j;
-    p.n = at < -before ? 0 : min(min(at + kSpan, L) - j, a.rows - p.row);
+    p.n = at < -before ? 0 : min(min(at + kGroup, L) - j, a.rows - p.row);
   } else {
     C = a.context_lens[b];
     if (C == 0) p.n = 0;
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(Q4RowsArgs a
   const int lane = threadIdx.x & 63;
   const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (slot >= slots) return;
-  const Group p = group_of<kOne, kGroup>(a, slot, lane);
+  const Group p = group_of<kOne>(a, slot, lane);
   if (p.n <= 0 || p.bad) return;
   for (int i = lane; i < a.H_kv * CH; i += 64) {
     const int g = i / CH, c = i % CH;
@@ -177,59 +177,68 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(Q4RowsArgs a
   }
 }
 
-// Eight values of a word of codes.
-template <typename T>
-__device__ __forceinline__ void put_eight(T* p, uint32_t w, uint32_t scale) {
+// The values of a lane's codes, 16 bytes of them: a word's eight or a half's four.
+// kPast: past the caches.
+template <bool kPast, typename T>
+__device__ __forceinline__ void put(T* p, uint32_t w, uint32_t scale) {
   const float s = __uint_as_float(scale << 23);
+  auto store = [&](const auto& x) {
+    auto* to = reinterpret_cast<std::remove_const_t<std::remove_reference_t<decltype(x)>>*>(p);
+    if constexpr (kPast) {
+      __builtin_nontemporal_store(x, to);
+    } else {
+      *to = x;
+    }
+  };
   if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<u32x4*>(p) = q4::eight_of(w, s);
+    store(q4::eight_of(w, s));
   } else {
     const q4::f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
-    const q4::f32x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
-    *reinterpret_cast<q4::f32x4_t*>(p) = q4::f32x4_t{a[0], a[1], b[0], b[1]};
-    *reinterpret_cast<q4::f32x4_t*>(p + 4) = q4::f32x4_t{c[0], c[1], d[0], d[1]};
+    store(q4::f32x4_t{a[0], a[1], b[0], b[1]});
   }
 }
 
-// A wave reads kGroups groups of tokens for 64 (KV head, eight dims): all loads are under
-// way before the first store, since loads after it would wait for it.
-template <typename T, int D, int kGroups>
+// A wave reads a group's tokens for 64 (KV head, 16 bytes of the output): its stores are
+// a KiB in a row each.  (Eight dims of fp32 a lane, in two stores that alternate by 16
+// bytes, take 104 us instead of 88 for 64 contexts of 512-2,048 tokens, 8 heads of 64
+// dims, through the caches.)
+template <typename T, int D, bool kPast>
 __global__ __launch_bounds__(64 * kRowsWaves) void q4_read_kernel(Q4RowsArgs a, int slots) {
-  constexpr int CH = D / 8, kSpan = kGroups * kGroup;
+  constexpr int kHalf = sizeof(T) == 4;  // four dims a lane, half a word's codes
+  constexpr int CH = D / 8 << kHalf, kV = kGroup >> kHalf;
   const int lane = threadIdx.x & 63;
-  const int slot = blockIdx.x * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = blockIdx.y * 64 + lane;
   if (slot >= slots) return;
-  const Group p = a.query_start_loc == nullptr ? group_of<true, kSpan>(a, slot, lane) : group_of<false, kSpan>(a, slot, lane);
+  const Group p = a.query_start_loc == nullptr ? group_of<true>(a, slot, lane) : group_of<false>(a, slot, lane);
   if (p.n <= 0 || i >= a.H_kv * CH) return;
-  const int g = i / CH, c = i % CH, first = p.token & ~(kSpan - 1);
-  // (all tokens of the groups, whichever are asked for)
-  uint32_t k[kSpan] = {}, v[kGroups][kGroup] = {}, ks[kSpan], vs[kSpan];
+  const int g = i / CH, c = i % CH >> kHalf, half = kHalf ? i & 1 : 0, first = p.token & ~(kGroup - 1);
+  // (all four tokens of the group, whichever are asked for)
+  uint32_t k[kGroup] = {}, v[kGroup] = {}, ks[kGroup], vs[kGroup];
   if (!p.bad) {
     const int64_t tile = ((int64_t)p.page * a.H_kv + g) * q4_tile_bytes(D);
 #pragma unroll
-    for (int t = 0; t < kSpan; ++t) {
+    for (int t = 0; t < kGroup; ++t) {
       k[t] = *reinterpret_cast<const uint32_t*>(a.k_pages + tile + Where<D>::k(first + t, c));
-      v[t / kGroup][t % kGroup] =
-          *reinterpret_cast<const uint32_t*>(a.v_pages + tile + Where<D>::v(first + t / kGroup * kGroup, c, t % kGroup));
       ks[t] = a.k_pages[tile + Where<D>::scale(first + t, c)];
       vs[t] = a.v_pages[tile + Where<D>::scale(first + t, c)];
     }
+#pragma unroll
+    for (int m = 0; m < kV; ++m) v[m] = *reinterpret_cast<const uint32_t*>(a.v_pages + tile + Where<D>::v(first, c, half * kV + m));
   } else {
 #pragma unroll
-    for (int t = 0; t < kSpan; ++t) ks[t] = vs[t] = 255;
+    for (int t = 0; t < kGroup; ++t) ks[t] = vs[t] = 255;
   }
-#pragma unroll
-  for (int t = 0; t < kGroups; ++t) transpose4(v[t]);
-  const int64_t to = ((int64_t)p.row * a.H_kv + g) * D + c * 8, step = (int64_t)a.H_kv * D;
+  transpose4(v);
+  const int64_t to = (int64_t)p.row * a.H_kv * D + (int64_t)i * (16 / sizeof(T)), step = (int64_t)a.H_kv * D;
   T* k_out = reinterpret_cast<T*>(const_cast<void*>(a.k_rows)) + to;
   T* v_out = reinterpret_cast<T*>(const_cast<void*>(a.v_rows)) + to;
 #pragma unroll
-  for (int t = 0; t < kSpan; ++t) {
+  for (int t = 0; t < kGroup; ++t) {
     const int r = first + t - p.token;  // (wave-uniform)
     if (r < 0 || r >= p.n) continue;
-    put_eight(k_out + r * step, k[t], ks[t]);
-    put_eight(v_out + r * step, v[t / kGroup][t % kGroup], vs[t]);
+    put<kPast>(k_out + r * step, k[t] >> (16 * half), ks[t]);
+    put<kPast>(v_out + r * step, v[t], vs[t]);
   }
 }
 
@@ -245,20 +254,20 @@ hipError_t by_type(int dtype, int D, const Q4RowsArgs& a, Fn fn) {
   return hipGetLastError();
 }
 
-// Slots of a call in spans of so many tokens (group_of).
-int slots_of(const Q4RowsArgs& a, int span) { return a.query_start_loc != nullptr ? a.rows / span + 2 * a.B : a.rows; }
+// Outputs of more bytes than the last-level cache has are stored past the caches, where
+// no reader would find them.  (336 MB in fp32 61 us and 85, in bf16 68 and 99, 208 us and
+// 218 with a copy of them after; 66 MB in fp32 13 and 14, but 39 and 35 with the copy.)
+constexpr int64_t kCached = 256 << 20;
 
-// Waves that read a whole page's 16 tokens rather than 4: those of calls that have so
-// many.  (64 contexts of 512-2,048 tokens, 8 heads of 64 dims in fp32, 5,300 such
-// waves: 92 us and 104; one of 4,001 tokens, 8 heads of 128 in bf16, 500: 6.7 and 5.9.)
-constexpr int64_t kWholePages = 4096;
+// Slots of a call (group_of).
+int slots_of(const Q4RowsArgs& a) { return a.query_start_loc != nullptr ? a.rows / kGroup + 2 * a.B : a.rows; }
 
 }  // namespace
 
 hipError_t launch_q4_append(int dtype, int D, const Q4RowsArgs& a, hipStream_t st) {
   return by_type(dtype, D, a, [&](auto t, auto d) {
     constexpr int D = decltype(d)::value;
-    const int slots = slots_of(a, kGroup);
+    const int slots = slots_of(a);
     const auto fn = a.query_start_loc == nullptr ? &q4_append_kernel<decltype(t), D, true> : &q4_append_kernel<decltype(t), D, false>;
     fn<<<(slots + kRowsWaves - 1) / kRowsWaves, 64 * kRowsWaves, 0, st>>>(a, slots);
   });
@@ -266,12 +275,11 @@ hipError_t launch_q4_append(int dtype, int D, const Q4RowsArgs& a, hipStream_t s
 
 hipError_t launch_q4_read(int dtype, int D, const Q4RowsArgs& a, hipStream_t st) {
   return by_type(dtype, D, a, [&](auto t, auto d) {
-    constexpr int D = decltype(d)::value;
-    const int parts = (a.H_kv * (D / 8) + 63) / 64;
-    const bool pages = a.query_start_loc != nullptr && (int64_t)(a.rows / kPage) * parts >= kWholePages;
-    const int slots = slots_of(a, pages ? kPage : kGroup), waves = pages ? 1 : kRowsWaves;
-    const auto fn = pages ? &q4_read_kernel<decltype(t), D, kPage / kGroup> : &q4_read_kernel<decltype(t), D, 1>;
-    fn<<<dim3((slots + waves - 1) / waves, parts), 64 * waves, 0, st>>>(a, slots);
+    const int slots = slots_of(a);
+    const dim3 grid((slots + kRowsWaves - 1) / kRowsWaves, (a.H_kv * D * (int)sizeof(t) / 16 + 63) / 64);
+    const bool past = (int64_t)2 * a.rows * a.H_kv * D * sizeof(t) > kCached;
+    const auto fn = past ? &q4_read_kernel<decltype(t), decltype(d)::value, true> : &q4_read_kernel<decltype(t), decltype(d)::value, false>;
+    fn<<<grid, 64 * kRowsWaves, 0, st>>>(a, slots);
   });
 }
 
