@@ -128,51 +128,51 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(Q4RowsArgs a
   if (slot >= slots) return;
   const Group p = group_of<kOne>(a, slot, lane);
   if (p.n <= 0 || p.bad) return;
-  for (int i = lane; i < a.H_kv * CH; i += 64) {
-    const int g = i / CH, c = i % CH;
-    const int64_t from = ((int64_t)p.row * a.H_kv + g) * D + c * 8, step = (int64_t)a.H_kv * D;
-    const int64_t tile = ((int64_t)p.page * a.H_kv + g) * q4_tile_bytes(D);
-    uint8_t* kt = a.k_pages + tile;
-    uint8_t* vt = a.v_pages + tile;
-    auto k_row = [&](int t, const float (&x)[8]) {
-      uint32_t scale;
-      const uint32_t k = quantise(x, scale);
-      *reinterpret_cast<uint32_t*>(kt + Where<D>::k(p.token + t, c)) = k;
-      if ((c & 3) == 0) kt[Where<D>::scale(p.token + t, c)] = (uint8_t)scale;
-    };
-    auto v_row = [&](int t, const float (&x)[8]) {
-      uint32_t scale;
-      const uint32_t v = quantise(x, scale);
-      if ((c & 3) == 0) vt[Where<D>::scale(p.token + t, c)] = (uint8_t)scale;
-      return v;
-    };
-    if (!kOne && p.n == kGroup) {
-      float x[kGroup][8], y[kGroup][8];
+  const int i = blockIdx.y * 64 + lane;
+  if (i >= a.H_kv * CH) return;
+  const int g = i / CH, c = i % CH;
+  const int64_t from = ((int64_t)p.row * a.H_kv + g) * D + c * 8, step = (int64_t)a.H_kv * D;
+  const int64_t tile = ((int64_t)p.page * a.H_kv + g) * q4_tile_bytes(D);
+  uint8_t* kt = a.k_pages + tile;
+  uint8_t* vt = a.v_pages + tile;
+  auto k_row = [&](int t, const float (&x)[8]) {
+    uint32_t scale;
+    const uint32_t k = quantise(x, scale);
+    *reinterpret_cast<uint32_t*>(kt + Where<D>::k(p.token + t, c)) = k;
+    if ((c & 3) == 0) kt[Where<D>::scale(p.token + t, c)] = (uint8_t)scale;
+  };
+  auto v_row = [&](int t, const float (&x)[8]) {
+    uint32_t scale;
+    const uint32_t v = quantise(x, scale);
+    if ((c & 3) == 0) vt[Where<D>::scale(p.token + t, c)] = (uint8_t)scale;
+    return v;
+  };
+  if (!kOne && p.n == kGroup) {
+    float x[kGroup][8], y[kGroup][8];
 #pragma unroll
-      for (int t = 0; t < kGroup; ++t) {
-        load_eight(reinterpret_cast<const T*>(a.k_rows) + from + t * step, x[t]);
-        load_eight(reinterpret_cast<const T*>(a.v_rows) + from + t * step, y[t]);
-      }
-      uint32_t v[4];
+    for (int t = 0; t < kGroup; ++t) {
+      load_eight(reinterpret_cast<const T*>(a.k_rows) + from + t * step, x[t]);
+      load_eight(reinterpret_cast<const T*>(a.v_rows) + from + t * step, y[t]);
+    }
+    uint32_t v[4];
 #pragma unroll
-      for (int t = 0; t < kGroup; ++t) {
-        k_row(t, x[t]);
-        v[t] = v_row(t, y[t]);
-      }
-      transpose4(v);
+    for (int t = 0; t < kGroup; ++t) {
+      k_row(t, x[t]);
+      v[t] = v_row(t, y[t]);
+    }
+    transpose4(v);
 #pragma unroll
-      for (int m = 0; m < 4; ++m) *reinterpret_cast<uint32_t*>(vt + Where<D>::v(p.token, c, m)) = v[m];
-    } else {
+    for (int m = 0; m < 4; ++m) *reinterpret_cast<uint32_t*>(vt + Where<D>::v(p.token, c, m)) = v[m];
+  } else {
 #pragma unroll 1
-      for (int t = 0; t < (kOne ? 1 : p.n); ++t) {
-        float x[8], y[8];
-        load_eight(reinterpret_cast<const T*>(a.k_rows) + from + t * step, x);
-        load_eight(reinterpret_cast<const T*>(a.v_rows) + from + t * step, y);
-        k_row(t, x);
-        const uint32_t v = v_row(t, y);
+    for (int t = 0; t < (kOne ? 1 : p.n); ++t) {
+      float x[8], y[8];
+      load_eight(reinterpret_cast<const T*>(a.k_rows) + from + t * step, x);
+      load_eight(reinterpret_cast<const T*>(a.v_rows) + from + t * step, y);
+      k_row(t, x);
+      const uint32_t v = v_row(t, y);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) vt[Where<D>::v(p.token + t, c, m)] = (uint8_t)(v >> (8 * m));
-      }
+      for (int m = 0; m < 4; ++m) vt[Where<D>::v(p.token + t, c, m)] = (uint8_t)(v >> (8 * m));
     }
   }
 }
@@ -269,7 +269,7 @@ hipError_t launch_q4_append(int dtype, int D, const Q4RowsArgs& a, hipStream_t s
     constexpr int D = decltype(d)::value;
     const int slots = slots_of(a);
     const auto fn = a.query_start_loc == nullptr ? &q4_append_kernel<decltype(t), D, true> : &q4_append_kernel<decltype(t), D, false>;
-    fn<<<(slots + kRowsWaves - 1) / kRowsWaves, 64 * kRowsWaves, 0, st>>>(a, slots);
+    fn<<<dim3((slots + kRowsWaves - 1) / kRowsWaves, (a.H_kv * D / 8 + 63) / 64), 64 * kRowsWaves, 0, st>>>(a, slots);
   });
 }
 
