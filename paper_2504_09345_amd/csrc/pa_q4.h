@@ -28,8 +28,8 @@ hipError_t launch_q4_read(int dtype, int D, const Q4RowsArgs& a, hipStream_t st)
 
 constexpr int kQ4Unit = 2 * 16;  // tokens of a step: two pages
 
-// Chunk rows.  A wave takes an item, a KV head's 16 NB columns (query row, head of
-// the group) of one sequence, over a part of its keys.
+// Chunk rows.  An item is a KV head's 16 columns (query row, head of the group) of one
+// sequence, or 128 in a workgroup that shares V, over a part of its keys.
 struct Q4AttnArgs {
   const void* q;
   const uint8_t* k_pages;
@@ -51,8 +51,8 @@ struct Q4AttnArgs {
 };
 constexpr int kQ4Waves = 4;  // waves of a workgroup, each with an item of its own
 
-// Column blocks (of 16) that a wave holds.
-constexpr int q4_positions(int blocks, int s) { return 16 * blocks / s; }  // query rows of an item
+// Query rows of an item of so many column blocks (of 16).
+constexpr int q4_positions(int blocks, int s) { return 16 * blocks / s; }
 constexpr int kQ4ChunkBlocks = 2 * kQ4Waves;  // of a workgroup that shares V's operands (launch_q4_chunk)
 
 hipError_t launch_q4_attn(int dtype, int D, const Q4AttnArgs& a, hipStream_t st, KernelEvents ev);

@@ -23,13 +23,12 @@ struct Group {
   bool bad;     // rows that the contract does not allow
   int page, token;  // token: of the first row
 };
-template <bool kOne>
 __device__ __forceinline__ Group group_of(const Q4RowsArgs& a, int slot, int lane) {
   Group p{slot, 1, false, 0, 0};
   int b = slot, L = 1, j = 0;
   const int32_t* qsl = a.query_start_loc;
   int C;
-  if constexpr (!kOne) {
+  if (qsl != nullptr) {
     // (a sequence of L rows has at most (L + 6) / 4 groups, which is what lies between
     // its first slot and the next one's)
     b = q4::wave_search(a.B, slot, lane, [&](int i) { return qsl[i] / kGroup + 2 * i; });
@@ -118,15 +117,13 @@ struct Where {  // a lane's place in a tile: chunk c of eight dims of a token
   static __device__ __forceinline__ int scale(int token, int c) { return q4::kScales<D> + token * (D / 32) + (c >> 2); }
 };
 
-// kOne: a decode call, whose groups are one row each (7.2 us for 256 rows of 8 heads with
-// the code of both, 6.6 without).
-template <typename T, int D, bool kOne>
+template <typename T, int D>
 __global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(Q4RowsArgs a, int slots) {
   constexpr int CH = D / 8;
   const int lane = threadIdx.x & 63;
   const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (slot >= slots) return;
-  const Group p = group_of<kOne>(a, slot, lane);
+  const Group p = group_of(a, slot, lane);
   if (p.n <= 0 || p.bad) return;
   const int i = blockIdx.y * 64 + lane;
   if (i >= a.H_kv * CH) return;
@@ -147,7 +144,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(Q4RowsArgs a
     if ((c & 3) == 0) vt[Where<D>::scale(p.token + t, c)] = (uint8_t)scale;
     return v;
   };
-  if (!kOne && p.n == kGroup) {
+  if (p.n == kGroup) {
     float x[kGroup][8], y[kGroup][8];
 #pragma unroll
     for (int t = 0; t < kGroup; ++t) {
@@ -165,7 +162,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(Q4RowsArgs a
     for (int m = 0; m < 4; ++m) *reinterpret_cast<uint32_t*>(vt + Where<D>::v(p.token, c, m)) = v[m];
   } else {
 #pragma unroll 1
-    for (int t = 0; t < (kOne ? 1 : p.n); ++t) {
+    for (int t = 0; t < p.n; ++t) {
       float x[8], y[8];
       load_eight(reinterpret_cast<const T*>(a.k_rows) + from + t * step, x);
       load_eight(reinterpret_cast<const T*>(a.v_rows) + from + t * step, y);
@@ -210,7 +207,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q4_read_kernel(Q4RowsArgs a, 
   const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = blockIdx.y * 64 + lane;
   if (slot >= slots) return;
-  const Group p = a.query_start_loc == nullptr ? group_of<true>(a, slot, lane) : group_of<false>(a, slot, lane);
+  const Group p = group_of(a, slot, lane);
   if (p.n <= 0 || i >= a.H_kv * CH) return;
   const int g = i / CH, c = i % CH >> kHalf, half = kHalf ? i & 1 : 0, first = p.token & ~(kGroup - 1);
   // (all four tokens of the group, whichever are asked for)
@@ -268,8 +265,8 @@ hipError_t launch_q4_append(int dtype, int D, const Q4RowsArgs& a, hipStream_t s
   return by_type(dtype, D, a, [&](auto t, auto d) {
     constexpr int D = decltype(d)::value;
     const int slots = slots_of(a);
-    const auto fn = a.query_start_loc == nullptr ? &q4_append_kernel<decltype(t), D, true> : &q4_append_kernel<decltype(t), D, false>;
-    fn<<<dim3((slots + kRowsWaves - 1) / kRowsWaves, (a.H_kv * D / 8 + 63) / 64), 64 * kRowsWaves, 0, st>>>(a, slots);
+    const dim3 grid((slots + kRowsWaves - 1) / kRowsWaves, (a.H_kv * (D / 8) + 63) / 64);
+    q4_append_kernel<decltype(t), D><<<grid, 64 * kRowsWaves, 0, st>>>(a, slots);
   });
 }
 

@@ -326,8 +326,8 @@ __device__ __forceinline__ void add_weights(State<T, D, NB>& st, const float (&x
     st.l[c] += ((x[c][0] + x[c][1]) + (x[c][2] + x[c][3])) + ((x[c][4] + x[c][5]) + (x[c][6] + x[c][7]));
 }
 // Only where one does the bases of the wave move (so a unit needs no maximum across
-// lanes); then the columns' sums.  The kernels' inner loops leave for this: a loop
-// that scales the outputs in one of its branches copies them in the others.
+// lanes); then the columns' sums.  The inner loops of waves alone leave for this: a
+// loop that scales the outputs in one of its branches copies them in the others.
 template <typename T, int D, int NB>
 __device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, bool big,
                                                float (&x)[NB][8]) {
@@ -350,6 +350,7 @@ __device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_
   add_weights(st, x);
 }
 
+// The same from the scores on.
 template <typename T, int D, int NB>
 __device__ __forceinline__ void fold_softmax(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, float (&x)[NB][8]) {
   const bool big = form_weights<T, D, NB>(st, s, scale_log2, x);
