@@ -43,7 +43,7 @@ struct Q4AttnArgs {
   int64_t bt_stride;
   float scale_log2;
   int B, s /* heads of a group */, H_q, H_kv, rows, num_pages, max_context_len;
-  int n_slots;   // row blocks, at most
+  int n_slots;   // items of a KV head, at most
   int min_rows;  // sequences of fewer rows are the stream kernel's
   int max_q_len;
   int n_split, split_units;

@@ -141,7 +141,7 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
                                 ((d->max_context_len - d->max_q_len / 2) / pa::kQ4Unit + 1);
     p->shared = d->dtype == PA_BF16 && d->max_q_len * (int64_t)s > kAloneColumns && alone_units > kAloneUnits;
     p->blocks = p->shared ? pa::kQ4ChunkBlocks : 1;
-    const int64_t slots = p->rows / pa::q4_positions(p->blocks, s) + (int64_t)d->num_seqs;
+    const int64_t slots = p->rows / pa::q4_positions(p->blocks, s) + 1 + (int64_t)d->num_seqs;
     const int64_t items = (chunk_rows / pa::q4_positions(p->blocks, s) + 1) * d->num_kv_heads;
     if (!p->shared)
       while (p->wave_parts < pa::kQ4Waves && items * p->wave_parts * 2 <= kPartWaves && units >= p->wave_parts * 2) p->wave_parts *= 2;

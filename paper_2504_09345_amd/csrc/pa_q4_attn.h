@@ -13,16 +13,33 @@ struct Q4Item {
   bool bad;            // rows are NaN
 };
 
-// Row block `slot` of the call: the blocks of sequence b are the slots from
-// query_start_loc[b] / positions + b on, which no two sequences share.
-__device__ __forceinline__ Q4Item q4_item(const Q4AttnArgs& a, int slot, int positions, int lane) {
+// Item `i` of the call: `positions` query rows of a sequence from a multiple of that on.
+// One begins, for each row r of the call that is a multiple of `positions`, within the
+// `positions` rows from r on in the sequence that has r (the last rows first: of a
+// sequence they see the most keys), and then one for each sequence that begins at no
+// such r.  (Sequences of one row, the stream kernel's, are thus looked at last and
+// without a search: before every other item, 512 of them beside 8 chunks of 512 rows
+// cost 10 us.)
+__device__ __forceinline__ Q4Item q4_item(const Q4AttnArgs& a, int i, int positions, int lane) {
   Q4Item it{0, 0, 0, 0, false};
   const int32_t* qsl = a.query_start_loc;
-  it.b = q4::wave_search(a.B, slot, lane, [&](int b) { return qsl[b] / positions + b; });
-  const int q0 = qsl[it.b], L = qsl[it.b + 1] - q0;
-  const int first = (slot - (q0 / positions + it.b)) * positions;
+  const int blocks = (a.rows + positions - 1) / positions;
+  int first = 0, q0;
+  if (i < blocks) {
+    const int r = (blocks - 1 - i) * positions;
+    it.b = q4::wave_search(a.B, r, lane, [&](int b) { return qsl[b]; });
+    q0 = qsl[it.b];
+    if (r < q0) return it;
+    first = (r - q0 + positions - 1) / positions * positions;
+  } else {
+    it.b = i - blocks;
+    if (it.b >= a.B) return it;
+    q0 = qsl[it.b];
+    if (q0 % positions == 0) return it;
+  }
+  const int L = qsl[it.b + 1] - q0;
   it.row0 = q0 + first;
-  if (q0 < 0 || first < 0 || it.row0 >= a.rows || L < a.min_rows) return it;  // (fewer rows: the stream kernel's)
+  if (q0 < 0 || it.row0 >= a.rows || L < a.min_rows) return it;  // (fewer rows: the stream kernel's)
   it.n_pos = max(0, min(positions, min(L - first, a.rows - it.row0)));
   const int C = a.context_lens[it.b];
   it.last0 = C - L + first;
@@ -79,12 +96,9 @@ void q4_attn_kernel(Q4AttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // row blocks of one head side by side
   const int split = blockIdx.x % a.n_split, g = blockIdx.x / a.n_split % a.H_kv;
-  // (the last blocks of a sequence see the most keys: they start first)
   // (a workgroup's waves have items of their own, or 2 or 4 share one)
   const int sharers = a.wave_parts, part = wave & (sharers - 1);
-  const int slot = ((gridDim.x / a.n_split / a.H_kv - 1 - blockIdx.x / a.n_split / a.H_kv) * kQ4Waves + wave) / sharers;
-  Q4Item it{0, 0, 0, 0, false};
-  if (slot < a.n_slots) it = q4_item(a, slot, q4_positions(NB, S), lane);
+  const Q4Item it = q4_item(a, (int)(blockIdx.x / a.n_split / a.H_kv * kQ4Waves + wave) / sharers, q4_positions(NB, S), lane);
 
   const int n = lane & 15;
   T* out = reinterpret_cast<T*>(a.out);

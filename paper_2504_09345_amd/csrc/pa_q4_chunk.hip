@@ -32,9 +32,7 @@ void q4_chunk_kernel(Q4AttnArgs a) {
   const int lane = threadIdx.x & 63, n = lane & 15, G = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int split = blockIdx.x % a.n_split, g = blockIdx.x / a.n_split % a.H_kv;
-  // (the last blocks of a sequence see the most keys: they start first)
-  const int slot = a.n_slots - 1 - blockIdx.x / a.n_split / a.H_kv;
-  const Q4Item it = q4_item(a, slot, kColumns / S, lane);
+  const Q4Item it = q4_item(a, blockIdx.x / a.n_split / a.H_kv, kColumns / S, lane);
   if (it.n_pos == 0) return;
   T* out = reinterpret_cast<T*>(a.out);
   if (it.bad) {
