@@ -80,8 +80,7 @@ struct Plan {
 // while the GPU still holds all of them at once (256 CUs of 12 waves).  Shared and
 // alone, 32 query heads over 8: a chunk of 16 rows on 200 tokens 7 and 10 us, of 300 9
 // and 11, of 64 on 1,500 14 and 18, 4 of 60 on 3,000 34 and 41, 16 of 8 on 2,000 25
-// and 31; with twice the waves that the GPU holds, 8 of 200 rows on 500 tokens take
-// 47 us instead of 41.
+// and 31.
 constexpr int kPartWaves = 3072;
 // Parts beyond those, through the workspace and a second launch: as many as give the
 // GPU 2,048 waves of at least kLeastUnits units, at most 64.  (Parts of 4 units cost one
@@ -92,13 +91,13 @@ constexpr int kWavesWanted = 2048, kLeastUnits = 8, kMaxSplit = 64;
 // workgroups of 128 columns that share V's operands.  The latter spend a third less
 // per column and unit, but need the columns (a chunk of at most 32 leaves three of
 // four waves without) and enough work: a wave alone is through its units sooner, and
-// there are more of them.  The line is 32 units for each of 2,048 waves, by the
+// there are more of them.  The line is 48 units for each of 2,048 waves, by the
 // longest context that the call declares.  Alone and together, 32 query heads over 8:
-// one chunk of 700 rows 20 and 35 us, of 1,400 36 and 46, of 2,000 62 and 61, of
-// 4,000 194 and 149; 8 of 205-256 rows on 500 tokens 57 and 47; 4 of 240-300 on
-// 1,000 64 and 59; 4 of 48-60 on 3,000 41 and 55; 2 of 102-128 on 20,000 171 and 128;
-// 16 of 8 rows on 2,000 35 and 45.
-constexpr int64_t kAloneUnits = 32 * 2048;
+// one chunk of 700 rows 17 and 32 us, of 1,400 37 and 46, of 2,000 57 and 62, of 2,800
+// 98 and 90, of 4,000 171 and 145; 8 of 205-256 rows on 500 tokens 53 and 57; 8 of
+// 320-400 on 300 67 and 66; 4 of 240-300 on 1,000 59 and 56; 4 of 48-60 on 3,000 34 and
+// 54; 2 of 102-128 on 20,000 153 and 123; 16 of 8 rows on 2,000 24 and 45.
+constexpr int64_t kAloneUnits = 48 * 2048;
 constexpr int kAloneColumns = 32;
 // Units of a launch of the stream kernel, at most (its counts are 32-bit).
 constexpr int64_t kStreamUnits = 1 << 30;
