@@ -315,31 +315,44 @@ def pa_workspace_size_q4(dims: PaDims) -> int:
     return int(n.value)
 
 
-def _check_q4(dims, heads, varlen, dense, pools, block_table, context_lens, query_start_loc):
-    """Refuses a tensor that is not what dims and the format say: of another type
-    or too few elements, not contiguous, not on the current device.  (Addresses
-    are taken as they are.)"""
+def _is_address(t):
+    return t is None or t.__class__ is int
+
+
+def _take(t, kind, n, device):
+    """Device address of a tensor of a call on the 4-bit cache.  (Addresses are taken
+    as they are.)"""
+    if t is None:
+        return None
+    if t.__class__ is int:
+        return t or None
+    if t.dtype is not kind:
+        raise TypeError(f"a tensor of {t.dtype} where {kind} is needed")
+    if t.get_device() != device:
+        raise ValueError(f"a tensor on {t.device}, not on the current device")
+    if t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"a tensor of {t.numel()} elements{'' if t.is_contiguous() else ', not contiguous'}, "
+                         f"where {n} in a row are needed")
+    return t.data_ptr() or None
+
+
+def _take_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc):
+    """The addresses of a call's arrays, in this order.  Refuses a tensor that is not
+    what dims and the format say: of another type or too few elements, not contiguous,
+    not on the current device."""
     import torch
+    i32, u8 = torch.int32, torch.uint8
+    # (addresses alone need no device)
     dev = None
+    if not _is_address(dense0) or not all(map(_is_address, (dense1, k_pages, v_pages, block_table, context_lens, query_start_loc))):
+        dev = torch.cuda.current_device()
     B, D = dims.num_seqs, dims.head_dim
-    rows = dims.num_q_rows if varlen else B
-    kind, code = (torch.bfloat16, "bfloat16") if dims.dtype == PA_BF16 else (torch.float32, "float32")
+    kind = torch.bfloat16 if dims.dtype == PA_BF16 else torch.float32
+    n = (dims.num_q_rows if varlen else B) * heads * D
     tiles = dims.num_pages * dims.num_kv_heads * _Q4_TILE.get(D, 0)
-    for t, want, name, n in ((dense[0], kind, code, rows * heads * D), (dense[1], kind, code, rows * heads * D),
-                             (pools[0], torch.uint8, "uint8", tiles), (pools[1], torch.uint8, "uint8", tiles),
-                             (block_table, torch.int32, "int32", B * dims.max_pages_per_seq),
-                             (context_lens, torch.int32, "int32", B), (query_start_loc, torch.int32, "int32", B + 1)):
-        if t is None or t.__class__ is int:
-            continue
-        if t.dtype is not want:
-            raise TypeError(f"a tensor of {t.dtype} where torch.{name} is needed")
-        if dev is None:
-            dev = torch.cuda.current_device()
-        if t.get_device() != dev:
-            raise ValueError(f"a tensor on {t.device}, not on the current device")
-        if t.numel() < n or not t.is_contiguous():
-            raise ValueError(f"a tensor of {t.numel()} elements{'' if t.is_contiguous() else ', not contiguous'}, "
-                             f"where {n} in a row are needed")
+    return (_take(dense0, kind, n, dev), _take(dense1, kind, n, dev), _take(k_pages, u8, tiles, dev),
+            _take(v_pages, u8, tiles, dev), _take(block_table, i32, B * dims.max_pages_per_seq, dev),
+            _take(context_lens, i32, B, dev), _take(query_start_loc, i32, B + 1, dev))
 
 
 def _workspace_q4(dims, workspace, q, stream):
@@ -350,40 +363,37 @@ def _workspace_q4(dims, workspace, q, stream):
     return workspace.data_ptr() or None, workspace.numel() * workspace.element_size(), workspace
 
 
-def _rows_q4(name, k_rows, v_rows, first, block_table, context_lens, last, dims, query_start_loc, stream, check):
-    _check_q4(dims, dims.num_kv_heads, query_start_loc is not None, (k_rows, v_rows),
-              last if name == "pa_kv_append_q4" else first, block_table, context_lens, query_start_loc)
-    rc = getattr(load(), name)(_addr(first[0]), _addr(first[1]), _addr(block_table), _addr(context_lens),
-                               _addr(query_start_loc), _addr(last[0]), _addr(last[1]), ctypes.byref(dims),
-                               _stream(stream))
-    if check and rc != PA_OK:
-        raise PagedAttnError(name, rc)
-    return rc
-
-
 def pa_kv_append_q4(k_new, v_new, block_table, context_lens, k_pages, v_pages, dims: PaDims, query_start_loc=None,
                     stream=None, check=True) -> int:
     """int pa_kv_append_q4(...): quantise the new tokens' K/V into the 4-bit pools."""
-    return _rows_q4("pa_kv_append_q4", k_new, v_new, (k_new, v_new), block_table, context_lens, (k_pages, v_pages),
-                    dims, query_start_loc, stream, check)
+    k, v, kp, vp, bt, cl, qsl = _take_q4(dims, dims.num_kv_heads, query_start_loc is not None, k_new, v_new, k_pages,
+                                         v_pages, block_table, context_lens, query_start_loc)
+    rc = load().pa_kv_append_q4(k, v, bt, cl, qsl, kp, vp, ctypes.byref(dims), _stream(stream))
+    if check and rc != PA_OK:
+        raise PagedAttnError("pa_kv_append_q4", rc)
+    return rc
 
 
 def pa_kv_read_q4(k_pages, v_pages, block_table, context_lens, k_out, v_out, dims: PaDims, query_start_loc=None,
                   stream=None, check=True) -> int:
     """int pa_kv_read_q4(...): the values that the 4-bit pools hold of the rows
     which pa_kv_append_q4 with the same arguments writes."""
-    return _rows_q4("pa_kv_read_q4", k_out, v_out, (k_pages, v_pages), block_table, context_lens, (k_out, v_out),
-                    dims, query_start_loc, stream, check)
+    k, v, kp, vp, bt, cl, qsl = _take_q4(dims, dims.num_kv_heads, query_start_loc is not None, k_out, v_out, k_pages,
+                                         v_pages, block_table, context_lens, query_start_loc)
+    rc = load().pa_kv_read_q4(kp, vp, bt, cl, qsl, k, v, ctypes.byref(dims), _stream(stream))
+    if check and rc != PA_OK:
+        raise PagedAttnError("pa_kv_read_q4", rc)
+    return rc
 
 
 def paged_attn_q4(q, k_pages, v_pages, block_table, context_lens, scale, out, dims: PaDims, workspace=None,
                   stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_q4(...): decode attention over the 4-bit cache; out is
     written in place."""
-    _check_q4(dims, dims.num_q_heads, False, (q, out), (k_pages, v_pages), block_table, context_lens, None)
+    qa, oa, kp, vp, bt, cl, _ = _take_q4(dims, dims.num_q_heads, False, q, out, k_pages, v_pages, block_table,
+                                         context_lens, None)
     ws, ws_bytes, owner = _workspace_q4(dims, workspace, q, stream)
-    rc = load().paged_attn_q4(_addr(q), _addr(k_pages), _addr(v_pages), _addr(block_table), _addr(context_lens),
-                              scale, _addr(out), ctypes.byref(dims), ws, ws_bytes, _stream(stream),
+    rc = load().paged_attn_q4(qa, kp, vp, bt, cl, scale, oa, ctypes.byref(dims), ws, ws_bytes, _stream(stream),
                               ctypes.byref(timing) if timing is not None else None)
     if check and rc != PA_OK:
         raise PagedAttnError("paged_attn_q4", rc)
@@ -394,10 +404,10 @@ def paged_attn_varlen_q4(q, k_pages, v_pages, block_table, context_lens, query_s
                          workspace=None, stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_varlen_q4(...): causal chunks plus decode rows over the
     4-bit cache."""
-    _check_q4(dims, dims.num_q_heads, True, (q, out), (k_pages, v_pages), block_table, context_lens, query_start_loc)
+    qa, oa, kp, vp, bt, cl, qsl = _take_q4(dims, dims.num_q_heads, True, q, out, k_pages, v_pages, block_table,
+                                           context_lens, query_start_loc)
     ws, ws_bytes, owner = _workspace_q4(dims, workspace, q, stream)
-    rc = load().paged_attn_varlen_q4(_addr(q), _addr(k_pages), _addr(v_pages), _addr(block_table), _addr(context_lens),
-                                     _addr(query_start_loc), scale, _addr(out), ctypes.byref(dims), ws, ws_bytes,
+    rc = load().paged_attn_varlen_q4(qa, kp, vp, bt, cl, qsl, scale, oa, ctypes.byref(dims), ws, ws_bytes,
                                      _stream(stream), ctypes.byref(timing) if timing is not None else None)
     if check and rc != PA_OK:
         raise PagedAttnError("paged_attn_varlen_q4", rc)

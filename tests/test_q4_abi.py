@@ -189,6 +189,9 @@ class Wrong:
     def is_contiguous(self):
         return self._c
 
+    def data_ptr(self):
+        return P
+
 
 @host_only
 def test_binding_refuses_tensors(monkeypatch):
@@ -201,9 +204,9 @@ def test_binding_refuses_tensors(monkeypatch):
         t = dict(q=Wrong(torch.bfloat16, n), out=Wrong(torch.bfloat16, n), k=Wrong(torch.uint8, tiles),
                  v=Wrong(torch.uint8, tiles), bt=Wrong(torch.int32, 8 * 64), cl=Wrong(torch.int32, 8))
         t.update(kw)
-        return pb._check_q4(d, 32, False, (t["q"], t["out"]), (t["k"], t["v"]), t["bt"], t["cl"], None)
+        return pb._take_q4(d, 32, False, t["q"], t["out"], t["k"], t["v"], t["bt"], t["cl"], None)
 
-    call()
+    assert call() == (P,) * 6 + (None,)
     for name, good, size in (("q", torch.bfloat16, n), ("out", torch.bfloat16, n), ("k", torch.uint8, tiles),
                              ("v", torch.uint8, tiles), ("bt", torch.int32, 512), ("cl", torch.int32, 8)):
         with pytest.raises(TypeError):
@@ -215,8 +218,19 @@ def test_binding_refuses_tensors(monkeypatch):
         with pytest.raises(ValueError, match="contiguous"):
             call(**{name: Wrong(good, size, contiguous=False)})
     with pytest.raises(ValueError, match="needed"):
-        pb._check_q4(dims(num_q_rows=9, max_q_len=2), 32, True, (Wrong(torch.bfloat16, 9 * 32 * 128),) * 2,
-                     (Wrong(torch.uint8, tiles),) * 2, Wrong(torch.int32, 512), Wrong(torch.int32, 8), Wrong(torch.int32, 8))
+        pb._take_q4(dims(num_q_rows=9, max_q_len=2), 32, True, *(Wrong(torch.bfloat16, 9 * 32 * 128),) * 2,
+                    *(Wrong(torch.uint8, tiles),) * 2, Wrong(torch.int32, 512), Wrong(torch.int32, 8), Wrong(torch.int32, 8))
+
+
+@host_only
+def test_binding_refuses_host_tensors(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    d = dims(num_seqs=2)
+    q = torch.zeros(2, 32, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="current device"):
+        pb.paged_attn_q4(q, P, P, P, P, 0.1, P, d, workspace=P, stream=S)
+    with pytest.raises(ValueError, match="current device"):
+        pb.pa_kv_append_q4(P, P, P, torch.zeros(2, dtype=torch.int32), P, P, d, stream=S)
 
 
 def test_dims_from_shapes():
