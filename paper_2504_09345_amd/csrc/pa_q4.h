@@ -78,17 +78,25 @@ struct Q4StreamArgs {
   float scale_log2;
   int B, H_q, H_kv, rows, num_pages, max_context_len;
   int max_q_len;  // longer chunks are NaN rows, where write_long
+  int cus;        // of the device
   int write_long;
 };
 constexpr int kQ4StreamSeqs = 4096;    // sequences of a launch
 constexpr int kQ4StreamGroups = 512;   // workgroups of a launch
 constexpr int kQ4StreamThreads = 512;  // of a workgroup
+// Units per wave below which a CU's second workgroup stays without a range (head_dim 64,
+// where two fit).  One and two, 32 query heads over 8 in bf16: 64 sequences of 512-2,048
+// tokens (5 units a wave of both) 17.2 us and 18.4, 4 of 8,192-32,768 (5) 19.6 and 21.0,
+// 128 of 512-2,048 (10) 25.3 and 24.7, 256 (20) 43.8 and 41.2, 512 of 1,024-4,096 (80)
+// 158 and 148; in fp32, 64 heads over 8: 64 of 256-2,048 (4) 22.3 and 23.4, 128 of
+// 512-2,048 (10) 31.6 and 31.9, 256 (20) 52.0 and 50.5.
+constexpr int kQ4FewUnits = 8;
 constexpr int kQ4CounterStride = 16;   // 128 bytes: atomics on one line follow each other 30 ns apart
 static_assert(kQ4StreamGroups <= kStreamMaxGrid, "a cut item's groups of records");
 
 // Workgroups that the current device holds at once, at most as many as a launch may
-// have; 0 on error.
-int q4_stream_workgroups(int dtype, int D, int s);
+// have, and its CUs; 0 on error.
+int q4_stream_workgroups(int dtype, int D, int s, int* cus);
 hipError_t launch_q4_stream(int dtype, int D, int s, const Q4StreamArgs& a, int workgroups, hipStream_t st, KernelEvents ev);
 template <typename T, int D> const void* q4_stream_pick(int s);
 

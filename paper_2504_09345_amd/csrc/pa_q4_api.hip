@@ -218,9 +218,9 @@ int attend(const void* q, const void* k_pages, const void* v_pages, const int32_
     if (p.n_split > 1 && pa::launch_q4_merge(d->dtype, d->head_dim, a, stream) != hipSuccess) return PA_EHIP;
   }
   if (p.stream) {
-    const int workgroups = pa::q4_stream_workgroups(d->dtype, d->head_dim, p.s);
-    if (workgroups <= 0) return PA_EHIP;
     pa::Q4StreamArgs a{};
+    const int workgroups = pa::q4_stream_workgroups(d->dtype, d->head_dim, p.s, &a.cus);
+    if (workgroups <= 0) return PA_EHIP;
     a.k_pages = static_cast<const uint8_t*>(k_pages);
     a.v_pages = static_cast<const uint8_t*>(v_pages);
     a.ws_o = reinterpret_cast<float*>(ws);

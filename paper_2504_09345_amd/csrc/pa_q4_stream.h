@@ -171,7 +171,8 @@ void q4_stream_kernel(Q4StreamArgs a) {
     for (int64_t i = from * a.H_q * D + tid; i < to * a.H_q * D; i += NT) store_out<T>(o + i, what == 2 ? 0.0f : NAN);
   }
   const int U = H * sm.cum[R];
-  const int G = max(1, min(n_wg * kWaves, U));  // ranges
+  // ranges: one per wave, in a workgroup per CU where more would have few units each
+  const int G = max(1, min((U < kQ4FewUnits * n_wg * kWaves ? min(a.cus, n_wg) : n_wg) * kWaves, U));
   if (wg * kWaves >= G || U == 0) return;
   // ranges of each or each + 1 units, the longer ones first
   const int each = U / G, longer = U % G;
@@ -183,48 +184,36 @@ void q4_stream_kernel(Q4StreamArgs a) {
   const int u0 = begin_of(bid);
   const int m = begin_of(bid + 1) - u0;  // units of the range
 
-  // 2. The range's units, 64 at a time, one per lane: the words that their lengths and
-  // pages come from are loaded when the 64 before begin.
-  struct Words {
+  // 2. The range's units, 64 at a time, one per lane.  (Loading the words that their
+  // lengths and pages come from ahead, when the 64 before begin, is no faster.)
+  struct Entries {
+    int64_t at[2];  // the tiles' first byte (0: outside the pool, or no page)
+    int info;       // tokens (6 bits) | page 0, 1 outside the pool | anything but 32 tokens of the pool
     int hb, p, np;  // KV head; unit of the item and the item's units
-    int row, len, page[2];
+    int row;
   };
-  auto load_entries = [&](int i0) {
-    Words e;
+  const int64_t tile = q4_tile_bytes(D);
+  auto entries = [&](int i0) {
+    Entries e;
     const int x = u0 + min(i0 + lane, m - 1);
     const int r = info_row_seq(sm.cum, R, H, x);
     const int rem = x - H * sm.cum[r];
     e.np = sm.cum[r + 1] - sm.cum[r];
     e.hb = rem / e.np;
     e.p = rem - e.hb * e.np;
-    e.len = a.context_lens[r];
     e.row = a.query_start_loc != nullptr ? a.query_start_loc[r] : r;
+    int page[2], odd = 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)  // (past the context's pages: any entry, unused)
-      e.page[h] = a.block_table[(int64_t)r * a.bt_stride + min((int64_t)2 * e.p + h, a.bt_stride - 1)];
-    return e;
-  };
-  struct Entries {
-    int64_t at[2];  // the tiles' first byte (0: outside the pool, or no page)
-    int info;       // tokens (6 bits) | page 0, 1 outside the pool | anything but 32 tokens of the pool
-    int hb, p, np, row;
-  };
-  const int64_t tile = q4_tile_bytes(D);
-  auto make_entries = [&](const Words& w) {
-    Entries e;
-    const int left = w.len - w.p * kQ4Unit;  // tokens from the unit on
-    int odd = 0;
+    for (int h = 0; h < 2; ++h)  // (past the context's pages: any entry, unused; read without waiting for the length)
+      page[h] = a.block_table[(int64_t)r * a.bt_stride + min((int64_t)2 * e.p + h, a.bt_stride - 1)];
+    const int left = a.context_lens[r] - e.p * kQ4Unit;  // tokens from the unit on
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const bool used = left > kPage * h, ok = used && w.page[h] >= 0 && w.page[h] < a.num_pages;
+      const bool used = left > kPage * h, ok = used && page[h] >= 0 && page[h] < a.num_pages;
       odd |= (ok || !used ? 0 : 1) << h;
-      e.at[h] = ok ? ((int64_t)w.page[h] * H + w.hb) * tile : 0;
+      e.at[h] = ok ? ((int64_t)page[h] * H + e.hb) * tile : 0;
     }
     e.info = min(left, kQ4Unit) | odd << 6 | (odd != 0 || left < kQ4Unit) << 8;
-    e.hb = w.hb;
-    e.p = w.p;
-    e.np = w.np;
-    e.row = w.row;
     return e;
   };
 
@@ -269,8 +258,7 @@ void q4_stream_kernel(Q4StreamArgs a) {
     int from = -1, to = -1, row = 0, g = 0;
   } job[2];
   if (m > 0) {
-    Entries es = make_entries(load_entries(0));
-    Words coming = load_entries(64);
+    Entries es = entries(0);
     int i0 = 0;  // unit of es's first lane
     auto of = [&](int x, int i) { return __builtin_amdgcn_readlane(x, i - i0); };
     auto tiles = [&](int i) {  // (wave-uniform)
@@ -299,15 +287,14 @@ void q4_stream_kernel(Q4StreamArgs a) {
         q4::reset(st);
         open = true;
       }
-      // units without anything else to do between them: the last of the 64 is alone,
-      // the next one's entry is among those coming
+      // units without anything else to do between them; the last of the 64 is alone: the
+      // next one's entry is among the 64 after
       int stop = min(min(m, i + left), i0 + 63);
       if (i + 1 - i0 == 64) {
         stop = i + 1;
         if (stop < m) {
-          es = make_entries(coming);
           i0 += 64;
-          coming = load_entries(i0 + 64);
+          es = entries(i0);
         }
       }
       const bool ends = stop == i + left;

@@ -49,20 +49,24 @@ static const void* q4_stream_fn(int dtype, int D, int s) {
 
 // (a property of the kernel and the device, so it is asked for once: the two
 // queries take as long as the rest of a small call on the host)
-int q4_stream_workgroups(int dtype, int D, int s) {
+int q4_stream_workgroups(int dtype, int D, int s, int* cus) {
   constexpr int kDevices = 64;
-  static std::atomic<int> known[kDevices][2][2][9];
-  int dev = 0, cus = 0, per_cu = 0;
+  static std::atomic<int64_t> known[kDevices][2][2][9];  // workgroups, and the CUs above them
+  int dev = 0, n_cus = 0, per_cu = 0;
   if (hipGetDevice(&dev) != hipSuccess) return 0;
-  std::atomic<int>* at = dev >= 0 && dev < kDevices && dtype >= 0 && dtype < 2 && s <= 8 ? &known[dev][dtype][D / 128][s] : nullptr;
-  int n = at != nullptr ? at->load(std::memory_order_relaxed) : 0;
-  if (n > 0) return n;
+  std::atomic<int64_t>* at = dev >= 0 && dev < kDevices && dtype >= 0 && dtype < 2 && s <= 8 ? &known[dev][dtype][D / 128][s] : nullptr;
+  const int64_t have = at != nullptr ? at->load(std::memory_order_relaxed) : 0;
+  if (have > 0) {
+    *cus = (int)(have >> 32);
+    return (int)have;
+  }
   const void* fn = q4_stream_fn(dtype, D, s);
-  if (fn == nullptr || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
+  if (fn == nullptr || hipDeviceGetAttribute(&n_cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
       hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, fn, kQ4StreamThreads, 0) != hipSuccess)
     return 0;
-  n = std::min(cus * per_cu, kQ4StreamGroups);
-  if (at != nullptr) at->store(n, std::memory_order_relaxed);
+  const int n = std::min(n_cus * per_cu, kQ4StreamGroups);
+  if (at != nullptr) at->store((int64_t)n_cus << 32 | n, std::memory_order_relaxed);
+  *cus = n_cus;
   return n;
 }
 
