@@ -134,8 +134,11 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
   }
   if (p->chunks) {
     p->min_rows = p->stream ? 2 : 1;
-    // rows of the sequences that can be chunks
-    const int64_t chunk_rows = p->stream ? (int64_t)p->rows - d->num_seqs + 1 : p->rows;
+    // rows of the chunks, as the plan reckons with them: all but a row of each other
+    // sequence, and one chunk at least (a batch may hold sequences of no rows)
+    const int64_t one = d->max_q_len < p->rows ? d->max_q_len : p->rows;
+    int64_t chunk_rows = p->stream ? (int64_t)p->rows - d->num_seqs + 1 : p->rows;
+    if (chunk_rows < one) chunk_rows = one;
     const int64_t alone_units = (chunk_rows / pa::q4_positions(1, s) + 1) * d->num_kv_heads *
                                 ((d->max_context_len - d->max_q_len / 2) / pa::kQ4Unit + 1);
     p->shared = d->dtype == PA_BF16 && d->max_q_len * (int64_t)s > kAloneColumns && alone_units > kAloneUnits;

@@ -109,6 +109,15 @@ def test_decode_items_and_workgroups(H_kv, n, ctx):
     check(b.attend(b.upload()).float().cpu(), b.expected_gpu(), ctx, "bf16")
 
 
+@pytest.mark.parametrize("D,dtype", [(128, "bf16"), (64, "fp32")])
+@pytest.mark.parametrize("lens", [[(0, 0)] * 40 + [(70, 2)] + [(9, 0)] * 30, [(300, 39)] + [(0, 0)] * 200 + [(33, 1)]],
+                         ids=["two rows", "a chunk and a row"])
+def test_more_sequences_than_rows(D, dtype, lens):
+    announce(f"q4 chunks among empty sequences D={D} {dtype}")
+    b = Batch(lens, 8, 2, D, dtype=dtype, seed=2)
+    check(b.attend(b.upload()).float().cpu(), b.expected_gpu(), 300, dtype)
+
+
 @pytest.mark.parametrize("varlen", [False, True])
 def test_shortest(varlen):
     """Contexts of one token (its value) and of none."""

@@ -243,3 +243,10 @@ def test_dims_from_shapes():
         pb.make_dims_q4(torch.empty(3, 4, 128), k, bt, 100)
     with pytest.raises(pb.PagedAttnError):
         pb.make_dims_q4(torch.empty(3, 4, 80), k, bt, 100)
+
+
+@pytest.mark.parametrize("seqs,rows,most", [(10, 2, 2), (1000, 2, 2), (5, 8, 8), (4096, 40, 39), (3, 3, 2)])
+def test_more_sequences_than_rows(seqs, rows, most):
+    """Batches padded with sequences of no rows are planned as what they can hold."""
+    n = pb.pa_workspace_size_q4(dims(num_seqs=seqs, num_q_rows=rows, max_q_len=most))
+    assert 0 < n < 1 << 28
