@@ -42,6 +42,7 @@ int rows_call(const void* k_rows, const void* v_rows, const int32_t* block_table
     rows = d->num_seqs;
   }
   if (rows == 0) return PA_OK;
+  if ((int64_t)rows + 2 * (int64_t)d->num_seqs > INT32_MAX) return PA_ENOTSUP;  // (32-bit slots)
   if (!k_rows || !v_rows || !block_table || !context_lens || !k_pages || !v_pages) return PA_EINVAL;
   if (misaligned(k_rows) || misaligned(v_rows) || misaligned(k_pages) || misaligned(v_pages)) return PA_EINVAL;
   pa::Q4RowsArgs a;

@@ -108,6 +108,7 @@ def test_refused_row_addresses(name, at):
     d = dims(num_q_rows=-2)
     assert rows_call(name, d, qsl=P) == pb.PA_EINVAL
     assert rows_call(name, dims(num_q_rows=3, num_seqs=0), qsl=P) == pb.PA_EINVAL
+    assert rows_call(name, dims(num_q_rows=3, num_seqs=1 << 30), qsl=P) == pb.PA_ENOTSUP
 
 
 @host_only
