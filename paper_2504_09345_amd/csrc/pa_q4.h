@@ -91,6 +91,13 @@ constexpr int kQ4StreamThreads = 512;  // of a workgroup
 // 158 and 148; in fp32, 64 heads over 8: 64 of 256-2,048 (4) 22.3 and 23.4, 128 of
 // 512-2,048 (10) 31.6 and 31.9, 256 (20) 52.0 and 50.5.
 constexpr int kQ4FewUnits = 8;
+// A workgroup takes an item whole, where there are no more items than CUs, if the longest
+// has at most so many units more than a workgroup's equal share: a wave's 3.5
+// units more are what the join through memory costs.  Whole and shared, 32 query heads
+// over 8 in bf16: 1 sequence of 200 tokens 8.4 us and 9.8, of 1,000 10.8 and 10.4, of
+// 2,000 13.9 and 11.6; 8 of 200-500 9.5 and 10.6, of 512-2,048 14.5 and 13.5; 32 of
+// 100-500 10.6 and 13.3, of 512-2,048 16.4 and 18.5.
+constexpr int kQ4AloneUnits = 28;
 constexpr int kQ4CounterStride = 16;   // 128 bytes: atomics on one line follow each other 30 ns apart
 static_assert(kQ4StreamGroups <= kStreamMaxGrid, "a cut item's groups of records");
 

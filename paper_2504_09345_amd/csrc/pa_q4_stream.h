@@ -171,9 +171,19 @@ void q4_stream_kernel(Q4StreamArgs a) {
     for (int64_t i = from * a.H_q * D + tid; i < to * a.H_q * D; i += NT) store_out<T>(o + i, what == 2 ? 0.0f : NAN);
   }
   const int U = H * sm.cum[R];
+  const int busy = min(a.cus, n_wg);  // workgroups, one per CU
   // ranges: one per wave, in a workgroup per CU where more would have few units each
-  const int G = max(1, min((U < kQ4FewUnits * n_wg * kWaves ? min(a.cus, n_wg) : n_wg) * kWaves, U));
-  if (wg * kWaves >= G || U == 0) return;
+  const int G = max(1, min((U < kQ4FewUnits * n_wg * kWaves ? busy : n_wg) * kWaves, U));
+  if (U == 0) return;
+  // Few short items: a workgroup has one of them alone, and nothing is joined through
+  // memory (kQ4AloneUnits).
+  bool alone = (int64_t)R * H <= busy;
+  if (alone) {
+    int most = 0;
+    for (int r = lane; r < R; r += 64) most = max(most, sm.cum[r + 1] - sm.cum[r]);
+    alone = __builtin_amdgcn_ballot_w64(most > U / busy + kQ4AloneUnits) == 0;
+  }
+  if (wg >= (alone ? R * H : (G + kWaves - 1) / kWaves)) return;
   // ranges of each or each + 1 units, the longer ones first
   const int each = U / G, longer = U % G;
   auto begin_of = [&](int x) { return min(x, G) * each + min(x, longer); };
@@ -181,8 +191,15 @@ void q4_stream_kernel(Q4StreamArgs a) {
     const int split = longer * (each + 1);
     return e < split ? e / (each + 1) : longer + (e - split) / each;
   };
-  const int u0 = begin_of(bid);
-  const int m = begin_of(bid + 1) - u0;  // units of the range
+  int u0, m;  // units of the range
+  if (alone) {
+    const int r = wg / H, np = sm.cum[r + 1] - sm.cum[r], per = (np + kWaves - 1) / kWaves;
+    u0 = H * sm.cum[r] + (wg - r * H) * np + wave * per;
+    m = max(0, min(per, np - wave * per));
+  } else {
+    u0 = begin_of(bid);
+    m = begin_of(bid + 1) - u0;
+  }
 
   // 2. The range's units, 64 at a time, one per lane.  (Loading the words that their
   // lengths and pages come from ahead, when the 64 before begin, is no faster.)
@@ -393,8 +410,15 @@ void q4_stream_kernel(Q4StreamArgs a) {
     const Job it = j == 0 ? job[0] : job[1];
     if (it.from < 0 || (j == 0 && wave > 0)) continue;  // (else an earlier wave has the item's first part)
     // parts: slot j of this wave, slot 0 of those up to the item's last
-    const int to = range_of(it.to), parts = min(to - wg * kWaves, kWaves - 1) - wave + 1;
-    const CutItem cut{range_of(it.from) / kWaves, to / kWaves};
+    int parts;
+    CutItem cut{wg, wg};
+    if (alone) {
+      parts = (it.to - it.from) / m + 1;
+    } else {
+      const int to = range_of(it.to);
+      parts = min(to - wg * kWaves, kWaves - 1) - wave + 1;
+      cut = CutItem{range_of(it.from) / kWaves, to / kWaves};
+    }
     const bool whole = cut.x0 == cut.x1;
     T* o = out + ((int64_t)it.row * a.H_q + (int64_t)it.g * S) * D;
     const int64_t slot = (int64_t)wg * 2 + j;

@@ -16,9 +16,11 @@
 //    item cut by the ranges' ends are then mostly waves of one workgroup, which meet in
 //    LDS, and only items cut by a workgroup's ends go through memory, where a level of
 //    the join costs 3-4 us.  Measured with eight waves of one range each and with a wave
-//    each, 32 query heads over 8, bf16: 1 sequence of 200 tokens 10.5 us and 9.7, 8 of
-//    512-2,048 22.1 and 14.0, 256 of those 75.0 and 69.6, 4 of 8,192-32,768 29.5 and
+//    each, 32 query heads over 8, bf16: 8 sequences of 512-2,048 tokens 22.1 us and 14.0, 256 of those 75.0 and 69.6, 4 of 8,192-32,768 29.5 and
 //    23.6.  (Two waves on two heads of one range each: 14.9, 68.0 and 24.9.)
+//  * Where a batch has few short items, a workgroup takes each whole, its eight waves a
+//    part of the units: nothing goes through memory then, and a call is 1.1-2.7 us
+//    shorter (kQ4AloneUnits).
 //  * Of a SIMD's waves the oldest issues first; left alone, the older half of a
 //    workgroup ended its ranges 7 us before the younger one on 256 sequences, which then
 //    streamed with half of the loads under way.  The waves take turns instead, a unit
