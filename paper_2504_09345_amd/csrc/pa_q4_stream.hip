@@ -16,8 +16,9 @@
 //    item cut by the ranges' ends are then mostly waves of one workgroup, which meet in
 //    LDS, and only items cut by a workgroup's ends go through memory, where a level of
 //    the join costs 3-4 us.  Measured with eight waves of one range each and with a wave
-//    each, 32 query heads over 8, bf16: 8 sequences of 512-2,048 tokens 22.1 us and 14.0, 256 of those 75.0 and 69.6, 4 of 8,192-32,768 29.5 and
-//    23.6.  (Two waves on two heads of one range each: 14.9, 68.0 and 24.9.)
+//    each, 32 query heads over 8, bf16: 8 sequences of 512-2,048 tokens 22.1 us and
+//    14.0, 256 of those 75.0 and 69.6, 4 of 8,192-32,768 29.5 and 23.6.  (Two waves on
+//    two heads of one range each: 14.9, 68.0 and 24.9.)
 //  * Where a batch has few short items, a workgroup takes each whole, its eight waves a
 //    part of the units: nothing goes through memory then, and a call is 1.1-2.7 us
 //    shorter (kQ4AloneUnits).
@@ -27,7 +28,7 @@
 //    each (64 sequences at 64 heads of 64 dims in fp32: 27 us instead of 35).
 //
 // 256 sequences of 512-2,048 tokens (348 MB): the waves stream for 56 us at 6.2 TB/s,
-// where loads of this pattern alone reach 6.4; launch, lengths and entries take 3.4 us
+// where loads of this pattern alone reach 6.4; launch, lengths and entries take 3 us
 // before and the joins of the last ranges 4-8 us after.
 #include "pa_q4_stream.h"
 
