@@ -38,7 +38,8 @@
  * dims (pa_dims_t): num_pages, num_kv_heads, head_dim (64 or 128), page_size (16),
  * max_pages_per_seq and max_context_len describe the cache as in pagedattn.h;
  * dtype (PA_BF16 or PA_FP32) is the type of the dense arrays: k_new, v_new,
- * k_out, v_out, q and out.  pages_per_split must be 0.
+ * k_out, v_out, q and out.  pages_per_split must be 0.  Arrays that a call writes
+ * overlap none that it reads.
  */
 #ifndef PAGEDATTN_Q4_H
 #define PAGEDATTN_Q4_H

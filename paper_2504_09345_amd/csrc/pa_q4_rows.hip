@@ -275,7 +275,8 @@ hipError_t launch_q4_read(int dtype, int D, const Q4RowsArgs& a, hipStream_t st)
     const int slots = slots_of(a);
     const dim3 grid((slots + kRowsWaves - 1) / kRowsWaves, (a.H_kv * D * (int)sizeof(t) / 16 + 63) / 64);
     const bool past = (int64_t)2 * a.rows * a.H_kv * D * sizeof(t) > kCached;
-    const auto fn = past ? &q4_read_kernel<decltype(t), decltype(d)::value, true> : &q4_read_kernel<decltype(t), decltype(d)::value, false>;
+    constexpr int D = decltype(d)::value;
+    const auto fn = past ? &q4_read_kernel<decltype(t), D, true> : &q4_read_kernel<decltype(t), D, false>;
     fn<<<grid, 64 * kRowsWaves, 0, st>>>(a, slots);
   });
 }

@@ -300,7 +300,8 @@ void q4_stream_kernel(Q4StreamArgs a) {
         head = p > 0;
         from = u0 + i - p;
         to = u0 + i + left - 1;
-        q4::load_query<T, D>(st.q[0], n < S ? reinterpret_cast<const T*>(a.q) + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D : nullptr, lane);
+        const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D;
+        q4::load_query<T, D>(st.q[0], n < S ? q : nullptr, lane);
         q4::reset(st);
         open = true;
       }

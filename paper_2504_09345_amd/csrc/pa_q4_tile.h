@@ -38,10 +38,13 @@ __device__ __forceinline__ int wave_search(int n, int x, int lane, Key key) {
 template <int B>
 __device__ __forceinline__ float scale_of(uint32_t w) {
   uint32_t r;
-  if constexpr (B == 0) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(r) : "v"(23u), "v"(w));
-  if constexpr (B == 1) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(r) : "v"(23u), "v"(w));
-  if constexpr (B == 2) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(r) : "v"(23u), "v"(w));
-  if constexpr (B == 3) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(r) : "v"(23u), "v"(w));
+#define Q4_SCALE_OF(BYTE)                                                                                                 \
+  asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:" BYTE : "=v"(r) : "v"(23u), "v"(w))
+  if constexpr (B == 0) Q4_SCALE_OF("BYTE_0");
+  if constexpr (B == 1) Q4_SCALE_OF("BYTE_1");
+  if constexpr (B == 2) Q4_SCALE_OF("BYTE_2");
+  if constexpr (B == 3) Q4_SCALE_OF("BYTE_3");
+#undef Q4_SCALE_OF
   return __uint_as_float(r);
 }
 
