@@ -118,6 +118,34 @@ def test_more_sequences_than_rows(D, dtype, lens):
     check(b.attend(b.upload()).float().cpu(), b.expected_gpu(), 300, dtype)
 
 
+@pytest.mark.parametrize("ctx", [4000, 20000, 70000, 300000, 1100000])
+@pytest.mark.parametrize("H_q", [1, 8])
+def test_items_over_many_workgroups(H_q, ctx):
+    """One item over 16 to 512 workgroups, each size of the joins' groups.  Queries of
+    zeros weigh every key alike, and all sums are exact: the output is the mean of V,
+    1 / l and one product from exact (2^-22 of it)."""
+    announce(f"q4 one item of {ctx} tokens H_q={H_q}")
+    D, pool = 64, 97
+    rng = np.random.default_rng(ctx)
+    k, v = (rng.integers(0, 256, (pool, 1, q4.tile_bytes(D)), dtype=np.uint8) for _ in range(2))
+    k[..., 8 * D:] = rng.integers(120, 130, k[..., 8 * D:].shape)
+    v[..., 8 * D:] = 127
+    pages = -(-ctx // 16)
+    bt = rng.integers(0, pool, (1, pages)).astype(np.int32)
+    count = np.bincount(bt[0, :ctx // 16], minlength=pool)
+    x = q4.unpack("v", v[:, 0], D)  # [page][token][dim]
+    total = np.einsum("p,ptd->d", count.astype(np.float64), x)
+    if ctx % 16:
+        total += x[bt[0, -1], :ctx % 16].sum(0)
+    t = [torch.from_numpy(a).cuda() for a in (k, v, bt, np.array([ctx], np.int32))]
+    q = torch.zeros(1, H_q, D, device="cuda")
+    for dtype, step in ((torch.float32, 2.0 ** -24), (torch.bfloat16, 2.0 ** -8)):
+        out = torch.empty(1, H_q, D, dtype=dtype, device="cuda")
+        pb.paged_attn_q4(q.to(dtype), t[0], t[1], t[2], t[3], 1.0, out, pb.make_dims_q4(out, t[0], t[2], ctx))
+        off = np.abs(out[0].double().cpu().numpy() - total / ctx)
+        assert (off <= (step + 2.0 ** -22) * np.abs(total / ctx)).all()
+
+
 @pytest.mark.parametrize("varlen", [False, True])
 def test_shortest(varlen):
     """Contexts of one token (its value) and of none."""
