@@ -93,7 +93,10 @@ int pa_workspace_size_q4(const pa_dims_t *dims, size_t *bytes);
  * its row's scale (an error of at most 2^-22 of the row's largest); fp32 ones as
  * sums of three bf16 parts.  Softmax weights: for bf16 outputs in fp16 where every V
  * of the step is exact in fp16 (scales 2^-23 .. 2^8) and as two bf16 parts elsewhere,
- * for fp32 outputs as three bf16 parts.  The same inputs give the same bits.
+ * for fp32 outputs as three bf16 parts.  Weighted sums do not overflow: an output is
+ * finite wherever the weighted mean is.  (A row that sees a V of 2^64 or more, or a NaN
+ * block of V, loses what V below 2^-78 beside it would add.)  The same inputs give the
+ * same bits.
  * GQA group size num_q_heads / num_kv_heads in {1, 2, 4, 6, 8}.  A row that sees
  * no key (context 0) is zeros; a row of a context above max_context_len, or that
  * sees a page entry outside [0, num_pages), is NaN.  q and out are 16-byte

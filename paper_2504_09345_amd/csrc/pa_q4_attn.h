@@ -178,17 +178,21 @@ void q4_attn_kernel(Q4AttnArgs a) {
       q4::f32x4_t s[NB][2];
       float x[NB][8];
       Pages next = t;
-      bool big = false;
-      auto weights = [&](bool usual) {  // the weights of unit k, and the next K; whether its base moves or V is beyond fp16
+      bool big = false, odd = false;  // the base moves; V takes other products
+      auto weights = [&](bool usual) {  // the weights of unit k, and the next K; whether it is big or odd
         if (k + 1 < u1) next = pages(k + 1);
         q4::fold_qk<T, D, NB>(st, u, k_shift, s);
         fetch_k(next, k + 1 < u1);
-        if (!usual) q4::mask_scores<T, D, NB>(st, k * kQ4Unit, t.bad, lane, s);
+        if (!usual) {
+          q4::mask_scores<T, D, NB>(st, k * kQ4Unit, t.bad, lane, s);
+          q4::clear_dead(u, k * kQ4Unit, all_last, lane);
+        }
         big = q4::form_weights<T, D, NB>(st, s, a.scale_log2, x);
         __builtin_amdgcn_sched_barrier(0);  // (V is not waited for before the weights are formed)
-        return __builtin_amdgcn_ballot_w64(big | (kF16 && q4::beyond_fp16<D>(u))) != 0;
+        odd = kF16 ? q4::beyond_fp16<D>(u) : q4::has_large<D>(u);
+        return __builtin_amdgcn_ballot_w64(big | odd) != 0;
       };
-      bool rare = weights(k < u_full && t.bad == 0);
+      bool rare = weights(k < u_full && t.bad == 0) | st.any_lifted;
       if (k < u_full) {
         // (one way out, and nothing but the usual unit: the sums stay in place, and the
         // loads under way are known)
@@ -202,8 +206,10 @@ void q4_attn_kernel(Q4AttnArgs a) {
           rare = weights(true);
         }
       }
-      q4::settle_weights<T, D, NB>(st, s, a.scale_log2, big, x);
-      q4::fold_pv_edge<T, D, NB>(st, u, x, k * kQ4Unit, all_last, lane);
+      int first = INT32_MAX;
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) first = q4::first_large(u, k * kQ4Unit, lane);
+      q4::settle_weights<true, T, D, NB>(st, s, a.scale_log2, big, x, first);
+      q4::fold_pv_edge<T, D, NB>(st, u, x, k * kQ4Unit, lane);
       fetch_v(next, k + 1 < u1);
       t = next;
     }

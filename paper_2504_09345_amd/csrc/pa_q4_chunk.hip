@@ -12,7 +12,7 @@
 //
 // A unit with a scale outside fp16's window, or that holds a NaN block, is flagged by
 // the wave that converts it, and every wave takes it by the general products instead,
-// with V of its own.
+// with V of its own; so does a wave all units after one with large V.
 #include "pa_q4_attn.h"
 
 namespace pa {
@@ -147,6 +147,14 @@ void q4_chunk_kernel(Q4AttnArgs a) {
     }
   };
 
+  auto load_scales = [&](q4::Unit<D>& whole, const Pages& t) {  // V's, of a unit
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const __amdgpu_buffer_rsrc_t r =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(vg + t.at[p]), (short)0, tile_size, 0x00020000);
+      q4::load_words<D, 0>(r, q4::kScales<D> + G * (D / 8), whole.vs[p]);
+    }
+  };
   auto flagged = [&](int k) {
     const int32_t* f = s_odd[k & 1];
     return __builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3]) != 0;
@@ -189,7 +197,7 @@ void q4_chunk_kernel(Q4AttnArgs a) {
     float x[kNB][8];
     bool entered = false;
 #pragma unroll 1
-    for (; k < plain && t.bad == 0; ++k) {  // (nothing but the usual unit, so that the sums stay in place)
+    for (; k < plain && t.bad == 0 && !st.any_lifted; ++k) {  // (nothing but the usual unit, so that the sums stay in place)
       __syncthreads();  // unit k is staged, and unit k - 1 is done with
       if (flagged(k)) {
         entered = true;
@@ -199,7 +207,7 @@ void q4_chunk_kernel(Q4AttnArgs a) {
       q4::fold_qk<T, D, kNB>(st, u, 0, sn);
       const bool big = q4::form_weights<T, D, kNB>(st, s, a.scale_log2, x);
       fetch_k(t2, k + 2 < w1);
-      q4::settle_weights<T, D, kNB>(st, s, a.scale_log2, big, x);
+      q4::settle_weights<false, T, D, kNB>(st, s, a.scale_log2, big, x);
       convert(k + 1);
       fold_staged(k, x);
       fetch_part(t2, k + 2 < u1);
@@ -218,12 +226,22 @@ void q4_chunk_kernel(Q4AttnArgs a) {
     fetch_k(t2, k + 2 < w1);
     if (active) {
       q4::mask_scores<T, D, kNB>(st, k * kQ4Unit, t.bad, lane, s);
-      q4::fold_softmax<T, D, kNB>(st, s, a.scale_log2, x);
-      if (flagged(k)) {
+      const bool odd = flagged(k);
+      int first = INT32_MAX;
+      if (__builtin_expect(odd, 0)) {  // (the scales alone: all of V would hold registers meanwhile)
+        q4::Unit<D> whole;
+        load_scales(whole, t);
+        q4::clear_dead(whole, k * kQ4Unit, all_last, lane);
+        first = q4::first_large(whole, k * kQ4Unit, lane);
+      }
+      const bool big = q4::form_weights<T, D, kNB>(st, s, a.scale_log2, x);
+      q4::settle_weights<true, T, D, kNB>(st, s, a.scale_log2, big, x, first);
+      if (__builtin_expect(odd | st.any_lifted, 0)) {
         q4::Unit<D> whole;
 #pragma unroll
         for (int p = 0; p < 2; ++p) q4::load_v<D, 0>(whole, p, vg + t.at[p], tile_size, lane);
-        q4::fold_pv_edge<T, D, kNB>(st, whole, x, k * kQ4Unit, all_last, lane);
+        q4::clear_dead(whole, k * kQ4Unit, all_last, lane);
+        q4::fold_pv_edge<T, D, kNB>(st, whole, x, k * kQ4Unit, lane);
       } else {
         fold_staged(k, x);
       }

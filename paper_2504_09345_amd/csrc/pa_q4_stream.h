@@ -303,6 +303,7 @@ void q4_stream_kernel(Q4StreamArgs a) {
         const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D;
         q4::load_query<T, D>(st.q[0], n < S ? q : nullptr, lane);
         q4::reset(st);
+        st.last[0] = kQ4Unit - 1;
         open = true;
       }
       // units without anything else to do between them; the last of the 64 is alone: the
@@ -321,23 +322,25 @@ void q4_stream_kernel(Q4StreamArgs a) {
         q4::f32x4_t s[1][2];
         float x[1][8];
         Tiles next;
-        bool big;  // the base moves
-        auto weights = [&](bool usual) {  // the weights of unit i, and the next K; whether a base moves or V is beyond fp16
+        bool big;      // the base moves
+        uint64_t odd;  // V takes other products (of the lanes)
+        auto weights = [&](bool usual) {  // the weights of unit i, and the next K; whether it is big or odd
           const bool more = i + 1 < m;
           next = tiles(more ? i + 1 : i);
           q4::fold_qk<T, D, 1>(st, u, k_shift, s);
           fetch_k(next, more);
           if (!usual) {
             const int tokens = t.info & 63;
-            st.last[0] = tokens - 1;
+            st.last[0] = tokens - 1;  // (of this unit; the item's last, or of pages outside the pool)
             q4::mask_scores<T, D, 1>(st, 0, t.info >> 6 & 3, lane, s);
             q4::clear_dead(u, 0, tokens - 1, lane);
           }
           big = q4::form_weights<T, D, 1>(st, s, a.scale_log2, x);
           __builtin_amdgcn_sched_barrier(0);  // (V is not waited for before the weights are formed)
-          return __builtin_amdgcn_ballot_w64(big | (kF16 && q4::beyond_fp16<D>(u))) != 0;
+          odd = __builtin_amdgcn_ballot_w64(kF16 ? q4::beyond_fp16<D>(u) : q4::has_large<D>(u));
+          return (odd | __builtin_amdgcn_ballot_w64(big)) != 0;
         };
-        bool rare = weights(!(t.info & 256));
+        bool rare = weights(!(t.info & 256)) | st.any_lifted;
         // (one way out, and nothing but the usual unit: the sums stay in place, and the
         // loads under way are known)
 #pragma unroll 1
@@ -355,7 +358,10 @@ void q4_stream_kernel(Q4StreamArgs a) {
           }
           rare = weights(true);
         }
-        q4::settle_weights<T, D, 1>(st, s, a.scale_log2, big, x);
+        int first = INT32_MAX;  // (every column sees every key of the unit)
+        if (__builtin_expect(odd != 0, 0))
+          first = __builtin_amdgcn_ballot_w64(q4::has_large(u)) != 0 ? 0 : INT32_MAX;
+        q4::settle_weights<true, T, D, 1>(st, s, a.scale_log2, big, x, first);
         q4::fold_pv<false, T, D, 1>(st, u, x);
         fetch_v(next, i + 1 < m);
         t = next;

@@ -187,6 +187,8 @@ struct State {
   f32x4_t acc[NB][D / 16];          // O^T: block 2 j + h, entry i: dim 32 j + 8 (lane / 16) + 2 i + h
   float m[NB], l[NB];               // base (log2 units, one per column), the lane's part of the sum
   int last[NB];                     // last key that the column sees, -1: no column
+  bool lifted[NB];                  // the base is that of large V (kLift)
+  bool any_lifted;                  // one of the wave's may be
 };
 
 template <typename T, int D, int NB>
@@ -195,9 +197,11 @@ __device__ __forceinline__ void reset(State<T, D, NB>& st) {
   for (int c = 0; c < NB; ++c) {
     st.m[c] = kMInit;
     st.l[c] = 0.0f;
+    st.lifted[c] = false;
 #pragma unroll
     for (int mb = 0; mb < D / 16; ++mb) st.acc[c][mb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
+  st.any_lifted = false;
 }
 
 // row: the column's D elements (nullptr: zeros).  (All lanes active.)
@@ -307,6 +311,15 @@ __device__ __forceinline__ void mask_scores(const State<T, D, NB>& st, int key0,
 // numbers, and what is rounded of a smaller one is 2^-32 of the largest at most.
 constexpr float kHeadroom = 7.0f;
 constexpr float kWeightLimit = 32768.0f;
+// From the first key with a V of 2^64 or more on (scale byte kLargeScale), the base of
+// the columns that see it lies kLift above instead, and their weights stay below 2^-31:
+// 2^30 keys of the largest V, 6 2^125, then sum to less than 2^128.  (Below that size
+// sums stay under 2^15 2^30 2^67.)  Weights are bf16 parts there, so a power of two
+// costs them nothing; what is lost are products below 2^-126, so V below 2^-78 or so
+// beside the large ones.
+constexpr float kLift = 39.0f;
+constexpr float kLiftedLimit = 0x1p-31f;
+constexpr int kLargeScale = 192;
 
 // Online softmax: the weights, formed with the base of the units before; whether
 // one exceeds the limit (as a column's first does, whose base is kMInit).
@@ -331,9 +344,27 @@ __device__ __forceinline__ void add_weights(State<T, D, NB>& st, const float (&x
 // Only where one does the bases of the wave move (so a unit needs no maximum across
 // lanes); then the columns' sums.  The inner loops of waves alone leave for this: a
 // loop that scales the outputs in one of its branches copies them in the others.
-template <typename T, int D, int NB>
+// LIFT: first is the unit's first key with large V (INT32_MAX: none); the bases of the
+// columns that see it are lifted.  They lie kHeadroom below the largest score so far, or
+// up to 8 log2 units more (the limit), so they come to lie kLift to kLift + 8 above.
+template <bool LIFT, typename T, int D, int NB>
 __device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, bool big,
-                                               float (&x)[NB][8]) {
+                                               float (&x)[NB][8], int first = INT32_MAX) {
+  float up[NB] = {};
+  if constexpr (LIFT) {
+    if (__builtin_expect(st.any_lifted | (first != INT32_MAX), 0)) {
+      big |= first != INT32_MAX;
+#pragma unroll
+      for (int c = 0; c < NB; ++c) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) big |= st.lifted[c] & (x[c][i] > kLiftedLimit);
+        const bool now = (st.last[c] >= first) & !st.lifted[c];
+        up[c] = now ? kLift + kHeadroom + 8.0f : 0.0f;
+        st.lifted[c] |= now;
+      }
+      st.any_lifted = true;
+    }
+  }
   if (__builtin_amdgcn_ballot_w64(big) != 0) {
 #pragma unroll
     for (int c = 0; c < NB; ++c) {
@@ -341,7 +372,9 @@ __device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_
 #pragma unroll
       for (int i = 0; i < 8; ++i) mx = fmaxf(mx, s[c][i >> 2][i & 3]);
       // (scale > 0, so the largest score is the scaled largest)
-      const float mc = fmaxf(st.m[c], rows4_max(mx) * scale_log2 - kHeadroom);
+      float mc = rows4_max(mx) * scale_log2;
+      if constexpr (LIFT) mc = fmaxf(st.m[c] + up[c], mc + (st.lifted[c] ? kLift : -kHeadroom));
+      else mc = fmaxf(st.m[c], mc - kHeadroom);
       const float alpha = fast_exp2(st.m[c] - mc);
       st.m[c] = mc;
       st.l[c] *= alpha;
@@ -351,13 +384,6 @@ __device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_
     form_weights<T, D, NB>(st, s, scale_log2, x);
   }
   add_weights(st, x);
-}
-
-// The same from the scores on.
-template <typename T, int D, int NB>
-__device__ __forceinline__ void fold_softmax(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, float (&x)[NB][8]) {
-  const bool big = form_weights<T, D, NB>(st, s, scale_log2, x);
-  settle_weights<T, D, NB>(st, s, scale_log2, big, x);
 }
 
 // V of keys past all_last, which no column sees: their weights are 0, but an unused
@@ -386,6 +412,38 @@ __device__ __forceinline__ bool beyond_fp16(const Unit<D>& u) {
 #pragma unroll
     for (int w = 0; w < kWords<D>; ++w) off |= u.vs[p][w] - 0x68686868u;
   return (off & 0xe0e0e0e0u) != 0;
+}
+
+// Whether the unit has a V of 2^64 or more (scale bytes from kLargeScale on, that of NaN
+// among them: bits 7 and 6), as this lane sees it.
+template <int D>
+__device__ __forceinline__ bool has_large(const Unit<D>& u) {
+  static_assert(kLargeScale == 0xc0);
+  uint32_t both = 0;
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int w = 0; w < kWords<D>; ++w) both |= u.vs[p][w] & (u.vs[p][w] << 1);
+  return (both & 0x80808080u) != 0;
+}
+
+// The first of keys key0 .. key0 + 31 with such a V (those that no column sees are
+// cleared), INT32_MAX: none.  (All lanes active; the same in all.)
+template <int D>
+__device__ __forceinline__ int first_large(const Unit<D>& u, int key0, int lane) {
+  int first = INT32_MAX;
+  if (__builtin_amdgcn_ballot_w64(has_large(u)) != 0) {
+#pragma unroll
+    for (int p = 1; p >= 0; --p)
+#pragma unroll
+      for (int i = 3; i >= 0; --i) {
+        const uint32_t w = D == 128 ? u.vs[p][i] : u.vs[p][i >> 1] >> (16 * (i & 1)) & 0xffffu;
+        if ((w & w << 1 & 0x80808080u) != 0) first = key0 + 16 * p + 4 * (lane >> 4) + i;
+      }
+    first = min(first, __shfl_xor(first, 16));
+    first = min(first, __shfl_xor(first, 32));
+  }
+  return __builtin_amdgcn_readfirstlane(first);
 }
 
 // O^T += V^T . P^T, in fp16 or in bf16 parts.
@@ -432,12 +490,10 @@ __device__ __forceinline__ void fold_pv(State<T, D, NB>& st, const Unit<D>& u, c
 // The same (in bf16) for a unit of which some columns see a part: a NaN block of
 // V reaches the columns that see its key, and no other (a weight of 0 times NaN
 // would be NaN; its codes are 0 already).  Its scale becomes 1, and the columns that see the first such key
-// of a block get NaN outright.
+// of a block get NaN outright.  (Keys that no column sees are cleared.)
 template <typename T, int D, int NB>
-__device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, const float (&x)[NB][8], int key0,
-                                             int all_last, int lane) {
+__device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, const float (&x)[NB][8], int key0, int lane) {
   constexpr int n = D / 32;
-  clear_dead(u, key0, all_last, lane);
   int nan_key[n];
   bool any = false;
 #pragma unroll
