@@ -90,7 +90,7 @@ int pa_workspace_size_q4(const pa_dims_t *dims, size_t *bytes);
  * formed from the values that the cache stands for, without rounding those, on the
  * matrix cores with fp32 accumulation; softmax bases and sums are fp32.  Queries:
  * bf16 ones as they are, except at head_dim 128, where a query is two e4m3 parts of
- * its row's scale (an error of at most 2^-22 of the row's largest); fp32 ones as
+ * its row's scale (an error of at most 2^-22 of the row's largest, or 2^-135); fp32 ones as
  * sums of three bf16 parts.  Softmax weights: for bf16 outputs in fp16 where every V
  * of the step is exact in fp16 (scales 2^-23 .. 2^8) and as two bf16 parts elsewhere,
  * for fp32 outputs as three bf16 parts.  Weighted sums do not overflow: an output is

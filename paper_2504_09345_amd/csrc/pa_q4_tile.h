@@ -163,15 +163,22 @@ struct Query<T, D, true> {
 };
 
 // x as a sum of N bf16 parts, each the rest of those before it to nearest even;
-// part i of the eight values as one operand.
-template <int N>
+// part i of the eight values as one operand.  CUT: the first part is x's upper half
+// instead, which the largest x does not round up out of range (three parts carry the 24
+// bits of an fp32 either way).
+template <int N, bool CUT = false>
 __device__ __forceinline__ void split8(const float (&x)[8], u32x4 (&part)[N]) {
   typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
 #pragma unroll
   for (int h = 0; h < 4; ++h) {
     f32x2_t r = f32x2_t{x[2 * h], x[2 * h + 1]};
+    if constexpr (CUT) {
+      const uint32_t a = __float_as_uint(r[0]) & 0xffff0000u, b = __float_as_uint(r[1]) & 0xffff0000u;
+      r -= f32x2_t{__uint_as_float(a), __uint_as_float(b)};
+      part[0][h] = a >> 16 | b;
+    }
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = CUT ? 1 : 0; i < N; ++i) {
       const bf16x2v_t b = __builtin_convertvector(r, bf16x2v_t);
       if (i + 1 < N) r -= __builtin_convertvector(b, f32x2_t);
       part[i][h] = __builtin_bit_cast(uint32_t, b);
@@ -223,9 +230,11 @@ __device__ __forceinline__ void load_query(Query<T, D>& q, const T* row, int lan
     for (int i = 0; i < 16; ++i) m2 = __builtin_elementwise_max(m2, __builtin_bit_cast(u16x2_t, f[i] & 0x7fff7fffu));
     const uint32_t most = __float_as_uint(rows4_max(__uint_as_float((uint32_t)max(m2[0], m2[1]) << 16)));
     const bool odd = rows4_max((uint32_t)max(m2[0], m2[1]) >= 0x7f80u ? 1.0f : 0.0f) != 0.0f;
-    // 2^E: the largest over it lies in [128, 256)
-    const int byte = min(max((int)(most >> 23) - 7, 6), 250);
-    const float sc = __uint_as_float((uint32_t)byte << 23), sc_lo = __uint_as_float((uint32_t)(byte - 5) << 23);
+    // 2^E: the largest over it lies in [128, 256).  The first part may be 256, which at
+    // the largest E is 2^128: what it leaves is formed of halves.
+    const int byte = min(max((int)(most >> 23) - 7, 7), 250);
+    const float sc = __uint_as_float((uint32_t)byte << 23), sc_half = __uint_as_float((uint32_t)(byte - 1) << 23);
+    const float sc_lo_half = __uint_as_float((uint32_t)(byte - 6) << 23);
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
       typedef short s16x2_t __attribute__((ext_vector_type(2)));
@@ -233,9 +242,9 @@ __device__ __forceinline__ void load_query(Query<T, D>& q, const T* row, int lan
       hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2_t, f[2 * w]), sc, false);
       hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2_t, f[2 * w + 1]), sc, true);
       const uint32_t hw = __builtin_bit_cast(uint32_t, hi);
-      const f32x2_t ab = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hw, sc, false), cd = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hw, sc, true);
-      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, bf16_lo(f[2 * w]) - ab[0], bf16_hi(f[2 * w]) - ab[1], sc_lo, false);
-      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, bf16_lo(f[2 * w + 1]) - cd[0], bf16_hi(f[2 * w + 1]) - cd[1], sc_lo, true);
+      const f32x2_t ab = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hw, sc_half, false), cd = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hw, sc_half, true);
+      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, fmaf(bf16_lo(f[2 * w]), 0.5f, -ab[0]), fmaf(bf16_hi(f[2 * w]), 0.5f, -ab[1]), sc_lo_half, false);
+      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, fmaf(bf16_lo(f[2 * w + 1]), 0.5f, -cd[0]), fmaf(bf16_hi(f[2 * w + 1]), 0.5f, -cd[1]), sc_lo_half, true);
       q.x[0][w] = odd ? 0 : (int)hw;
       q.x[1][w] = odd ? 0 : __builtin_bit_cast(int, lo);
     }
@@ -251,7 +260,7 @@ __device__ __forceinline__ void load_query(Query<T, D>& q, const T* row, int lan
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = row != nullptr ? row[G * (D / 4) + 8 * s + e] : 0.0f;
-        split8(x, q.x[s]);
+        split8<kQParts<T>, true>(x, q.x[s]);
       }
     }
   }

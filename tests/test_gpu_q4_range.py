@@ -1,5 +1,5 @@
 """The 4-bit cache's attention over the whole range of its values: V up to the largest
-that a block holds, and every code with every scale byte."""
+that a block holds, queries up to the largest, and every code with every scale byte."""
 import numpy as np
 import pytest
 import torch
@@ -88,6 +88,24 @@ def test_large_values_leave_other_rows_alone(dtype):
     off = np.abs(out[:30].double().numpy() - ref[0])
     tight = bound(*ref, 60, dtype, 64) - 1e-37 + 2.0 ** -133  # (bf16's last step)
     assert (off <= tight).all()
+
+
+# --- scores --------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_queries_up_to_the_largest(kind, dtype, D):
+    """The largest finite queries, on keys small enough that the scores are usual ones."""
+    announce(f"q4 {kind} {dtype} D={D}, queries up to the largest")
+    b = Batch(_lens(kind, [50, 90, 17]), 8, 2, D, dtype, seed=3, varlen=kind != "decode")
+    at = _scales(D)
+    b.k[:, :, at] = np.clip(b.k[:, :, at].astype(int) - 127 + 2, 2, 8)
+    top = float(np.finfo(np.float32).max) if dtype == "fp32" else float(np.uint32(0x7F7F0000).view(np.float32))
+    b.q[:] = b.round(np.clip(b.q, -1, 1) * 1e37)
+    b.q[:, 1, 7], b.q[:, 2, 40], b.q[:, 6, 0] = top, -top, top
+    b.scale = 0.02
+    check(_attend(b, kind), b.expected_gpu(), 90, dtype)
 
 
 # --- every code and scale byte ---------------------------------------------------
