@@ -356,10 +356,16 @@ def _take_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table,
 
 
 def _workspace_q4(dims, workspace, q, stream):
-    """(address, bytes, owner) of the caller's workspace or of a temporary one."""
+    """(address, bytes, owner) of the caller's workspace or of a temporary one.  A
+    tensor of another device than the current one, or not contiguous, is refused."""
     if workspace is None or workspace.__class__ is int:
         ws, size = _workspace(dims, workspace, getattr(q, "device", None), stream, pa_workspace_size_q4)
         return _addr(ws), size, ws
+    import torch
+    if workspace.get_device() != torch.cuda.current_device():
+        raise ValueError(f"a workspace on {workspace.device}, not on the current device")
+    if not workspace.is_contiguous():
+        raise ValueError("a workspace that is not contiguous")
     return workspace.data_ptr() or None, workspace.numel() * workspace.element_size(), workspace
 
 
