@@ -195,9 +195,10 @@ def pa_strerror(code: int) -> str:
 
 def _workspace(dims, workspace, device, stream=None, size_of=pa_workspace_size):
     """The caller's workspace, or a temporary one of pa_workspace_size()
-    bytes (size_of: of another call's size).  A temporary is allocated on torch's current stream; when the call
-    runs on another stream, the allocation is also recorded on that stream, so
-    torch's caching allocator does not hand the memory to other work before
+    bytes (size_of: of another call's size) on the device (None, of arrays given as
+    addresses: the current GPU).  A temporary is allocated on torch's current stream;
+    when the call runs on another stream, the allocation is also recorded on that
+    stream, so torch's caching allocator does not hand the memory to other work before
     the call's kernels have finished with it."""
     need = size_of(dims)
     if workspace is None and need > 0:
@@ -205,7 +206,7 @@ def _workspace(dims, workspace, device, stream=None, size_of=pa_workspace_size):
         if isinstance(stream, int) and stream:
             # torch cannot track work on a raw stream handle
             raise ValueError("pass a workspace (or a torch stream) when calling on a raw stream handle")
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = torch.empty(need, dtype=torch.uint8, device="cuda" if device is None else device)
         if stream is not None and stream != torch.cuda.current_stream(workspace.device):
             workspace.record_stream(stream)
     size = 0 if workspace is None else (workspace.numel() * workspace.element_size()

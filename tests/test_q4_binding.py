@@ -50,3 +50,18 @@ def test_workspaces_that_are_refused(name, d, device, wide, match, unreached, mo
     with pytest.raises(ValueError, match=match):
         attend(name, d, workspace=torch.zeros(n // wide, dtype=torch.uint8).expand(wide, n // wide) if wide > 1
                else torch.zeros(n, dtype=torch.uint8))
+
+
+@host_only
+@pytest.mark.parametrize("name,d", CALLS)
+def test_temporary_workspaces_are_on_the_gpu(name, d, unreached, monkeypatch):
+    """Also of calls whose arrays are addresses, which have no device."""
+    class Made(Exception):
+        pass
+
+    def empty(*shape, dtype, device):
+        raise Made(device)
+
+    monkeypatch.setattr(torch, "empty", empty)
+    with pytest.raises(Made, match="cuda"):
+        attend(name, d, stream=None)
