@@ -337,6 +337,24 @@ def _take(t, kind, n, device):
     return t.data_ptr() or None
 
 
+def _fit_q4(dims, heads, dense0, dense1, k_pages, v_pages, block_table):
+    """Refuses arrays whose rows are not those that dims say: read with their strides
+    they would be other values.  (Addresses, and arrays of other ranks, are taken by
+    their elements.)"""
+    H_kv, D, width = dims.num_kv_heads, dims.head_dim, dims.max_pages_per_seq
+    tile = _Q4_TILE.get(D)
+    try:  # (the usual call: tensors, and of these shapes)
+        d, k = dense0.shape, k_pages.shape
+        if (d[1] == heads and d[2] == D and dense1.shape == d and k[1] == H_kv and k[2] == tile and v_pages.shape == k
+                and block_table.shape[1] == width):
+            return
+    except (AttributeError, IndexError):
+        pass
+    for t, row in ((dense0, (heads, D)), (dense1, (heads, D)), (k_pages, (H_kv, tile)), (v_pages, (H_kv, tile)), (block_table, (width,))):
+        if not _is_address(t) and t.dim() == len(row) + 1 and tuple(t.shape[1:]) != row:
+            raise ValueError(f"a tensor of shape {tuple(t.shape)} where dims say rows of {row}")
+
+
 def _take_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc):
     """The addresses of a call's arrays, in this order.  Refuses a tensor that is not
     what dims and the format say: of another type or too few elements, not contiguous,
@@ -362,8 +380,12 @@ def _workspace_q4(dims, workspace, q, stream):
     if workspace is None or workspace.__class__ is int:
         ws, size = _workspace(dims, workspace, getattr(q, "device", None), stream, pa_workspace_size_q4)
         return _addr(ws), size, ws
-    import torch
-    if workspace.get_device() != torch.cuda.current_device():
+    if _is_address(q):
+        import torch
+        device = torch.cuda.current_device()
+    else:  # (which is on the current device: _take)
+        device = q.get_device()
+    if workspace.get_device() != device:
         raise ValueError(f"a workspace on {workspace.device}, not on the current device")
     if not workspace.is_contiguous():
         raise ValueError("a workspace that is not contiguous")
@@ -373,6 +395,7 @@ def _workspace_q4(dims, workspace, q, stream):
 def pa_kv_append_q4(k_new, v_new, block_table, context_lens, k_pages, v_pages, dims: PaDims, query_start_loc=None,
                     stream=None, check=True) -> int:
     """int pa_kv_append_q4(...): quantise the new tokens' K/V into the 4-bit pools."""
+    _fit_q4(dims, dims.num_kv_heads, k_new, v_new, k_pages, v_pages, block_table)
     k, v, kp, vp, bt, cl, qsl = _take_q4(dims, dims.num_kv_heads, query_start_loc is not None, k_new, v_new, k_pages,
                                          v_pages, block_table, context_lens, query_start_loc)
     rc = load().pa_kv_append_q4(k, v, bt, cl, qsl, kp, vp, ctypes.byref(dims), _stream(stream))
@@ -385,6 +408,7 @@ def pa_kv_read_q4(k_pages, v_pages, block_table, context_lens, k_out, v_out, dim
                   stream=None, check=True) -> int:
     """int pa_kv_read_q4(...): the values that the 4-bit pools hold of the rows
     which pa_kv_append_q4 with the same arguments writes."""
+    _fit_q4(dims, dims.num_kv_heads, k_out, v_out, k_pages, v_pages, block_table)
     k, v, kp, vp, bt, cl, qsl = _take_q4(dims, dims.num_kv_heads, query_start_loc is not None, k_out, v_out, k_pages,
                                          v_pages, block_table, context_lens, query_start_loc)
     rc = load().pa_kv_read_q4(kp, vp, bt, cl, qsl, k, v, ctypes.byref(dims), _stream(stream))
@@ -397,6 +421,7 @@ def paged_attn_q4(q, k_pages, v_pages, block_table, context_lens, scale, out, di
                   stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_q4(...): decode attention over the 4-bit cache; out is
     written in place."""
+    _fit_q4(dims, dims.num_q_heads, q, out, k_pages, v_pages, block_table)
     qa, oa, kp, vp, bt, cl, _ = _take_q4(dims, dims.num_q_heads, False, q, out, k_pages, v_pages, block_table,
                                          context_lens, None)
     ws, ws_bytes, owner = _workspace_q4(dims, workspace, q, stream)
@@ -411,6 +436,7 @@ def paged_attn_varlen_q4(q, k_pages, v_pages, block_table, context_lens, query_s
                          workspace=None, stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_varlen_q4(...): causal chunks plus decode rows over the
     4-bit cache."""
+    _fit_q4(dims, dims.num_q_heads, q, out, k_pages, v_pages, block_table)
     qa, oa, kp, vp, bt, cl, qsl = _take_q4(dims, dims.num_q_heads, True, q, out, k_pages, v_pages, block_table,
                                            context_lens, query_start_loc)
     ws, ws_bytes, owner = _workspace_q4(dims, workspace, q, stream)

@@ -65,3 +65,66 @@ def test_temporary_workspaces_are_on_the_gpu(name, d, unreached, monkeypatch):
     monkeypatch.setattr(torch, "empty", empty)
     with pytest.raises(Made, match="cuda"):
         attend(name, d, stream=None)
+
+
+def arrays(name, d):
+    """Arrays of the call that dims describe, of meta tensors: shapes without memory."""
+    rows = d.num_q_rows or d.num_seqs
+    heads = d.num_kv_heads if name.startswith("pa_kv") else d.num_q_heads
+    dense = [torch.empty(rows, heads, d.head_dim, dtype=torch.bfloat16, device="meta") for _ in range(2)]
+    pools = [torch.empty(d.num_pages, d.num_kv_heads, 1088, dtype=torch.uint8, device="meta") for _ in range(2)]
+    return dense + pools + [torch.empty(d.num_seqs, d.max_pages_per_seq, dtype=torch.int32, device="meta")]
+
+
+def call(name, d, t):
+    qsl = torch.empty(d.num_seqs + 1, dtype=torch.int32, device="meta") if d.num_q_rows else None
+    x, y, k, v, bt = t
+    cl = torch.empty(d.num_seqs, dtype=torch.int32, device="meta")
+    if name == "pa_kv_append_q4":
+        return pb.pa_kv_append_q4(x, y, bt, cl, k, v, d, query_start_loc=qsl, stream=S)
+    if name == "pa_kv_read_q4":
+        return pb.pa_kv_read_q4(k, v, bt, cl, x, y, d, query_start_loc=qsl, stream=S)
+    if name == "paged_attn_q4":
+        return pb.paged_attn_q4(x, k, v, bt, cl, 0.1, y, d, workspace=P, stream=S)
+    return pb.paged_attn_varlen_q4(x, k, v, bt, cl, qsl, 0.1, y, d, workspace=P, stream=S)
+
+
+class Reached(Exception):
+    pass
+
+
+@host_only
+@pytest.mark.parametrize("name", ["pa_kv_append_q4", "pa_kv_read_q4", "paged_attn_q4", "paged_attn_varlen_q4"])
+def test_rows_of_other_shapes_are_refused(name, monkeypatch):
+    """Arrays with more heads, dims or pages a sequence than dims say hold enough
+    elements, and would be read with the strides of others."""
+    d = dims(**(VARLEN if name == "paged_attn_varlen_q4" else {}))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    monkeypatch.setattr(torch.Tensor, "data_ptr", lambda t: P)
+
+    class Lib:
+        def __getattr__(self, what):
+            def entry(*a):
+                raise Reached
+            return entry
+
+    n = pb.pa_workspace_size_q4(d)
+    monkeypatch.setattr(pb, "pa_workspace_size_q4", lambda dims: n)
+    monkeypatch.setattr(pb, "load", lambda: Lib())
+    good = arrays(name, d)
+    with pytest.raises(Reached):
+        call(name, d, good)
+    flat = list(good)
+    flat[0] = good[0].reshape(-1)  # (an array of another rank is taken by its elements)
+    with pytest.raises(Reached):
+        call(name, d, flat)
+    for i, t in enumerate(good):
+        wider = [(t.shape[0], 2 * t.shape[1], *t.shape[2:])]
+        if i < 2:
+            wider.append((t.shape[0], t.shape[1], 2 * t.shape[2]))
+            wider.append((2 * t.shape[0], t.shape[1], t.shape[2] // 2))
+        for shape in wider:
+            bad = list(good)
+            bad[i] = torch.empty(shape, dtype=t.dtype, device="meta")
+            with pytest.raises(ValueError, match="rows of"):
+                call(name, d, bad)
