@@ -88,6 +88,13 @@ constexpr int kPartWaves = 3072;
 // chunk of 64 rows on 1,500 tokens 17 us instead of 14; 8 or 16 are one as good as the
 // other.  Twice the waves: one chunk of 700 rows 31 us instead of 19.)
 constexpr int kWavesWanted = 2048, kLeastUnits = 8, kMaxSplit = 64;
+// Bytes of all parts' records, which the host can only reckon for every row of the call:
+// it does not know which are of chunks, nor does the grid.  With bounds of 32, 64, 128 and
+// 4,096 MiB, 32 query heads over 8: two rows on 65,536 tokens beside 512 decode rows of
+// 500 tokens 169, 128, 197 and 624 us, beside 256 87, 109, 180 and 329; on 131,072 beside
+// 1,023 of 300 708, 346, 298 and 1,200, beside 4,096 of 100 805, 804, 805 and 4,455; 16
+// rows on 32,768 beside 512 of 500 118, 135, 179 and 180.
+constexpr int64_t kRecordBytes = 64 << 20;
 // Which kernel takes a call's chunks (bf16): waves of 16 columns, each alone, or
 // workgroups of 128 columns that share V's operands.  The latter spend a third less
 // per column and unit, but need the columns (a chunk of at most 32 leaves three of
@@ -152,6 +159,8 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
     int64_t split = kWavesWanted / (items * waves);
     if (split > units / (kLeastUnits * p->wave_parts)) split = units / (kLeastUnits * p->wave_parts);
     if (split > kMaxSplit) split = kMaxSplit;
+    const int64_t record = (int64_t)p->rows * d->num_q_heads * (d->head_dim + 2) * (int64_t)sizeof(float);  // of one part
+    if (split > kRecordBytes / record) split = kRecordBytes / record;
     if (split < 1) split = 1;
     p->split_units = (int)((units + split - 1) / split);
     p->n_split = (int)((units + p->split_units - 1) / p->split_units);

@@ -128,3 +128,16 @@ def test_rows_of_other_shapes_are_refused(name, monkeypatch):
             bad[i] = torch.empty(shape, dtype=t.dtype, device="meta")
             with pytest.raises(ValueError, match="rows of"):
                 call(name, d, bad)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [pb.PA_BF16, pb.PA_FP32])
+@pytest.mark.parametrize("seqs", [2, 33, 257, 513, 1024, 4096, 100000])
+@pytest.mark.parametrize("ctx", [1000, 32768, 65536, 131072, 1 << 20])
+def test_workspaces_of_chunks_beside_decode_rows(D, dtype, seqs, ctx):
+    """One chunk of two rows (or 60) among decode rows: records of parts take 64 MiB at
+    most, whatever the other rows are."""
+    for most in (2, 60):
+        n = pb.pa_workspace_size_q4(dims(num_seqs=seqs, num_q_rows=seqs - 1 + most, max_q_len=most, max_context_len=ctx,
+                                         max_pages_per_seq=1 << 16, head_dim=D, dtype=dtype))
+        assert 0 < n <= (64 << 20) + 512, (n, most)
