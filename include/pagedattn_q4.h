@@ -39,7 +39,9 @@
  * max_pages_per_seq and max_context_len describe the cache as in pagedattn.h;
  * dtype (PA_BF16 or PA_FP32) is the type of the dense arrays: k_new, v_new,
  * k_out, v_out, q and out.  pages_per_split must be 0.  Arrays that a call writes
- * overlap none that it reads.
+ * overlap none that it reads.  Calls of more work than a launch can have threads
+ * (appends and reads from 2^26 single rows or 2^28 rows of chunks on) are refused:
+ * PA_ENOTSUP.
  */
 #ifndef PAGEDATTN_Q4_H
 #define PAGEDATTN_Q4_H

@@ -11,6 +11,9 @@ namespace pa {
 
 constexpr int q4_tile_bytes(int D) { return 8 * D + D / 2; }
 
+// HIP launches fewer than 2^32 threads in a dimension.
+constexpr int64_t kQ4MaxThreads = ((int64_t)1 << 32) - 1;
+
 // The cache write and its mirror, the read.
 struct Q4RowsArgs {
   const void* k_rows;  // [rows][H_kv][D]; written by the read
@@ -23,6 +26,10 @@ struct Q4RowsArgs {
   int64_t bt_stride;
   int B, rows, H_kv, num_pages, max_context_len;
 };
+constexpr int kQ4RowsWaves = 4;  // waves of a workgroup, each with the rows of a slot
+constexpr int kQ4RowsGroup = 4;  // tokens of a slot, whose V bytes are a word
+// Slots of a call.
+constexpr int64_t q4_row_slots(bool varlen, int64_t rows, int64_t seqs) { return varlen ? rows / kQ4RowsGroup + 2 * seqs : rows; }
 hipError_t launch_q4_append(int dtype, int D, const Q4RowsArgs& a, hipStream_t st);
 hipError_t launch_q4_read(int dtype, int D, const Q4RowsArgs& a, hipStream_t st);
 

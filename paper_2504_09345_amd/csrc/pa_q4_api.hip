@@ -42,7 +42,9 @@ int rows_call(const void* k_rows, const void* v_rows, const int32_t* block_table
     rows = d->num_seqs;
   }
   if (rows == 0) return PA_OK;
-  if ((int64_t)rows + 2 * (int64_t)d->num_seqs > INT32_MAX) return PA_ENOTSUP;  // (32-bit slots)
+  if ((int64_t)rows + 2 * (int64_t)d->num_seqs > INT32_MAX) return PA_ENOTSUP;  // (32-bit rows and slots)
+  if ((pa::q4_row_slots(query_start_loc != nullptr, rows, d->num_seqs) / pa::kQ4RowsWaves + 1) * 64 * pa::kQ4RowsWaves > pa::kQ4MaxThreads)
+    return PA_ENOTSUP;
   if (!k_rows || !v_rows || !block_table || !context_lens || !k_pages || !v_pages) return PA_EINVAL;
   if (misaligned(k_rows) || misaligned(v_rows) || misaligned(k_pages) || misaligned(v_pages)) return PA_EINVAL;
   pa::Q4RowsArgs a;
@@ -164,7 +166,8 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
     if (split < 1) split = 1;
     p->split_units = (int)((units + split - 1) / split);
     p->n_split = (int)((units + p->split_units - 1) / p->split_units);
-    if ((slots + pa::kQ4Waves) * d->num_kv_heads * p->n_split > INT32_MAX) return PA_ENOTSUP;
+    const int64_t groups = (slots / (p->shared ? 1 : pa::kQ4Waves / p->wave_parts) + 1) * d->num_kv_heads * p->n_split;
+    if (groups * 64 * pa::kQ4Waves > pa::kQ4MaxThreads) return PA_ENOTSUP;
     p->n_slots = (int)slots;
     if (p->n_split > 1) {
       const size_t recs = (size_t)p->rows * d->num_q_heads * p->n_split;

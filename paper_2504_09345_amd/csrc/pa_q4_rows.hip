@@ -13,8 +13,8 @@ namespace pa {
 
 namespace {
 
-constexpr int kRowsWaves = 4;
-constexpr int kGroup = 4;  // tokens whose V bytes are a word
+constexpr int kRowsWaves = kQ4RowsWaves;
+constexpr int kGroup = kQ4RowsGroup;
 
 // A wave's rows: those of one sequence that lie in four slots of a page from a multiple
 // of four on (a decode call's: one).
@@ -256,8 +256,8 @@ hipError_t by_type(int dtype, int D, const Q4RowsArgs& a, Fn fn) {
 // 218 with a copy of them after; 66 MB in fp32 13 and 14, but 39 and 35 with the copy.)
 constexpr int64_t kCached = 256 << 20;
 
-// Slots of a call (group_of).
-int slots_of(const Q4RowsArgs& a) { return a.query_start_loc != nullptr ? a.rows / kGroup + 2 * a.B : a.rows; }
+// Slots of a call (group_of; checked to be 32-bit).
+int slots_of(const Q4RowsArgs& a) { return (int)q4_row_slots(a.query_start_loc != nullptr, a.rows, a.B); }
 
 }  // namespace
 

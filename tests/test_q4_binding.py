@@ -1,6 +1,8 @@
 """What the binding of the 4-bit cache takes and refuses, on the host.  Refused calls
 enqueue nothing; they use placeholder addresses and therefore run only where no GPU is
 visible."""
+import ctypes
+
 import pytest
 import torch
 
@@ -141,3 +143,21 @@ def test_workspaces_of_chunks_beside_decode_rows(D, dtype, seqs, ctx):
         n = pb.pa_workspace_size_q4(dims(num_seqs=seqs, num_q_rows=seqs - 1 + most, max_q_len=most, max_context_len=ctx,
                                          max_pages_per_seq=1 << 16, head_dim=D, dtype=dtype))
         assert 0 < n <= (64 << 20) + 512, (n, most)
+
+
+@host_only
+@pytest.mark.parametrize("name", ["pa_kv_append_q4", "pa_kv_read_q4"])
+def test_more_rows_than_a_launch_has_threads(name):
+    """A wave of 64 threads a row, or four rows of a sequence, and fewer than 2^32 in all."""
+    for kw, qsl in ((dict(num_seqs=1 << 26), None), (dict(num_seqs=3, num_q_rows=1 << 28), P), (dict(num_seqs=1 << 25, num_q_rows=1 << 25), P)):
+        assert getattr(pb, name)(P, P, P, P, P, P, dims(**kw), query_start_loc=qsl, stream=S, check=False) == pb.PA_ENOTSUP, kw
+
+
+@host_only
+@pytest.mark.parametrize("dtype", [pb.PA_BF16, pb.PA_FP32])
+def test_more_chunk_rows_than_a_launch_has_threads(dtype):
+    """(Contexts of 16 tokens; one head, whose 16 rows are a wave's.)"""
+    for rows, fits in ((1 << 28, True), (1 << 29, False)):
+        d = dims(num_seqs=rows // 16, num_q_rows=rows, max_q_len=16, num_q_heads=1, num_kv_heads=1, max_context_len=16, dtype=dtype)
+        n = ctypes.c_size_t()
+        assert pb.load().pa_workspace_size_q4(ctypes.byref(d), ctypes.byref(n)) == (pb.PA_OK if fits else pb.PA_ENOTSUP)
