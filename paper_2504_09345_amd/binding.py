@@ -152,8 +152,12 @@ def _addr(x):
 def _stream(stream):
     if stream is None:
         import torch
-        # (the current stream's handle without a Stream object around it, which takes 3 us)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
+        # The current stream's handle without a Stream object around it, which takes 3 us,
+        # where torch has this function (it is not among its documented ones).
+        handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if handle is None:
+            return torch.cuda.current_stream().cuda_stream or None
+        return handle(torch.cuda.current_device()) or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None

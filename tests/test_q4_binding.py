@@ -161,3 +161,19 @@ def test_more_chunk_rows_than_a_launch_has_threads(dtype):
         d = dims(num_seqs=rows // 16, num_q_rows=rows, max_q_len=16, num_q_heads=1, num_kv_heads=1, max_context_len=16, dtype=dtype)
         n = ctypes.c_size_t()
         assert pb.load().pa_workspace_size_q4(ctypes.byref(d), ctypes.byref(n)) == (pb.PA_OK if fits else pb.PA_ENOTSUP)
+
+
+@pytest.mark.parametrize("has", [True, False])
+def test_current_stream(has, monkeypatch):
+    """The current stream's handle, also from a torch without the shorter way to it."""
+    class Stream:
+        cuda_stream = 0x50
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: Stream)
+    if has:
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0x40 + device, raising=False)
+    else:
+        monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    assert pb._stream(None) == (0x43 if has else 0x50)
+    assert pb._stream(0) is None and pb._stream(7) == 7 and pb._stream(Stream) == 0x50
