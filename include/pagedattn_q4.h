@@ -90,7 +90,9 @@ int pa_workspace_size_q4(const pa_dims_t *dims, size_t *bytes);
 
 /* Decode attention over the 4-bit cache: paged_attn with 4-bit pools.  Products are
  * formed from the values that the cache stands for, without rounding those, on the
- * matrix cores with fp32 accumulation; softmax bases and sums are fp32.  Queries:
+ * matrix cores with fp32 accumulation; softmax bases and sums are fp32, and so are the
+ * scores: scale q.k log2 e may be up to 2^27 in magnitude (its steps there are 8; beyond,
+ * an output may be NaN).  Queries:
  * bf16 ones as they are, except at head_dim 128, where a query is two e4m3 parts of
  * its row's scale (an error of at most 2^-22 of the row's largest, or 2^-135); fp32 ones as
  * sums of three bf16 parts.  Softmax weights: for bf16 outputs in fp16 where every V

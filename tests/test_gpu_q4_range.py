@@ -1,10 +1,12 @@
 """The 4-bit cache's attention over the whole range of its values: V up to the largest
-that a block holds, queries up to the largest, and every code with every scale byte."""
+that a block holds, scores up to 2^27 in log2 units, queries up to the largest and ones
+that are not finite, and every code with every scale byte."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import q4
+from paper_2504_09345_amd import binding as pb
 from q4_util import Batch, bound, check
 
 from parity_util import announce
@@ -95,6 +97,35 @@ def test_large_values_leave_other_rows_alone(dtype):
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_largest_scores(kind, dtype, D, sign):
+    """Keys that all score the same, up to 2^27 in log2 units, weigh alike."""
+    announce(f"q4 {kind} {dtype} D={D}, scores of {sign} 2^27")
+    ctx = [1, 40, 700]
+    b = Batch(_lens(kind, ctx), 8, 2, D, dtype, seed=2, varlen=kind != "decode")
+    b.k[..., :8 * D] = 0x77
+    b.k[..., 8 * D:] = 127 + 23
+    b.q[:] = 0
+    for h in range(8):
+        b.q[:, h, 5] = sign * 1.75 * 2.0 ** -h
+    b.scale = 1.0
+    assert 2.0 ** 26 < 6 * 2.0 ** 23 * 1.75 / np.log(2) < 2.0 ** 27
+    got = _attend(b, kind).double().numpy()
+    for i, C in enumerate(ctx):
+        v = q4.dense("v", b.v, b.bt, i, C, D)
+        r0, L = (i, 1) if kind == "decode" else (int(b.qsl[i]), b.n_rows[i])
+        for r in range(L):
+            n = C - L + r + 1
+            for h in range(8):
+                x = v[h // 4, :n]
+                # (equal weights: the output's rounding, and of the sums)
+                tol = (2.0 ** -8 * (dtype == "bf16") + 2 * n * 2.0 ** -24 + 2.0 ** -22) * np.abs(x).mean(0)
+                assert (np.abs(got[r0 + r, h] - x.mean(0)) <= tol).all(), (C, r, h)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
 def test_queries_up_to_the_largest(kind, dtype, D):
     """The largest finite queries, on keys small enough that the scores are usual ones."""
     announce(f"q4 {kind} {dtype} D={D}, queries up to the largest")
@@ -108,9 +139,81 @@ def test_queries_up_to_the_largest(kind, dtype, D):
     check(_attend(b, kind), b.expected_gpu(), 90, dtype)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+def test_queries_that_are_not_finite(kind, dtype, D, value):
+    """Such a (row, head) is NaN, and the others of its columns keep their values."""
+    announce(f"q4 {kind} {dtype} D={D}, a query of {value}")
+    b = Batch(_lens(kind, [50, 90, 7]), 8, 2, D, dtype, seed=5, varlen=kind != "decode")
+    for r, h, d in ((1, 2, 5), (1, 4, D - 1), (2, 0, 33)):
+        b.q[r, h, d] = value
+    ref = b.expected_gpu()
+    for r, h in ((1, 2), (1, 4), (2, 0)):  # (an infinity times a code of zero, or infinities less each other)
+        for x in ref:
+            x[r, h] = np.nan
+    assert np.isfinite(ref[0][0]).all() and np.isfinite(ref[0][1, [0, 1, 3, 5, 6, 7]]).all()
+    check(_attend(b, kind), ref, 90, dtype)
+
+
 # --- every code and scale byte ---------------------------------------------------
 
 CODES = np.concatenate([q4.MAGS, -q4.MAGS])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scores_of_every_code_and_scale(kind, dtype, D):
+    """16 keys hold the 16 codes, in another order in each dim, and a query of 1 in one
+    dim alone makes them scores; each key's V is 1 in a dim of its own, so the outputs
+    are the softmax of the codes' values."""
+    announce(f"q4 {kind} {dtype} D={D}, scores of every code and scale byte")
+    H_q = 8
+    rows, extra = (1, 0) if kind == "decode" else (5, 4)  # a chunk's first row sees the 16 keys
+    pages = 1 if kind == "decode" else 2
+    k, v = (np.zeros((pages, 1, q4.tile_bytes(D)), np.uint8) for _ in range(2))
+    v[..., 8 * D:] = 127
+    for t in range(16):
+        codes = (t + np.arange(D)) % 16
+        for m in range(D // 2):
+            k[0, 0, q4.byte_of("k", D, t, m)] = codes[2 * m] | codes[2 * m + 1] << 4
+        v[0, 0, q4.byte_of("v", D, t, t // 2)] |= 2 << 4 * (t % 2)
+    kind_t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    q = torch.zeros(D, rows, H_q, D, dtype=kind_t, device="cuda")
+    q[torch.arange(D), :, :, torch.arange(D)] = 1
+    q = q.view(D * rows, H_q, D)
+    far = FAR if kind == "shared" else 32
+    bt = torch.full((D, far // 16), -1, dtype=torch.int32, device="cuda")
+    bt[:, :pages] = torch.arange(pages, device="cuda")
+    cl = torch.full((D,), 16 + extra, dtype=torch.int32, device="cuda")
+    qsl = torch.arange(D + 1, dtype=torch.int32, device="cuda") * rows
+    dk, dv, out = torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda(), torch.empty_like(q)
+    ws = None
+    if kind == "decode":
+        dims = pb.make_dims_q4(q, dk, bt, far)
+    else:
+        dims = pb.make_dims_q4(q, dk, bt, far, num_q_rows=D * rows, max_q_len=rows)
+    ws = torch.empty(max(1, pb.pa_workspace_size_q4(dims)), dtype=torch.uint8, device="cuda")
+    got = []
+    for byte in range(2, 253):
+        dk[..., 8 * D:] = byte
+        scale = 2.0 ** (127 - byte)
+        if kind == "decode":
+            pb.paged_attn_q4(q, dk, dv, bt, cl, scale, out, dims, workspace=ws)
+        else:
+            pb.paged_attn_varlen_q4(q, dk, dv, bt, cl, qsl, scale, out, dims, workspace=ws)
+        got.append(out.view(D, rows, H_q, D)[:, 0].float().cpu().numpy())
+    x = CODES[(np.arange(16)[None, :] + np.arange(D)[:, None]) % 16]
+    w = np.exp(x)
+    ref = np.zeros((D, H_q, D))
+    ref[..., :16] = (w / w.sum(-1, keepdims=True))[:, None]
+    mass = (ref > 0).astype(np.float64)
+    size, reach = np.full((D, H_q), 6.0), np.full((D, H_q), float(np.abs(CODES).mean() * D))
+    most = bound(ref, ref, mass, size, reach, 16, dtype, D)
+    for byte, g in zip(range(2, 253), got):
+        assert (np.abs(g - ref) <= most).all(), byte
 
 
 @pytest.mark.parametrize("kind", KINDS)
