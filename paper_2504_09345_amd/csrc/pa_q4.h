@@ -56,7 +56,7 @@ struct Q4AttnArgs {
   int n_split, split_units;
   int wave_parts;  // waves (1, 2 or 4) that share an item's units, where a wave has 16 columns
 };
-constexpr int kQ4Waves = 4;  // waves of a workgroup, each with an item of its own
+constexpr int kQ4Waves = 4;  // waves of a workgroup: each has an item of its own, 2 or 4 share one, or all share V
 
 // Query rows of an item of so many column blocks (of 16).
 constexpr int q4_positions(int blocks, int s) { return 16 * blocks / s; }
@@ -93,10 +93,10 @@ constexpr int kQ4StreamGroups = 512;   // workgroups of a launch
 constexpr int kQ4StreamThreads = 512;  // of a workgroup
 // Units per wave below which a CU's second workgroup stays without a range (head_dim 64,
 // where two fit).  One and two, 32 query heads over 8 in bf16: 64 sequences of 512-2,048
-// tokens (5 units a wave of both) 17.2 us and 18.4, 4 of 8,192-32,768 (5) 19.6 and 21.0,
-// 128 of 512-2,048 (10) 25.3 and 24.7, 256 (20) 43.8 and 41.2, 512 of 1,024-4,096 (80)
-// 158 and 148; in fp32, 64 heads over 8: 64 of 256-2,048 (4) 22.3 and 23.4, 128 of
-// 512-2,048 (10) 31.6 and 31.9, 256 (20) 52.0 and 50.5.
+// tokens (5 units a wave of both) 18.8 us and 19.0, 4 of 8,192-32,768 (5) 17.3 and 19.8,
+// 128 of 512-2,048 (10) 28.5 and 27.1, 256 (20) 48.8 and 47.6, 512 of 1,024-4,096 (80)
+// 157 and 149; in fp32, 64 heads over 8: 64 of 256-2,048 (4) 23.4 and 24.6, 128 of
+// 512-2,048 (10) 38.0 and 38.0, 256 (20) 61.4 and 62.6.
 constexpr int kQ4FewUnits = 8;
 // A workgroup takes an item whole, where there are no more items than CUs, if the longest
 // has at most so many units more than a workgroup's equal share: a wave's 3.5

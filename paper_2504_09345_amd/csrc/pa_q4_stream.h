@@ -133,7 +133,7 @@ __device__ __forceinline__ void q4_join(const Q4StreamArgs& a, int x0, int xs, i
 }
 
 template <typename T, int D, int S>
-__global__ __launch_bounds__(kQ4StreamThreads) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(kQ4StreamThreads) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2)))  // (two workgroups a CU at head_dim 64)
 void q4_stream_kernel(Q4StreamArgs a) {
   using Rec = Q4Record<D, S>;
   constexpr int NT = kQ4StreamThreads, kWaves = NT / 64;
