@@ -102,11 +102,16 @@ constexpr int64_t kRecordBytes = 64 << 20;
 // per column and unit, but need the columns (a chunk of at most 32 leaves three of
 // four waves without) and enough work: a wave alone is through its units sooner, and
 // there are more of them.  The line is 48 units for each of 2,048 waves, by the
-// longest context that the call declares.  Alone and together, 32 query heads over 8:
+// longest context that the call declares, which is all that the host knows of the
+// chunks' own: a bound far above those takes the wrong kernel (below).  Alone and together, 32 query heads over 8:
 // one chunk of 700 rows 17 and 32 us, of 1,400 37 and 46, of 2,000 57 and 62, of 2,800
 // 98 and 90, of 4,000 171 and 145; 8 of 205-256 rows on 500 tokens 53 and 57; 8 of
 // 320-400 on 300 67 and 66; 4 of 240-300 on 1,000 59 and 56; 4 of 48-60 on 3,000 34 and
-// 54; 2 of 102-128 on 20,000 153 and 123; 16 of 8 rows on 2,000 24 and 45.
+// 54; 2 of 102-128 on 20,000 153 and 123; 16 of 8 rows on 2,000 24 and 45.  Declared as
+// they are and as 4,096, 32,768 and 131,072: one of 16 rows on 200 8.4, 11.0, 11.2 and
+// 20.6; one of 700 19.0 and 40.7 with any of them; 4 of 64 on 300 10.7, 10.7, 23.5 and
+// 23.6; 16 of 8 on 2,000 17.5 with all; and one of 700 beside a decode row of 32,768
+// tokens 62, where the two alone take 19 and 18.
 constexpr int64_t kAloneUnits = 48 * 2048;
 constexpr int kAloneColumns = 32;
 // Units of a launch of the stream kernel, at most (its counts are 32-bit).

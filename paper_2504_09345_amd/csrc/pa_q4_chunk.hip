@@ -3,9 +3,9 @@
 // As pa_q4_attn.hip, with V's operands shared: the four waves of a workgroup hold
 // 128 columns (query row, head of the group) of one sequence and KV head, 32 each,
 // and step through the units together.  Turning a unit's V codes into fp16 operands
-// takes 96 vector instructions, more than the softmax and the rest of a wave's unit
-// together (75), so each wave converts a quarter (one page, half of the blocks) and
-// stages it in LDS, 8 KiB per unit at head_dim 128 and read back as whole operands
+// takes 96 vector instructions, nearly as many as the softmax and the rest of a wave's
+// unit together (some 110), so each wave converts a quarter (one page, half of the
+// blocks) and stages it in LDS, 8 KiB per unit at head_dim 128 and read back as whole operands
 // with no bank conflict; K's codes are operands already (head_dim 128) and every
 // wave loads its own, out of the L1 after the first.  One barrier per unit: unit k is
 // multiplied while unit k + 1 is converted into the other buffer.

@@ -27,9 +27,11 @@
 //    streamed with half of the loads under way.  The waves take turns instead, a unit
 //    each (64 sequences at 64 heads of 64 dims in fp32: 27 us instead of 35).
 //
-// 256 sequences of 512-2,048 tokens (348 MB): the waves stream for 56 us at 6.2 TB/s,
-// where loads of this pattern alone reach 6.4; launch, lengths and entries take 3 us
-// before and the joins of the last ranges 4-8 us after.
+// 256 sequences of 512-2,048 tokens, 361 MB of codes and scales: 69 us.  With longer
+// contexts the time grows with the bytes at 6.4-6.5 TB/s (512 sequences of 512-8,192
+// tokens 2.4 GB in 401 us, of 1,024-16,384 4.9 GB in 780), the rate that loads of this
+// pattern alone reach; the rest, some 13 us here, is launch, lengths and entries (3), the
+// first units' loads and the joins of the last ranges (4-8).
 #include "pa_q4_stream.h"
 
 #include <algorithm>
