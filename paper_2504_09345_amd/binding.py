@@ -347,8 +347,11 @@ def _fit_q4(dims, heads, dense0, dense1, k_pages, v_pages, block_table):
     they would be other values.  (Addresses, and arrays of other ranks, are taken by
     their elements.)"""
     H_kv, D = dims.num_kv_heads, dims.head_dim
-    tiles = (H_kv, _Q4_TILE.get(D))
-    for t, row in ((dense0, (heads, D)), (dense1, (heads, D)), (k_pages, tiles), (v_pages, tiles), (block_table, (dims.max_pages_per_seq,))):
+    if D not in _Q4_TILE:  # (the library's to refuse)
+        return
+    tiles = (H_kv, _Q4_TILE[D])
+    for t, row in ((dense0, (heads, D)), (dense1, (heads, D)), (k_pages, tiles), (v_pages, tiles),
+                   (block_table, (dims.max_pages_per_seq,))):
         if not _is_address(t) and t.dim() == len(row) + 1 and tuple(t.shape[1:]) != row:
             raise ValueError(f"a tensor of shape {tuple(t.shape)} where dims say rows of {row}")
 
@@ -373,8 +376,9 @@ def _take_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table,
 
 
 def _args_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc):
-    """_fit_q4 and _take_q4, and the current device if it was looked up; the usual call, tensors of just the shapes that dims say, in
-    one pass (one by one the checks take 1.3 us more)."""
+    """_take_q4, checked by _fit_q4, and the current device if it was looked up.  The
+    usual call, tensors of just the shapes that dims say, is checked in one pass (one by
+    one the checks take 1.3 us more)."""
     try:
         d, k, w = dense0.shape, k_pages.shape, block_table.shape
         import torch
@@ -396,8 +400,9 @@ def _args_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table,
                     context_lens.data_ptr(), _take(query_start_loc, i32, B + 1, dev), dev)
     except (AttributeError, IndexError):  # (addresses, other ranks)
         pass
+    taken = _take_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc)
     _fit_q4(dims, heads, dense0, dense1, k_pages, v_pages, block_table)
-    return *_take_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc), None
+    return *taken, None
 
 
 def _workspace_q4(dims, workspace, q, stream):

@@ -3,6 +3,7 @@ enqueue nothing; they use placeholder addresses and therefore run only where no 
 visible."""
 import ctypes
 
+import numpy as np
 import pytest
 import torch
 
@@ -130,6 +131,28 @@ def test_rows_of_other_shapes_are_refused(name, monkeypatch):
             bad[i] = torch.empty(shape, dtype=t.dtype, device="meta")
             with pytest.raises(ValueError, match="rows of"):
                 call(name, d, bad)
+
+
+@host_only
+@pytest.mark.parametrize("name", ["pa_kv_append_q4", "pa_kv_read_q4", "paged_attn_q4", "paged_attn_varlen_q4"])
+def test_head_dims_are_the_librarys_to_refuse(name, monkeypatch):
+    d = dims(head_dim=96, **(VARLEN if name == "paged_attn_varlen_q4" else {}))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    with pytest.raises(pb.PagedAttnError, match="not compiled|ENOTSUP|-2"):
+        call(name, d, arrays(name, d))
+
+
+@host_only
+@pytest.mark.parametrize("name", ["pa_kv_append_q4", "paged_attn_q4"])
+def test_arrays_that_are_no_tensors(name, monkeypatch):
+    d = dims()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    good = arrays(name, d)
+    for i in range(len(good)):
+        bad = list(good)
+        bad[i] = np.zeros(1, np.int8)
+        with pytest.raises(TypeError):
+            call(name, d, bad)
 
 
 @pytest.mark.parametrize("D", [64, 128])
