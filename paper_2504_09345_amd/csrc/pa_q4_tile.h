@@ -163,23 +163,21 @@ struct Query<T, D, true> {
 };
 
 // x as a sum of N bf16 parts, each the rest of those before it to nearest even;
-// part i of the eight values as one operand.  CUT: the first part is x's upper half
-// instead, which the largest x does not round up out of range (three parts carry the 24
-// bits of an fp32 either way).
-template <int N, bool CUT = false>
+// part i of the eight values as one operand.  LIMIT: the first part is the
+// largest bf16 where x, from 3.396e38 on, would round up to an infinity (the parts after
+// it carry what is left).
+template <int N, bool LIMIT = false>
 __device__ __forceinline__ void split8(const float (&x)[8], u32x4 (&part)[N]) {
   typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
+  constexpr float kMost = 0x1.fep127f;
 #pragma unroll
   for (int h = 0; h < 4; ++h) {
     f32x2_t r = f32x2_t{x[2 * h], x[2 * h + 1]};
-    if constexpr (CUT) {
-      const uint32_t a = __float_as_uint(r[0]) & 0xffff0000u, b = __float_as_uint(r[1]) & 0xffff0000u;
-      r -= f32x2_t{__uint_as_float(a), __uint_as_float(b)};
-      part[0][h] = a >> 16 | b;
-    }
 #pragma unroll
-    for (int i = CUT ? 1 : 0; i < N; ++i) {
-      const bf16x2v_t b = __builtin_convertvector(r, bf16x2v_t);
+    for (int i = 0; i < N; ++i) {
+      f32x2_t t = r;
+      if (LIMIT && i == 0) t = f32x2_t{__builtin_amdgcn_fmed3f(r[0], -kMost, kMost), __builtin_amdgcn_fmed3f(r[1], -kMost, kMost)};
+      const bf16x2v_t b = __builtin_convertvector(t, bf16x2v_t);
       if (i + 1 < N) r -= __builtin_convertvector(b, f32x2_t);
       part[i][h] = __builtin_bit_cast(uint32_t, b);
     }
