@@ -84,8 +84,9 @@ int pa_kv_read_q4(const void *k_pages, const void *v_pages, const int32_t *block
                   void *v_out, const pa_dims_t *dims, hipStream_t stream);
 
 /* Bytes of device workspace that a paged_attn_q4 / paged_attn_varlen_q4 call with
- * these dims needs.  A call whose dims carry chunked rows (max_q_len > 1 or
- * num_q_rows != num_seqs) is sized as varlen.  Host only; no HIP call. */
+ * these dims needs, 64 MiB and an alignment at most.  A call whose dims carry chunked
+ * rows (max_q_len > 1 or num_q_rows != num_seqs) is sized as varlen.  Host only; no HIP
+ * call. */
 int pa_workspace_size_q4(const pa_dims_t *dims, size_t *bytes);
 
 /* Decode attention over the 4-bit cache: paged_attn with 4-bit pools.  Products are
