@@ -14,7 +14,7 @@
 
 #include "pa_counter.h"
 #include "pa_kernels.h"
-#include "pa_q4.h"
+#include "pa_q.h"
 #include "pa_route.h"
 #include "pa_sched.h"
 #include "pagedattn.h"

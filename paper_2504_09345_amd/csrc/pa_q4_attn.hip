@@ -19,43 +19,27 @@
 //
 // What bounds it is issue: a unit takes some 190 vector instructions (96 of them V's
 // conversion) and 12 products, about 1,300 cycles, which two or three waves of a SIMD
-// overlap little.  So large calls share V's conversion (pa_q4_chunk.hip).  Where a call
+// overlap little.  So large calls share V's conversion (pa_q_chunk.h).  Where a call
 // has fewer items than the GPU holds waves, 2 or 4 waves of a workgroup share an item's
 // units and join their sums in LDS.
-#include "pa_q4_attn.h"
+#include "pa_q4_tile.h"
+#include "pa_q_attn.h"
 
 namespace pa {
 
-extern template const void* q4_attn_pick<uint16_t, 64>();
-extern template const void* q4_attn_pick<float, 128>();
-extern template const void* q4_attn_pick<float, 64>();
-template const void* q4_attn_pick<uint16_t, 128>();
+extern template const void* q_attn_pick<q4::Format, uint16_t, 64>();
+extern template const void* q_attn_pick<q4::Format, float, 128>();
+extern template const void* q_attn_pick<q4::Format, float, 64>();
+template const void* q_attn_pick<q4::Format, uint16_t, 128>();
 
-static const void* q4_attn_fn(int dtype, int D) {
-  if (dtype == 0 && D == 128) return q4_attn_pick<uint16_t, 128>();
-  if (dtype == 0 && D == 64) return q4_attn_pick<uint16_t, 64>();
-  if (dtype == 1 && D == 128) return q4_attn_pick<float, 128>();
-  if (dtype == 1 && D == 64) return q4_attn_pick<float, 64>();
-  return nullptr;
-}
+template hipError_t launch_q_attn<q4::Format>(int, int, const QAttnArgs&, hipStream_t, KernelEvents);
 
-hipError_t launch_q4_attn(int dtype, int D, const Q4AttnArgs& a, hipStream_t st, KernelEvents ev) {
-  const void* fn = q4_attn_fn(dtype, D);
-  if (fn == nullptr) return hipErrorInvalidValue;
-  const int64_t parts = (int64_t)a.H_kv * a.n_split;
-  const int items = kQ4Waves / a.wave_parts;  // of a workgroup
-  const int64_t grid = (a.n_slots + items - 1) / items * parts;
-  void* args[] = {const_cast<Q4AttnArgs*>(&a)};
-  hipError_t e = hipExtLaunchKernel(fn, dim3((uint32_t)grid), dim3(64 * kQ4Waves), args, 0, st, ev.start, ev.stop, 0);
-  return e != hipSuccess ? e : hipGetLastError();
-}
-
-hipError_t launch_q4_merge(int dtype, int D, const Q4AttnArgs& a, hipStream_t st) {
+hipError_t launch_q_merge(int dtype, int D, const QAttnArgs& a, hipStream_t st) {
   const uint32_t grid = (uint32_t)(((int64_t)a.rows * a.H_q + 3) / 4);
-  if (dtype == 0 && D == 128) q4_merge_kernel<uint16_t, 128><<<grid, 256, 0, st>>>(a);
-  else if (dtype == 0 && D == 64) q4_merge_kernel<uint16_t, 64><<<grid, 256, 0, st>>>(a);
-  else if (dtype == 1 && D == 128) q4_merge_kernel<float, 128><<<grid, 256, 0, st>>>(a);
-  else if (dtype == 1 && D == 64) q4_merge_kernel<float, 64><<<grid, 256, 0, st>>>(a);
+  if (dtype == 0 && D == 128) q_merge_kernel<uint16_t, 128><<<grid, 256, 0, st>>>(a);
+  else if (dtype == 0 && D == 64) q_merge_kernel<uint16_t, 64><<<grid, 256, 0, st>>>(a);
+  else if (dtype == 1 && D == 128) q_merge_kernel<float, 128><<<grid, 256, 0, st>>>(a);
+  else if (dtype == 1 && D == 64) q_merge_kernel<float, 64><<<grid, 256, 0, st>>>(a);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }

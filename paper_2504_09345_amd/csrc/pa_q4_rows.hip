@@ -13,8 +13,8 @@ namespace pa {
 
 namespace {
 
-constexpr int kRowsWaves = kQ4RowsWaves;
-constexpr int kGroup = kQ4RowsGroup;
+constexpr int kRowsWaves = kQRowsWaves;
+constexpr int kGroup = kQRowsGroup;
 
 // A wave's rows: those of one sequence that lie in four slots of a page from a multiple
 // of four on (a decode call's: one).
@@ -23,7 +23,7 @@ struct Group {
   bool bad;     // rows that the contract does not allow
   int page, token;  // token: of the first row
 };
-__device__ __forceinline__ Group group_of(const Q4RowsArgs& a, int slot, int lane) {
+__device__ __forceinline__ Group group_of(const QRowsArgs& a, int slot, int lane) {
   Group p{slot, 1, false, 0, 0};
   int b = slot, L = 1, j = 0;
   const int32_t* qsl = a.query_start_loc;
@@ -118,7 +118,7 @@ struct Where {  // a lane's place in a tile: chunk c of eight dims of a token
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(Q4RowsArgs a, int slots) {
+__global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(QRowsArgs a, int slots) {
   constexpr int CH = D / 8;
   const int lane = threadIdx.x & 63;
   const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -200,7 +200,7 @@ __device__ __forceinline__ void put(T* p, uint32_t w, uint32_t scale) {
 // bytes, take 104 us instead of 88 for 64 contexts of 512-2,048 tokens, 8 heads of 64
 // dims, through the caches.)
 template <typename T, int D, bool kPast>
-__global__ __launch_bounds__(64 * kRowsWaves) void q4_read_kernel(Q4RowsArgs a, int slots) {
+__global__ __launch_bounds__(64 * kRowsWaves) void q4_read_kernel(QRowsArgs a, int slots) {
   constexpr int kHalf = sizeof(T) == 4;  // four dims a lane, half a word's codes
   constexpr int CH = D / 8 << kHalf, kV = kGroup >> kHalf;
   const int lane = threadIdx.x & 63;
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q4_read_kernel(Q4RowsArgs a, 
 
 // fn(element, head dim), by type.
 template <typename Fn>
-hipError_t by_type(int dtype, int D, const Q4RowsArgs& a, Fn fn) {
+hipError_t by_type(int dtype, int D, const QRowsArgs& a, Fn fn) {
   if (a.rows == 0) return hipSuccess;
   if (dtype == 0 && D == 128) fn(uint16_t(), std::integral_constant<int, 128>{});
   else if (dtype == 0 && D == 64) fn(uint16_t(), std::integral_constant<int, 64>{});
@@ -257,11 +257,11 @@ hipError_t by_type(int dtype, int D, const Q4RowsArgs& a, Fn fn) {
 constexpr int64_t kCached = 256 << 20;
 
 // Slots of a call (group_of; checked to be 32-bit).
-int slots_of(const Q4RowsArgs& a) { return (int)q4_row_slots(a.query_start_loc != nullptr, a.rows, a.B); }
+int slots_of(const QRowsArgs& a) { return (int)q_row_slots(a.query_start_loc != nullptr, a.rows, a.B); }
 
 }  // namespace
 
-hipError_t launch_q4_append(int dtype, int D, const Q4RowsArgs& a, hipStream_t st) {
+hipError_t launch_q4_append(int dtype, int D, const QRowsArgs& a, hipStream_t st) {
   return by_type(dtype, D, a, [&](auto t, auto d) {
     constexpr int D = decltype(d)::value;
     const int slots = slots_of(a);
@@ -270,7 +270,7 @@ hipError_t launch_q4_append(int dtype, int D, const Q4RowsArgs& a, hipStream_t s
   });
 }
 
-hipError_t launch_q4_read(int dtype, int D, const Q4RowsArgs& a, hipStream_t st) {
+hipError_t launch_q4_read(int dtype, int D, const QRowsArgs& a, hipStream_t st) {
   return by_type(dtype, D, a, [&](auto t, auto d) {
     const int slots = slots_of(a);
     const dim3 grid((slots + kRowsWaves - 1) / kRowsWaves, (a.H_kv * D * (int)sizeof(t) / 16 + 63) / 64);

@@ -21,7 +21,7 @@
 //    two heads of one range each: 14.9, 68.0 and 24.9.)
 //  * Where a batch has few short items, a workgroup takes each whole, its eight waves a
 //    part of the units: nothing goes through memory then, and a call is 1.1-2.7 us
-//    shorter (kQ4AloneUnits).
+//    shorter (kQAloneUnits).
 //  * Of a SIMD's waves the oldest issues first; left alone, the older half of a
 //    workgroup ended its ranges 7 us before the younger one on 256 sequences, which then
 //    streamed with half of the loads under way.  The waves take turns instead, a unit
@@ -32,56 +32,17 @@
 // tokens 2.4 GB in 401 us, of 1,024-16,384 4.9 GB in 780), the rate that loads of this
 // pattern alone reach; the rest, some 13 us here, is launch, lengths and entries (3), the
 // first units' loads and the joins of the last ranges (4-8).
-#include "pa_q4_stream.h"
-
-#include <algorithm>
-#include <atomic>
+#include "pa_q4_tile.h"
+#include "pa_q_stream.h"
 
 namespace pa {
 
-extern template const void* q4_stream_pick<uint16_t, 64>(int);
-extern template const void* q4_stream_pick<float, 128>(int);
-extern template const void* q4_stream_pick<float, 64>(int);
-template const void* q4_stream_pick<uint16_t, 128>(int);
+extern template const void* q_stream_pick<q4::Format, uint16_t, 64>(int);
+extern template const void* q_stream_pick<q4::Format, float, 128>(int);
+extern template const void* q_stream_pick<q4::Format, float, 64>(int);
+template const void* q_stream_pick<q4::Format, uint16_t, 128>(int);
 
-static const void* q4_stream_fn(int dtype, int D, int s) {
-  if (dtype == 0 && D == 128) return q4_stream_pick<uint16_t, 128>(s);
-  if (dtype == 0 && D == 64) return q4_stream_pick<uint16_t, 64>(s);
-  if (dtype == 1 && D == 128) return q4_stream_pick<float, 128>(s);
-  if (dtype == 1 && D == 64) return q4_stream_pick<float, 64>(s);
-  return nullptr;
-}
-
-// (a property of the kernel and the device, so it is asked for once: the two
-// queries take as long as the rest of a small call on the host)
-int q4_stream_workgroups(int dtype, int D, int s, int* cus) {
-  constexpr int kDevices = 64;
-  static std::atomic<int64_t> known[kDevices][2][2][9];  // workgroups, and the CUs above them
-  int dev = 0, n_cus = 0, per_cu = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return 0;
-  std::atomic<int64_t>* at = dev >= 0 && dev < kDevices && dtype >= 0 && dtype < 2 && s <= 8 ? &known[dev][dtype][D / 128][s] : nullptr;
-  const int64_t have = at != nullptr ? at->load(std::memory_order_relaxed) : 0;
-  if (have > 0) {
-    *cus = (int)(have >> 32);
-    return (int)have;
-  }
-  const void* fn = q4_stream_fn(dtype, D, s);
-  if (fn == nullptr || hipDeviceGetAttribute(&n_cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
-      hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, fn, kQ4StreamThreads, 0) != hipSuccess)
-    return 0;
-  const int n = std::min(n_cus * per_cu, kQ4StreamGroups);
-  if (at != nullptr) at->store((int64_t)n_cus << 32 | n, std::memory_order_relaxed);
-  *cus = n_cus;
-  return n;
-}
-
-hipError_t launch_q4_stream(int dtype, int D, int s, const Q4StreamArgs& a, int workgroups, hipStream_t st,
-                            KernelEvents ev) {
-  const void* fn = q4_stream_fn(dtype, D, s);
-  if (fn == nullptr || workgroups <= 0) return hipErrorInvalidValue;
-  void* args[] = {const_cast<Q4StreamArgs*>(&a)};
-  hipError_t e = hipExtLaunchKernel(fn, dim3(workgroups), dim3(kQ4StreamThreads), args, 0, st, ev.start, ev.stop, 0);
-  return e != hipSuccess ? e : hipGetLastError();
-}
+template int q_stream_workgroups<q4::Format>(int, int, int, int*);
+template hipError_t launch_q_stream<q4::Format>(int, int, int, const QStreamArgs&, int, hipStream_t, KernelEvents);
 
 }  // namespace pa

@@ -1,8 +1,9 @@
 // The 4-bit cache's decode kernels, fp32 at head dim 64 (design in pa_q4_stream.hip).
-#include "pa_q4_stream.h"
+#include "pa_q4_tile.h"
+#include "pa_q_stream.h"
 
 namespace pa {
 
-template const void* q4_stream_pick<float, 64>(int);
+template const void* q_stream_pick<q4::Format, float, 64>(int);
 
 }  // namespace pa

@@ -1,13 +1,14 @@
-// The 4-bit cache's attention kernel and its picker (design in pa_q4_attn.hip).
-// Each (element type, head dim) is instantiated in one translation unit.
+// The kernel of chunk rows over the caches held in few bits, its picker and launcher
+// (design in pa_q4_attn.hip).  Each (format, element type, head dim) is instantiated in
+// one translation unit, which includes the format before this file.
 #pragma once
 
-#include "pa_q4_tile.h"
+#include "pa_q_tile.h"
 
 namespace pa {
 
 // An item's sequence and rows.
-struct Q4Item {
+struct QItem {
   int b, row0, n_pos;  // sequence, first query row, query rows (0: none)
   int last0;           // last key of the first row
   bool bad;            // rows are NaN
@@ -20,14 +21,14 @@ struct Q4Item {
 // such r.  (Sequences of one row, the stream kernel's, are thus looked at last and
 // without a search: before every other item, 512 of them beside 8 chunks of 512 rows
 // cost 10 us.)
-__device__ __forceinline__ Q4Item q4_item(const Q4AttnArgs& a, int i, int positions, int lane) {
-  Q4Item it{0, 0, 0, 0, false};
+__device__ __forceinline__ QItem q_item(const QAttnArgs& a, int i, int positions, int lane) {
+  QItem it{0, 0, 0, 0, false};
   const int32_t* qsl = a.query_start_loc;
   const int blocks = (a.rows + positions - 1) / positions;
   int first = 0, q0;
   if (i < blocks) {
     const int r = (blocks - 1 - i) * positions;
-    it.b = q4::wave_search(a.B, r, lane, [&](int b) { return qsl[b]; });
+    it.b = q::wave_search(a.B, r, lane, [&](int b) { return qsl[b]; });
     q0 = qsl[it.b];
     if (r < q0) return it;
     first = (r - q0 + positions - 1) / positions * positions;
@@ -50,7 +51,7 @@ __device__ __forceinline__ Q4Item q4_item(const Q4AttnArgs& a, int i, int positi
 // The outputs of a wave's columns, or the records of part `split` of them; at: the
 // column's (row, head) vector among all.
 template <typename T, int D, int NB>
-__device__ __forceinline__ void q4_finish(const Q4AttnArgs& a, const q4::State<T, D, NB>& st, const int64_t (&at)[NB], int split,
+__device__ __forceinline__ void q_finish(const QAttnArgs& a, const q::State<T, D, NB>& st, const int64_t (&at)[NB], int split,
                                           int lane) {
   const int G = lane >> 4;
   T* out = reinterpret_cast<T*>(a.out);
@@ -63,14 +64,14 @@ __device__ __forceinline__ void q4_finish(const Q4AttnArgs& a, const q4::State<T
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) {
       float o[8];
-      q4::eight_out(st, c, j, o);
+      q::eight_out(st, c, j, o);
       const int d = 32 * j + 8 * G;
       if (a.n_split == 1) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] *= inv;
-        q4::store_eight(out + at[c] * D + d, o);
+        q::store_eight(out + at[c] * D + d, o);
       } else {
-        q4::store_eight(a.ws_o + rec * D + d, o);
+        q::store_eight(a.ws_o + rec * D + d, o);
       }
     }
     if (a.n_split > 1 && G == 0) {
@@ -82,16 +83,16 @@ __device__ __forceinline__ void q4_finish(const Q4AttnArgs& a, const q4::State<T
 
 // What a wave hands to the one that joins an item's parts.
 template <int D>
-struct Q4Part {
-  q4::f32x4_t o[D / 16][64];
+struct QPart {
+  q::f32x4_t o[D / 16][64];
   float m[64], l[64];
 };
 
 // (Three waves a SIMD: in fp32 at head_dim 128, whose registers would hold two, four
 // chunks of 1,024 rows take 130 us instead of 144.)
-template <typename T, int D>
-__global__ __launch_bounds__(64 * kQ4Waves) __attribute__((amdgpu_waves_per_eu(3)))
-void q4_attn_kernel(Q4AttnArgs a) {
+template <class F, typename T, int D>
+__global__ __launch_bounds__(64 * kQWaves) __attribute__((amdgpu_waves_per_eu(3)))
+void q_attn_kernel(QAttnArgs a) {
   constexpr int NB = 1;  // column blocks of the wave
   const int S = a.s;
   const int lane = threadIdx.x & 63;
@@ -100,7 +101,7 @@ void q4_attn_kernel(Q4AttnArgs a) {
   const int split = blockIdx.x % a.n_split, g = blockIdx.x / a.n_split % a.H_kv;
   // (a workgroup's waves have items of their own, or 2 or 4 share one)
   const int sharers = a.wave_parts, part = wave & (sharers - 1);
-  const Q4Item it = q4_item(a, (int)(blockIdx.x / a.n_split / a.H_kv * kQ4Waves + wave) / sharers, q4_positions(NB, S), lane);
+  const QItem it = q_item(a, (int)(blockIdx.x / a.n_split / a.H_kv * kQWaves + wave) / sharers, q_positions(NB, S), lane);
 
   const int n = lane & 15;
   T* out = reinterpret_cast<T*>(a.out);
@@ -110,15 +111,15 @@ void q4_attn_kernel(Q4AttnArgs a) {
       store_out<T>(out + ((int64_t)(it.row0 + i / (S * D)) * a.H_q + (int64_t)g * S) * D + i % (S * D), NAN);
   }
   // units of the item that the workgroup takes, and the wave's of them
-  const int n_units = it.n_pos == 0 || it.bad ? 0 : all_last / kQ4Unit + 1;
+  const int n_units = it.n_pos == 0 || it.bad ? 0 : all_last / kQUnit + 1;
   const int s0 = split * a.split_units, s1 = min(n_units, s0 + a.split_units);
   const int per = (max(s1 - s0, 0) + sharers - 1) / sharers;
   const int u0 = s0 + part * per, u1 = min(s1, u0 + per);
   if (u0 >= u1 && sharers == 1) return;
 
-  q4::State<T, D, NB> st;
+  q::State<T, D, NB> st;
   int64_t at[NB];  // of the column's (row, head) vector, among all
-  q4::reset(st);
+  q::reset(st);
   if (u0 < u1) {
 #pragma unroll
     for (int c = 0; c < NB; ++c) {
@@ -126,14 +127,15 @@ void q4_attn_kernel(Q4AttnArgs a) {
       const bool there = pos < it.n_pos;  // (columns past the item's positions are none)
       st.last[c] = there ? it.last0 + pos : -1;
       at[c] = (int64_t)(it.row0 + (there ? pos : 0)) * a.H_q + (int64_t)g * S + col % S;
-      q4::load_query<T, D>(st.q[c], there ? reinterpret_cast<const T*>(a.q) + at[c] * D : nullptr, lane);
+      q::load_query<F::kSliced, T, D>(st.q[c], there ? reinterpret_cast<const T*>(a.q) + at[c] * D : nullptr, lane);
     }
 
     const int n_pages = all_last / kPage + 1;
-    const int64_t tile = q4_tile_bytes(D), page_bytes = tile * a.H_kv;
-    const int tile_size = a.num_pages > 0 ? q4_tile_bytes(D) : 0;
+    const int64_t tile = F::tile_bytes(D), page_bytes = tile * a.H_kv;
+    const int tile_size = a.num_pages > 0 ? F::tile_bytes(D) : 0;
     const uint8_t* kg = a.k_pages + g * tile;
     const uint8_t* vg = a.v_pages + g * tile;
+    const uint8_t* sg = F::scales_of_head(a.scales, g);
     const int32_t* table = a.block_table + (int64_t)it.b * a.bt_stride;
     // lane i: entries of page 64 (k / 32) + i of the present unit k and of the 64 after
     auto entries = [&](int k) {
@@ -160,38 +162,39 @@ void q4_attn_kernel(Q4AttnArgs a) {
       }
       return t;
     };
-    q4::Unit<D> u;
-    const int k_shift = q4::k_shift<D>(lane);
+    typename F::template Unit<D> u;
+    const int k_shift = F::template shift<D>(lane);
     auto fetch_k = [&](const Pages& t, bool any) {
 #pragma unroll
-      for (int p = 0; p < 2; ++p) q4::load_k<D, 0>(u, p, kg + t.at[p], any ? tile_size : 0, lane);
+      for (int p = 0; p < 2; ++p) F::template load_k<0>(u, p, kg, t.at[p], sg, any ? tile_size : 0, lane);
     };
     auto fetch_v = [&](const Pages& t, bool any) {
 #pragma unroll
-      for (int p = 0; p < 2; ++p) q4::load_v<D, 0>(u, p, vg + t.at[p], any ? tile_size : 0, lane);
+      for (int p = 0; p < 2; ++p) F::template load_v<0>(u, p, vg, t.at[p], sg, any ? tile_size : 0, lane);
     };
     Pages t = pages(u0);
     fetch_k(t, true);
     __builtin_amdgcn_sched_barrier(0);  // (K before V, as the loop's waits expect)
     fetch_v(t, true);
-    constexpr bool kF16 = q4::kF16<T>;
-    const int u_full = min(u1, (it.last0 + 1) / kQ4Unit);  // units before are seen whole by every column
+    constexpr bool kF16 = q::kF16<T>;
+    const int u_full = min(u1, (it.last0 + 1) / kQUnit);  // units before are seen whole by every column
     for (int k = u0; k < u1; ++k) {
-      q4::f32x4_t s[NB][2];
+      q::f32x4_t s[NB][2];
       float x[NB][8];
       Pages next = t;
       bool big = false, odd = false;  // the base moves; V takes other products
       auto weights = [&](bool usual) {  // the weights of unit k, and the next K; whether it is big or odd
         if (k + 1 < u1) next = pages(k + 1);
-        q4::fold_qk<T, D, NB>(st, u, k_shift, s);
+        F::fold_qk(st, u, k_shift, s);
+        F::keep_scales(u);
         fetch_k(next, k + 1 < u1);
         if (!usual) {
-          q4::mask_scores<T, D, NB>(st, k * kQ4Unit, t.bad, lane, s);
-          q4::clear_dead(u, k * kQ4Unit, all_last, lane);
+          q::mask_scores<T, D, NB>(st, k * kQUnit, t.bad, lane, s);
+          F::clear_dead(u, k * kQUnit, all_last, lane);
         }
-        big = q4::form_weights<T, D, NB>(st, s, a.scale_log2, x);
+        big = q::form_weights<T, D, NB>(st, s, a.scale_log2, x);
         __builtin_amdgcn_sched_barrier(0);  // (V is not waited for before the weights are formed)
-        odd = kF16 ? q4::beyond_fp16<D>(u) : q4::has_large<D>(u);
+        odd = F::template odd<kF16>(u);
         return __builtin_amdgcn_ballot_w64(big | odd) != 0;
       };
       bool rare = weights(k < u_full && t.bad == 0) | st.any_lifted;
@@ -200,8 +203,8 @@ void q4_attn_kernel(Q4AttnArgs a) {
         // loads under way are known)
 #pragma unroll 1
         while (!rare & (k + 1 < u_full) & (next.bad == 0)) {
-          q4::add_weights(st, x);
-          q4::fold_pv<kF16, T, D, NB>(st, u, x);
+          q::add_weights(st, x);
+          F::template fold_pv<kF16>(st, u, x);
           fetch_v(next, true);
           t = next;
           ++k;
@@ -209,15 +212,15 @@ void q4_attn_kernel(Q4AttnArgs a) {
         }
       }
       int first = INT32_MAX;
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) first = q4::first_large(u, k * kQ4Unit, lane);
-      q4::settle_weights<true, T, D, NB>(st, s, a.scale_log2, big, x, first);
-      q4::fold_pv_edge<T, D, NB>(st, u, x, k * kQ4Unit, lane);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) first = F::first_large(u, k * kQUnit, lane);
+      q::settle_weights<true, T, D, NB>(st, s, a.scale_log2, big, x, first);
+      F::fold_pv_edge(st, u, x, k * kQUnit, lane);
       fetch_v(next, k + 1 < u1);
       t = next;
     }
   }
   if (sharers > 1) {  // join the parts that have units: the first one's wave takes the others'
-    __shared__ Q4Part<D> parts[kQ4Waves];
+    __shared__ QPart<D> parts[kQWaves];
     if (part > 0 && u0 < u1) {
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) parts[wave].o[j][lane] = st.acc[0][j];
@@ -242,25 +245,25 @@ void q4_attn_kernel(Q4AttnArgs a) {
       for (int j = 0; j < D / 16; ++j) st.acc[0][j] = other.o[j][lane] * ci + st.acc[0][j];
     }
   }
-  q4_finish<T, D, NB>(a, st, at, split, lane);
+  q_finish<T, D, NB>(a, st, at, split, lane);
 }
 
 // Join the parts of one (query row, head) per wave.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
+__global__ __launch_bounds__(256) void q_merge_kernel(QAttnArgs a) {
   const int lane = threadIdx.x & 63;
   const int f = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = f / a.H_q;
   if (row >= a.rows) return;
   const int32_t* qsl = a.query_start_loc;
-  const int b = q4::wave_search(a.B, row, lane, [&](int i) { return qsl[i]; });
+  const int b = q::wave_search(a.B, row, lane, [&](int i) { return qsl[i]; });
   const int L = qsl[b + 1] - qsl[b], j = row - qsl[b];
   if (j < 0 || j >= L || L < a.min_rows || L > a.max_q_len) return;
   const int C = a.context_lens[b];
   // (rows without keys or with an error are written already)
   if (C < L || C > a.max_context_len || (C + kPage - 1) / kPage > a.bt_stride) return;
   // the parts that have a key of the row: any later ones of its item weigh nothing
-  const int n = min(a.n_split, (C - L + j) / kQ4Unit / a.split_units + 1);
+  const int n = min(a.n_split, (C - L + j) / kQUnit / a.split_units + 1);
   const int64_t rec = (int64_t)f * a.n_split;
   float m = kMInit, l = 0.0f;
   if (lane < n) {
@@ -281,9 +284,30 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
   for (int e = 0; e < E; ++e) store_out<T>(reinterpret_cast<T*>(a.out) + (int64_t)f * D + lane * E + e, o[e] / total);
 }
 
-template <typename T, int D>
-const void* q4_attn_pick() {
-  return reinterpret_cast<const void*>(&q4_attn_kernel<T, D>);
+template <class F, typename T, int D>
+const void* q_attn_pick() {
+  return reinterpret_cast<const void*>(&q_attn_kernel<F, T, D>);
+}
+
+template <class F>
+const void* q_attn_fn(int dtype, int D) {
+  if (dtype == 0 && D == 128) return q_attn_pick<F, uint16_t, 128>();
+  if (dtype == 0 && D == 64) return q_attn_pick<F, uint16_t, 64>();
+  if (dtype == 1 && D == 128) return q_attn_pick<F, float, 128>();
+  if (dtype == 1 && D == 64) return q_attn_pick<F, float, 64>();
+  return nullptr;
+}
+
+template <class F>
+hipError_t launch_q_attn(int dtype, int D, const QAttnArgs& a, hipStream_t st, KernelEvents ev) {
+  const void* fn = q_attn_fn<F>(dtype, D);
+  if (fn == nullptr) return hipErrorInvalidValue;
+  const int64_t parts = (int64_t)a.H_kv * a.n_split;
+  const int items = kQWaves / a.wave_parts;  // of a workgroup
+  const int64_t grid = (a.n_slots + items - 1) / items * parts;
+  void* args[] = {const_cast<QAttnArgs*>(&a)};
+  hipError_t e = hipExtLaunchKernel(fn, dim3((uint32_t)grid), dim3(64 * kQWaves), args, 0, st, ev.start, ev.stop, 0);
+  return e != hipSuccess ? e : hipGetLastError();
 }
 
 }  // namespace pa

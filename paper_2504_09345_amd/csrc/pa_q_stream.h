@@ -1,8 +1,12 @@
-// The 4-bit cache's decode kernel and its picker (design in pa_q4_stream.hip).
-// Each (element type, head dim) is instantiated in one translation unit.
+// The decode kernel of the caches held in few bits, its picker and launcher (design in
+// pa_q4_stream.hip).  Each (format, element type, head dim) is instantiated in one
+// translation unit, which includes the format before this file.
 #pragma once
 
-#include "pa_q4_tile.h"
+#include <algorithm>
+#include <atomic>
+
+#include "pa_q_tile.h"
 #include "pa_stream_body.h"
 
 namespace pa {
@@ -10,26 +14,26 @@ namespace pa {
 // A record's 16-byte chunks: chunk c holds head c / 4 mod S, dims 32 j + 8 (c mod 4)
 // + 4 h .. +3 with 2 j + h = c / 4 S (the accumulators' order, a lane's own pairs).
 template <int D, int S>
-struct Q4Record {
+struct QRecord {
   static __device__ __forceinline__ int head(int c) { return c / 4 % S; }
   static __device__ __forceinline__ int dim(int c) { return (c / (8 * S)) * 32 + c % 4 * 8 + c / (4 * S) % 2 * 4; }
   static __device__ __forceinline__ int chunk(int n, int jh, int G) { return (jh * S + n) * 4 + G; }
 };
 
 template <int D, int S>
-struct Q4StreamSmem {
-  int32_t cum[kQ4StreamSeqs + 1];  // units of the sequences before, per KV head
-  int32_t scan[kQ4StreamThreads / 64];
+struct QStreamSmem {
+  int32_t cum[kQStreamSeqs + 1];  // units of the sequences before, per KV head
+  int32_t scan[kQStreamThreads / 64];
   // of each wave, its parts of the items cut by its range's start (0) and end (1)
   struct Part {
     float ml[S][2];
     alignas(16) float o[S * D];
-  } part[kQ4StreamThreads / 64][2];
+  } part[kQStreamThreads / 64][2];
 };
 
 // What the kernel does with sequence b: 1 (its row sees nv > 0 keys), 0 (nothing),
 // 2 (zeros), -1 (rows row .. row + n - 1 are NaN).
-__device__ __forceinline__ int q4_decode_row(const Q4StreamArgs& a, int b, int& row, int& n, int& nv) {
+__device__ __forceinline__ int q_decode_row(const QStreamArgs& a, int b, int& row, int& n, int& nv) {
   nv = a.context_lens[b];
   n = 1;
   row = b;
@@ -51,8 +55,8 @@ __device__ __forceinline__ int q4_decode_row(const Q4StreamArgs& a, int b, int& 
 // bypass the L2 (a round trip of 1 to 2 us), so all (m, l), record i by lane i, and
 // the first kBatch records' outputs are loaded at once.
 template <typename T, int D, int S>
-__device__ __forceinline__ void q4_join(const Q4StreamArgs& a, int x0, int xs, int step, int n, bool final, int lane, T* out) {
-  using Rec = Q4Record<D, S>;
+__device__ __forceinline__ void q_join(const QStreamArgs& a, int x0, int xs, int step, int n, bool final, int lane, T* out) {
+  using Rec = QRecord<D, S>;
   constexpr int kChunks = S * D / 4, C = (kChunks + 63) / 64;  // chunks per lane
   constexpr int kBatch = 4;  // (8 are no faster)
   asm volatile("" ::: "memory");  // (the loads stay below the arrival)
@@ -121,7 +125,7 @@ __device__ __forceinline__ void q4_join(const Q4StreamArgs& a, int x0, int xs, i
     const int ch = u * 64 + lane;
     if (final) {
       const f32x4_dev_t o = acc[u] * (1.0f / pick(L, Rec::head(ch)));
-      if (kChunks % 64 == 0 || ch < kChunks) q4::store_four(out + Rec::head(ch) * D + Rec::dim(ch), o);
+      if (kChunks % 64 == 0 || ch < kChunks) q::store_four(out + Rec::head(ch) * D + Rec::dim(ch), o);
     } else {
       store_dev4(r, ch * 4, acc[u]);  // (a chunk past the record is out of the descriptor's range)
     }
@@ -132,12 +136,12 @@ __device__ __forceinline__ void q4_join(const Q4StreamArgs& a, int x0, int xs, i
   }
 }
 
-template <typename T, int D, int S>
-__global__ __launch_bounds__(kQ4StreamThreads) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2)))  // (two workgroups a CU at head_dim 64)
-void q4_stream_kernel(Q4StreamArgs a) {
-  using Rec = Q4Record<D, S>;
-  constexpr int NT = kQ4StreamThreads, kWaves = NT / 64;
-  __shared__ Q4StreamSmem<D, S> sm;
+template <class F, typename T, int D, int S>
+__global__ __launch_bounds__(kQStreamThreads) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2)))  // (two workgroups a CU at head_dim 64)
+void q_stream_kernel(QStreamArgs a) {
+  using Rec = QRecord<D, S>;
+  constexpr int NT = kQStreamThreads, kWaves = NT / 64;
+  __shared__ QStreamSmem<D, S> sm;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wg = blockIdx.x, n_wg = gridDim.x;
@@ -152,9 +156,9 @@ void q4_stream_kernel(Q4StreamArgs a) {
     int local = 0;
     for (int r = r0; r < r1; ++r) {
       int row, n, nv;
-      const int what = q4_decode_row(a, r, row, n, nv);
+      const int what = q_decode_row(a, r, row, n, nv);
       sm.cum[r] = local;
-      local += what == 1 ? (nv + kQ4Unit - 1) / kQ4Unit : 0;
+      local += what == 1 ? (nv + kQUnit - 1) / kQUnit : 0;
     }
     const int off = block_exclusive_scan<NT>(local, sm.scan);
     for (int r = r0; r < r1; ++r) sm.cum[r] += off;
@@ -164,7 +168,7 @@ void q4_stream_kernel(Q4StreamArgs a) {
   for (int r = wg; r < R; r += n_wg) {
     if (sm.cum[r + 1] != sm.cum[r]) continue;
     int row, n, nv;
-    const int what = q4_decode_row(a, r, row, n, nv);
+    const int what = q_decode_row(a, r, row, n, nv);
     if (what == 0) continue;
     const int64_t from = max(row, 0), to = min((int64_t)row + n, (int64_t)a.rows);
     T* o = reinterpret_cast<T*>(a.out);
@@ -173,15 +177,15 @@ void q4_stream_kernel(Q4StreamArgs a) {
   const int U = H * sm.cum[R];
   const int busy = min(a.cus, n_wg);  // workgroups, one per CU
   // ranges: one per wave, in a workgroup per CU where more would have few units each
-  const int G = max(1, min((U < kQ4FewUnits * n_wg * kWaves ? busy : n_wg) * kWaves, U));
+  const int G = max(1, min((U < kQFewUnits * n_wg * kWaves ? busy : n_wg) * kWaves, U));
   if (U == 0) return;
   // Few short items: a workgroup has one of them alone, and nothing is joined through
-  // memory (kQ4AloneUnits).
+  // memory (kQAloneUnits).
   bool alone = (int64_t)R * H <= busy;
   if (alone) {
     int most = 0;
     for (int r = lane; r < R; r += 64) most = max(most, sm.cum[r + 1] - sm.cum[r]);
-    alone = __builtin_amdgcn_ballot_w64(most > U / busy + kQ4AloneUnits) == 0;
+    alone = __builtin_amdgcn_ballot_w64(most > U / busy + kQAloneUnits) == 0;
   }
   if (wg >= (alone ? R * H : (G + kWaves - 1) / kWaves)) return;
   // ranges of each or each + 1 units, the longer ones first
@@ -209,7 +213,7 @@ void q4_stream_kernel(Q4StreamArgs a) {
     int hb, p, np;  // KV head; unit of the item and the item's units
     int row;
   };
-  const int64_t tile = q4_tile_bytes(D);
+  const int64_t tile = F::tile_bytes(D);
   auto entries = [&](int i0) {
     Entries e;
     const int x = u0 + min(i0 + lane, m - 1);
@@ -223,34 +227,34 @@ void q4_stream_kernel(Q4StreamArgs a) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)  // (past the context's pages: any entry, unused; read without waiting for the length)
       page[h] = a.block_table[(int64_t)r * a.bt_stride + min((int64_t)2 * e.p + h, a.bt_stride - 1)];
-    const int left = a.context_lens[r] - e.p * kQ4Unit;  // tokens from the unit on
+    const int left = a.context_lens[r] - e.p * kQUnit;  // tokens from the unit on
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const bool used = left > kPage * h, ok = used && page[h] >= 0 && page[h] < a.num_pages;
       odd |= (ok || !used ? 0 : 1) << h;
       e.at[h] = ok ? ((int64_t)page[h] * H + e.hb) * tile : 0;
     }
-    e.info = min(left, kQ4Unit) | odd << 6 | (odd != 0 || left < kQ4Unit) << 8;
+    e.info = min(left, kQUnit) | odd << 6 | (odd != 0 || left < kQUnit) << 8;
     return e;
   };
 
-  q4::State<T, D, 1> st;
-  q4::Unit<D> u;
-  const int k_shift = q4::k_shift<D>(lane);
+  q::State<T, D, 1> st;
+  typename F::template Unit<D> u;
+  const int k_shift = F::template shift<D>(lane);
   const int n = lane & 15, Gl = lane >> 4;
   T* out = reinterpret_cast<T*>(a.out);
-  const int tile_size = a.num_pages > 0 ? q4_tile_bytes(D) : 0;
+  const int tile_size = a.num_pages > 0 ? F::tile_bytes(D) : 0;
   struct Tiles {
     int64_t at[2];
     int info;
   };
   auto fetch_k = [&](const Tiles& e, bool any) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_k<D, kKvLoadPolicy>(u, p, a.k_pages + e.at[p], any ? tile_size : 0, lane);
+    for (int p = 0; p < 2; ++p) F::template load_k<kKvLoadPolicy>(u, p, a.k_pages, e.at[p], a.scales, any ? tile_size : 0, lane);
   };
   auto fetch_v = [&](const Tiles& e, bool any) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) q4::load_v<D, kKvLoadPolicy>(u, p, a.v_pages + e.at[p], any ? tile_size : 0, lane);
+    for (int p = 0; p < 2; ++p) F::template load_v<kKvLoadPolicy>(u, p, a.v_pages, e.at[p], a.scales, any ? tile_size : 0, lane);
   };
   auto put_part = [&](int which, float l) {
     auto& part = sm.part[wave][which];
@@ -258,7 +262,7 @@ void q4_stream_kernel(Q4StreamArgs a) {
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) {
         float o[8];
-        q4::eight_out(st, 0, j, o);
+        q::eight_out(st, 0, j, o);
         *reinterpret_cast<f32x4_dev_t*>(&part.o[Rec::chunk(n, 2 * j, Gl) * 4]) = f32x4_dev_t{o[0], o[1], o[2], o[3]};
         *reinterpret_cast<f32x4_dev_t*>(&part.o[Rec::chunk(n, 2 * j + 1, Gl) * 4]) = f32x4_dev_t{o[4], o[5], o[6], o[7]};
       }
@@ -301,9 +305,9 @@ void q4_stream_kernel(Q4StreamArgs a) {
         from = u0 + i - p;
         to = u0 + i + left - 1;
         const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D;
-        q4::load_query<T, D>(st.q[0], n < S ? q : nullptr, lane);
-        q4::reset(st);
-        st.last[0] = kQ4Unit - 1;
+        q::load_query<F::kSliced, T, D>(st.q[0], n < S ? q : nullptr, lane);
+        q::reset(st);
+        st.last[0] = kQUnit - 1;
         open = true;
       }
       // units without anything else to do between them; the last of the 64 is alone: the
@@ -318,8 +322,8 @@ void q4_stream_kernel(Q4StreamArgs a) {
       }
       const bool ends = stop == i + left;
       for (; i < stop; ++i) {
-        constexpr bool kF16 = q4::kF16<T>;
-        q4::f32x4_t s[1][2];
+        constexpr bool kF16 = q::kF16<T>;
+        q::f32x4_t s[1][2];
         float x[1][8];
         Tiles next;
         bool big;      // the base moves
@@ -327,17 +331,18 @@ void q4_stream_kernel(Q4StreamArgs a) {
         auto weights = [&](bool usual) {  // the weights of unit i, and the next K; whether it is big or odd
           const bool more = i + 1 < m;
           next = tiles(more ? i + 1 : i);
-          q4::fold_qk<T, D, 1>(st, u, k_shift, s);
+          F::fold_qk(st, u, k_shift, s);
+          F::keep_scales(u);
           fetch_k(next, more);
           if (!usual) {
             const int tokens = t.info & 63;
             st.last[0] = tokens - 1;  // (of this unit; the item's last, or of pages outside the pool)
-            q4::mask_scores<T, D, 1>(st, 0, t.info >> 6 & 3, lane, s);
-            q4::clear_dead(u, 0, tokens - 1, lane);
+            q::mask_scores<T, D, 1>(st, 0, t.info >> 6 & 3, lane, s);
+            F::clear_dead(u, 0, tokens - 1, lane);
           }
-          big = q4::form_weights<T, D, 1>(st, s, a.scale_log2, x);
+          big = q::form_weights<T, D, 1>(st, s, a.scale_log2, x);
           __builtin_amdgcn_sched_barrier(0);  // (V is not waited for before the weights are formed)
-          odd = __builtin_amdgcn_ballot_w64(kF16 ? q4::beyond_fp16<D>(u) : q4::has_large<D>(u));
+          odd = __builtin_amdgcn_ballot_w64(F::template odd<kF16>(u));
           return (odd | __builtin_amdgcn_ballot_w64(big)) != 0;
         };
         bool rare = weights(!(t.info & 256)) | st.any_lifted;
@@ -345,8 +350,8 @@ void q4_stream_kernel(Q4StreamArgs a) {
         // loads under way are known)
 #pragma unroll 1
         while (!rare & (i + 1 < stop) & !(next.info & 256)) {
-          q4::add_weights(st, x);
-          q4::fold_pv<kF16, T, D, 1>(st, u, x);
+          q::add_weights(st, x);
+          F::template fold_pv<kF16>(st, u, x);
           fetch_v(next, true);
           t = next;
           ++i;
@@ -360,9 +365,9 @@ void q4_stream_kernel(Q4StreamArgs a) {
         }
         int first = INT32_MAX;  // (every column sees every key of the unit)
         if (__builtin_expect(odd != 0, 0))
-          first = __builtin_amdgcn_ballot_w64(q4::has_large(u)) != 0 ? 0 : INT32_MAX;
-        q4::settle_weights<true, T, D, 1>(st, s, a.scale_log2, big, x, first);
-        q4::fold_pv<false, T, D, 1>(st, u, x);
+          first = __builtin_amdgcn_ballot_w64(F::has_large(u)) != 0 ? 0 : INT32_MAX;
+        q::settle_weights<true, T, D, 1>(st, s, a.scale_log2, big, x, first);
+        F::template fold_pv<false>(st, u, x);
         fetch_v(next, i + 1 < m);
         t = next;
       }
@@ -375,10 +380,10 @@ void q4_stream_kernel(Q4StreamArgs a) {
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) {
             float o[8];
-            q4::eight_out(st, 0, j, o);
+            q::eight_out(st, 0, j, o);
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] *= inv;
-            q4::store_eight(out + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D + 32 * j + 8 * Gl, o);
+            q::store_eight(out + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D + 32 * j + 8 * Gl, o);
           }
         }
       } else {
@@ -408,7 +413,7 @@ void q4_stream_kernel(Q4StreamArgs a) {
   auto counter_at = [&](int x) {
     // (global memory for certain: while a generic access is under way, every wait is for all)
     using Global = __attribute__((address_space(1))) unsigned long long;
-    Global* p = (Global*)(a.ws_flag + (int64_t)x * kQ4CounterStride);
+    Global* p = (Global*)(a.ws_flag + (int64_t)x * kQCounterStride);
     asm("" : "+v"(p));  // (an address of lanes: one atomic, not a wave's reduction)
     return DeviceCounter{(unsigned long long*)p};
   };
@@ -445,7 +450,7 @@ void q4_stream_kernel(Q4StreamArgs a) {
         acc = *reinterpret_cast<const f32x4_dev_t*>(&part.o[c * 4]) * ci + acc;
       }
       if (whole) {
-        q4::store_four(o + h * D + Rec::dim(c), acc * (1.0f / L));
+        q::store_four(o + h * D + Rec::dim(c), acc * (1.0f / L));
       } else {
         store_dev4(r, c * 4, acc);
         if (Rec::dim(c) == 0) store_dev(a.ws_ml + (slot * S + h) * 2, M, L);
@@ -464,21 +469,64 @@ void q4_stream_kernel(Q4StreamArgs a) {
       }
       if (!__builtin_amdgcn_readfirstlane(last)) break;
       // (a group's record counts in the item next)
-      q4_join<T, D, S>(a, cut.x0, cut.first(lv, wg), cut.step(lv), records, lv == 1, lane, o);
+      q_join<T, D, S>(a, cut.x0, cut.first(lv, wg), cut.step(lv), records, lv == 1, lane, o);
     }
   }
 }
 
-template <typename T, int D>
-const void* q4_stream_pick(int s) {
+template <class F, typename T, int D>
+const void* q_stream_pick(int s) {
   switch (s) {
-    case 1: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, 1>);
-    case 2: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, 2>);
-    case 4: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, 4>);
-    case 6: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, 6>);
-    case 8: return reinterpret_cast<const void*>(&q4_stream_kernel<T, D, 8>);
+    case 1: return reinterpret_cast<const void*>(&q_stream_kernel<F, T, D, 1>);
+    case 2: return reinterpret_cast<const void*>(&q_stream_kernel<F, T, D, 2>);
+    case 4: return reinterpret_cast<const void*>(&q_stream_kernel<F, T, D, 4>);
+    case 6: return reinterpret_cast<const void*>(&q_stream_kernel<F, T, D, 6>);
+    case 8: return reinterpret_cast<const void*>(&q_stream_kernel<F, T, D, 8>);
   }
   return nullptr;
+}
+
+template <class F>
+const void* q_stream_fn(int dtype, int D, int s) {
+  if (dtype == 0 && D == 128) return q_stream_pick<F, uint16_t, 128>(s);
+  if (dtype == 0 && D == 64) return q_stream_pick<F, uint16_t, 64>(s);
+  if (dtype == 1 && D == 128) return q_stream_pick<F, float, 128>(s);
+  if (dtype == 1 && D == 64) return q_stream_pick<F, float, 64>(s);
+  return nullptr;
+}
+
+// (a property of the kernel and the device, so it is asked for once: the two
+// queries take as long as the rest of a small call on the host)
+template <class F>
+int q_stream_workgroups(int dtype, int D, int s, int* cus) {
+  constexpr int kDevices = 64;
+  static std::atomic<int64_t> known[kDevices][2][2][9];  // workgroups, and the CUs above them
+  int dev = 0, n_cus = 0, per_cu = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return 0;
+  std::atomic<int64_t>* at = dev >= 0 && dev < kDevices && dtype >= 0 && dtype < 2 && s <= 8 ? &known[dev][dtype][D / 128][s] : nullptr;
+  const int64_t have = at != nullptr ? at->load(std::memory_order_relaxed) : 0;
+  if (have > 0) {
+    *cus = (int)(have >> 32);
+    return (int)have;
+  }
+  const void* fn = q_stream_fn<F>(dtype, D, s);
+  if (fn == nullptr || hipDeviceGetAttribute(&n_cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
+      hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, fn, kQStreamThreads, 0) != hipSuccess)
+    return 0;
+  const int n = std::min(n_cus * per_cu, kQStreamGroups);
+  if (at != nullptr) at->store((int64_t)n_cus << 32 | n, std::memory_order_relaxed);
+  *cus = n_cus;
+  return n;
+}
+
+template <class F>
+hipError_t launch_q_stream(int dtype, int D, int s, const QStreamArgs& a, int workgroups, hipStream_t st,
+                            KernelEvents ev) {
+  const void* fn = q_stream_fn<F>(dtype, D, s);
+  if (fn == nullptr || workgroups <= 0) return hipErrorInvalidValue;
+  void* args[] = {const_cast<QStreamArgs*>(&a)};
+  hipError_t e = hipExtLaunchKernel(fn, dim3(workgroups), dim3(kQStreamThreads), args, 0, st, ev.start, ev.stop, 0);
+  return e != hipSuccess ? e : hipGetLastError();
 }
 
 }  // namespace pa
