@@ -1,5 +1,6 @@
 """ctypes binding of libpagedattn.so, the C ABI declared in include/pagedattn.h
-and, for the cache held in 4 bits, include/pagedattn_q4.h.
+and, for the caches held in 4 and in 8 bits, include/pagedattn_q4.h and
+include/pagedattn_q8.h.
 
 Argument marshalling only: every step of the attention runs in the library's
 HIP kernels.  Device buffers are passed as torch tensors (torch provides
@@ -26,7 +27,7 @@ EXPORTED = ("pa_workspace_size", "paged_attn", "paged_attn_varlen", "paged_attn_
             "pa_kv_append", "pa_schedule_step", "pa_perf_model", "pa_read_probe", "pa_issue_probe",
             "pa_strerror",
             "pa_q4_tile_bytes", "pa_kv_append_q4", "pa_kv_read_q4", "pa_workspace_size_q4", "paged_attn_q4",
-            "paged_attn_varlen_q4")
+            "paged_attn_varlen_q4", "pa_kv_append_q8", "pa_kv_read_q8")
 
 
 class PaDims(ctypes.Structure):
@@ -133,8 +134,10 @@ def load():
     lib.pa_workspace_size_q4.argtypes = [DP, ctypes.POINTER(SZ)]
     lib.paged_attn_q4.argtypes = [P, P, P, P, P, ctypes.c_float, P, DP, P, SZ, P, TP]
     lib.paged_attn_varlen_q4.argtypes = [P, P, P, P, P, P, ctypes.c_float, P, DP, P, SZ, P, TP]
+    lib.pa_kv_append_q8.argtypes = [P, P, P, P, P, P, P, P, DP, P]
+    lib.pa_kv_read_q8.argtypes = [P, P, P, P, P, P, P, P, DP, P]
     for name in ("pa_q4_tile_bytes", "pa_kv_append_q4", "pa_kv_read_q4", "pa_workspace_size_q4", "paged_attn_q4",
-                 "paged_attn_varlen_q4"):
+                 "paged_attn_varlen_q4", "pa_kv_append_q8", "pa_kv_read_q8"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -298,6 +301,7 @@ def pa_q4_tile_bytes(head_dim) -> int:
 
 
 _Q4_TILE = {64: 544, 128: 1088}  # pa_q4_tile_bytes (checked against it by the tests)
+_Q8_TILE = {64: 1024, 128: 2048}
 
 
 def make_dims_q4(rows, k_pages, block_table, max_context_len, num_q_rows=0, max_q_len=0, num_seqs=None) -> PaDims:
@@ -326,7 +330,7 @@ def _is_address(t):
 
 
 def _take(t, kind, n, device):
-    """Device address of a tensor of a call on the 4-bit cache.  (Addresses are taken
+    """Device address of a tensor of a call on a cache in few bits.  (Addresses are taken
     as they are.)"""
     if t is None:
         return None
@@ -342,21 +346,21 @@ def _take(t, kind, n, device):
     return t.data_ptr() or None
 
 
-def _fit_q4(dims, heads, dense0, dense1, k_pages, v_pages, block_table):
+def _fit_q(tile, dims, heads, dense0, dense1, k_pages, v_pages, block_table):
     """Refuses arrays whose rows are not those that dims say: read with their strides
     they would be other values.  (Addresses, and arrays of other ranks, are taken by
     their elements.)"""
     H_kv, D = dims.num_kv_heads, dims.head_dim
-    if D not in _Q4_TILE:  # (the library's to refuse)
+    if D not in tile:  # (the library's to refuse)
         return
-    tiles = (H_kv, _Q4_TILE[D])
+    tiles = (H_kv, tile[D])
     for t, row in ((dense0, (heads, D)), (dense1, (heads, D)), (k_pages, tiles), (v_pages, tiles),
                    (block_table, (dims.max_pages_per_seq,))):
         if not _is_address(t) and t.dim() == len(row) + 1 and tuple(t.shape[1:]) != row:
             raise ValueError(f"a tensor of shape {tuple(t.shape)} where dims say rows of {row}")
 
 
-def _take_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc):
+def _take_q(tile, dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc):
     """The addresses of a call's arrays, in this order.  Refuses a tensor that is not
     what dims and the format say: of another type or too few elements, not contiguous,
     not on the current device."""
@@ -369,14 +373,18 @@ def _take_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table,
     B, D = dims.num_seqs, dims.head_dim
     kind = torch.bfloat16 if dims.dtype == PA_BF16 else torch.float32
     n = (dims.num_q_rows if varlen else B) * heads * D
-    tiles = dims.num_pages * dims.num_kv_heads * _Q4_TILE.get(D, 0)
+    tiles = dims.num_pages * dims.num_kv_heads * tile.get(D, 0)
     return (_take(dense0, kind, n, dev), _take(dense1, kind, n, dev), _take(k_pages, u8, tiles, dev),
             _take(v_pages, u8, tiles, dev), _take(block_table, i32, B * dims.max_pages_per_seq, dev),
             _take(context_lens, i32, B, dev), _take(query_start_loc, i32, B + 1, dev))
 
 
-def _args_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc):
-    """_take_q4, checked by _fit_q4, and the current device if it was looked up.  The
+def _take_q4(dims, *arrays):
+    return _take_q(_Q4_TILE, dims, *arrays)
+
+
+def _args_q(tile, dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc):
+    """_take_q, checked by _fit_q, and the current device if it was looked up.  The
     usual call, tensors of just the shapes that dims say, is checked in one pass (one by
     one the checks take 1.3 us more)."""
     try:
@@ -387,7 +395,7 @@ def _args_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table,
         dev = torch.cuda.current_device()
         B, H_kv, D = dims.num_seqs, dims.num_kv_heads, dims.head_dim
         if (d[1] == heads and d[2] == D and d[0] >= (dims.num_q_rows if varlen else B) and dense1.shape == d
-                and k[1] == H_kv and k[2] == _Q4_TILE.get(D) and k[0] >= dims.num_pages and v_pages.shape == k
+                and k[1] == H_kv and k[2] == tile.get(D) and k[0] >= dims.num_pages and v_pages.shape == k
                 and w[1] == dims.max_pages_per_seq and w[0] >= B and context_lens.numel() >= B
                 and dense0.dtype is kind and dense1.dtype is kind and k_pages.dtype is u8 and v_pages.dtype is u8
                 and block_table.dtype is i32 and context_lens.dtype is i32
@@ -400,16 +408,16 @@ def _args_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table,
                     context_lens.data_ptr(), _take(query_start_loc, i32, B + 1, dev), dev)
     except (AttributeError, IndexError):  # (addresses, other ranks)
         pass
-    taken = _take_q4(dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc)
-    _fit_q4(dims, heads, dense0, dense1, k_pages, v_pages, block_table)
+    taken = _take_q(tile, dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc)
+    _fit_q(tile, dims, heads, dense0, dense1, k_pages, v_pages, block_table)
     return *taken, None
 
 
-def _workspace_q4(dims, workspace, q, stream):
+def _workspace_q(size_of, dims, workspace, q, stream):
     """(address, bytes, owner) of the caller's workspace or of a temporary one.  A
     tensor of another device than the current one, or not contiguous, is refused."""
     if workspace is None or workspace.__class__ is int:
-        ws, size = _workspace(dims, workspace, getattr(q, "device", None), stream, pa_workspace_size_q4)
+        ws, size = _workspace(dims, workspace, getattr(q, "device", None), stream, size_of)
         return _addr(ws), size, ws
     if _is_address(q):
         import torch
@@ -426,7 +434,7 @@ def _workspace_q4(dims, workspace, q, stream):
 def pa_kv_append_q4(k_new, v_new, block_table, context_lens, k_pages, v_pages, dims: PaDims, query_start_loc=None,
                     stream=None, check=True) -> int:
     """int pa_kv_append_q4(...): quantise the new tokens' K/V into the 4-bit pools."""
-    k, v, kp, vp, bt, cl, qsl, dev = _args_q4(dims, dims.num_kv_heads, query_start_loc is not None, k_new, v_new, k_pages,
+    k, v, kp, vp, bt, cl, qsl, dev = _args_q(_Q4_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_new, v_new, k_pages,
                                               v_pages, block_table, context_lens, query_start_loc)
     rc = load().pa_kv_append_q4(k, v, bt, cl, qsl, kp, vp, ctypes.byref(dims), _stream(stream, dev))
     if check and rc != PA_OK:
@@ -438,7 +446,7 @@ def pa_kv_read_q4(k_pages, v_pages, block_table, context_lens, k_out, v_out, dim
                   stream=None, check=True) -> int:
     """int pa_kv_read_q4(...): the values that the 4-bit pools hold of the rows
     which pa_kv_append_q4 with the same arguments writes."""
-    k, v, kp, vp, bt, cl, qsl, dev = _args_q4(dims, dims.num_kv_heads, query_start_loc is not None, k_out, v_out, k_pages,
+    k, v, kp, vp, bt, cl, qsl, dev = _args_q(_Q4_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_out, v_out, k_pages,
                                               v_pages, block_table, context_lens, query_start_loc)
     rc = load().pa_kv_read_q4(kp, vp, bt, cl, qsl, k, v, ctypes.byref(dims), _stream(stream, dev))
     if check and rc != PA_OK:
@@ -450,9 +458,9 @@ def paged_attn_q4(q, k_pages, v_pages, block_table, context_lens, scale, out, di
                   stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_q4(...): decode attention over the 4-bit cache; out is
     written in place."""
-    qa, oa, kp, vp, bt, cl, _, dev = _args_q4(dims, dims.num_q_heads, False, q, out, k_pages, v_pages, block_table,
+    qa, oa, kp, vp, bt, cl, _, dev = _args_q(_Q4_TILE, dims, dims.num_q_heads, False, q, out, k_pages, v_pages, block_table,
                                               context_lens, None)
-    ws, ws_bytes, owner = _workspace_q4(dims, workspace, q, stream)
+    ws, ws_bytes, owner = _workspace_q(pa_workspace_size_q4, dims, workspace, q, stream)
     rc = load().paged_attn_q4(qa, kp, vp, bt, cl, scale, oa, ctypes.byref(dims), ws, ws_bytes, _stream(stream, dev),
                               ctypes.byref(timing) if timing is not None else None)
     if check and rc != PA_OK:
@@ -464,13 +472,60 @@ def paged_attn_varlen_q4(q, k_pages, v_pages, block_table, context_lens, query_s
                          workspace=None, stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_varlen_q4(...): causal chunks plus decode rows over the
     4-bit cache."""
-    qa, oa, kp, vp, bt, cl, qsl, dev = _args_q4(dims, dims.num_q_heads, True, q, out, k_pages, v_pages, block_table,
+    qa, oa, kp, vp, bt, cl, qsl, dev = _args_q(_Q4_TILE, dims, dims.num_q_heads, True, q, out, k_pages, v_pages, block_table,
                                                 context_lens, query_start_loc)
-    ws, ws_bytes, owner = _workspace_q4(dims, workspace, q, stream)
+    ws, ws_bytes, owner = _workspace_q(pa_workspace_size_q4, dims, workspace, q, stream)
     rc = load().paged_attn_varlen_q4(qa, kp, vp, bt, cl, qsl, scale, oa, ctypes.byref(dims), ws, ws_bytes,
                                      _stream(stream, dev), ctypes.byref(timing) if timing is not None else None)
     if check and rc != PA_OK:
         raise PagedAttnError("paged_attn_varlen_q4", rc)
+    return rc
+
+
+def make_dims_q8(rows, k_pages, block_table, max_context_len, num_q_rows=0, max_q_len=0, num_seqs=None) -> PaDims:
+    """pa_dims_t of a call on the 8-bit cache from tensor shapes: rows
+    [rows][H][D] (q, or k_new / k_out of the append and the read), k_pages uint8
+    [N][H_kv][16 D], block_table [B][max_pages_per_seq]."""
+    _, H, D = rows.shape
+    N, H_kv, tile = k_pages.shape
+    B, width = block_table.shape
+    if PAGE_SIZE * D != tile:
+        raise ValueError(f"k_pages holds tiles of {tile} bytes, head_dim {D} takes {PAGE_SIZE * D}")
+    return PaDims(B if num_seqs is None else num_seqs, H, H_kv, D, PAGE_SIZE, N, width, int(max_context_len), 0,
+                  _dtype_code(rows), int(num_q_rows), int(max_q_len))
+
+
+def _scales_q8(dims, scales):
+    """Address of the scales, uint8 [num_pages][num_kv_heads][2]."""
+    if _is_address(scales):
+        return scales or None
+    import torch
+    shape = tuple(scales.shape)
+    if scales.dim() == 3 and shape[1:] != (dims.num_kv_heads, 2):
+        raise ValueError(f"scales of shape {shape} where dims say rows of {(dims.num_kv_heads, 2)}")
+    return _take(scales, torch.uint8, dims.num_pages * dims.num_kv_heads * 2, torch.cuda.current_device())
+
+
+def pa_kv_append_q8(k_new, v_new, block_table, context_lens, k_pages, v_pages, scales, dims: PaDims, query_start_loc=None,
+                    stream=None, check=True) -> int:
+    """int pa_kv_append_q8(...): quantise the new tokens' K/V into the 8-bit pools."""
+    k, v, kp, vp, bt, cl, qsl, dev = _args_q(_Q8_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_new, v_new,
+                                             k_pages, v_pages, block_table, context_lens, query_start_loc)
+    rc = load().pa_kv_append_q8(k, v, bt, cl, qsl, kp, vp, _scales_q8(dims, scales), ctypes.byref(dims), _stream(stream, dev))
+    if check and rc != PA_OK:
+        raise PagedAttnError("pa_kv_append_q8", rc)
+    return rc
+
+
+def pa_kv_read_q8(k_pages, v_pages, scales, block_table, context_lens, k_out, v_out, dims: PaDims, query_start_loc=None,
+                  stream=None, check=True) -> int:
+    """int pa_kv_read_q8(...): the values that the 8-bit pools hold of the rows
+    which pa_kv_append_q8 with the same arguments writes."""
+    k, v, kp, vp, bt, cl, qsl, dev = _args_q(_Q8_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_out, v_out,
+                                             k_pages, v_pages, block_table, context_lens, query_start_loc)
+    rc = load().pa_kv_read_q8(kp, vp, _scales_q8(dims, scales), bt, cl, qsl, k, v, ctypes.byref(dims), _stream(stream, dev))
+    if check and rc != PA_OK:
+        raise PagedAttnError("pa_kv_read_q8", rc)
     return rc
 
 

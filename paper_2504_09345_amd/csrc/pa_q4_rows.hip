@@ -6,74 +6,14 @@
 // rounding is the format's).  A lane's four bytes are one word of the K tile and four
 // bytes of the V tile, each in a word with those of three neighbouring tokens: a wave
 // takes four tokens and swaps the bytes in registers.  Reading mirrors it.
-#include "pa_device.h"
 #include "pa_q4_tile.h"
+#include "pa_q_rows.h"
 
 namespace pa {
 
 namespace {
 
-constexpr int kRowsWaves = kQRowsWaves;
 constexpr int kGroup = kQRowsGroup;
-
-// A wave's rows: those of one sequence that lie in four slots of a page from a multiple
-// of four on (a decode call's: one).
-struct Group {
-  int row, n;   // the first row, rows (0: none)
-  bool bad;     // rows that the contract does not allow
-  int page, token;  // token: of the first row
-};
-__device__ __forceinline__ Group group_of(const QRowsArgs& a, int slot, int lane) {
-  Group p{slot, 1, false, 0, 0};
-  int b = slot, L = 1, j = 0;
-  const int32_t* qsl = a.query_start_loc;
-  int C;
-  if (qsl != nullptr) {
-    // (a sequence of L rows has at most (L + 6) / 4 groups, which is what lies between
-    // its first slot and the next one's)
-    b = q4::wave_search(a.B, slot, lane, [&](int i) { return qsl[i] / kGroup + 2 * i; });
-    const int q0 = qsl[b];
-    L = qsl[b + 1] - q0;
-    C = a.context_lens[b];
-    const int before = C > L ? (C - L) % kGroup : 0;  // slots of the first group that are not the call's
-    const int at = (slot - q0 / kGroup - 2 * b) * kGroup - before;
-    j = max(max(at, 0), -q0);
-    p.row = q0 + j;
-    p.n = at < -before ? 0 : min(min(at + kGroup, L) - j, a.rows - p.row);
-  } else {
-    C = a.context_lens[b];
-    if (C == 0) p.n = 0;
-  }
-  if (p.n <= 0) return p;
-  const int pos = C - L + j;
-  p.bad = C < 0 || L > C || C > a.max_context_len || pos / kPage >= a.bt_stride;
-  if (p.bad) return p;
-  p.page = a.block_table[(int64_t)b * a.bt_stride + pos / kPage];
-  p.token = pos % kPage;
-  p.bad = p.page < 0 || p.page >= a.num_pages;
-  return p;
-}
-
-// x[t] with bytes m -> x[m] with bytes t.
-__device__ __forceinline__ void transpose4(uint32_t (&x)[4]) {
-  const uint32_t a = __builtin_amdgcn_perm(x[1], x[0], 0x05010400u), b = __builtin_amdgcn_perm(x[1], x[0], 0x07030602u);
-  const uint32_t c = __builtin_amdgcn_perm(x[3], x[2], 0x05010400u), d = __builtin_amdgcn_perm(x[3], x[2], 0x07030602u);
-  x[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
-  x[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
-  x[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
-  x[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
-}
-
-template <typename T>
-__device__ __forceinline__ void load_eight(const T* p, float (&x)[8]) {
-  if constexpr (sizeof(T) == 2) {
-    widen(*reinterpret_cast<const u32x4*>(p), x, uint16_t());
-  } else {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(p), b = *reinterpret_cast<const u32x4*>(p + 4);
-    widen(a, x, 0.0f);
-    widen(b, x + 4, 0.0f);
-  }
-}
 
 // Codes (a byte per pair) of a lane's eight elements and their block's scale byte.
 __device__ __forceinline__ uint32_t quantise(const float (&x)[8], uint32_t& scale) {
@@ -123,7 +63,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(QRowsArgs a,
   const int lane = threadIdx.x & 63;
   const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (slot >= slots) return;
-  const Group p = group_of(a, slot, lane);
+  const Group p = group_of<kGroup>(a, slot, lane);
   if (p.n <= 0 || p.bad) return;
   const int i = blockIdx.y * 64 + lane;
   if (i >= a.H_kv * CH) return;
@@ -175,23 +115,14 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q4_append_kernel(QRowsArgs a,
 }
 
 // The values of a lane's codes, 16 bytes of them: a word's eight or a half's four.
-// kPast: past the caches.
 template <bool kPast, typename T>
 __device__ __forceinline__ void put(T* p, uint32_t w, uint32_t scale) {
   const float s = __uint_as_float(scale << 23);
-  auto store = [&](const auto& x) {
-    auto* to = reinterpret_cast<std::remove_const_t<std::remove_reference_t<decltype(x)>>*>(p);
-    if constexpr (kPast) {
-      __builtin_nontemporal_store(x, to);
-    } else {
-      *to = x;
-    }
-  };
   if constexpr (sizeof(T) == 2) {
-    store(q4::eight_of(w, s));
+    store_row<kPast>(p, q4::eight_of(w, s));
   } else {
     const q4::f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
-    store(q4::f32x4_t{a[0], a[1], b[0], b[1]});
+    store_row<kPast>(p, q4::f32x4_t{a[0], a[1], b[0], b[1]});
   }
 }
 
@@ -207,7 +138,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q4_read_kernel(QRowsArgs a, i
   const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = blockIdx.y * 64 + lane;
   if (slot >= slots) return;
-  const Group p = group_of(a, slot, lane);
+  const Group p = group_of<kGroup>(a, slot, lane);
   if (p.n <= 0 || i >= a.H_kv * CH) return;
   const int g = i / CH, c = i % CH >> kHalf, half = kHalf ? i & 1 : 0, first = p.token & ~(kGroup - 1);
   // (all four tokens of the group, whichever are asked for)
@@ -238,23 +169,6 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q4_read_kernel(QRowsArgs a, i
     put<kPast>(v_out + r * step, v[t], vs[t]);
   }
 }
-
-// fn(element, head dim), by type.
-template <typename Fn>
-hipError_t by_type(int dtype, int D, const QRowsArgs& a, Fn fn) {
-  if (a.rows == 0) return hipSuccess;
-  if (dtype == 0 && D == 128) fn(uint16_t(), std::integral_constant<int, 128>{});
-  else if (dtype == 0 && D == 64) fn(uint16_t(), std::integral_constant<int, 64>{});
-  else if (dtype == 1 && D == 128) fn(float(), std::integral_constant<int, 128>{});
-  else if (dtype == 1 && D == 64) fn(float(), std::integral_constant<int, 64>{});
-  else return hipErrorInvalidValue;
-  return hipGetLastError();
-}
-
-// Outputs of more bytes than the last-level cache has are stored past the caches, where
-// no reader would find them.  (336 MB in fp32 61 us and 85, in bf16 68 and 99, 208 us and
-// 218 with a copy of them after; 66 MB in fp32 13 and 14, but 39 and 35 with the copy.)
-constexpr int64_t kCached = 256 << 20;
 
 // Slots of a call (group_of; checked to be 32-bit).
 int slots_of(const QRowsArgs& a) { return (int)q_row_slots(a.query_start_loc != nullptr, a.rows, a.B); }

@@ -1,0 +1,288 @@
+// The 8-bit cache's write and read of rows (format in pagedattn_q8.h).
+//
+// Writing: a page's scale is that of its largest value, so a wave takes a page's new rows
+// whole, for 64 / (D / 8) KV heads: D / 8 lanes of 8 dims each to a head.  The largest
+// magnitude over the rows and then the lanes (DPP), the exponent from its bits, v_cvt_pk_fp8_f32
+// to codes (its rounding is the format's).  Where the page holds earlier tokens and their
+// scale is too small, the same lanes round those again: a power of two apart, their values
+// are exact in fp32.  K and V are waves of their own.
+// A lane's eight bytes of a token are eight in a row of the K tile; in the V tile they lie
+// in eight words, each with the bytes of four tokens, swapped in registers where all four
+// are new.  Reading mirrors it, four tokens a wave.
+#include "pa_q_rows.h"
+#include "pa_q8_tile.h"
+
+namespace pa {
+namespace {
+
+constexpr int kLow = 17, kHigh = 246;  // scale bytes
+
+template <int D>
+struct Place {  // of a lane's chunk c of eight dims
+  static __device__ __forceinline__ int k(int token, int c) { return ((c >> 1) * kPage + token) * 16 + (c & 1) * 8; }
+  // of the words of dims 8 c + 2 m and + 1, tokens 4 t ..
+  static __device__ __forceinline__ int v(int t, int c, int m) {
+    return (c >> 3) * 1024 + (t * 16 + (c & 3) * 4 + m) * 16 + (c >> 2 & 1) * 8;
+  }
+};
+
+__device__ __forceinline__ float power(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+
+// Two codes (a half of w) from values that e4m3 holds or rounds to at most 448.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t codes_of(uint32_t w, float a, float b) {
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)w, HIGH);
+}
+// The codes of x times inv.
+__device__ __forceinline__ u32x2_t encode(const float (&x)[8], float inv) {
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    // (infinities too are held as NaN)
+    y[e] = fabsf(x[e]) <= __FLT_MAX__ ? __builtin_amdgcn_fmed3f(x[e] * inv, -448.0f, 448.0f) : NAN;
+  }
+  u32x2_t w = {0, 0};
+  w.x = codes_of<false>(w.x, y[0], y[1]);
+  w.x = codes_of<true>(w.x, y[2], y[3]);
+  w.y = codes_of<false>(w.y, y[4], y[5]);
+  w.y = codes_of<true>(w.y, y[6], y[7]);
+  return w;
+}
+// Four codes rounded again, f (a power of two below 1) times their values.
+__device__ __forceinline__ uint32_t again(uint32_t w, float f) {
+  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  return codes_of<true>(codes_of<false>(0, a[0] * f, a[1] * f), b[0] * f, b[1] * f);
+}
+
+// The largest finite magnitude's bits, of m and x.
+__device__ __forceinline__ uint32_t most_of(uint32_t m, const float (&x)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t u = __float_as_uint(x[e]) & 0x7fffffffu;
+    m = max(m, u < 0x7f800000u ? u : 0u);
+  }
+  return m;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(64 * kRowsWaves) void q8_append_kernel(QRowsArgs a, int slots) {
+  constexpr int CH = D / 8;
+  const int lane = threadIdx.x & 63;
+  const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (slot >= slots) return;
+  const Group p = group_of<kPage>(a, slot, lane);
+  if (p.n <= 0 || p.bad) return;
+  const int i = blockIdx.y * 64 + lane, which = blockIdx.z;
+  if (i >= a.H_kv * CH) return;  // (whole heads)
+  const int g = i / CH, c = i % CH;
+  const int64_t step = (int64_t)a.H_kv * D;
+  const T* from = reinterpret_cast<const T*>(which == 0 ? a.k_rows : a.v_rows) + (int64_t)p.row * step + (int64_t)i * 8;
+  const int64_t head = (int64_t)p.page * a.H_kv + g;
+  uint8_t* tile = (which == 0 ? a.k_pages : a.v_pages) + head * q8_tile_bytes(D);
+  uint8_t* scale = a.scales + head * 2 + which;
+  const int held = p.token > 0 ? *scale : 0;  // (no earlier tokens: none that bounds it)
+
+  // The page's scale, given the largest of the lane's new values; the earlier tokens are
+  // brought to it.  Its inverse.
+  auto settle = [&](uint32_t most) {
+    float m = __uint_as_float(most);
+    m = fmaxf(m, dpp_xor1(m));
+    m = fmaxf(m, dpp_xor2(m));
+    m = fmaxf(m, dpp_half_mirror(m));
+    if constexpr (CH == 16) m = fmaxf(m, dpp_mirror(m));
+    // the exponent's byte less 8, or 7 above 1.75 (a carry out of the mantissa)
+    const int need = min(max((int)((__float_as_uint(m) + 0x1fffffu) >> 23) - 8, kLow), kHigh);
+    const int e = max(need, held);
+    if (p.token > 0 && e > held) {
+      const float f = power(127 + max(held - e, -64));  // (2^-64 of any code is 0)
+      if (which == 0) {
+        for (int t = 0; t < p.token; ++t) {
+          u32x2_t* at = reinterpret_cast<u32x2_t*>(tile + Place<D>::k(t, c));
+          const u32x2_t w = *at;
+          *at = u32x2_t{again(w.x, f), again(w.y, f)};
+        }
+      } else {
+        for (int t = 0; t * 4 < p.token; ++t) {
+          const uint32_t early = p.token - 4 * t >= 4 ? ~0u : (1u << 8 * (p.token - 4 * t)) - 1;  // bytes
+#pragma unroll
+          for (int m4 = 0; m4 < 4; ++m4) {
+            u32x2_t* at = reinterpret_cast<u32x2_t*>(tile + Place<D>::v(t, c, m4));
+            const u32x2_t w = *at;
+            *at = u32x2_t{(again(w.x, f) & early) | (w.x & ~early), (again(w.y, f) & early) | (w.y & ~early)};
+          }
+        }
+      }
+    }
+    if (c == 0 && (p.token == 0 || e > held)) *scale = (uint8_t)e;
+    return power(254 - e);
+  };
+  auto put_v = [&](int t, u32x2_t w) {  // a token's bytes alone
+#pragma unroll
+    for (int m4 = 0; m4 < 4; ++m4) {
+      uint8_t* at = tile + Place<D>::v(t >> 2, c, m4) + (t & 3);
+      const uint32_t pair = (m4 < 2 ? w.x : w.y) >> 16 * (m4 & 1);
+      at[0] = (uint8_t)pair;
+      at[4] = (uint8_t)(pair >> 8);
+    }
+  };
+
+  if (p.n == 1) {
+    float x[8];
+    load_eight(from, x);
+    const u32x2_t w = encode(x, settle(most_of(0, x)));
+    if (which == 0) *reinterpret_cast<u32x2_t*>(tile + Place<D>::k(p.token, c)) = w;
+    else put_v(p.token, w);
+    return;
+  }
+  // all 16 tokens of the page, whichever are new (the others: a new row again, unused)
+  u32x4 raw[kPage][sizeof(T) / 2];
+#pragma unroll
+  for (int t = 0; t < kPage; ++t) {
+    const T* row = from + min(max(t - p.token, 0), p.n - 1) * step;
+#pragma unroll
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) raw[t][h] = *reinterpret_cast<const u32x4*>(row + h * 4);
+  }
+  auto widened = [&](int t, float (&x)[8]) {
+    if constexpr (sizeof(T) == 2) {
+      widen(raw[t][0], x, uint16_t());
+    } else {
+      widen(raw[t][0], x, 0.0f);
+      widen(raw[t][1], x + 4, 0.0f);
+    }
+  };
+  uint32_t most = 0;
+#pragma unroll
+  for (int t = 0; t < kPage; ++t) {
+    float x[8];
+    widened(t, x);
+    most = most_of(most, x);
+  }
+  const float inv = settle(most);
+  const int first = p.token, end = p.token + p.n;
+#pragma unroll
+  for (int t4 = 0; t4 < kPage / 4; ++t4) {
+    if (4 * t4 + 4 <= first || 4 * t4 >= end) continue;  // (wave-uniform, as those below)
+    uint32_t lo[4], hi[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      float x[8];
+      widened(4 * t4 + t, x);
+      const u32x2_t w = encode(x, inv);
+      lo[t] = w.x;
+      hi[t] = w.y;
+    }
+    const bool whole = 4 * t4 >= first && 4 * t4 + 4 <= end;
+    if (which == 0) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (4 * t4 + t >= first && 4 * t4 + t < end)
+          *reinterpret_cast<u32x2_t*>(tile + Place<D>::k(4 * t4 + t, c)) = u32x2_t{lo[t], hi[t]};
+    } else if (whole) {
+      transpose4(lo);
+      transpose4(hi);
+#pragma unroll
+      for (int m4 = 0; m4 < 4; ++m4) {
+        const int o = m4 % 2 * 2;
+        *reinterpret_cast<u32x2_t*>(tile + Place<D>::v(t4, c, m4)) = m4 < 2 ? u32x2_t{lo[o], lo[o + 1]} : u32x2_t{hi[o], hi[o + 1]};
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (4 * t4 + t >= first && 4 * t4 + t < end) put_v(4 * t4 + t, u32x2_t{lo[t], hi[t]});
+    }
+  }
+}
+
+// The values of a lane's codes, 16 bytes of them: eight codes or (fp32) w.x's four.
+template <bool kPast, typename T>
+__device__ __forceinline__ void put(T* p, u32x2_t w, float scale) {
+  if constexpr (sizeof(T) == 2) {
+    store_row<kPast>(p, u32x4{q8::pair_of<0, false>(w.x, scale), q8::pair_of<1, false>(w.x, scale), q8::pair_of<0, false>(w.y, scale),
+                              q8::pair_of<1, false>(w.y, scale)});
+  } else {
+    const q::f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, scale, true);
+    store_row<kPast>(p, q::f32x4_t{a[0], a[1], b[0], b[1]});
+  }
+}
+
+// A wave reads a group's tokens for 64 (KV head, 16 bytes of the output): its stores are
+// a KiB in a row each.
+template <typename T, int D, bool kPast>
+__global__ __launch_bounds__(64 * kRowsWaves) void q8_read_kernel(QRowsArgs a, int slots) {
+  constexpr int kGroup = kQRowsGroup;
+  constexpr int kHalf = sizeof(T) == 4;  // four dims a lane
+  constexpr int CH = D / 8 << kHalf;
+  const int lane = threadIdx.x & 63;
+  const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = blockIdx.y * 64 + lane;
+  if (slot >= slots) return;
+  const Group p = group_of<kGroup>(a, slot, lane);
+  if (p.n <= 0 || i >= a.H_kv * CH) return;
+  const int g = i / CH, c = i % CH >> kHalf, half = kHalf ? i & 1 : 0, first = p.token & ~(kGroup - 1);
+  // (all four tokens of the group, whichever are asked for)
+  u32x2_t k[kGroup], v[kGroup];
+  float ks = 1.0f, vs = 1.0f;
+  if (!p.bad) {
+    const int64_t head = (int64_t)p.page * a.H_kv + g, tile = head * q8_tile_bytes(D);
+    const uint32_t sc = *reinterpret_cast<const uint16_t*>(a.scales + head * 2);
+    ks = q::scale_of<0>(sc);
+    vs = q::scale_of<1>(sc);
+    uint32_t lo[4], hi[4] = {};
+#pragma unroll
+    for (int t = 0; t < kGroup; ++t) {
+      const uint8_t* at = a.k_pages + tile + Place<D>::k(first + t, c);
+      if constexpr (kHalf) k[t] = u32x2_t{*reinterpret_cast<const uint32_t*>(at + 4 * half), 0};
+      else k[t] = *reinterpret_cast<const u32x2_t*>(at);
+    }
+#pragma unroll
+    for (int m = 0; m < (kHalf ? 2 : 4); ++m) {
+      const u32x2_t w = *reinterpret_cast<const u32x2_t*>(a.v_pages + tile + Place<D>::v(first >> 2, c, 2 * half + m));
+      (m < 2 ? lo : hi)[m % 2 * 2] = w.x;
+      (m < 2 ? lo : hi)[m % 2 * 2 + 1] = w.y;
+    }
+    transpose4(lo);
+    if constexpr (!kHalf) transpose4(hi);
+#pragma unroll
+    for (int t = 0; t < kGroup; ++t) v[t] = u32x2_t{lo[t], hi[t]};
+  } else {
+#pragma unroll
+    for (int t = 0; t < kGroup; ++t) k[t] = v[t] = u32x2_t{0x7f7f7f7fu, 0x7f7f7f7fu};
+  }
+  const int64_t to = (int64_t)p.row * a.H_kv * D + (int64_t)i * (16 / sizeof(T)), step = (int64_t)a.H_kv * D;
+  T* k_out = reinterpret_cast<T*>(const_cast<void*>(a.k_rows)) + to;
+  T* v_out = reinterpret_cast<T*>(const_cast<void*>(a.v_rows)) + to;
+#pragma unroll
+  for (int t = 0; t < kGroup; ++t) {
+    const int r = first + t - p.token;  // (wave-uniform)
+    if (r < 0 || r >= p.n) continue;
+    put<kPast>(k_out + r * step, k[t], ks);
+    put<kPast>(v_out + r * step, v[t], vs);
+  }
+}
+
+// Slots of a call (group_of; checked to be 32-bit).
+int slots_of(const QRowsArgs& a, int group) { return (int)q_row_slots(a.query_start_loc != nullptr, a.rows, a.B, group); }
+
+}  // namespace
+
+hipError_t launch_q8_append(int dtype, int D, const QRowsArgs& a, hipStream_t st) {
+  return by_type(dtype, D, a, [&](auto t, auto d) {
+    constexpr int D = decltype(d)::value;
+    const int slots = slots_of(a, kPage);
+    const dim3 grid((slots + kRowsWaves - 1) / kRowsWaves, (a.H_kv * (D / 8) + 63) / 64, 2);
+    q8_append_kernel<decltype(t), D><<<grid, 64 * kRowsWaves, 0, st>>>(a, slots);
+  });
+}
+
+hipError_t launch_q8_read(int dtype, int D, const QRowsArgs& a, hipStream_t st) {
+  return by_type(dtype, D, a, [&](auto t, auto d) {
+    const int slots = slots_of(a, kQRowsGroup);
+    const dim3 grid((slots + kRowsWaves - 1) / kRowsWaves, (a.H_kv * D * (int)sizeof(t) / 16 + 63) / 64);
+    const bool past = (int64_t)2 * a.rows * a.H_kv * D * sizeof(t) > kCached;
+    constexpr int D = decltype(d)::value;
+    const auto fn = past ? &q8_read_kernel<decltype(t), D, true> : &q8_read_kernel<decltype(t), D, false>;
+    fn<<<grid, 64 * kRowsWaves, 0, st>>>(a, slots);
+  });
+}
+
+}  // namespace pa
