@@ -83,6 +83,50 @@ int pa_kv_read_q8(const void *k_pages, const void *v_pages, const uint8_t *scale
                   const int32_t *query_start_loc, void *k_out, void *v_out, const pa_dims_t *dims,
                   hipStream_t stream);
 
+/* Bytes of device workspace that a paged_attn_q8 / paged_attn_varlen_q8 call with
+ * these dims needs, 64 MiB and an alignment at most.  A call whose dims carry chunked
+ * rows (max_q_len > 1 or num_q_rows != num_seqs) is sized as varlen.  Host only; no HIP
+ * call. */
+int pa_workspace_size_q8(const pa_dims_t *dims, size_t *bytes);
+
+/* Decode attention over the 8-bit cache: paged_attn with 8-bit pools.  Products are
+ * formed from the values that the cache stands for, without rounding those, on the
+ * matrix cores with fp32 accumulation; softmax bases and sums are fp32, and so are the
+ * scores: scale q.k log2 e may be up to 2^27 in magnitude (its steps there are 8; beyond,
+ * an output may be NaN).  Queries:
+ * bf16 ones as they are, except at head_dim 128, where a query is two e4m3 parts of
+ * its row's scale (an error of at most 2^-22 of the row's largest, or 2^-135); fp32 ones as
+ * sums of three bf16 parts.  Softmax weights: for bf16 outputs in fp16 where every V
+ * of the step is exact in fp16 (scales 2^-15 .. 2^7) and as two bf16 parts elsewhere,
+ * for fp32 outputs as three bf16 parts.  Weighted sums do not overflow: an output is
+ * finite wherever the weighted mean is.  (A row that sees a page whose V has a scale of
+ * 2^56 or more loses what V below 2^-78 beside it would add.)  The same inputs give the
+ * same bits.
+ * GQA group size num_q_heads / num_kv_heads in {1, 2, 4, 6, 8}.  A row that sees
+ * no key (context 0) is zeros; a row of a context above max_context_len, or that
+ * sees a page entry outside [0, num_pages), is NaN.  q and out are 16-byte
+ * aligned.
+ * Errors: PA_EINVAL, PA_ENOTSUP, PA_ENOSPC, PA_EHIP. */
+int paged_attn_q8(const void *q, const void *k_pages, const void *v_pages, const uint8_t *scales,
+                  const int32_t *block_table, const int32_t *context_lens, float scale, void *out,
+                  const pa_dims_t *dims, void *workspace, size_t workspace_bytes,
+                  hipStream_t stream, const pa_timing_t *timing);
+
+/* Causal chunks and decode rows in one call over the 8-bit cache:
+ * paged_attn_varlen with 8-bit pools.  Row j of a chunk of length L in a context C
+ * attends to positions 0 .. C - L + j; keys that a row does not see never reach
+ * it, whatever they hold (NaN included), though they share their page's scale.  Rows of a
+ * chunk longer than its
+ * context or than max_q_len are NaN, rows of no sequence are left as they were.
+ * max_context_len, beside bounding the contexts, decides how the chunks' work is divided,
+ * so it should be no larger than they need.
+ * Errors: PA_EINVAL, PA_ENOTSUP, PA_ENOSPC, PA_EHIP. */
+int paged_attn_varlen_q8(const void *q, const void *k_pages, const void *v_pages,
+                         const uint8_t *scales, const int32_t *block_table,
+                         const int32_t *context_lens, const int32_t *query_start_loc, float scale,
+                         void *out, const pa_dims_t *dims, void *workspace,
+                         size_t workspace_bytes, hipStream_t stream, const pa_timing_t *timing);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,7 +27,8 @@ EXPORTED = ("pa_workspace_size", "paged_attn", "paged_attn_varlen", "paged_attn_
             "pa_kv_append", "pa_schedule_step", "pa_perf_model", "pa_read_probe", "pa_issue_probe",
             "pa_strerror",
             "pa_q4_tile_bytes", "pa_kv_append_q4", "pa_kv_read_q4", "pa_workspace_size_q4", "paged_attn_q4",
-            "paged_attn_varlen_q4", "pa_kv_append_q8", "pa_kv_read_q8")
+            "paged_attn_varlen_q4", "pa_kv_append_q8", "pa_kv_read_q8", "pa_workspace_size_q8", "paged_attn_q8",
+            "paged_attn_varlen_q8")
 
 
 class PaDims(ctypes.Structure):
@@ -136,8 +137,12 @@ def load():
     lib.paged_attn_varlen_q4.argtypes = [P, P, P, P, P, P, ctypes.c_float, P, DP, P, SZ, P, TP]
     lib.pa_kv_append_q8.argtypes = [P, P, P, P, P, P, P, P, DP, P]
     lib.pa_kv_read_q8.argtypes = [P, P, P, P, P, P, P, P, DP, P]
+    lib.pa_workspace_size_q8.argtypes = [DP, ctypes.POINTER(SZ)]
+    lib.paged_attn_q8.argtypes = [P, P, P, P, P, P, ctypes.c_float, P, DP, P, SZ, P, TP]
+    lib.paged_attn_varlen_q8.argtypes = [P, P, P, P, P, P, P, ctypes.c_float, P, DP, P, SZ, P, TP]
     for name in ("pa_q4_tile_bytes", "pa_kv_append_q4", "pa_kv_read_q4", "pa_workspace_size_q4", "paged_attn_q4",
-                 "paged_attn_varlen_q4", "pa_kv_append_q8", "pa_kv_read_q8"):
+                 "paged_attn_varlen_q4", "pa_kv_append_q8", "pa_kv_read_q8", "pa_workspace_size_q8", "paged_attn_q8",
+                 "paged_attn_varlen_q8"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -526,6 +531,42 @@ def pa_kv_read_q8(k_pages, v_pages, scales, block_table, context_lens, k_out, v_
     rc = load().pa_kv_read_q8(kp, vp, _scales_q8(dims, scales), bt, cl, qsl, k, v, ctypes.byref(dims), _stream(stream, dev))
     if check and rc != PA_OK:
         raise PagedAttnError("pa_kv_read_q8", rc)
+    return rc
+
+
+def pa_workspace_size_q8(dims: PaDims) -> int:
+    n = ctypes.c_size_t(0)
+    rc = load().pa_workspace_size_q8(ctypes.byref(dims), ctypes.byref(n))
+    if rc != PA_OK:
+        raise PagedAttnError("pa_workspace_size_q8", rc)
+    return int(n.value)
+
+
+def paged_attn_q8(q, k_pages, v_pages, scales, block_table, context_lens, scale, out, dims: PaDims, workspace=None,
+                  stream=None, timing: PaTiming | None = None, check=True) -> int:
+    """int paged_attn_q8(...): decode attention over the 8-bit cache; out is
+    written in place."""
+    qa, oa, kp, vp, bt, cl, _, dev = _args_q(_Q8_TILE, dims, dims.num_q_heads, False, q, out, k_pages, v_pages, block_table,
+                                             context_lens, None)
+    ws, ws_bytes, owner = _workspace_q(pa_workspace_size_q8, dims, workspace, q, stream)
+    rc = load().paged_attn_q8(qa, kp, vp, _scales_q8(dims, scales), bt, cl, scale, oa, ctypes.byref(dims), ws, ws_bytes,
+                              _stream(stream, dev), ctypes.byref(timing) if timing is not None else None)
+    if check and rc != PA_OK:
+        raise PagedAttnError("paged_attn_q8", rc)
+    return rc
+
+
+def paged_attn_varlen_q8(q, k_pages, v_pages, scales, block_table, context_lens, query_start_loc, scale, out, dims: PaDims,
+                         workspace=None, stream=None, timing: PaTiming | None = None, check=True) -> int:
+    """int paged_attn_varlen_q8(...): causal chunks plus decode rows over the
+    8-bit cache."""
+    qa, oa, kp, vp, bt, cl, qsl, dev = _args_q(_Q8_TILE, dims, dims.num_q_heads, True, q, out, k_pages, v_pages, block_table,
+                                               context_lens, query_start_loc)
+    ws, ws_bytes, owner = _workspace_q(pa_workspace_size_q8, dims, workspace, q, stream)
+    rc = load().paged_attn_varlen_q8(qa, kp, vp, _scales_q8(dims, scales), bt, cl, qsl, scale, oa, ctypes.byref(dims), ws,
+                                     ws_bytes, _stream(stream, dev), ctypes.byref(timing) if timing is not None else None)
+    if check and rc != PA_OK:
+        raise PagedAttnError("paged_attn_varlen_q8", rc)
     return rc
 
 

@@ -357,7 +357,7 @@ struct Format {
     q4::fold_pv_edge<T, D, NB>(st, u, x, key0, lane);
   }
   // A workgroup that shares V (pa_q_chunk.h): K alone, as all of its waves need it; V's
-  // scales of a unit; a wave's part of V.
+  // scales of a unit; V with its scales; a wave's part of V.
   template <int D>
   static __device__ __forceinline__ void load_k_shared(Unit<D>& u, int p, const uint8_t* pool, int64_t at, const uint8_t*, int bytes, int lane) {
     // (The scale bytes alone, although that waits for K here, behind the present unit's
@@ -374,12 +374,16 @@ struct Format {
     load_words<D, 0>(r, kScales<D> + (lane >> 4) * (D / 8), u.vs[p]);
   }
   template <int D>
+  static __device__ __forceinline__ void load_v_whole(Unit<D>& u, int p, const uint8_t* pool, int64_t at, const uint8_t*, int bytes, int lane) {
+    q4::load_v<D, 0>(u, p, pool + at, bytes, lane);
+  }
+  template <int D>
   static __device__ __forceinline__ void load_part(Part<D>& t, const uint8_t* pool, int64_t at, const uint8_t*, int jb, int bytes, int lane) {
     q4::load_part<D>(t, pool + at, jb, bytes, lane);
   }
   // (edge: of the unit's keys, some are seen by a part of the workgroup's columns)
   template <int D, typename Flag, typename Store>
-  static __device__ __forceinline__ void convert_part(const Part<D>& t, int jb, int key0, int all_last, bool edge, Flag flag, Store store) {
+  static __device__ __forceinline__ void convert_part(const Part<D>& t, int jb, int key0, int all_last, bool edge, int lane, Flag flag, Store store) {
     q4::convert_part<D>(t, jb, key0, all_last, flag, store);
   }
 };

@@ -26,4 +26,25 @@ int pa_kv_read_q8(const void* k_pages, const void* v_pages, const uint8_t* scale
                        dims, stream, pa::launch_q8_read);
 }
 
+int pa_workspace_size_q8(const pa_dims_t* dims, size_t* bytes) {
+  return pa::workspace_bytes_of(dims, bytes);
+}
+
+int paged_attn_q8(const void* q, const void* k_pages, const void* v_pages, const uint8_t* scales, const int32_t* block_table,
+                  const int32_t* context_lens, float scale, void* out, const pa_dims_t* dims, void* workspace,
+                  size_t workspace_bytes, hipStream_t stream, const pa_timing_t* timing) {
+  if (misaligned2(scales)) return PA_EINVAL;
+  return pa::attend<pa::q8::Format>(q, {k_pages, v_pages, scales, block_table, context_lens, nullptr}, true, scale, out, dims,
+                                    workspace, workspace_bytes, stream, timing, false);
+}
+
+int paged_attn_varlen_q8(const void* q, const void* k_pages, const void* v_pages, const uint8_t* scales,
+                         const int32_t* block_table, const int32_t* context_lens, const int32_t* query_start_loc, float scale,
+                         void* out, const pa_dims_t* dims, void* workspace, size_t workspace_bytes, hipStream_t stream,
+                         const pa_timing_t* timing) {
+  if (misaligned2(scales)) return PA_EINVAL;
+  return pa::attend<pa::q8::Format>(q, {k_pages, v_pages, scales, block_table, context_lens, query_start_loc}, true, scale, out, dims,
+                                    workspace, workspace_bytes, stream, timing, true);
+}
+
 }  // extern "C"

@@ -105,7 +105,7 @@ void q_chunk_kernel(QAttnArgs a) {
   };
   auto convert = [&](int k) {
     const int buf = k & 1;
-    F::convert_part(part, jb, k * kQUnit + 16 * vp + 4 * G, all_last, k >= edge,
+    F::convert_part(part, jb, k * kQUnit + 16 * vp + 4 * G, all_last, k >= edge, lane,
                     [&](bool odd) {
                       const bool any_odd = __builtin_amdgcn_ballot_w64(odd) != 0;
                       if (lane == 0) s_odd[buf][w] = any_odd;
@@ -208,7 +208,7 @@ void q_chunk_kernel(QAttnArgs a) {
       if (__builtin_expect(odd | st.any_lifted, 0)) {
         typename F::template Unit<D> whole;
 #pragma unroll
-        for (int p = 0; p < 2; ++p) F::template load_v<0>(whole, p, vg, t.at[p], sg, tile_size, lane);
+        for (int p = 0; p < 2; ++p) F::load_v_whole(whole, p, vg, t.at[p], sg, tile_size, lane);
         F::clear_dead(whole, k * kQUnit, all_last, lane);
         F::fold_pv_edge(st, whole, x, k * kQUnit, lane);
       } else {

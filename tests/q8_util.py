@@ -68,6 +68,47 @@ class Batch(Q4Batch):
         pb.pa_kv_read_q8(d["k"], d["v"], d["scales"], d["bt"], d["cl"], out[0], out[1], self.dims(d, out[0], **kw), query_start_loc=d["qsl"])
         return out.float().cpu().numpy()
 
+    def attend(self, d, dims=None, out=None, **kw):
+        """The call's output, a device tensor (NaN where it wrote nothing)."""
+        import torch
+        out = torch.full_like(d["q"], float("nan")) if out is None else out
+        dims = self.dims(d) if dims is None else dims
+        pool = (d["k"], d["v"], d["scales"], d["bt"], d["cl"])
+        if self.qsl is None:
+            pb.paged_attn_q8(d["q"], *pool, self.scale, out, dims, **kw)
+        else:
+            pb.paged_attn_varlen_q8(d["q"], *pool, d["qsl"], self.scale, out, dims, **kw)
+        return out
+
+    def expected(self):
+        """(out, spread, mass, size, reach) as oracle.q4.attention's, a sequence's rows and
+        keys at once, in float64 on the GPU.  A NaN of V reaches the rows that see it, in its
+        dim; of K, the whole of those rows."""
+        import torch
+        s = self.H_q // self.H_kv
+        res = [np.zeros(self.q.shape) for _ in range(3)] + [np.zeros(self.q.shape[:2]) for _ in range(2)]
+        for b, C in enumerate(int(c) for c in self.ctx):
+            r0, L = (b, 1) if self.qsl is None else (int(self.qsl[b]), self.n_rows[b])
+            if L == 0 or C == 0:
+                continue
+            k, v = (torch.from_numpy(q8.dense(w, p, self.scales, self.bt, b, C, self.D)).cuda() for w, p in (("k", self.k), ("v", self.v)))
+            q = torch.from_numpy(self.q[r0:r0 + L].astype(np.float64)).cuda()
+            seen = torch.arange(C, device="cuda")[None, :] <= torch.arange(C - L, C, device="cuda")[:, None]
+            for h in range(self.H_q):
+                kt, vh = k[h // s].t().contiguous(), v[h // s].contiguous()
+                x = (self.scale * torch.matmul(q[:, h].contiguous(), kt)).masked_fill(~seen, -torch.inf)
+                w = torch.softmax(x, -1)
+                odd = torch.matmul(seen.double(), vh.isnan().double()) > 0
+                vh, kt = vh.nan_to_num(0.0), kt.nan_to_num(0.0)
+                size = (self.scale * torch.matmul(q[:, h].abs().contiguous(), kt.abs())).masked_fill(~seen, 0).amax(-1)
+                reach = self.scale * q[:, h].abs().amax(-1) * (seen * kt.abs().sum(0)).amax(-1)
+                out = torch.matmul(w, vh).masked_fill(odd, torch.nan)
+                for to, what in zip(res, (out, torch.matmul(w, vh.abs()), torch.matmul(seen.double(), vh.abs()), size, reach)):
+                    to[r0:r0 + L, h] = what.cpu().numpy()
+        return res
+
+    expected_gpu = expected
+
     def new_rows(self, seed, odd=False):
         """Rows of widely different sizes, as the call's type holds them."""
         rng = np.random.default_rng(seed)
