@@ -367,6 +367,8 @@ struct Format {
     load_words<D, 0>(r, lane * (D / 8), u.k[p]);
     u.ks[p] = __builtin_amdgcn_raw_buffer_load_b8(r, kScales<D> + (lane & 15) * (D / 32) + (lane >> 4) * D / 128, 0, 0);
   }
+  static constexpr bool kSharedK = false;  // (into each wave's registers)
+  template <int D> struct SharedK {};
   template <int D>
   static __device__ __forceinline__ void load_scales(Unit<D>& u, int p, const uint8_t* pool, int64_t at, const uint8_t*, int bytes, int lane) {
     const __amdgpu_buffer_rsrc_t r =

@@ -167,6 +167,7 @@ __device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, co
       }
 #pragma unroll
     for (int mb = 0; mb < D / 16; ++mb) {
+      __builtin_amdgcn_sched_barrier(0);
       u32x4 a;
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
@@ -244,9 +245,35 @@ struct Format {
     q8::fold_pv_edge<T, D, NB>(st, u, x, key0, lane);
   }
 
+  // (K of a unit takes 16 registers of a wave from its load on, which with 32 columns'
+  // queries and outputs are too many at head_dim 128: the queries moved to scratch memory,
+  // whose loads wait behind K's.)
+  static constexpr bool kSharedK = true;
   template <int D>
-  static __device__ __forceinline__ void load_k_shared(Unit<D>& u, int p, const uint8_t* pool, int64_t at, const uint8_t* scales, int bytes, int lane) {
-    load_k<0>(u, p, pool, at, scales, bytes, lane);
+  struct SharedK {
+    u32x4 x[2][D / 64][64];  // a page's KiB as lanes hold it
+  };
+  // Wave w's part of a unit's K: page w mod 2, KiB w / 2, straight into LDS.
+  template <int D>
+  static __device__ __forceinline__ void stage_k(SharedK<D>& to, Unit<D>& u, int w, const uint8_t* pool, int64_t at0, int64_t at1,
+                                                 const uint8_t* scales, int bytes, int lane) {
+    if (w < 2 * (D / 64)) {
+      using Lds = __attribute__((address_space(3))) void;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(tile_at(pool + ((w & 1) == 0 ? at0 : at1), bytes), (Lds*)&to.x[w & 1][w >> 1][0], 16,
+                                               (w >> 1) * 1024 + lane * 16, 0, 0, 0);
+    }
+    u.ks[0] = scale_bytes<D>(scales, at0);
+    u.ks[1] = scale_bytes<D>(scales, at1);
+  }
+  template <int D>
+  static __device__ __forceinline__ void take_k(const SharedK<D>& from, Unit<D>& u, int lane) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int h = 0; h < D / 64; ++h) {
+        const u32x4 w = from.x[p][h][lane];
+        u.k[p][4 * h] = w.x; u.k[p][4 * h + 1] = w.y; u.k[p][4 * h + 2] = w.z; u.k[p][4 * h + 3] = w.w;
+      }
   }
   template <int D>
   static __device__ __forceinline__ void load_scales(Unit<D>& u, int p, const uint8_t*, int64_t at, const uint8_t* scales, int, int) {

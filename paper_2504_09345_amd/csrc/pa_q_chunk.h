@@ -20,6 +20,7 @@
 
 namespace pa {
 
+constexpr int kVmWaitAll = 0x0f70;  // s_waitcnt vmcnt(0), whatever the other counters
 constexpr int kQChunkNB = 2;                               // column blocks of a wave
 constexpr int kQChunkColumns = 16 * kQChunkNB * kQWaves;  // of a workgroup
 
@@ -31,6 +32,7 @@ void q_chunk_kernel(QAttnArgs a) {
   // V operands of block j, half h (even or odd dims), page p: 8 bytes per lane
   __shared__ __attribute__((aligned(16))) u32x2_t s_v[2][D / 32][2][2][64];
   __shared__ int32_t s_odd[2][kQWaves];
+  __shared__ typename F::template SharedK<D> s_k[2];
   const int S = a.s;
   const int lane = threadIdx.x & 63, n = lane & 15, G = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -116,9 +118,26 @@ void q_chunk_kernel(QAttnArgs a) {
                     });
   };
   typename F::template Unit<D> u;  // K of the unit; V only of a flagged one
-  auto fetch_k = [&](const Pages& t, bool any) {
+  // K of a unit of the item: into the wave's registers, or its part of it into LDS, from
+  // where the waves take it once all parts have arrived (settle, before a barrier).
+  auto fetch_k = [&](int k, const Pages& t, bool wave_any) {
+    if constexpr (F::kSharedK) {
+      if (k < u1) F::stage_k(s_k[k & 1], u, w, kg, t.at[0], t.at[1], sg, tile_size, lane);
+    } else {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) F::load_k_shared(u, p, kg, t.at[p], sg, any ? tile_size : 0, lane);
+      for (int p = 0; p < 2; ++p) F::load_k_shared(u, p, kg, t.at[p], sg, wave_any ? tile_size : 0, lane);
+    }
+  };
+  auto settle_k = [&]() {
+    if constexpr (F::kSharedK) {
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(kVmWaitAll);
+      asm volatile("" ::: "memory");
+    }
+  };
+  auto scores = [&](int k, q::f32x4_t (&x)[kNB][2]) {
+    if constexpr (F::kSharedK) F::take_k(s_k[k & 1], u, lane);
+    F::fold_qk(st, u, 0, x);
   };
   auto load_scales = [&](typename F::template Unit<D>& whole, const Pages& t) {  // V's, of a unit
 #pragma unroll
@@ -153,13 +172,18 @@ void q_chunk_kernel(QAttnArgs a) {
   // beside its own PV products, so the matrix cores and the vector unit work side
   // by side within a wave.
   Pages t = pages(u0), t1 = t, t2 = t;
-  fetch_k(t, true);
+  fetch_k(u0, t, true);
   fetch_part(t, true);
   if (u0 + 1 < u1) t1 = pages(u0 + 1);
   q::f32x4_t s[kNB][2], sn[kNB][2];
-  F::fold_qk(st, u, 0, s);
-  fetch_k(t1, u0 + 1 < w1);
+  if constexpr (F::kSharedK) {
+    settle_k();
+    __syncthreads();
+  }
+  scores(u0, s);
+  fetch_k(u0 + 1, t1, u0 + 1 < w1);
   convert(u0);
+  settle_k();
   fetch_part(t1, u0 + 1 < u1);
   const int plain = min(w1, (first_last + 1) / kQUnit);  // units before are seen whole by the wave's columns
   for (int k = u0; k < u1;) {
@@ -173,12 +197,13 @@ void q_chunk_kernel(QAttnArgs a) {
         break;
       }
       t2 = k + 2 < u1 ? pages(k + 2) : t1;
-      F::fold_qk(st, u, 0, sn);
+      scores(k + 1, sn);
       const bool big = q::form_weights<T, D, kNB>(st, s, a.scale_log2, x);
-      fetch_k(t2, k + 2 < w1);
+      fetch_k(k + 2, t2, k + 2 < w1);
       q::settle_weights<false, T, D, kNB>(st, s, a.scale_log2, big, x);
       convert(k + 1);
       fold_staged(k, x);
+      settle_k();
       fetch_part(t2, k + 2 < u1);
 #pragma unroll
       for (int c = 0; c < kNB; ++c)
@@ -191,8 +216,8 @@ void q_chunk_kernel(QAttnArgs a) {
     if (!entered) __syncthreads();
     const bool active = k < w1;
     t2 = k + 2 < u1 ? pages(k + 2) : t1;
-    if (k + 1 < w1) F::fold_qk(st, u, 0, sn);
-    fetch_k(t2, k + 2 < w1);
+    if (k + 1 < w1) scores(k + 1, sn);
+    fetch_k(k + 2, t2, k + 2 < w1);
     if (active) {
       q::mask_scores<T, D, kNB>(st, k * kQUnit, t.bad, lane, s);
       const bool odd = flagged(k);
@@ -216,6 +241,7 @@ void q_chunk_kernel(QAttnArgs a) {
       }
     }
     if (k + 1 < u1) convert(k + 1);
+    settle_k();
     fetch_part(t2, k + 2 < u1);
     if (k + 1 < w1) {
 #pragma unroll
