@@ -1,6 +1,6 @@
 """ctypes binding of libpagedattn.so, the C ABI declared in include/pagedattn.h
-and, for the caches held in 4 and in 8 bits, include/pagedattn_q4.h and
-include/pagedattn_q8.h.
+and, for the caches held in 4 and in 8 bits and for rotary positions,
+include/pagedattn_q4.h, include/pagedattn_q8.h and include/pa_rope.h.
 
 Argument marshalling only: every step of the attention runs in the library's
 HIP kernels.  Device buffers are passed as torch tensors (torch provides
@@ -28,7 +28,7 @@ EXPORTED = ("pa_workspace_size", "paged_attn", "paged_attn_varlen", "paged_attn_
             "pa_strerror",
             "pa_q4_tile_bytes", "pa_kv_append_q4", "pa_kv_read_q4", "pa_workspace_size_q4", "paged_attn_q4",
             "paged_attn_varlen_q4", "pa_kv_append_q8", "pa_kv_read_q8", "pa_workspace_size_q8", "paged_attn_q8",
-            "paged_attn_varlen_q8")
+            "paged_attn_varlen_q8", "pa_rope", "pa_rope_frequencies")
 
 
 class PaDims(ctypes.Structure):
@@ -86,6 +86,21 @@ class PaPmOutput(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in PM_OUTPUTS]
 
 
+class PaRope(ctypes.Structure):
+    """pa_rope_t (include/pa_rope.h)"""
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("factor", ctypes.c_float), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64)]
+
+
+ROPE_KINDS = ("plain", "linear", "base", "turns", "pairs")
+
+
+class PaRopeScaling(ctypes.Structure):
+    """pa_rope_scaling_t"""
+    _fields_ = [("kind", ctypes.c_int32), ("rot_dim", ctypes.c_int32)] + [(n, ctypes.c_double) for n in (
+        "base", "stretch", "trained_context", "low_turns", "high_turns")]
+
+
 class PagedAttnError(RuntimeError):
     def __init__(self, fn, code):
         super().__init__(f"{fn} returned {code}: {pa_strerror(code)}")
@@ -137,6 +152,10 @@ def load():
     lib.paged_attn_varlen_q4.argtypes = [P, P, P, P, P, P, ctypes.c_float, P, DP, P, SZ, P, TP]
     lib.pa_kv_append_q8.argtypes = [P, P, P, P, P, P, P, P, DP, P]
     lib.pa_kv_read_q8.argtypes = [P, P, P, P, P, P, P, P, DP, P]
+    lib.pa_rope.argtypes = [P, P, P, P, P, P, P, ctypes.POINTER(PaRope), DP, P]
+    lib.pa_rope.restype = ctypes.c_int
+    lib.pa_rope_frequencies.argtypes = [ctypes.POINTER(PaRopeScaling), ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_float)]
+    lib.pa_rope_frequencies.restype = ctypes.c_int
     lib.pa_workspace_size_q8.argtypes = [DP, ctypes.POINTER(SZ)]
     lib.paged_attn_q8.argtypes = [P, P, P, P, P, P, ctypes.c_float, P, DP, P, SZ, P, TP]
     lib.paged_attn_varlen_q8.argtypes = [P, P, P, P, P, P, P, ctypes.c_float, P, DP, P, SZ, P, TP]
@@ -567,6 +586,73 @@ def paged_attn_varlen_q8(q, k_pages, v_pages, scales, block_table, context_lens,
                                      ws_bytes, _stream(stream, dev), ctypes.byref(timing) if timing is not None else None)
     if check and rc != PA_OK:
         raise PagedAttnError("paged_attn_varlen_q8", rc)
+    return rc
+
+
+def pa_rope_frequencies(rot_dim, base=10000.0, kind="plain", stretch=1.0, trained_context=4096, low_turns=1.0, high_turns=32.0):
+    """(inv_freq, factor) of a call to pa_rope: a CPU tensor of rot_dim / 2 float64 (move it to
+    the GPU), and the factor.  kind: one of ROPE_KINDS (include/pa_rope.h)."""
+    import torch
+    if kind not in ROPE_KINDS:
+        raise ValueError(f"kind {kind!r} is none of {ROPE_KINDS}")
+    c = PaRopeScaling(ROPE_KINDS.index(kind), int(rot_dim), float(base), float(stretch), float(trained_context), float(low_turns), float(high_turns))
+    out, factor = torch.empty(max(0, int(rot_dim)) // 2, dtype=torch.float64), ctypes.c_float(0)
+    rc = load().pa_rope_frequencies(ctypes.byref(c), ctypes.cast(out.data_ptr(), ctypes.POINTER(ctypes.c_double)), ctypes.byref(factor))
+    if rc != PA_OK:
+        raise PagedAttnError("pa_rope_frequencies", rc)
+    return out, float(factor.value)
+
+
+def make_dims_rope(q, k, max_context_len, num_q_rows=0, num_seqs=None) -> PaDims:
+    """pa_dims_t of a pa_rope call from tensor shapes: q [rows][H_q][D], k
+    [rows][H_kv][D], of which one may be None."""
+    one = q if q is not None else k
+    rows, _, D = one.shape
+    return PaDims(num_seqs=rows if num_seqs is None else num_seqs, num_q_heads=0 if q is None else q.shape[1],
+                  num_kv_heads=0 if k is None else k.shape[1], head_dim=D, page_size=PAGE_SIZE, max_context_len=int(max_context_len),
+                  dtype=_dtype_code(one), num_q_rows=int(num_q_rows))
+
+
+def _rows_rope(t, kind, rows, heads, D, device):
+    """(address, row stride) of rows [rows][heads][D]; the rows may lie apart."""
+    if t is None or t.__class__ is int:
+        return t or None, 0
+    if t.dtype is not kind:
+        raise TypeError(f"a tensor of {t.dtype} where {kind} is needed")
+    if t.get_device() != device:
+        raise ValueError(f"a tensor on {t.device}, not on the current device")
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != D:
+        raise ValueError(f"a tensor of shape {tuple(shape)} where {(rows, heads, D)} is needed")
+    if strides[2] != 1 or (heads > 1 and strides[1] != D):
+        raise ValueError(f"a tensor of strides {strides}, whose rows' heads do not lie one after the other")
+    # (a lone row's stride is any number: none is used)
+    return t.data_ptr() or None, strides[0] if rows > 1 else 0
+
+
+def pa_rope(q, k, context_lens, inv_freq, q_out, k_out, dims: PaDims, interleaved=False, factor=1.0, positions=None, query_start_loc=None,
+            rot_dim=None, stream=None, check=True) -> int:
+    """int pa_rope(...): rotary positions of q and k (either may be None, with its
+    output); rot_dim is twice the length of inv_freq (float64) unless given.  Rows of tensors
+    may lie apart (q and k as parts of a joint projection's rows)."""
+    import torch
+    # (addresses alone need no device)
+    dev = None
+    if not all(map(_is_address, (q, k, context_lens, inv_freq, q_out, k_out, positions, query_start_loc))):
+        dev = torch.cuda.current_device()
+    if rot_dim is None:
+        rot_dim = 2 * inv_freq.numel()
+    kind, D = torch.bfloat16 if dims.dtype == PA_BF16 else torch.float32, dims.head_dim
+    rows = dims.num_q_rows if query_start_loc is not None or (positions is not None and dims.num_q_rows) else dims.num_seqs
+    (qa, qs), (qo, qos) = (_rows_rope(t, kind, rows, dims.num_q_heads, D, dev) for t in (q, q_out))
+    (ka, ks), (ko, kos) = (_rows_rope(t, kind, rows, dims.num_kv_heads, D, dev) for t in (k, k_out))
+    i32 = torch.int32
+    rope = PaRope(_take(inv_freq, torch.float64, rot_dim // 2, dev), float(factor), int(rot_dim), 1 if interleaved else 0, qs, ks, qos, kos)
+    rc = load().pa_rope(qa, ka, _take(positions, i32, rows, dev), _take(context_lens, i32, dims.num_seqs if positions is None else 0, dev),
+                        _take(query_start_loc, i32, dims.num_seqs + 1 if positions is None else 0, dev), qo, ko, ctypes.byref(rope),
+                        ctypes.byref(dims), _stream(stream, dev))
+    if check and rc != PA_OK:
+        raise PagedAttnError("pa_rope", rc)
     return rc
 
 

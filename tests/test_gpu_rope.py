@@ -1,0 +1,239 @@
+"""Rotary positions on the GPU against the formula in float64."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2504_09345_amd import binding as pb
+
+from parity_util import announce
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+# (context, rows) of the sequences
+LENS = [(1, 1), (40, 40), (33, 1), (0, 0), (70, 6), (100007, 5), (1000003, 2)]
+
+
+def expected(x, pos, w, factor, interleaved):
+    """float64 [rows][H][D], and the sum of the magnitudes that each result is of."""
+    x = x.double().cpu().numpy()
+    n = len(w)
+    a = np.asarray(pos, np.float64)[:, None, None] * w.numpy()
+    c, s = factor * np.cos(a), factor * np.sin(a)
+    i, j = (np.arange(0, 2 * n, 2), np.arange(1, 2 * n, 2)) if interleaved else (np.arange(n), np.arange(n, 2 * n))
+    out, mass = x.copy(), np.zeros_like(x)
+    out[..., i], out[..., j] = x[..., i] * c - x[..., j] * s, x[..., j] * c + x[..., i] * s
+    mass[..., i] = mass[..., j] = abs(factor) * (np.abs(x[..., i]) + np.abs(x[..., j]))
+    return out, mass
+
+
+def check(got, x, pos, w, factor, interleaved, what=""):
+    """The output's rounding, half a step; of each magnitude cosine and sine (series, the
+    argument's rounding and the factor's: 4 half steps of 32 bits), the two products and
+    the sum (3); and the angle's 2^-51 of itself."""
+    ref, mass = expected(x, pos, w, factor, interleaved)
+    angle = np.abs(np.asarray(pos, np.float64))[:, None, None] * float(w.abs().max())
+    step = 2.0 ** -8 if x.dtype == torch.bfloat16 else 2.0 ** -24
+    off = np.abs(got.double().cpu().numpy() - ref)
+    tol = step * np.abs(ref) + (7 * 2.0 ** -24 + 2.0 ** -51 * angle) * mass * (1 + step) + 1e-37 * (mass > 0)
+    assert (off <= tol).all(), f"{what}: {np.max(off / np.maximum(tol, 1e-300)):.3g} times the bound"
+    n = 2 * len(w)
+    assert torch.equal(got[..., n:], x[..., n:]), f"{what}: dims behind rot_dim"
+
+
+def rows(T, H_q, H_kv, D, dtype, seed=0, packed=False):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    joint = torch.randn(T, H_q + 2 * H_kv, D, device="cuda", generator=g).to(TYPES[dtype])
+    q, k = joint[:, :H_q], joint[:, H_q:H_q + H_kv]
+    return (q, k) if packed else (q.contiguous(), k.contiguous())
+
+
+def i32(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
+
+
+def varlen(lens):
+    """(context_lens, query_start_loc, positions of the rows)"""
+    starts = np.concatenate([[0], np.cumsum([n for _, n in lens])])
+    pos = np.concatenate([np.arange(c - n, c) for c, n in lens])
+    return i32([c for c, _ in lens]), i32(starts), pos
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rot", ["all", "half", 2, 6, 20, 40, 62])
+def test_varlen(dtype, D, interleaved, rot):
+    announce(f"rope varlen {dtype} D={D} rot={rot} interleaved={interleaved}")
+    rot = {"all": D, "half": D // 2}.get(rot, rot)
+    cl, qsl, pos = varlen(LENS)
+    T = len(pos)
+    w, factor = pb.pa_rope_frequencies(rot, kind="pairs", stretch=8)
+    for H_q, H_kv, packed in ((5, 1, True), (32, 8, False), (3, 3, False)):
+        q, k = rows(T, H_q, H_kv, D, dtype, packed=packed)
+        qo, ko = torch.full((T, H_q, D), 7.0, device="cuda", dtype=q.dtype), torch.full((T, H_kv, D), 7.0, device="cuda", dtype=q.dtype)
+        pb.pa_rope(q, k, cl, w.cuda(), qo, ko, pb.make_dims_rope(q, k, 1 << 20, T, len(LENS)), interleaved, factor, query_start_loc=qsl)
+        check(qo, q, pos, w, np.float32(factor), interleaved, "q")
+        check(ko, k, pos, w, np.float32(factor), interleaved, "k")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_decode_and_rows_of_no_sequence(dtype, interleaved):
+    announce(f"rope decode {dtype} interleaved={interleaved}")
+    ctx = [1, 0, 17, 300000, 0, 64]
+    q, k = rows(6, 8, 2, 128, dtype)
+    qo, ko = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+    w, _ = pb.pa_rope_frequencies(128)
+    pb.pa_rope(q, k, i32(ctx), w.cuda(), qo, ko, pb.make_dims_rope(q, k, 300000), interleaved)
+    live = [i for i, c in enumerate(ctx) if c]
+    for got, x in ((qo, q), (ko, k)):
+        check(got[live], x[live], [ctx[i] - 1 for i in live], w, 1.0, interleaved)
+        assert (got[[1, 4]] == 7.0).all()
+
+
+@pytest.mark.parametrize("T", [1, 2, 1023, 1024, 5000])
+def test_any_number_of_rows(T):
+    announce(f"rope {T} rows")
+    rng = np.random.default_rng(T)
+    pos = rng.integers(-5000, 100000, T)
+    q, k = rows(T, 12, 2, 128, "bf16", seed=T)
+    w, _ = pb.pa_rope_frequencies(64)
+    for a, b in ((q, k), (q, None), (None, k)):
+        ao, bo = (None if x is None else torch.zeros_like(x) for x in (a, b))
+        pb.pa_rope(a, b, None, w.cuda(), ao, bo, pb.make_dims_rope(a, b, 0, T, 1), positions=i32(pos))
+        for got, x in ((ao, a), (bo, b)):
+            if x is not None:
+                check(got, x, pos, w, 1.0, False)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("rot", [128, 64, 22])
+def test_in_place(interleaved, packed, rot):
+    announce(f"rope in place interleaved={interleaved} packed={packed} rot={rot}")
+    cl, qsl, pos = varlen(LENS)
+    w, _ = pb.pa_rope_frequencies(rot)
+    q, k = rows(len(pos), 8, 2, 128, "bf16", packed=packed)
+    was = q.clone(), k.clone()
+    pb.pa_rope(q, k, cl, w.cuda(), q, k, pb.make_dims_rope(q, k, 1 << 20, len(pos), len(LENS)), interleaved, query_start_loc=qsl)
+    check(q, was[0], pos, w, 1.0, interleaved)
+    check(k, was[1], pos, w, 1.0, interleaved)
+
+
+def test_packed_rows_leave_the_values_alone():
+    announce("rope within a joint projection's rows")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    joint = torch.randn(9, 8 + 2 * 2, 64, device="cuda", generator=g).bfloat16()
+    was = joint.clone()
+    w, _ = pb.pa_rope_frequencies(64)
+    q, k = joint[:, :8], joint[:, 8:10]
+    pb.pa_rope(q, k, None, w.cuda(), q, k, pb.make_dims_rope(q, k, 0), positions=i32(range(9)))
+    assert torch.equal(joint[:, 10:], was[:, 10:]) and torch.equal(joint[0], was[0]) and not torch.equal(joint[1:, :10], was[1:, :10])
+
+
+def test_rows_outside_the_contract():
+    announce("rope, rows outside the contract")
+    lens = [(3, 5), (50, 4), (2000, 2), (20, 3)]
+    cl, qsl, _ = varlen([(max(c, n), n) for c, n in lens])
+    cl = i32([c for c, _ in lens])
+    w, _ = pb.pa_rope_frequencies(32)
+    for interleaved in (False, True):
+        q, k = rows(14 + 3, 4, 2, 64, "fp32")
+        qo, ko = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+        pb.pa_rope(q, k, cl, w.cuda(), qo, ko, pb.make_dims_rope(q, k, 1000, 17, 4), interleaved, query_start_loc=qsl)
+        for got, x in ((qo, q), (ko, k)):
+            assert got[:5].isnan().all() and got[9:11].isnan().all() and (got[14:] == 7.0).all()
+            check(got[5:9], x[5:9], np.arange(46, 50), w, 1.0, interleaved)
+            check(got[11:14], x[11:14], np.arange(17, 20), w, 1.0, interleaved)
+
+
+def test_values_that_are_not_finite_stay_in_their_pairs():
+    announce("rope, infinities and NaN")
+    w, _ = pb.pa_rope_frequencies(32)
+    for interleaved in (False, True):
+        q, _ = rows(3, 2, 2, 64, "fp32")
+        q[0, 0, 40], q[1, 1, 50], q[2, 0, 4] = np.inf, np.nan, np.nan
+        out = torch.zeros_like(q)
+        pb.pa_rope(q, None, None, w.cuda(), out, None, pb.make_dims_rope(q, None, 0), interleaved, positions=i32([5, 6, 7]))
+        assert out[0, 0, 40] == np.inf and out[1, 1, 50].isnan()
+        other = 5 if interleaved else 20
+        bad = out[2, 0].isnan().nonzero().flatten().tolist()
+        assert bad == sorted([4, other]) and not out[2, 1].isnan().any()
+
+
+@pytest.mark.parametrize("p", [0, 1, 2 ** 20 - 1, 2 ** 24 + 1, 2 ** 31 - 1, -(2 ** 31), -12345])
+def test_far_positions(p):
+    """Frequencies whose angles fall on every eighth of a turn, and arbitrary ones."""
+    announce(f"rope at position {p}")
+    rng = np.random.default_rng(3)
+    w = torch.tensor(np.concatenate([np.arange(32) * np.pi / 4 / max(1, abs(p)), np.exp(rng.uniform(-12, 1, 32))]))
+    q, _ = rows(1, 4, 1, 128, "fp32")
+    out = torch.zeros_like(q)
+    pb.pa_rope(q, None, None, w.cuda(), out, None, pb.make_dims_rope(q, None, 0), positions=i32([p]))
+    check(out, q, [p], w, 1.0, False)
+
+
+def test_a_rotation_and_back():
+    announce("rope there and back")
+    q, _ = rows(64, 8, 2, 128, "fp32")
+    w, _ = pb.pa_rope_frequencies(128, 500000.0)
+    w = w.cuda()
+    there, back = torch.zeros_like(q), torch.zeros_like(q)
+    pos = torch.arange(64, dtype=torch.int32, device="cuda") * 1009
+    d = pb.make_dims_rope(q, None, 0)
+    pb.pa_rope(q, None, None, w, there, None, d, positions=pos)
+    pb.pa_rope(there, None, None, w, back, None, d, positions=-pos)
+    n = q.unflatten(-1, (2, 64)).abs().sum(-2, keepdim=True).expand(-1, -1, 2, -1).flatten(-2)
+    # (twice what check allows a result, the first's carried through the second)
+    assert ((back - q).abs() <= 4 * 8 * 2.0 ** -24 * n).all()
+
+
+def test_scores_depend_on_distance():
+    """q at p + d against k at p: the same product for every p."""
+    announce("rope, products by distance")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, y = (torch.randn(1, 1, 128, device="cuda", generator=g).expand(50, 1, 128).contiguous() for _ in range(2))
+    w, _ = pb.pa_rope_frequencies(128)
+    p = torch.arange(50, dtype=torch.int32, device="cuda") * 12345
+    d = pb.make_dims_rope(x, None, 0)
+    a, b = torch.zeros_like(x), torch.zeros_like(x)
+    pb.pa_rope(x, None, None, w.cuda(), a, None, d, positions=p + 77)
+    pb.pa_rope(y, None, None, w.cuda(), b, None, d, positions=p)
+    dot = (a.double() * b.double()).sum(-1)
+    size = float(x[0].norm() * y[0].norm())
+    assert float(dot.max() - dot.min()) <= 4 * 8 * 2.0 ** -24 * size * 2
+
+
+def test_on_a_stream_and_in_a_graph():
+    announce("rope on another stream and captured")
+    cl, qsl, pos = varlen(LENS)
+    T = len(pos)
+    w, _ = pb.pa_rope_frequencies(128)
+    wd = w.cuda()
+    q, k = rows(T, 8, 2, 128, "bf16")
+    qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+    d = pb.make_dims_rope(q, k, 1 << 20, T, len(LENS))
+
+    def step(stream=None):
+        pb.pa_rope(q, k, cl, wd, qo, ko, d, query_start_loc=qsl, stream=stream)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    side.synchronize()
+    want = qo.clone(), ko.clone()
+    check(qo, q, pos, w, 1.0, False)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        qo.zero_()
+        ko.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(qo, want[0]) and torch.equal(ko, want[1])
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(qo, want[0])
