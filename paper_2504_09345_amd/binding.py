@@ -535,7 +535,8 @@ def pa_kv_append_q8(k_new, v_new, block_table, context_lens, k_pages, v_pages, s
     """int pa_kv_append_q8(...): quantise the new tokens' K/V into the 8-bit pools."""
     k, v, kp, vp, bt, cl, qsl, dev = _args_q(_Q8_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_new, v_new,
                                              k_pages, v_pages, block_table, context_lens, query_start_loc)
-    rc = load().pa_kv_append_q8(k, v, bt, cl, qsl, kp, vp, _scales_q8(dims, scales), ctypes.byref(dims), _stream(stream, dev))
+    sc = _scales_q8(dims, scales)
+    rc = load().pa_kv_append_q8(k, v, bt, cl, qsl, kp, vp, sc, ctypes.byref(dims), _stream(stream, dev))
     if check and rc != PA_OK:
         raise PagedAttnError("pa_kv_append_q8", rc)
     return rc
@@ -547,7 +548,8 @@ def pa_kv_read_q8(k_pages, v_pages, scales, block_table, context_lens, k_out, v_
     which pa_kv_append_q8 with the same arguments writes."""
     k, v, kp, vp, bt, cl, qsl, dev = _args_q(_Q8_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_out, v_out,
                                              k_pages, v_pages, block_table, context_lens, query_start_loc)
-    rc = load().pa_kv_read_q8(kp, vp, _scales_q8(dims, scales), bt, cl, qsl, k, v, ctypes.byref(dims), _stream(stream, dev))
+    sc = _scales_q8(dims, scales)
+    rc = load().pa_kv_read_q8(kp, vp, sc, bt, cl, qsl, k, v, ctypes.byref(dims), _stream(stream, dev))
     if check and rc != PA_OK:
         raise PagedAttnError("pa_kv_read_q8", rc)
     return rc
@@ -567,8 +569,9 @@ def paged_attn_q8(q, k_pages, v_pages, scales, block_table, context_lens, scale,
     written in place."""
     qa, oa, kp, vp, bt, cl, _, dev = _args_q(_Q8_TILE, dims, dims.num_q_heads, False, q, out, k_pages, v_pages, block_table,
                                              context_lens, None)
+    sc = _scales_q8(dims, scales)
     ws, ws_bytes, owner = _workspace_q(pa_workspace_size_q8, dims, workspace, q, stream)
-    rc = load().paged_attn_q8(qa, kp, vp, _scales_q8(dims, scales), bt, cl, scale, oa, ctypes.byref(dims), ws, ws_bytes,
+    rc = load().paged_attn_q8(qa, kp, vp, sc, bt, cl, scale, oa, ctypes.byref(dims), ws, ws_bytes,
                               _stream(stream, dev), ctypes.byref(timing) if timing is not None else None)
     if check and rc != PA_OK:
         raise PagedAttnError("paged_attn_q8", rc)
@@ -581,8 +584,9 @@ def paged_attn_varlen_q8(q, k_pages, v_pages, scales, block_table, context_lens,
     8-bit cache."""
     qa, oa, kp, vp, bt, cl, qsl, dev = _args_q(_Q8_TILE, dims, dims.num_q_heads, True, q, out, k_pages, v_pages, block_table,
                                                context_lens, query_start_loc)
+    sc = _scales_q8(dims, scales)
     ws, ws_bytes, owner = _workspace_q(pa_workspace_size_q8, dims, workspace, q, stream)
-    rc = load().paged_attn_varlen_q8(qa, kp, vp, _scales_q8(dims, scales), bt, cl, qsl, scale, oa, ctypes.byref(dims), ws,
+    rc = load().paged_attn_varlen_q8(qa, kp, vp, sc, bt, cl, qsl, scale, oa, ctypes.byref(dims), ws,
                                      ws_bytes, _stream(stream, dev), ctypes.byref(timing) if timing is not None else None)
     if check and rc != PA_OK:
         raise PagedAttnError("paged_attn_varlen_q8", rc)
