@@ -407,10 +407,21 @@ def _take_q4(dims, *arrays):
     return _take_q(_Q4_TILE, dims, *arrays)
 
 
-def _args_q(tile, dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc):
-    """_take_q, checked by _fit_q, and the current device if it was looked up.  The
-    usual call, tensors of just the shapes that dims say, is checked in one pass (one by
-    one the checks take 1.3 us more)."""
+def _scales_q8(dims, scales):
+    """Address of the scales, uint8 [num_pages][num_kv_heads][2]."""
+    if _is_address(scales):
+        return scales or None
+    import torch
+    if scales.dim() == 3 and tuple(scales.shape[1:]) != (dims.num_kv_heads, 2):
+        raise ValueError(f"scales of shape {tuple(scales.shape)} where dims say rows of {(dims.num_kv_heads, 2)}")
+    return _take(scales, torch.uint8, dims.num_pages * dims.num_kv_heads * 2, torch.cuda.current_device())
+
+
+def _args_q(tile, dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc, scales=None):
+    """_take_q, checked by _fit_q, the scales' address (None: a cache without), and the
+    current device if it was looked up.  The usual call, tensors of just the shapes that
+    dims say, is checked in one pass (one by one the checks take 1.3 us more, 2 us with
+    scales)."""
     try:
         d, k, w = dense0.shape, k_pages.shape, block_table.shape
         import torch
@@ -427,14 +438,17 @@ def _args_q(tile, dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_t
                 and block_table.get_device() == dev == context_lens.get_device()
                 and dense0.is_contiguous() and dense1.is_contiguous() and k_pages.is_contiguous() and v_pages.is_contiguous()
                 and block_table.is_contiguous() and context_lens.is_contiguous()
-                and len(d) == 3 and len(k) == 3 and len(w) == 2):
+                and len(d) == 3 and len(k) == 3 and len(w) == 2
+                and (scales is None or (scales.shape == (k[0], H_kv, 2) and scales.dtype is u8 and scales.get_device() == dev
+                                        and scales.is_contiguous()))):
             return (dense0.data_ptr(), dense1.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(),
-                    context_lens.data_ptr(), _take(query_start_loc, i32, B + 1, dev), dev)
+                    context_lens.data_ptr(), None if query_start_loc is None else _take(query_start_loc, i32, B + 1, dev),
+                    None if scales is None else scales.data_ptr(), dev)
     except (AttributeError, IndexError):  # (addresses, other ranks)
         pass
     taken = _take_q(tile, dims, heads, varlen, dense0, dense1, k_pages, v_pages, block_table, context_lens, query_start_loc)
     _fit_q(tile, dims, heads, dense0, dense1, k_pages, v_pages, block_table)
-    return *taken, None
+    return *taken, _scales_q8(dims, scales), None
 
 
 def _workspace_q(size_of, dims, workspace, q, stream):
@@ -458,7 +472,7 @@ def _workspace_q(size_of, dims, workspace, q, stream):
 def pa_kv_append_q4(k_new, v_new, block_table, context_lens, k_pages, v_pages, dims: PaDims, query_start_loc=None,
                     stream=None, check=True) -> int:
     """int pa_kv_append_q4(...): quantise the new tokens' K/V into the 4-bit pools."""
-    k, v, kp, vp, bt, cl, qsl, dev = _args_q(_Q4_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_new, v_new, k_pages,
+    k, v, kp, vp, bt, cl, qsl, _, dev = _args_q(_Q4_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_new, v_new, k_pages,
                                               v_pages, block_table, context_lens, query_start_loc)
     rc = load().pa_kv_append_q4(k, v, bt, cl, qsl, kp, vp, ctypes.byref(dims), _stream(stream, dev))
     if check and rc != PA_OK:
@@ -470,7 +484,7 @@ def pa_kv_read_q4(k_pages, v_pages, block_table, context_lens, k_out, v_out, dim
                   stream=None, check=True) -> int:
     """int pa_kv_read_q4(...): the values that the 4-bit pools hold of the rows
     which pa_kv_append_q4 with the same arguments writes."""
-    k, v, kp, vp, bt, cl, qsl, dev = _args_q(_Q4_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_out, v_out, k_pages,
+    k, v, kp, vp, bt, cl, qsl, _, dev = _args_q(_Q4_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_out, v_out, k_pages,
                                               v_pages, block_table, context_lens, query_start_loc)
     rc = load().pa_kv_read_q4(kp, vp, bt, cl, qsl, k, v, ctypes.byref(dims), _stream(stream, dev))
     if check and rc != PA_OK:
@@ -482,7 +496,7 @@ def paged_attn_q4(q, k_pages, v_pages, block_table, context_lens, scale, out, di
                   stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_q4(...): decode attention over the 4-bit cache; out is
     written in place."""
-    qa, oa, kp, vp, bt, cl, _, dev = _args_q(_Q4_TILE, dims, dims.num_q_heads, False, q, out, k_pages, v_pages, block_table,
+    qa, oa, kp, vp, bt, cl, _, _, dev = _args_q(_Q4_TILE, dims, dims.num_q_heads, False, q, out, k_pages, v_pages, block_table,
                                               context_lens, None)
     ws, ws_bytes, owner = _workspace_q(pa_workspace_size_q4, dims, workspace, q, stream)
     rc = load().paged_attn_q4(qa, kp, vp, bt, cl, scale, oa, ctypes.byref(dims), ws, ws_bytes, _stream(stream, dev),
@@ -496,7 +510,7 @@ def paged_attn_varlen_q4(q, k_pages, v_pages, block_table, context_lens, query_s
                          workspace=None, stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_varlen_q4(...): causal chunks plus decode rows over the
     4-bit cache."""
-    qa, oa, kp, vp, bt, cl, qsl, dev = _args_q(_Q4_TILE, dims, dims.num_q_heads, True, q, out, k_pages, v_pages, block_table,
+    qa, oa, kp, vp, bt, cl, qsl, _, dev = _args_q(_Q4_TILE, dims, dims.num_q_heads, True, q, out, k_pages, v_pages, block_table,
                                                 context_lens, query_start_loc)
     ws, ws_bytes, owner = _workspace_q(pa_workspace_size_q4, dims, workspace, q, stream)
     rc = load().paged_attn_varlen_q4(qa, kp, vp, bt, cl, qsl, scale, oa, ctypes.byref(dims), ws, ws_bytes,
@@ -519,23 +533,11 @@ def make_dims_q8(rows, k_pages, block_table, max_context_len, num_q_rows=0, max_
                   _dtype_code(rows), int(num_q_rows), int(max_q_len))
 
 
-def _scales_q8(dims, scales):
-    """Address of the scales, uint8 [num_pages][num_kv_heads][2]."""
-    if _is_address(scales):
-        return scales or None
-    import torch
-    shape = tuple(scales.shape)
-    if scales.dim() == 3 and shape[1:] != (dims.num_kv_heads, 2):
-        raise ValueError(f"scales of shape {shape} where dims say rows of {(dims.num_kv_heads, 2)}")
-    return _take(scales, torch.uint8, dims.num_pages * dims.num_kv_heads * 2, torch.cuda.current_device())
-
-
 def pa_kv_append_q8(k_new, v_new, block_table, context_lens, k_pages, v_pages, scales, dims: PaDims, query_start_loc=None,
                     stream=None, check=True) -> int:
     """int pa_kv_append_q8(...): quantise the new tokens' K/V into the 8-bit pools."""
-    k, v, kp, vp, bt, cl, qsl, dev = _args_q(_Q8_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_new, v_new,
-                                             k_pages, v_pages, block_table, context_lens, query_start_loc)
-    sc = _scales_q8(dims, scales)
+    k, v, kp, vp, bt, cl, qsl, sc, dev = _args_q(_Q8_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_new, v_new,
+                                             k_pages, v_pages, block_table, context_lens, query_start_loc, scales)
     rc = load().pa_kv_append_q8(k, v, bt, cl, qsl, kp, vp, sc, ctypes.byref(dims), _stream(stream, dev))
     if check and rc != PA_OK:
         raise PagedAttnError("pa_kv_append_q8", rc)
@@ -546,9 +548,8 @@ def pa_kv_read_q8(k_pages, v_pages, scales, block_table, context_lens, k_out, v_
                   stream=None, check=True) -> int:
     """int pa_kv_read_q8(...): the values that the 8-bit pools hold of the rows
     which pa_kv_append_q8 with the same arguments writes."""
-    k, v, kp, vp, bt, cl, qsl, dev = _args_q(_Q8_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_out, v_out,
-                                             k_pages, v_pages, block_table, context_lens, query_start_loc)
-    sc = _scales_q8(dims, scales)
+    k, v, kp, vp, bt, cl, qsl, sc, dev = _args_q(_Q8_TILE, dims, dims.num_kv_heads, query_start_loc is not None, k_out, v_out,
+                                             k_pages, v_pages, block_table, context_lens, query_start_loc, scales)
     rc = load().pa_kv_read_q8(kp, vp, sc, bt, cl, qsl, k, v, ctypes.byref(dims), _stream(stream, dev))
     if check and rc != PA_OK:
         raise PagedAttnError("pa_kv_read_q8", rc)
@@ -567,9 +568,8 @@ def paged_attn_q8(q, k_pages, v_pages, scales, block_table, context_lens, scale,
                   stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_q8(...): decode attention over the 8-bit cache; out is
     written in place."""
-    qa, oa, kp, vp, bt, cl, _, dev = _args_q(_Q8_TILE, dims, dims.num_q_heads, False, q, out, k_pages, v_pages, block_table,
-                                             context_lens, None)
-    sc = _scales_q8(dims, scales)
+    qa, oa, kp, vp, bt, cl, _, sc, dev = _args_q(_Q8_TILE, dims, dims.num_q_heads, False, q, out, k_pages, v_pages, block_table,
+                                             context_lens, None, scales)
     ws, ws_bytes, owner = _workspace_q(pa_workspace_size_q8, dims, workspace, q, stream)
     rc = load().paged_attn_q8(qa, kp, vp, sc, bt, cl, scale, oa, ctypes.byref(dims), ws, ws_bytes,
                               _stream(stream, dev), ctypes.byref(timing) if timing is not None else None)
@@ -582,9 +582,8 @@ def paged_attn_varlen_q8(q, k_pages, v_pages, scales, block_table, context_lens,
                          workspace=None, stream=None, timing: PaTiming | None = None, check=True) -> int:
     """int paged_attn_varlen_q8(...): causal chunks plus decode rows over the
     8-bit cache."""
-    qa, oa, kp, vp, bt, cl, qsl, dev = _args_q(_Q8_TILE, dims, dims.num_q_heads, True, q, out, k_pages, v_pages, block_table,
-                                               context_lens, query_start_loc)
-    sc = _scales_q8(dims, scales)
+    qa, oa, kp, vp, bt, cl, qsl, sc, dev = _args_q(_Q8_TILE, dims, dims.num_q_heads, True, q, out, k_pages, v_pages, block_table,
+                                               context_lens, query_start_loc, scales)
     ws, ws_bytes, owner = _workspace_q(pa_workspace_size_q8, dims, workspace, q, stream)
     rc = load().paged_attn_varlen_q8(qa, kp, vp, sc, bt, cl, qsl, scale, oa, ctypes.byref(dims), ws,
                                      ws_bytes, _stream(stream, dev), ctypes.byref(timing) if timing is not None else None)
@@ -619,15 +618,20 @@ def make_dims_rope(q, k, max_context_len, num_q_rows=0, num_seqs=None) -> PaDims
 
 def _rows_rope(t, kind, rows, heads, D, device):
     """(address, row stride) of rows [rows][heads][D]; the rows may lie apart."""
-    if t is None or t.__class__ is int:
+    if t is None:
+        return None, 0
+    if t.__class__ is int:
         return t or None, 0
     if t.dtype is not kind:
         raise TypeError(f"a tensor of {t.dtype} where {kind} is needed")
     if t.get_device() != device:
         raise ValueError(f"a tensor on {t.device}, not on the current device")
-    shape, strides = t.shape, t.stride()
+    shape = t.shape
     if len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != D:
         raise ValueError(f"a tensor of shape {tuple(shape)} where {(rows, heads, D)} is needed")
+    if t.is_contiguous():
+        return t.data_ptr() or None, 0
+    strides = t.stride()
     if strides[2] != 1 or (heads > 1 and strides[1] != D):
         raise ValueError(f"a tensor of strides {strides}, whose rows' heads do not lie one after the other")
     # (a lone row's stride is any number: none is used)
@@ -646,15 +650,21 @@ def pa_rope(q, k, context_lens, inv_freq, q_out, k_out, dims: PaDims, interleave
         dev = torch.cuda.current_device()
     if rot_dim is None:
         rot_dim = 2 * inv_freq.numel()
-    kind, D = torch.bfloat16 if dims.dtype == PA_BF16 else torch.float32, dims.head_dim
+    kind, D, i32 = torch.bfloat16 if dims.dtype == PA_BF16 else torch.float32, dims.head_dim, torch.int32
     rows = dims.num_q_rows if query_start_loc is not None or (positions is not None and dims.num_q_rows) else dims.num_seqs
-    (qa, qs), (qo, qos) = (_rows_rope(t, kind, rows, dims.num_q_heads, D, dev) for t in (q, q_out))
-    (ka, ks), (ko, kos) = (_rows_rope(t, kind, rows, dims.num_kv_heads, D, dev) for t in (k, k_out))
-    i32 = torch.int32
+    H_q, H_kv = dims.num_q_heads, dims.num_kv_heads
+    qa, qs = _rows_rope(q, kind, rows, H_q, D, dev)
+    qo, qos = _rows_rope(q_out, kind, rows, H_q, D, dev)
+    ka, ks = _rows_rope(k, kind, rows, H_kv, D, dev)
+    ko, kos = _rows_rope(k_out, kind, rows, H_kv, D, dev)
+    if positions is None:
+        B = dims.num_seqs
+        pos, cl = None, _take(context_lens, i32, B, dev)
+        qsl = None if query_start_loc is None else _take(query_start_loc, i32, B + 1, dev)
+    else:  # (the others are not read)
+        pos, cl, qsl = _take(positions, i32, rows, dev), None, None
     rope = PaRope(_take(inv_freq, torch.float64, rot_dim // 2, dev), float(factor), int(rot_dim), 1 if interleaved else 0, qs, ks, qos, kos)
-    rc = load().pa_rope(qa, ka, _take(positions, i32, rows, dev), _take(context_lens, i32, dims.num_seqs if positions is None else 0, dev),
-                        _take(query_start_loc, i32, dims.num_seqs + 1 if positions is None else 0, dev), qo, ko, ctypes.byref(rope),
-                        ctypes.byref(dims), _stream(stream, dev))
+    rc = load().pa_rope(qa, ka, pos, cl, qsl, qo, ko, ctypes.byref(rope), ctypes.byref(dims), _stream(stream, dev))
     if check and rc != PA_OK:
         raise PagedAttnError("pa_rope", rc)
     return rc

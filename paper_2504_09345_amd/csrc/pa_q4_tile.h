@@ -369,6 +369,7 @@ struct Format {
   }
   static constexpr bool kSharedK = false;  // (into each wave's registers)
   template <int D> struct SharedK {};
+  template <int D> struct KPart {};
   template <int D>
   static __device__ __forceinline__ void load_scales(Unit<D>& u, int p, const uint8_t* pool, int64_t at, const uint8_t*, int bytes, int lane) {
     const __amdgpu_buffer_rsrc_t r =

@@ -252,28 +252,38 @@ struct Format {
   template <int D>
   struct SharedK {
     u32x4 x[2][D / 64][64];  // a page's KiB as lanes hold it
+    uint32_t scale[2];
   };
-  // Wave w's part of a unit's K: page w mod 2, KiB w / 2, straight into LDS.
+  // A wave's part: page w mod 2, KiB w / 2 (of those that there are).  (Loaded into LDS
+  // directly it needs no registers, but every read of LDS then waits for those loads.)
   template <int D>
-  static __device__ __forceinline__ void stage_k(SharedK<D>& to, Unit<D>& u, int w, const uint8_t* pool, int64_t at0, int64_t at1,
-                                                 const uint8_t* scales, int bytes, int lane) {
+  struct KPart {
+    u32x4 x;
+    uint32_t scale;
+  };
+  template <int D>
+  static __device__ __forceinline__ void load_k_part(KPart<D>& t, int w, const uint8_t* pool, int64_t at, const uint8_t* scales, int bytes, int lane) {
+    t.scale = scale_bytes<D>(scales, at);
+    t.x = __builtin_amdgcn_raw_buffer_load_b128(tile_at(pool + at, bytes), (w >> 1) % (D / 64) * 1024 + lane * 16, 0, 0);
+  }
+  template <int D>
+  static __device__ __forceinline__ void put_k_part(SharedK<D>& to, const KPart<D>& t, int w, int lane) {
     if (w < 2 * (D / 64)) {
-      using Lds = __attribute__((address_space(3))) void;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(tile_at(pool + ((w & 1) == 0 ? at0 : at1), bytes), (Lds*)&to.x[w & 1][w >> 1][0], 16,
-                                               (w >> 1) * 1024 + lane * 16, 0, 0, 0);
+      to.x[w & 1][w >> 1][lane] = t.x;
+      if (lane == 0) to.scale[w & 1] = t.scale;  // (two waves write the same)
     }
-    u.ks[0] = scale_bytes<D>(scales, at0);
-    u.ks[1] = scale_bytes<D>(scales, at1);
   }
   template <int D>
   static __device__ __forceinline__ void take_k(const SharedK<D>& from, Unit<D>& u, int lane) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
+    for (int p = 0; p < 2; ++p) {
+      u.ks[p] = from.scale[p];
 #pragma unroll
       for (int h = 0; h < D / 64; ++h) {
         const u32x4 w = from.x[p][h][lane];
         u.k[p][4 * h] = w.x; u.k[p][4 * h + 1] = w.y; u.k[p][4 * h + 2] = w.z; u.k[p][4 * h + 3] = w.w;
       }
+    }
   }
   template <int D>
   static __device__ __forceinline__ void load_scales(Unit<D>& u, int p, const uint8_t*, int64_t at, const uint8_t* scales, int, int) {

@@ -20,7 +20,6 @@
 
 namespace pa {
 
-constexpr int kVmWaitAll = 0x0f70;  // s_waitcnt vmcnt(0), whatever the other counters
 constexpr int kQChunkNB = 2;                               // column blocks of a wave
 constexpr int kQChunkColumns = 16 * kQChunkNB * kQWaves;  // of a workgroup
 
@@ -99,11 +98,16 @@ void q_chunk_kernel(QAttnArgs a) {
     }
     return t;
   };
+  // (chosen between as values: of addresses, the pages would move to memory)
+  auto at_of = [](const Pages& t, int p) {
+    const int64_t a = t.at[0], b = t.at[1];
+    return p == 0 ? +a : +b;
+  };
   // This wave's part of a unit's V: page w % 2, blocks jb .. jb + D / 64 - 1.
   const int vp = w & 1, jb = (w >> 1) * (D / 64);
   typename F::template Part<D> part;
   auto fetch_part = [&](const Pages& t, bool any) {
-    F::load_part(part, vg, vp == 0 ? t.at[0] : t.at[1], sg, jb, any ? tile_size : 0, lane);
+    F::load_part(part, vg, at_of(t, vp), sg, jb, any ? tile_size : 0, lane);
   };
   auto convert = [&](int k) {
     const int buf = k & 1;
@@ -118,22 +122,19 @@ void q_chunk_kernel(QAttnArgs a) {
                     });
   };
   typename F::template Unit<D> u;  // K of the unit; V only of a flagged one
-  // K of a unit of the item: into the wave's registers, or its part of it into LDS, from
-  // where the waves take it once all parts have arrived (settle, before a barrier).
-  auto fetch_k = [&](int k, const Pages& t, bool wave_any) {
+  // K of a unit: into each wave's registers, or (kSharedK) a part of it, which the wave
+  // puts into LDS for all.
+  typename F::template KPart<D> kpart;
+  auto fetch_k = [&](const Pages& t, bool any) {
     if constexpr (F::kSharedK) {
-      if (k < u1) F::stage_k(s_k[k & 1], u, w, kg, t.at[0], t.at[1], sg, tile_size, lane);
+      F::load_k_part(kpart, w, kg, at_of(t, w & 1), sg, any ? tile_size : 0, lane);
     } else {
 #pragma unroll
-      for (int p = 0; p < 2; ++p) F::load_k_shared(u, p, kg, t.at[p], sg, wave_any ? tile_size : 0, lane);
+      for (int p = 0; p < 2; ++p) F::load_k_shared(u, p, kg, t.at[p], sg, any ? tile_size : 0, lane);
     }
   };
-  auto settle_k = [&]() {
-    if constexpr (F::kSharedK) {
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_waitcnt(kVmWaitAll);
-      asm volatile("" ::: "memory");
-    }
+  auto put_k = [&](int k) {
+    if constexpr (F::kSharedK) F::put_k_part(s_k[k & 1], kpart, w, lane);
   };
   auto scores = [&](int k, q::f32x4_t (&x)[kNB][2]) {
     if constexpr (F::kSharedK) F::take_k(s_k[k & 1], u, lane);
@@ -170,21 +171,37 @@ void q_chunk_kernel(QAttnArgs a) {
   // of k + 1 are on their way, and V of k is staged (after the barrier).  A unit forms
   // the next one's scores beside its own weights, and converts the next one's V
   // beside its own PV products, so the matrix cores and the vector unit work side
-  // by side within a wave.
-  Pages t = pages(u0), t1 = t, t2 = t;
-  fetch_k(u0, t, true);
-  fetch_part(t, true);
-  if (u0 + 1 < u1) t1 = pages(u0 + 1);
+  // by side within a wave.  K that goes through LDS is a unit further ahead: that of k + 1
+  // is there when unit k starts, and the part of k + 2 on its way.
+  Pages t = pages(u0), t1 = t, t2 = t, t3 = t;
   q::f32x4_t s[kNB][2], sn[kNB][2];
+  fetch_k(t, true);
+  fetch_part(t, true);
+  if (u0 + 1 < u1) t1 = t2 = t3 = pages(u0 + 1);
   if constexpr (F::kSharedK) {
-    settle_k();
+    put_k(u0);
+    fetch_k(t1, u0 + 1 < u1);
+    if (u0 + 2 < u1) t2 = t3 = pages(u0 + 2);
+    put_k(u0 + 1);
     __syncthreads();
+    scores(u0, s);
+    fetch_k(t2, u0 + 2 < u1);
+  } else {
+    scores(u0, s);
+    fetch_k(t1, u0 + 1 < w1);
   }
-  scores(u0, s);
-  fetch_k(u0 + 1, t1, u0 + 1 < w1);
   convert(u0);
-  settle_k();
   fetch_part(t1, u0 + 1 < u1);
+  // the pages of the units after k, when unit k starts
+  auto look_ahead = [&](int k) {
+    if constexpr (F::kSharedK) t3 = k + 3 < u1 ? pages(k + 3) : t2;
+    else t2 = k + 2 < u1 ? pages(k + 2) : t1;
+  };
+  auto move_on = [&]() {
+    t = t1;
+    t1 = t2;
+    if constexpr (F::kSharedK) t2 = t3;
+  };
   const int plain = min(w1, (first_last + 1) / kQUnit);  // units before are seen whole by the wave's columns
   for (int k = u0; k < u1;) {
     float x[kNB][8];
@@ -196,28 +213,28 @@ void q_chunk_kernel(QAttnArgs a) {
         entered = true;
         break;
       }
-      t2 = k + 2 < u1 ? pages(k + 2) : t1;
+      look_ahead(k);
       scores(k + 1, sn);
       const bool big = q::form_weights<T, D, kNB>(st, s, a.scale_log2, x);
-      fetch_k(k + 2, t2, k + 2 < w1);
+      if constexpr (!F::kSharedK) fetch_k(t2, k + 2 < w1);
       q::settle_weights<false, T, D, kNB>(st, s, a.scale_log2, big, x);
       convert(k + 1);
+      put_k(k + 2);
       fold_staged(k, x);
-      settle_k();
       fetch_part(t2, k + 2 < u1);
+      if constexpr (F::kSharedK) fetch_k(t3, k + 3 < u1);
 #pragma unroll
       for (int c = 0; c < kNB; ++c)
 #pragma unroll
         for (int p = 0; p < 2; ++p) s[c][p] = sn[c][p];
-      t = t1;
-      t1 = t2;
+      move_on();
     }
     if (k >= u1) break;
     if (!entered) __syncthreads();
     const bool active = k < w1;
-    t2 = k + 2 < u1 ? pages(k + 2) : t1;
+    look_ahead(k);
     if (k + 1 < w1) scores(k + 1, sn);
-    fetch_k(k + 2, t2, k + 2 < w1);
+    if constexpr (!F::kSharedK) fetch_k(t2, k + 2 < w1);
     if (active) {
       q::mask_scores<T, D, kNB>(st, k * kQUnit, t.bad, lane, s);
       const bool odd = flagged(k);
@@ -241,16 +258,16 @@ void q_chunk_kernel(QAttnArgs a) {
       }
     }
     if (k + 1 < u1) convert(k + 1);
-    settle_k();
+    if (k + 2 < u1) put_k(k + 2);
     fetch_part(t2, k + 2 < u1);
+    if constexpr (F::kSharedK) fetch_k(t3, k + 3 < u1);
     if (k + 1 < w1) {
 #pragma unroll
       for (int c = 0; c < kNB; ++c)
 #pragma unroll
         for (int p = 0; p < 2; ++p) s[c][p] = sn[c][p];
     }
-    t = t1;
-    t1 = t2;
+    move_on();
     ++k;
   }
   q_finish<T, D, kNB>(a, st, at, split, lane);
