@@ -268,56 +268,11 @@ __device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, co
   }
 }
 
-// V's operands of a unit, made by the four waves of a workgroup, a page and half of the
-// blocks each: blocks jb .. jb + D / 64 - 1.
-template <int D>
-struct Part {
-  static constexpr int kBlocks = D / 64;
-  uint32_t vc[kBlocks], vs[kWords<D>];
-};
-template <int D>
-__device__ __forceinline__ void load_part(Part<D>& t, const uint8_t* v, int jb, int bytes, int lane) {
-  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(v), (short)0, bytes, 0x00020000);
-  if constexpr (D == 128) {
-    const u32x2_t x = __builtin_amdgcn_raw_buffer_load_b64(r, lane * 16 + jb * 4, 0, 0);
-    t.vc[0] = x.x;
-    t.vc[1] = x.y;
-  } else {
-    t.vc[0] = __builtin_amdgcn_raw_buffer_load_b32(r, lane * 8 + jb * 4, 0, 0);
-  }
-  load_words<D, 0>(r, kScales<D> + (lane >> 4) * (D / 8), t.vs);
-}
-// key0: of the lane's first token.  flag(whether a lane's V takes other products), then
-// store(block of the part, even dims, odd dims).
-template <int D, typename Flag, typename Store>
-__device__ __forceinline__ void convert_part(const Part<D>& t, int jb, int key0, int all_last, Flag flag, Store store) {
-  uint32_t sc[4];  // scales of the part's blocks, a token each, from byte 0 on
-  bool odd = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    sc[i] = (D == 128 ? t.vs[i] >> (8 * jb) : t.vs[i >> 1] >> (16 * (i & 1) + 8 * jb)) & (D == 128 ? 0xffffu : 0xffu);
-    // (an unused slot may hold anything: its weight is 0, its scale becomes 1)
-    if (key0 + i > all_last) sc[i] = 0x7f7fu & (D == 128 ? 0xffffu : 0xffu);
-    // (bytes within 104 .. 135, as in beyond_fp16)
-    odd |= ((sc[i] - (D == 128 ? 0x6868u : 0x68u)) & (D == 128 ? 0xffffe0e0u : 0xffffffe0u)) != 0;
-  }
-  flag(odd);
-  auto block = [&](auto b_) {
-    constexpr int b = decltype(b_)::value;
-    const uint32_t t0 = pair_of<0, true>(t.vc[b], scale_of<b>(sc[0])), t1 = pair_of<1, true>(t.vc[b], scale_of<b>(sc[1]));
-    const uint32_t t2 = pair_of<2, true>(t.vc[b], scale_of<b>(sc[2])), t3 = pair_of<3, true>(t.vc[b], scale_of<b>(sc[3]));
-    store(b, u32x2_t{__builtin_amdgcn_perm(t1, t0, 0x05040100u), __builtin_amdgcn_perm(t3, t2, 0x05040100u)},
-          u32x2_t{__builtin_amdgcn_perm(t1, t0, 0x07060302u), __builtin_amdgcn_perm(t3, t2, 0x07060302u)});
-  };
-  block(std::integral_constant<int, 0>{});
-  if constexpr (Part<D>::kBlocks == 2) block(std::integral_constant<int, 1>{});
-}
-
 // What the kernels ask of a format.
 struct Format {
   template <int D> using Unit = q4::Unit<D>;
-  template <int D> using Part = q4::Part<D>;
   static constexpr bool kSliced = false;  // K operands in bf16: a lane's dims in a row
+  static constexpr bool kSums = false;  // a base moves by sums of weights
   static constexpr int tile_bytes(int D) { return q4_tile_bytes(D); }
 
   static __device__ __forceinline__ const uint8_t* scales_of_head(const uint8_t*, int) { return nullptr; }  // (in the tile)
@@ -355,39 +310,6 @@ struct Format {
   template <typename T, int D, int NB>
   static __device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, const float (&x)[NB][8], int key0, int lane) {
     q4::fold_pv_edge<T, D, NB>(st, u, x, key0, lane);
-  }
-  // A workgroup that shares V (pa_q_chunk.h): K alone, as all of its waves need it; V's
-  // scales of a unit; V with its scales; a wave's part of V.
-  template <int D>
-  static __device__ __forceinline__ void load_k_shared(Unit<D>& u, int p, const uint8_t* pool, int64_t at, const uint8_t*, int bytes, int lane) {
-    // (The scale bytes alone, although that waits for K here, behind the present unit's
-    // softmax: 698 us instead of 715 for eight chunks of 2,048 rows on 0-2,048 tokens.)
-    const __amdgpu_buffer_rsrc_t r =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(pool + at), (short)0, bytes, 0x00020000);
-    load_words<D, 0>(r, lane * (D / 8), u.k[p]);
-    u.ks[p] = __builtin_amdgcn_raw_buffer_load_b8(r, kScales<D> + (lane & 15) * (D / 32) + (lane >> 4) * D / 128, 0, 0);
-  }
-  static constexpr bool kSharedK = false;  // (into each wave's registers)
-  template <int D> struct SharedK {};
-  template <int D> struct KPart {};
-  template <int D>
-  static __device__ __forceinline__ void load_scales(Unit<D>& u, int p, const uint8_t* pool, int64_t at, const uint8_t*, int bytes, int lane) {
-    const __amdgpu_buffer_rsrc_t r =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(pool + at), (short)0, bytes, 0x00020000);
-    load_words<D, 0>(r, kScales<D> + (lane >> 4) * (D / 8), u.vs[p]);
-  }
-  template <int D>
-  static __device__ __forceinline__ void load_v_whole(Unit<D>& u, int p, const uint8_t* pool, int64_t at, const uint8_t*, int bytes, int lane) {
-    q4::load_v<D, 0>(u, p, pool + at, bytes, lane);
-  }
-  template <int D>
-  static __device__ __forceinline__ void load_part(Part<D>& t, const uint8_t* pool, int64_t at, const uint8_t*, int jb, int bytes, int lane) {
-    q4::load_part<D>(t, pool + at, jb, bytes, lane);
-  }
-  // (edge: of the unit's keys, some are seen by a part of the workgroup's columns)
-  template <int D, typename Flag, typename Store>
-  static __device__ __forceinline__ void convert_part(const Part<D>& t, int jb, int key0, int all_last, bool edge, int lane, Flag flag, Store store) {
-    q4::convert_part<D>(t, jb, key0, all_last, flag, store);
   }
 };
 

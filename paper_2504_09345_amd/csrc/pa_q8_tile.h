@@ -40,11 +40,11 @@ __device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int lane, u
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_at(const uint8_t* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), (short)0, bytes, 0x00020000);
 }
-// The scale bytes of the tile `at` bytes into the pool.  (Two bytes per tile of 2 KiB, so
+// The scale bytes (two) of the tile `at` (a multiple of 16 D) bytes into the pool.  (Two bytes per tile of 2 KiB, so
 // they stay in the caches.)
 template <int D>
 __device__ __forceinline__ uint32_t scale_bytes(const uint8_t* scales, int64_t at) {
-  return *reinterpret_cast<const uint16_t*>(scales + at / (16 * D) * 2);
+  return *reinterpret_cast<const uint16_t*>(scales + ((uint64_t)at / (8 * D)));
 }
 
 // The score product's operand and scale of a page (kCodeScores), and K in bf16.
@@ -190,19 +190,11 @@ __device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, co
   fold_pv<false, T, D, NB>(st, u, x);
 }
 
-// V's operands of a unit, made by the four waves of a workgroup, a page and half of the
-// blocks each: blocks jb .. jb + D / 64 - 1.
-template <int D>
-struct Part {
-  static constexpr int kBlocks = D / 64;
-  uint32_t v[2 * kBlocks], vs;
-};
-
 // What the kernels ask of a format (pa_q4_tile.h).
 struct Format {
   template <int D> using Unit = q8::Unit<D>;
-  template <int D> using Part = q8::Part<D>;
   static constexpr bool kSliced = true;  // K operands in bf16: 16 dims in a row of each 64
+  static constexpr bool kSums = true;  // a base moves by sums of weights (not by the largest)
   static constexpr int tile_bytes(int D) { return q8_tile_bytes(D); }
   static __device__ __forceinline__ const uint8_t* scales_of_head(const uint8_t* scales, int g) { return scales + 2 * g; }
 
@@ -243,86 +235,6 @@ struct Format {
   template <typename T, int D, int NB>
   static __device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, const float (&x)[NB][8], int key0, int lane) {
     q8::fold_pv_edge<T, D, NB>(st, u, x, key0, lane);
-  }
-
-  // (K of a unit takes 16 registers of a wave from its load on, which with 32 columns'
-  // queries and outputs are too many at head_dim 128: the queries moved to scratch memory,
-  // whose loads wait behind K's.)
-  static constexpr bool kSharedK = true;
-  template <int D>
-  struct SharedK {
-    u32x4 x[2][D / 64][64];  // a page's KiB as lanes hold it
-    uint32_t scale[2];
-  };
-  // A wave's part: page w mod 2, KiB w / 2 (of those that there are).  (Loaded into LDS
-  // directly it needs no registers, but every read of LDS then waits for those loads.)
-  template <int D>
-  struct KPart {
-    u32x4 x;
-    uint32_t scale;
-  };
-  template <int D>
-  static __device__ __forceinline__ void load_k_part(KPart<D>& t, int w, const uint8_t* pool, int64_t at, const uint8_t* scales, int bytes, int lane) {
-    t.scale = scale_bytes<D>(scales, at);
-    t.x = __builtin_amdgcn_raw_buffer_load_b128(tile_at(pool + at, bytes), (w >> 1) % (D / 64) * 1024 + lane * 16, 0, 0);
-  }
-  template <int D>
-  static __device__ __forceinline__ void put_k_part(SharedK<D>& to, const KPart<D>& t, int w, int lane) {
-    if (w < 2 * (D / 64)) {
-      to.x[w & 1][w >> 1][lane] = t.x;
-      if (lane == 0) to.scale[w & 1] = t.scale;  // (two waves write the same)
-    }
-  }
-  template <int D>
-  static __device__ __forceinline__ void take_k(const SharedK<D>& from, Unit<D>& u, int lane) {
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      u.ks[p] = from.scale[p];
-#pragma unroll
-      for (int h = 0; h < D / 64; ++h) {
-        const u32x4 w = from.x[p][h][lane];
-        u.k[p][4 * h] = w.x; u.k[p][4 * h + 1] = w.y; u.k[p][4 * h + 2] = w.z; u.k[p][4 * h + 3] = w.w;
-      }
-    }
-  }
-  template <int D>
-  static __device__ __forceinline__ void load_scales(Unit<D>& u, int p, const uint8_t*, int64_t at, const uint8_t* scales, int, int) {
-    u.vs[p] = scale_bytes<D>(scales, at);
-  }
-  template <int D>
-  static __device__ __forceinline__ void load_v_whole(Unit<D>& u, int p, const uint8_t* pool, int64_t at, const uint8_t* scales, int bytes, int lane) {
-    load_v<0>(u, p, pool, at, scales, bytes, lane);
-    u.vs[p] = scale_bytes<D>(scales, at);
-  }
-  template <int D>
-  static __device__ __forceinline__ void load_part(Part<D>& t, const uint8_t* pool, int64_t at, const uint8_t* scales, int jb, int bytes, int lane) {
-    const __amdgpu_buffer_rsrc_t r = tile_at(pool + at, bytes);
-    t.vs = scale_bytes<D>(scales, at);
-    if constexpr (D == 128) {  // (blocks 0 and 1, or 2 and 3: a KiB of the tile)
-      const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(r, jb * 512 + lane * 16, 0, 0);
-      t.v[0] = w.x; t.v[1] = w.y; t.v[2] = w.z; t.v[3] = w.w;
-    } else {
-      const u32x2_t w = __builtin_amdgcn_raw_buffer_load_b64(r, lane * 16 + jb * 8, 0, 0);
-      t.v[0] = w.x; t.v[1] = w.y;
-    }
-  }
-  template <int D, typename Flag, typename Store>
-  static __device__ __forceinline__ void convert_part(Part<D>& t, int, int key0, int all_last, bool edge, int lane, Flag flag, Store store) {
-    bool odd = false;
-    if (edge) {  // (a NaN may be one that some columns do not see)
-      if (key0 - 4 * (lane >> 4) > all_last) t.vs = kScaleOne;
-      const uint32_t live = live_bytes(key0, all_last);
-      uint32_t any = 0;
-#pragma unroll
-      for (int w = 0; w < 2 * Part<D>::kBlocks; ++w) any |= nan_bytes(t.v[w] &= live);
-      odd |= any != 0;
-    }
-    flag(odd | beyond_fp16(t.vs));
-    const float s = scale_of<1>(t.vs);
-#pragma unroll
-    for (int b = 0; b < Part<D>::kBlocks; ++b)
-      store(b, u32x2_t{pair_of<0, true>(t.v[2 * b], s), pair_of<1, true>(t.v[2 * b], s)},
-            u32x2_t{pair_of<0, true>(t.v[2 * b + 1], s), pair_of<1, true>(t.v[2 * b + 1], s)});
   }
 };
 

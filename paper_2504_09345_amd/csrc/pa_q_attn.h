@@ -180,7 +180,7 @@ void q_attn_kernel(QAttnArgs a) {
     const int u_full = min(u1, (it.last0 + 1) / kQUnit);  // units before are seen whole by every column
     for (int k = u0; k < u1; ++k) {
       q::f32x4_t s[NB][2];
-      float x[NB][8];
+      float x[NB][8], sum[NB];
       Pages next = t;
       bool big = false, odd = false;  // the base moves; V takes other products
       auto weights = [&](bool usual) {  // the weights of unit k, and the next K; whether it is big or odd
@@ -192,7 +192,7 @@ void q_attn_kernel(QAttnArgs a) {
           q::mask_scores<T, D, NB>(st, k * kQUnit, t.bad, lane, s);
           F::clear_dead(u, k * kQUnit, all_last, lane);
         }
-        big = q::form_weights<T, D, NB>(st, s, a.scale_log2, x);
+        big = q::form_weights<F::kSums>(st, s, a.scale_log2, x, sum);
         __builtin_amdgcn_sched_barrier(0);  // (V is not waited for before the weights are formed)
         odd = F::template odd<kF16>(u);
         return __builtin_amdgcn_ballot_w64(big | odd) != 0;
@@ -203,7 +203,7 @@ void q_attn_kernel(QAttnArgs a) {
         // loads under way are known)
 #pragma unroll 1
         while (!rare & (k + 1 < u_full) & (next.bad == 0)) {
-          q::add_weights(st, x);
+          q::add_weights<F::kSums>(st, x, sum);
           F::template fold_pv<kF16>(st, u, x);
           fetch_v(next, true);
           t = next;
@@ -213,7 +213,7 @@ void q_attn_kernel(QAttnArgs a) {
       }
       int first = INT32_MAX;
       if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) first = F::first_large(u, k * kQUnit, lane);
-      q::settle_weights<true, T, D, NB>(st, s, a.scale_log2, big, x, first);
+      q::settle_weights<true, F::kSums>(st, s, a.scale_log2, big, x, sum, first);
       F::fold_pv_edge(st, u, x, k * kQUnit, lane);
       fetch_v(next, k + 1 < u1);
       t = next;

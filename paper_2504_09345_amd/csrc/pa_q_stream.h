@@ -324,7 +324,7 @@ void q_stream_kernel(QStreamArgs a) {
       for (; i < stop; ++i) {
         constexpr bool kF16 = q::kF16<T>;
         q::f32x4_t s[1][2];
-        float x[1][8];
+        float x[1][8], sum[1];
         Tiles next;
         bool big;      // the base moves
         uint64_t odd;  // V takes other products (of the lanes)
@@ -340,7 +340,7 @@ void q_stream_kernel(QStreamArgs a) {
             q::mask_scores<T, D, 1>(st, 0, t.info >> 6 & 3, lane, s);
             F::clear_dead(u, 0, tokens - 1, lane);
           }
-          big = q::form_weights<T, D, 1>(st, s, a.scale_log2, x);
+          big = q::form_weights<F::kSums>(st, s, a.scale_log2, x, sum);
           __builtin_amdgcn_sched_barrier(0);  // (V is not waited for before the weights are formed)
           odd = __builtin_amdgcn_ballot_w64(F::template odd<kF16>(u));
           return (odd | __builtin_amdgcn_ballot_w64(big)) != 0;
@@ -350,7 +350,7 @@ void q_stream_kernel(QStreamArgs a) {
         // loads under way are known)
 #pragma unroll 1
         while (!rare & (i + 1 < stop) & !(next.info & 256)) {
-          q::add_weights(st, x);
+          q::add_weights<F::kSums>(st, x, sum);
           F::template fold_pv<kF16>(st, u, x);
           fetch_v(next, true);
           t = next;
@@ -366,7 +366,7 @@ void q_stream_kernel(QStreamArgs a) {
         int first = INT32_MAX;  // (every column sees every key of the unit)
         if (__builtin_expect(odd != 0, 0))
           first = __builtin_amdgcn_ballot_w64(F::has_large(u)) != 0 ? 0 : INT32_MAX;
-        q::settle_weights<true, T, D, 1>(st, s, a.scale_log2, big, x, first);
+        q::settle_weights<true, F::kSums>(st, s, a.scale_log2, big, x, sum, first);
         F::template fold_pv<false>(st, u, x);
         fetch_v(next, i + 1 < m);
         t = next;

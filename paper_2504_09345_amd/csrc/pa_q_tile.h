@@ -221,9 +221,22 @@ constexpr float kLift = 39.0f;
 constexpr float kLiftedLimit = 0x1p-31f;
 
 // Online softmax: the weights, formed with the base of the units before; whether
-// one exceeds the limit (as a column's first does, whose base is kMInit).
-template <typename T, int D, int NB>
-__device__ __forceinline__ bool form_weights(const State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, float (&x)[NB][8]) {
+// one exceeds the limit (as a column's first does, whose base is kMInit).  SUMS: whether
+// the lane's sum of a column does, which is formed anyway, and moves the base no later.
+template <bool SUMS, typename T, int D, int NB>
+__device__ __forceinline__ bool form_weights(const State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, float (&x)[NB][8],
+                                             float (&sum)[NB]) {
+  if constexpr (SUMS) {
+    float most = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NB; ++c) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[c][i] = fast_exp2(fmaf(s[c][i >> 2][i & 3], scale_log2, -st.m[c]));
+      sum[c] = ((x[c][0] + x[c][1]) + (x[c][2] + x[c][3])) + ((x[c][4] + x[c][5]) + (x[c][6] + x[c][7]));
+      most = fmaxf(most, sum[c]);
+    }
+    return most > kWeightLimit;
+  }
   float most = 0.0f;
 #pragma unroll
   for (int c = 0; c < NB; ++c)
@@ -234,11 +247,12 @@ __device__ __forceinline__ bool form_weights(const State<T, D, NB>& st, const f3
     }
   return most > kWeightLimit;
 }
-template <typename T, int D, int NB>
-__device__ __forceinline__ void add_weights(State<T, D, NB>& st, const float (&x)[NB][8]) {
+template <bool SUMS, typename T, int D, int NB>
+__device__ __forceinline__ void add_weights(State<T, D, NB>& st, const float (&x)[NB][8], const float (&sum)[NB]) {
 #pragma unroll
   for (int c = 0; c < NB; ++c)
-    st.l[c] += ((x[c][0] + x[c][1]) + (x[c][2] + x[c][3])) + ((x[c][4] + x[c][5]) + (x[c][6] + x[c][7]));
+    if constexpr (SUMS) st.l[c] += sum[c];
+    else st.l[c] += ((x[c][0] + x[c][1]) + (x[c][2] + x[c][3])) + ((x[c][4] + x[c][5]) + (x[c][6] + x[c][7]));
 }
 // Only where one does the bases of the wave move (so a unit needs no maximum across
 // lanes); then the columns' sums.  The inner loops of waves alone leave for this: a
@@ -246,9 +260,9 @@ __device__ __forceinline__ void add_weights(State<T, D, NB>& st, const float (&x
 // LIFT: first is the unit's first key with large V (INT32_MAX: none); the bases of the
 // columns that see it are lifted.  They lie kHeadroom below the largest score so far, or
 // up to 8 log2 units more (the limit), so they come to lie kLift to kLift + 8 above.
-template <bool LIFT, typename T, int D, int NB>
+template <bool LIFT, bool SUMS, typename T, int D, int NB>
 __device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, bool big,
-                                               float (&x)[NB][8], int first = INT32_MAX) {
+                                               float (&x)[NB][8], float (&sum)[NB], int first = INT32_MAX) {
   float up[NB] = {};
   if constexpr (LIFT) {
     if (__builtin_expect(st.any_lifted | (first != INT32_MAX), 0)) {
@@ -280,9 +294,9 @@ __device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_
 #pragma unroll
       for (int mb = 0; mb < D / 16; ++mb) st.acc[c][mb] *= alpha;
     }
-    form_weights<T, D, NB>(st, s, scale_log2, x);
+    form_weights<SUMS>(st, s, scale_log2, x, sum);
   }
-  add_weights(st, x);
+  add_weights<SUMS>(st, x, sum);
 }
 
 // The lane's eight consecutive outputs of block j (dims 32 j + 8 (lane / 16) ..).
