@@ -12,10 +12,9 @@
 // 690.  One barrier per unit: unit k is multiplied while V of unit k + 1 is converted and
 // K of unit k + 2 put into the other buffers.
 //
-// A page with a V scale outside fp16's window, or that holds a NaN among keys which some
-// columns do not see, is flagged by the waves that convert it, and every wave takes the
-// unit by the general products instead, with V of its own; so does a wave all units after
-// one with large V.
+// A unit with a V scale outside fp16's window every wave takes by the general products
+// instead, with V of its own; also one with a NaN among keys that some columns do not see
+// (flagged by the waves that convert it), and a wave all units after one with large V.
 #include "pa_q8_tile.h"
 #include "pa_q_attn.h"
 
@@ -39,7 +38,7 @@ void q8_chunk_kernel(QAttnArgs a) {
   constexpr int kNB = kChunkNB;
   // V operands of block j, half h (even or odd dims), page p: 8 bytes per lane
   __shared__ __attribute__((aligned(16))) u32x2_t s_v[2][D / 32][2][2][64];
-  __shared__ int32_t s_odd[2][kQWaves];
+  __shared__ int32_t s_nan[2][kQWaves];
   __shared__ SharedK<D> s_k[2];
   const int S = a.s;
   const int lane = threadIdx.x & 63, n = lane & 15, G = lane >> 4;
@@ -131,7 +130,6 @@ void q8_chunk_kernel(QAttnArgs a) {
   };
   auto convert = [&](int k) {
     const int buf = k & 1;
-    bool odd = false;
     if (k >= edge) {  // (a NaN may be one that some columns do not see)
       const int key0 = k * kQUnit + 16 * vp;
       if (key0 > all_last) vs = q8::kScaleOne;
@@ -139,10 +137,9 @@ void q8_chunk_kernel(QAttnArgs a) {
       uint32_t any = 0;
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) any |= q8::nan_bytes(vc[i] &= live);
-      odd = any != 0;
+      const bool any_lane = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+      if (lane == 0) s_nan[buf][w] = any_lane;
     }
-    const bool any_odd = __builtin_amdgcn_ballot_w64(odd | q8::beyond_fp16(vs)) != 0;
-    if (lane == 0) s_odd[buf][w] = any_odd;
     const float s = q::scale_of<1>(vs);
 #pragma unroll
     for (int b = 0; b < D / 64; ++b)
@@ -151,7 +148,10 @@ void q8_chunk_kernel(QAttnArgs a) {
         s_v[buf][jb + b][h][vp][lane] = u32x2_t{q8::pair_of<0, true>(vc[2 * b + h], s), q8::pair_of<1, true>(vc[2 * b + h], s)};
   };
   q8::Unit<D> u;  // K of a unit; V only of a flagged one
-  auto scores = [&](int k, q::f32x4_t (&x)[kNB][2]) {
+  // The scores of unit k, and whether fp16 does not hold its V exactly.  (Known a unit
+  // ahead from the scales beside K: a flag of the waves that convert V would be read
+  // right after the barrier, 35 us of the 687.)
+  auto scores = [&](int k, q::f32x4_t (&x)[kNB][2]) -> bool {
     const SharedK<D>& from = s_k[k & 1];
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
@@ -163,9 +163,11 @@ void q8_chunk_kernel(QAttnArgs a) {
       }
     }
     q8::fold_qk<T, D, kNB>(st, u, x);
+    // (a page past the item's last key may be any)
+    return __builtin_amdgcn_ballot_w64(q8::beyond_fp16(u.ks[0]) || (k * kQUnit + kPage <= all_last && q8::beyond_fp16(u.ks[1]))) != 0;
   };
-  auto flagged = [&](int k) {
-    const int32_t* f = s_odd[k & 1];
+  auto has_nan = [&](int k) {  // (k >= edge)
+    const int32_t* f = s_nan[k & 1];
     return __builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3]) != 0;
   };
   auto fold_staged = [&](int k, const float (&x)[kNB][8]) {
@@ -202,30 +204,25 @@ void q8_chunk_kernel(QAttnArgs a) {
   if (u0 + 2 < u1) t2 = t3 = pages(u0 + 2);
   put_k(u0 + 1);
   __syncthreads();
-  scores(u0, s);
+  bool odd = scores(u0, s);  // V of unit k takes other products
   fetch_k(t2);
   convert(u0);
   fetch_v(t1);
   const int plain = min(w1, (first_last + 1) / kQUnit);  // units before are seen whole by the wave's columns
   for (int k = u0; k < u1;) {
     float x[kNB][8], sum[kNB];
-    bool entered = false;
 #pragma unroll 1
-    for (; k < plain && (t.a | t.b) >= 0 && !st.any_lifted; ++k) {  // (nothing but the usual unit, so that the sums stay in place)
+    for (; k < plain && (t.a | t.b) >= 0 && !odd && !st.any_lifted; ++k) {  // (nothing but the usual unit, so that the sums stay in place)
       __syncthreads();  // unit k is staged, and unit k - 1 is done with
-      if (flagged(k)) {
-        entered = true;
-        break;
-      }
       if (k + 3 < u1) t3 = pages(k + 3);
-      scores(k + 1, sn);
+      odd = scores(k + 1, sn);
       const bool big = q::form_weights<true>(st, s, a.scale_log2, x, sum);
       q::settle_weights<false, true>(st, s, a.scale_log2, big, x, sum);
       convert(k + 1);
-      put_k(k + 2);
-      fold_staged(k, x);
       fetch_v(t2);
+      put_k(k + 2);
       fetch_k(t3);
+      fold_staged(k, x);
 #pragma unroll
       for (int c = 0; c < kNB; ++c)
 #pragma unroll
@@ -235,12 +232,12 @@ void q8_chunk_kernel(QAttnArgs a) {
       t2 = t3;
     }
     if (k >= u1) break;
-    if (!entered) __syncthreads();
+    __syncthreads();
     if (k + 3 < u1) t3 = pages(k + 3);
-    if (k + 1 < w1) scores(k + 1, sn);
+    bool odd_next = false;
+    if (k + 1 < w1) odd_next = scores(k + 1, sn);
     if (k < w1) {
       q::mask_scores<T, D, kNB>(st, k * kQUnit, (t.a < 0 ? 1 : 0) | (t.b < 0 ? 2 : 0), lane, s);
-      const bool odd = flagged(k);
       q8::Unit<D> whole;
       int first = INT32_MAX;
       if (__builtin_expect(odd, 0)) {  // (the scales alone: all of V would hold registers meanwhile)
@@ -250,7 +247,7 @@ void q8_chunk_kernel(QAttnArgs a) {
       }
       const bool big = q::form_weights<true>(st, s, a.scale_log2, x, sum);
       q::settle_weights<true, true>(st, s, a.scale_log2, big, x, sum, first);
-      if (__builtin_expect(odd | st.any_lifted, 0)) {
+      if (__builtin_expect(odd || st.any_lifted || (k >= edge && has_nan(k)), 0)) {
         q8::load_words<D, 0>(q8::tile_at(vg + at_of(t.a), q8_tile_bytes(D)), lane, whole.v[0]);
         q8::load_words<D, 0>(q8::tile_at(vg + at_of(t.b), q8_tile_bytes(D)), lane, whole.v[1]);
         whole.vs[0] = q8::scale_bytes<D>(sg, at_of(t.a));
@@ -271,6 +268,7 @@ void q8_chunk_kernel(QAttnArgs a) {
 #pragma unroll
         for (int p = 0; p < 2; ++p) s[c][p] = sn[c][p];
     }
+    odd = odd_next;
     t = t1;
     t1 = t2;
     t2 = t3;
