@@ -151,7 +151,7 @@ void q8_chunk_kernel(QAttnArgs a) {
   // The scores of unit k, and whether fp16 does not hold its V exactly.  (Known a unit
   // ahead from the scales beside K: a flag of the waves that convert V would be read
   // right after the barrier, 35 us of the 687.)
-  auto scores = [&](int k, q::f32x4_t (&x)[kNB][2]) -> bool {
+  auto scores = [&](int k, q::f32x4_t (&x)[kNB][2]) -> uint32_t {  // (the same in all lanes)
     const SharedK<D>& from = s_k[k & 1];
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
@@ -164,7 +164,8 @@ void q8_chunk_kernel(QAttnArgs a) {
     }
     q8::fold_qk<T, D, kNB>(st, u, x);
     // (a page past the item's last key may be any)
-    return __builtin_amdgcn_ballot_w64(q8::beyond_fp16(u.ks[0]) || (k * kQUnit + kPage <= all_last && q8::beyond_fp16(u.ks[1]))) != 0;
+    const uint32_t second = k * kQUnit + kPage <= all_last ? 1u : 0u;
+    return (uint32_t)q8::beyond_fp16(u.ks[0]) | ((uint32_t)q8::beyond_fp16(u.ks[1]) & second);
   };
   auto has_nan = [&](int k) {  // (k >= edge)
     const int32_t* f = s_nan[k & 1];
@@ -204,7 +205,7 @@ void q8_chunk_kernel(QAttnArgs a) {
   if (u0 + 2 < u1) t2 = t3 = pages(u0 + 2);
   put_k(u0 + 1);
   __syncthreads();
-  bool odd = scores(u0, s);  // V of unit k takes other products
+  bool odd = __builtin_amdgcn_readfirstlane(scores(u0, s)) != 0;  // V of unit k takes other products
   fetch_k(t2);
   convert(u0);
   fetch_v(t1);
@@ -215,8 +216,14 @@ void q8_chunk_kernel(QAttnArgs a) {
     for (; k < plain && (t.a | t.b) >= 0 && !odd && !st.any_lifted; ++k) {  // (nothing but the usual unit, so that the sums stay in place)
       __syncthreads();  // unit k is staged, and unit k - 1 is done with
       if (k + 3 < u1) t3 = pages(k + 3);
-      odd = scores(k + 1, sn);
+      const uint32_t odd_next = scores(k + 1, sn);
       const bool big = q::form_weights<true>(st, s, a.scale_log2, x, sum);
+      // (the next unit's scores are formed here, between the weights, and not behind the
+      // branch where the base moves: used only then, they would sink to the loop's end)
+#pragma unroll
+      for (int c = 0; c < kNB; ++c)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) asm volatile("" : "+v"(sn[c][p]));
       q::settle_weights<false, true>(st, s, a.scale_log2, big, x, sum);
       convert(k + 1);
       fetch_v(t2);
@@ -227,6 +234,7 @@ void q8_chunk_kernel(QAttnArgs a) {
       for (int c = 0; c < kNB; ++c)
 #pragma unroll
         for (int p = 0; p < 2; ++p) s[c][p] = sn[c][p];
+      odd = __builtin_amdgcn_readfirstlane(odd_next) != 0;
       t = t1;
       t1 = t2;
       t2 = t3;
@@ -234,7 +242,7 @@ void q8_chunk_kernel(QAttnArgs a) {
     if (k >= u1) break;
     __syncthreads();
     if (k + 3 < u1) t3 = pages(k + 3);
-    bool odd_next = false;
+    uint32_t odd_next = 0;
     if (k + 1 < w1) odd_next = scores(k + 1, sn);
     if (k < w1) {
       q::mask_scores<T, D, kNB>(st, k * kQUnit, (t.a < 0 ? 1 : 0) | (t.b < 0 ? 2 : 0), lane, s);
@@ -268,7 +276,7 @@ void q8_chunk_kernel(QAttnArgs a) {
 #pragma unroll
         for (int p = 0; p < 2; ++p) s[c][p] = sn[c][p];
     }
-    odd = odd_next;
+    odd = __builtin_amdgcn_readfirstlane(odd_next) != 0;
     t = t1;
     t1 = t2;
     t2 = t3;
