@@ -224,6 +224,14 @@ void q8_chunk_kernel(QAttnArgs a) {
       for (int c = 0; c < kNB; ++c)
 #pragma unroll
         for (int p = 0; p < 2; ++p) asm volatile("" : "+v"(sn[c][p]));
+      // (that order of issue: 644 us instead of 650)
+      __builtin_amdgcn_sched_group_barrier(0x100, D == 128 ? 5 : 3, 0);  // K from LDS
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);    // a product
+        __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);    // vector instructions
+        __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);  // exponentials
+      }
       q::settle_weights<false, true>(st, s, a.scale_log2, big, x, sum);
       convert(k + 1);
       fetch_v(t2);
