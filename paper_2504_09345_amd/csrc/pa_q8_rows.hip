@@ -33,9 +33,21 @@ template <bool HIGH>
 __device__ __forceinline__ uint32_t codes_of(uint32_t w, float a, float b) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)w, HIGH);
 }
-// The codes of x times inv.
-__device__ __forceinline__ u32x2_t encode(const float (&x)[8], float inv) {
-  float y[8];
+// Eight elements as they lie in memory.
+template <typename T>
+struct Raw {
+  u32x4 w[sizeof(T) / 2];
+};
+__device__ __forceinline__ void widen_raw(const Raw<uint16_t>& r, float (&x)[8]) { widen(r.w[0], x, uint16_t()); }
+__device__ __forceinline__ void widen_raw(const Raw<float>& r, float (&x)[8]) {
+  widen(r.w[0], x, 0.0f);
+  widen(r.w[1], x + 4, 0.0f);
+}
+// The codes of x times inv, whatever x is.
+template <typename T>
+__device__ __forceinline__ u32x2_t encode_any(const Raw<T>& r, float inv) {
+  float x[8], y[8];
+  widen_raw(r, x);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     // (infinities too are held as NaN)
@@ -48,19 +60,57 @@ __device__ __forceinline__ u32x2_t encode(const float (&x)[8], float inv) {
   w.y = codes_of<true>(w.y, y[6], y[7]);
   return w;
 }
+// The same of finite x of at most 448 scale, in four instructions.
+template <typename T>
+__device__ __forceinline__ u32x2_t encode(const Raw<T>& r, float scale) {
+  typedef short s16x2_t __attribute__((ext_vector_type(2)));
+  u32x2_t w;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    s16x2_t c = {0, 0};
+    if constexpr (sizeof(T) == 2) {
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, as_bf16x2(r.w[0][2 * h]), scale, false);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, as_bf16x2(r.w[0][2 * h + 1]), scale, true);
+    } else {
+      const u32x4 x = r.w[h];
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, __uint_as_float(x[0]), __uint_as_float(x[1]), scale, false);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, __uint_as_float(x[2]), __uint_as_float(x[3]), scale, true);
+    }
+    w[h] = __builtin_bit_cast(uint32_t, c);
+  }
+  return w;
+}
 // Four codes rounded again, f (a power of two below 1) times their values.
 __device__ __forceinline__ uint32_t again(uint32_t w, float f) {
   const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
   return codes_of<true>(codes_of<false>(0, a[0] * f, a[1] * f), b[0] * f, b[1] * f);
 }
 
-// The largest finite magnitude's bits, of m and x.
-__device__ __forceinline__ uint32_t most_of(uint32_t m, const float (&x)[8]) {
+// The largest magnitude of m and the elements, an infinity or (bf16) a NaN where there is
+// one; and the largest finite one.
+__device__ __forceinline__ float most_of(float m, const Raw<uint16_t>& r) {
+  typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+  u16x2_t x = {0, 0};  // (bits of magnitudes compare as they do)
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t u = __float_as_uint(x[e]) & 0x7fffffffu;
-    m = max(m, u < 0x7f800000u ? u : 0u);
-  }
+  for (int i = 0; i < 4; ++i) x = __builtin_elementwise_max(x, __builtin_bit_cast(u16x2_t, r.w[0][i] & 0x7fff7fffu));
+  return __uint_as_float(max(__float_as_uint(m), (uint32_t)max(x[0], x[1]) << 16));
+}
+__device__ __forceinline__ float most_of(float m, const Raw<float>& r) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t u = r.w[h][i] & 0x7fffffffu;  // (NaN too)
+      m = __uint_as_float(max(__float_as_uint(m), u));
+    }
+  return m;
+}
+template <typename T>
+__device__ __forceinline__ float finite_most_of(float m, const Raw<T>& r) {
+  float x[8];
+  widen_raw(r, x);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = fabsf(x[e]) <= __FLT_MAX__ ? fmaxf(m, fabsf(x[e])) : m;
   return m;
 }
 
@@ -70,22 +120,36 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q8_append_kernel(QRowsArgs a,
   const int lane = threadIdx.x & 63;
   const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (slot >= slots) return;
-  const Group p = group_of<kPage>(a, slot, lane);
+  Group p = group_of<kPage, false>(a, slot, lane);
   if (p.n <= 0 || p.bad) return;
   const int i = blockIdx.y * 64 + lane, which = blockIdx.z;
   if (i >= a.H_kv * CH) return;  // (whole heads)
   const int g = i / CH, c = i % CH;
   const int64_t step = (int64_t)a.H_kv * D;
   const T* from = reinterpret_cast<const T*>(which == 0 ? a.k_rows : a.v_rows) + (int64_t)p.row * step + (int64_t)i * 8;
+  // all 16 tokens of the page, whichever are new (the others: a new row again, unused),
+  // loaded while the page's entry is
+  Raw<T> raw[kPage];
+  auto load_row = [&](int t, int row) {
+#pragma unroll
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) raw[t].w[h] = *reinterpret_cast<const u32x4*>(from + row * step + h * (16 / (int)sizeof(T)));
+  };
+  const bool one = p.n == 1;
+  if (one) {
+    load_row(0, 0);
+  } else {
+#pragma unroll
+    for (int t = 0; t < kPage; ++t) load_row(t, min(max(t - p.token, 0), p.n - 1));
+  }
+  checked_page(a, p);
+  if (p.bad) return;
   const int64_t head = (int64_t)p.page * a.H_kv + g;
   uint8_t* tile = (which == 0 ? a.k_pages : a.v_pages) + head * q8_tile_bytes(D);
   uint8_t* scale = a.scales + head * 2 + which;
   const int held = p.token > 0 ? *scale : 0;  // (no earlier tokens: none that bounds it)
-
-  // The page's scale, given the largest of the lane's new values; the earlier tokens are
-  // brought to it.  Its inverse.
-  auto settle = [&](uint32_t most) {
-    float m = __uint_as_float(most);
+  // The page's scale byte, given the largest of the lane's new finite values; the earlier
+  // tokens are brought to it.
+  auto settle = [&](float m) {
     m = fmaxf(m, dpp_xor1(m));
     m = fmaxf(m, dpp_xor2(m));
     m = fmaxf(m, dpp_half_mirror(m));
@@ -114,7 +178,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q8_append_kernel(QRowsArgs a,
       }
     }
     if (c == 0 && (p.token == 0 || e > held)) *scale = (uint8_t)e;
-    return power(254 - e);
+    return e;
   };
   auto put_v = [&](int t, u32x2_t w) {  // a token's bytes alone
 #pragma unroll
@@ -126,38 +190,34 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q8_append_kernel(QRowsArgs a,
     }
   };
 
-  if (p.n == 1) {
-    float x[8];
-    load_eight(from, x);
-    const u32x2_t w = encode(x, settle(most_of(0, x)));
+  float most = 0.0f;
+  if (one) {
+    most = most_of(most, raw[0]);
+  } else {
+#pragma unroll
+    for (int t = 0; t < kPage; ++t) most = most_of(most, raw[t]);
+  }
+  // (rare: values that are not finite are left out of the scale, and those beyond the
+  // largest scale's are cut)
+  bool plain = most <= __FLT_MAX__;
+  if (__builtin_amdgcn_ballot_w64(!plain) != 0) {
+    plain = false;
+    most = 0.0f;
+#pragma unroll
+    for (int t = 0; t < kPage; ++t)
+      if (t == 0 || !one) most = finite_most_of(most, raw[t]);
+  }
+  const int e = settle(most);
+  plain = __builtin_amdgcn_ballot_w64(!plain || e >= kHigh) == 0;
+  const float size = power(e), inv = power(254 - e);
+  auto codes = [&](int t) { return plain ? encode(raw[t], size) : encode_any(raw[t], inv); };
+
+  if (one) {
+    const u32x2_t w = codes(0);
     if (which == 0) *reinterpret_cast<u32x2_t*>(tile + Place<D>::k(p.token, c)) = w;
     else put_v(p.token, w);
     return;
   }
-  // all 16 tokens of the page, whichever are new (the others: a new row again, unused)
-  u32x4 raw[kPage][sizeof(T) / 2];
-#pragma unroll
-  for (int t = 0; t < kPage; ++t) {
-    const T* row = from + min(max(t - p.token, 0), p.n - 1) * step;
-#pragma unroll
-    for (int h = 0; h < (int)sizeof(T) / 2; ++h) raw[t][h] = *reinterpret_cast<const u32x4*>(row + h * 4);
-  }
-  auto widened = [&](int t, float (&x)[8]) {
-    if constexpr (sizeof(T) == 2) {
-      widen(raw[t][0], x, uint16_t());
-    } else {
-      widen(raw[t][0], x, 0.0f);
-      widen(raw[t][1], x + 4, 0.0f);
-    }
-  };
-  uint32_t most = 0;
-#pragma unroll
-  for (int t = 0; t < kPage; ++t) {
-    float x[8];
-    widened(t, x);
-    most = most_of(most, x);
-  }
-  const float inv = settle(most);
   const int first = p.token, end = p.token + p.n;
 #pragma unroll
   for (int t4 = 0; t4 < kPage / 4; ++t4) {
@@ -165,9 +225,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q8_append_kernel(QRowsArgs a,
     uint32_t lo[4], hi[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      float x[8];
-      widened(4 * t4 + t, x);
-      const u32x2_t w = encode(x, inv);
+      const u32x2_t w = codes(4 * t4 + t);
       lo[t] = w.x;
       hi[t] = w.y;
     }

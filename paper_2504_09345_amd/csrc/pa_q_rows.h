@@ -19,7 +19,10 @@ struct Group {
   bool bad;     // rows that the contract does not allow
   int page, token;  // token: of the first row
 };
-template <int kGroup>
+// PAGE: false leaves the page's entry, which `page` then is, unchecked (checked_page), so
+// that what does not depend on it need not wait for it.
+__device__ __forceinline__ void checked_page(const QRowsArgs& a, Group& p) { p.bad |= p.page < 0 || p.page >= a.num_pages; }
+template <int kGroup, bool PAGE = true>
 __device__ __forceinline__ Group group_of(const QRowsArgs& a, int slot, int lane) {
   Group p{slot, 1, false, 0, 0};
   int b = slot, L = 1, j = 0;
@@ -47,7 +50,7 @@ __device__ __forceinline__ Group group_of(const QRowsArgs& a, int slot, int lane
   if (p.bad) return p;
   p.page = a.block_table[(int64_t)b * a.bt_stride + pos / kPage];
   p.token = pos % kPage;
-  p.bad = p.page < 0 || p.page >= a.num_pages;
+  if constexpr (PAGE) checked_page(a, p);
   return p;
 }
 
