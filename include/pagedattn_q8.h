@@ -94,9 +94,7 @@ int pa_workspace_size_q8(const pa_dims_t *dims, size_t *bytes);
  * matrix cores with fp32 accumulation; softmax bases and sums are fp32, and so are the
  * scores: scale q.k log2 e may be up to 2^27 in magnitude (its steps there are 8; beyond,
  * an output may be NaN).  Queries:
- * bf16 ones as they are, except at head_dim 128, where a query is two e4m3 parts of
- * its row's scale (an error of at most 2^-22 of the row's largest, or 2^-135); fp32 ones as
- * sums of three bf16 parts.  Softmax weights: for bf16 outputs in fp16 where every V
+ * bf16 ones as they are, fp32 ones as sums of three bf16 parts.  Softmax weights: for bf16 outputs in fp16 where every V
  * of the step is exact in fp16 (scales 2^-15 .. 2^7) and as two bf16 parts elsewhere,
  * for fp32 outputs as three bf16 parts.  Weighted sums do not overflow: an output is
  * finite wherever the weighted mean is.  (A row that sees a page whose V has a scale of

@@ -55,7 +55,7 @@ void q4_chunk_kernel(QAttnArgs a) {
     const bool there = pos < it.n_pos;
     st.last[c] = there ? it.last0 + pos : -1;
     at[c] = (int64_t)(it.row0 + (there ? pos : 0)) * a.H_q + (int64_t)g * S + col % S;
-    q4::load_query<false, T, D>(st.q[c], there ? reinterpret_cast<const T*>(a.q) + at[c] * D : nullptr, lane);
+    q4::load_query<false>(st.q[c], there ? reinterpret_cast<const T*>(a.q) + at[c] * D : nullptr, lane);
   }
   q4::reset(st);
   const int pos0 = 16 * kNB * w / S, pos1 = min(it.n_pos - 1, (16 * kNB * (w + 1) - 1) / S);

@@ -96,13 +96,13 @@ __device__ __forceinline__ void v_operands(const Unit<D>& u, u32x4 (&a)[2]) {
 //
 // Scores S^T[token][column] = K . Q^T, the K operand shared by the columns.  shift: of
 // the scale words.
-template <typename T, int D, int NB>
-__device__ __forceinline__ void fold_qk(const State<T, D, NB>& st, const Unit<D>& u, int shift, f32x4_t (&s)[NB][2]) {
+template <typename T, int D, int NB, bool C>
+__device__ __forceinline__ void fold_qk(const State<T, D, NB, C>& st, const Unit<D>& u, int shift, f32x4_t (&s)[NB][2]) {
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
 #pragma unroll
     for (int c = 0; c < NB; ++c) s[c][p] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    if constexpr (kCodeScores<T, D>) {
+    if constexpr (C) {
       const int ks = (int)(u.ks[p] >> shift);  // (the product reads the lowest byte)
       const i32x8_t a = {(int)u.k[p][0], (int)u.k[p][1], (int)u.k[p][2], (int)u.k[p][3], 0, 0, 0, 0};
 #pragma unroll
@@ -187,8 +187,8 @@ __device__ __forceinline__ int first_large(const Unit<D>& u, int key0, int lane)
 }
 
 // O^T += V^T . P^T, in fp16 or in bf16 parts.
-template <bool F16, typename T, int D, int NB>
-__device__ __forceinline__ void fold_pv(State<T, D, NB>& st, const Unit<D>& u, const float (&x)[NB][8]) {
+template <bool F16, typename T, int D, int NB, bool C>
+__device__ __forceinline__ void fold_pv(State<T, D, NB, C>& st, const Unit<D>& u, const float (&x)[NB][8]) {
   constexpr int N = F16 ? 1 : kPParts<T>;
   u32x4 pt[NB][N];
 #pragma unroll
@@ -231,8 +231,8 @@ __device__ __forceinline__ void fold_pv(State<T, D, NB>& st, const Unit<D>& u, c
 // V reaches the columns that see its key, and no other (a weight of 0 times NaN
 // would be NaN; its codes are 0 already).  Its scale becomes 1, and the columns that see the first such key
 // of a block get NaN outright.  (Keys that no column sees are cleared.)
-template <typename T, int D, int NB>
-__device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, const float (&x)[NB][8], int key0, int lane) {
+template <typename T, int D, int NB, bool C>
+__device__ __forceinline__ void fold_pv_edge(State<T, D, NB, C>& st, Unit<D>& u, const float (&x)[NB][8], int key0, int lane) {
   constexpr int n = D / 32;
   int nan_key[n];
   bool any = false;
@@ -254,7 +254,7 @@ __device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, co
       }
     }
   const bool nans = __builtin_amdgcn_ballot_w64(any) != 0;
-  fold_pv<false, T, D, NB>(st, u, x);
+  fold_pv<false>(st, u, x);
   if (nans) {
 #pragma unroll
     for (int j = 0; j < n; ++j) {
@@ -271,6 +271,7 @@ __device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, co
 // What the kernels ask of a format.
 struct Format {
   template <int D> using Unit = q4::Unit<D>;
+  template <typename T, int D> static constexpr bool kCodes = kCodeScores<T, D>;
   static constexpr bool kSliced = false;  // K operands in bf16: a lane's dims in a row
   static constexpr bool kSums = false;  // a base moves by sums of weights
   static constexpr int tile_bytes(int D) { return q4_tile_bytes(D); }
@@ -299,17 +300,17 @@ struct Format {
   static __device__ __forceinline__ int first_large(const Unit<D>& u, int key0, int lane) { return q4::first_large(u, key0, lane); }
   template <int D>
   static __device__ __forceinline__ void clear_dead(Unit<D>& u, int key0, int all_last, int lane) { q4::clear_dead(u, key0, all_last, lane); }
-  template <typename T, int D, int NB>
-  static __device__ __forceinline__ void fold_qk(const State<T, D, NB>& st, const Unit<D>& u, int shift, f32x4_t (&s)[NB][2]) {
-    q4::fold_qk<T, D, NB>(st, u, shift, s);
+  template <typename T, int D, int NB, bool C>
+  static __device__ __forceinline__ void fold_qk(const State<T, D, NB, C>& st, const Unit<D>& u, int shift, f32x4_t (&s)[NB][2]) {
+    q4::fold_qk(st, u, shift, s);
   }
-  template <bool F16, typename T, int D, int NB>
-  static __device__ __forceinline__ void fold_pv(State<T, D, NB>& st, const Unit<D>& u, const float (&x)[NB][8]) {
-    q4::fold_pv<F16, T, D, NB>(st, u, x);
+  template <bool F16, typename T, int D, int NB, bool C>
+  static __device__ __forceinline__ void fold_pv(State<T, D, NB, C>& st, const Unit<D>& u, const float (&x)[NB][8]) {
+    q4::fold_pv<F16>(st, u, x);
   }
-  template <typename T, int D, int NB>
-  static __device__ __forceinline__ void fold_pv_edge(State<T, D, NB>& st, Unit<D>& u, const float (&x)[NB][8], int key0, int lane) {
-    q4::fold_pv_edge<T, D, NB>(st, u, x, key0, lane);
+  template <typename T, int D, int NB, bool C>
+  static __device__ __forceinline__ void fold_pv_edge(State<T, D, NB, C>& st, Unit<D>& u, const float (&x)[NB][8], int key0, int lane) {
+    q4::fold_pv_edge(st, u, x, key0, lane);
   }
 };
 

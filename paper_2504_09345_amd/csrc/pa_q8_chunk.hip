@@ -27,7 +27,7 @@ constexpr int kColumns = 16 * kChunkNB * kQWaves;  // of a workgroup
 // K of a unit in LDS.
 template <int D>
 struct SharedK {
-  u32x4 x[2][D / 64][64];  // a page's KiB as lanes hold it
+  u32x4 x[2][D / 32][64];  // a page's operands in bf16, one step's after the other's
   uint32_t scale[2];       // the pages' scale bytes
 };
 
@@ -60,7 +60,7 @@ void q8_chunk_kernel(QAttnArgs a) {
   if (u0 >= u1) return;
 
   // the wave's columns, and the keys that its first and its last one see
-  q::State<T, D, kNB> st;
+  q::State<T, D, kNB, false> st;
   int64_t at[kNB];
 #pragma unroll
   for (int c = 0; c < kNB; ++c) {
@@ -68,7 +68,7 @@ void q8_chunk_kernel(QAttnArgs a) {
     const bool there = pos < it.n_pos;
     st.last[c] = there ? it.last0 + pos : -1;
     at[c] = (int64_t)(it.row0 + (there ? pos : 0)) * a.H_q + (int64_t)g * S + col % S;
-    q::load_query<true, T, D>(st.q[c], there ? reinterpret_cast<const T*>(a.q) + at[c] * D : nullptr, lane);
+    q::load_query<true>(st.q[c], there ? reinterpret_cast<const T*>(a.q) + at[c] * D : nullptr, lane);
   }
   q::reset(st);
   const int pos0 = 16 * kNB * w / S, pos1 = min(it.n_pos - 1, (16 * kNB * (w + 1) - 1) / S);
@@ -102,11 +102,10 @@ void q8_chunk_kernel(QAttnArgs a) {
   };
   auto at_of = [&](int id) { return max(id, 0) * page_bytes; };  // (of the pool's first tile, where the entry lies outside)
 
-  // The wave's parts: page w mod 2, of V blocks jb .. jb + D / 64 - 1, of K KiB kk.
-  const int vp = w & 1, jb = (w >> 1) * (D / 64), kk = (w >> 1) % (D / 64);
+  // The wave's parts: page w mod 2, of V blocks jb .. jb + D / 64 - 1, of K as many steps.
+  const int vp = w & 1, jb = (w >> 1) * (D / 64);
   uint32_t vc[D / 32], vs;  // V: words of even and odd dims of each block, and the scale bytes
-  u32x4 kc;
-  uint32_t ks;
+  uint32_t kc[D / 32], ks;  // K: eight codes of each step
   auto fetch_v = [&](const Pages& t) {
     const int64_t at = at_of(t.own);
     vs = q8::scale_bytes<D>(sg, at);
@@ -121,14 +120,20 @@ void q8_chunk_kernel(QAttnArgs a) {
   auto fetch_k = [&](const Pages& t) {
     const int64_t at = at_of(t.own);
     ks = q8::scale_bytes<D>(sg, at);
-    kc = *reinterpret_cast<const u32x4*>(kg + at + (kk * 1024 + lane * 16));
+    if constexpr (D == 128) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(kg + at + (jb * 512 + lane * 16));
+      kc[0] = x.x; kc[1] = x.y; kc[2] = x.z; kc[3] = x.w;
+    } else {
+      const u32x2_t x = *reinterpret_cast<const u32x2_t*>(kg + at + (jb * 8 + lane * 16));
+      kc[0] = x.x; kc[1] = x.y;
+    }
   };
   auto put_k = [&](int k) {
     SharedK<D>& to = s_k[k & 1];
-    if (D == 128 || w < 2) {
-      to.x[vp][kk][lane] = kc;
-      if (lane == 0) to.scale[vp] = ks;  // (two waves write the same)
-    }
+    const float s = q::scale_of<0>(ks);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) to.x[vp][jb + i][lane] = q8::eight_of(kc[2 * i], kc[2 * i + 1], s);
+    if (lane == 0) to.scale[vp] = ks;  // (two waves write the same)
   };
   auto convert = [&](int k) {
     const int buf = k & 1;
@@ -149,25 +154,28 @@ void q8_chunk_kernel(QAttnArgs a) {
       for (int h = 0; h < 2; ++h)
         s_v[buf][jb + b][h][vp][lane] = u32x2_t{q8::pair_of<0, true>(vc[2 * b + h], s), q8::pair_of<1, true>(vc[2 * b + h], s)};
   };
-  q8::Unit<D> u;  // K of a unit; V only of a flagged one
   // The scores of unit k, and whether fp16 does not hold its V exactly.  (Known a unit
   // ahead from the scales beside K: a flag of the waves that convert V would be read
-  // right after the barrier, 35 us of the 687.)
+  // right after the barrier, 35 us of 687.)
   auto scores = [&](int k, q::f32x4_t (&x)[kNB][2]) -> uint32_t {  // (the same in all lanes)
     const SharedK<D>& from = s_k[k & 1];
+    const uint32_t ks0 = from.scale[0], ks1 = from.scale[1];
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      u.ks[p] = from.scale[p];
+    for (int c = 0; c < kNB; ++c)
 #pragma unroll
-      for (int h = 0; h < D / 64; ++h) {
-        const u32x4 x4 = from.x[p][h][lane];
-        u.k[p][4 * h] = x4.x; u.k[p][4 * h + 1] = x4.y; u.k[p][4 * h + 2] = x4.z; u.k[p][4 * h + 3] = x4.w;
+      for (int p = 0; p < 2; ++p) x[c][p] = q::f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const q::bf16x8_t ka = __builtin_bit_cast(q::bf16x8_t, from.x[p][i][lane]);
+#pragma unroll
+        for (int c = 0; c < kNB; ++c)
+          x[c][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, __builtin_bit_cast(q::bf16x8_t, st.q[c].x[i][0]), x[c][p], 0, 0, 0);
       }
-    }
-    q8::fold_qk<T, D, kNB>(st, u, x);
     // (a page past the item's last key may be any)
     const uint32_t second = k * kQUnit + kPage <= all_last ? 1u : 0u;
-    return (uint32_t)q8::beyond_fp16(u.ks[0]) | ((uint32_t)q8::beyond_fp16(u.ks[1]) & second);
+    return (uint32_t)q8::beyond_fp16(ks0) | ((uint32_t)q8::beyond_fp16(ks1) & second);
   };
   auto has_nan = [&](int k) {  // (k >= edge)
     const int32_t* f = s_nan[k & 1];
@@ -227,12 +235,12 @@ void q8_chunk_kernel(QAttnArgs a) {
 #pragma unroll
         for (int p = 0; p < 2; ++p) asm volatile("" : "+v"(sn[c][p]));
       // (that order of issue: 644 us instead of 650)
-      __builtin_amdgcn_sched_group_barrier(0x100, D == 128 ? 5 : 3, 0);  // K from LDS
+      __builtin_amdgcn_sched_group_barrier(0x100, D / 16 + 1, 0);  // K from LDS
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);    // a product
-        __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);    // vector instructions
-        __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);  // exponentials
+      for (int i = 0; i < D / 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);                // a product
+        __builtin_amdgcn_sched_group_barrier(0x2, 2 * 128 / D, 0);      // vector instructions
+        __builtin_amdgcn_sched_group_barrier(0x400, 128 / D, 0);        // exponentials
       }
       q::settle_weights<false, true>(st, s, a.scale_log2, big, x, sum);
       convert(k + 1);
@@ -271,7 +279,7 @@ void q8_chunk_kernel(QAttnArgs a) {
         whole.vs[0] = q8::scale_bytes<D>(sg, at_of(t.a));
         whole.vs[1] = q8::scale_bytes<D>(sg, at_of(t.b));
         q8::clear_dead(whole, k * kQUnit, all_last, lane);
-        q8::fold_pv_edge<T, D, kNB>(st, whole, x, k * kQUnit, lane);
+        q8::fold_pv_edge(st, whole, x, k * kQUnit, lane);
       } else {
         fold_staged(k, x);
       }

@@ -255,8 +255,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q8_append_kernel(QRowsArgs a,
 template <bool kPast, typename T>
 __device__ __forceinline__ void put(T* p, u32x2_t w, float scale) {
   if constexpr (sizeof(T) == 2) {
-    store_row<kPast>(p, u32x4{q8::pair_of<0, false>(w.x, scale), q8::pair_of<1, false>(w.x, scale), q8::pair_of<0, false>(w.y, scale),
-                              q8::pair_of<1, false>(w.y, scale)});
+    store_row<kPast>(p, q8::eight_of(w.x, w.y, scale));
   } else {
     const q::f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, scale, true);
     store_row<kPast>(p, q::f32x4_t{a[0], a[1], b[0], b[1]});

@@ -50,8 +50,8 @@ __device__ __forceinline__ QItem q_item(const QAttnArgs& a, int i, int positions
 
 // The outputs of a wave's columns, or the records of part `split` of them; at: the
 // column's (row, head) vector among all.
-template <typename T, int D, int NB>
-__device__ __forceinline__ void q_finish(const QAttnArgs& a, const q::State<T, D, NB>& st, const int64_t (&at)[NB], int split,
+template <typename T, int D, int NB, bool C>
+__device__ __forceinline__ void q_finish(const QAttnArgs& a, const q::State<T, D, NB, C>& st, const int64_t (&at)[NB], int split,
                                           int lane) {
   const int G = lane >> 4;
   T* out = reinterpret_cast<T*>(a.out);
@@ -117,7 +117,7 @@ void q_attn_kernel(QAttnArgs a) {
   const int u0 = s0 + part * per, u1 = min(s1, u0 + per);
   if (u0 >= u1 && sharers == 1) return;
 
-  q::State<T, D, NB> st;
+  q::State<T, D, NB, F::template kCodes<T, D>> st;
   int64_t at[NB];  // of the column's (row, head) vector, among all
   q::reset(st);
   if (u0 < u1) {
@@ -127,7 +127,7 @@ void q_attn_kernel(QAttnArgs a) {
       const bool there = pos < it.n_pos;  // (columns past the item's positions are none)
       st.last[c] = there ? it.last0 + pos : -1;
       at[c] = (int64_t)(it.row0 + (there ? pos : 0)) * a.H_q + (int64_t)g * S + col % S;
-      q::load_query<F::kSliced, T, D>(st.q[c], there ? reinterpret_cast<const T*>(a.q) + at[c] * D : nullptr, lane);
+      q::load_query<F::kSliced>(st.q[c], there ? reinterpret_cast<const T*>(a.q) + at[c] * D : nullptr, lane);
     }
 
     const int n_pages = all_last / kPage + 1;

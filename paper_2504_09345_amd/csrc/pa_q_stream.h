@@ -238,7 +238,7 @@ void q_stream_kernel(QStreamArgs a) {
     return e;
   };
 
-  q::State<T, D, 1> st;
+  q::State<T, D, 1, F::template kCodes<T, D>> st;
   typename F::template Unit<D> u;
   const int k_shift = F::template shift<D>(lane);
   const int n = lane & 15, Gl = lane >> 4;
@@ -305,7 +305,7 @@ void q_stream_kernel(QStreamArgs a) {
         from = u0 + i - p;
         to = u0 + i + left - 1;
         const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)row * a.H_q + (int64_t)g * S + n) * D;
-        q::load_query<F::kSliced, T, D>(st.q[0], n < S ? q : nullptr, lane);
+        q::load_query<F::kSliced>(st.q[0], n < S ? q : nullptr, lane);
         q::reset(st);
         st.last[0] = kQUnit - 1;
         open = true;

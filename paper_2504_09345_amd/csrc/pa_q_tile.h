@@ -88,7 +88,6 @@ struct Query<T, D, true> {
   i32x8_t x[2];   // dims 16 (lane / 16) .. +15, then 64 more
   uint32_t s[2];  // the parts' scale bytes
 };
-
 // x as a sum of N bf16 parts, each the rest of those before it to nearest even;
 // part i of the eight values as one operand.  LIMIT: the first part is the
 // largest bf16 where x, from 3.396e38 on, would round up to an infinity (the parts after
@@ -113,9 +112,10 @@ __device__ __forceinline__ void split8(const float (&x)[8], u32x4 (&part)[N]) {
 
 // Softmax state of a wave's 16 NB columns: column 16 c + lane % 16 in the lanes of
 // equal lane % 16.
-template <typename T, int D, int NB>
+// C: whether scores are formed from the codes (kCodeScores, or not at all).
+template <typename T, int D, int NB, bool C = kCodeScores<T, D>>
 struct State {
-  Query<T, D> q[NB];
+  Query<T, D, C> q[NB];
   f32x4_t acc[NB][D / 16];          // O^T: block 2 j + h, entry i: dim 32 j + 8 (lane / 16) + 2 i + h
   float m[NB], l[NB];               // base (log2 units, one per column), the lane's part of the sum
   int last[NB];                     // last key that the column sees, -1: no column
@@ -123,8 +123,8 @@ struct State {
   bool any_lifted;                  // one of the wave's may be
 };
 
-template <typename T, int D, int NB>
-__device__ __forceinline__ void reset(State<T, D, NB>& st) {
+template <typename T, int D, int NB, bool C>
+__device__ __forceinline__ void reset(State<T, D, NB, C>& st) {
 #pragma unroll
   for (int c = 0; c < NB; ++c) {
     st.m[c] = kMInit;
@@ -137,10 +137,10 @@ __device__ __forceinline__ void reset(State<T, D, NB>& st) {
 }
 
 // row: the column's D elements (nullptr: zeros).  (All lanes active.)
-template <bool SLICED, typename T, int D>
-__device__ __forceinline__ void load_query(Query<T, D>& q, const T* row, int lane) {
+template <bool SLICED, typename T, int D, bool C>
+__device__ __forceinline__ void load_query(Query<T, D, C>& q, const T* row, int lane) {
   const int G = lane >> 4;
-  if constexpr (kCodeScores<T, D>) {
+  if constexpr (C) {
     uint32_t f[16];
 #pragma unroll
     for (int h = 0; h < 4; ++h) {  // 16-byte pieces: two of dims 16 G, two of 64 + 16 G
@@ -194,8 +194,8 @@ __device__ __forceinline__ void load_query(Query<T, D>& q, const T* row, int lan
 // Scores of a unit that some columns see in part, or of which a page's entry lies
 // outside the pool (bit p of bad): those of the latter are NaN, and of keys that a
 // column does not see -inf.
-template <typename T, int D, int NB>
-__device__ __forceinline__ void mask_scores(const State<T, D, NB>& st, int key0, int bad, int lane, f32x4_t (&s)[NB][2]) {
+template <typename T, int D, int NB, bool C>
+__device__ __forceinline__ void mask_scores(const State<T, D, NB, C>& st, int key0, int bad, int lane, f32x4_t (&s)[NB][2]) {
 #pragma unroll
   for (int c = 0; c < NB; ++c)
 #pragma unroll
@@ -223,8 +223,8 @@ constexpr float kLiftedLimit = 0x1p-31f;
 // Online softmax: the weights, formed with the base of the units before; whether
 // one exceeds the limit (as a column's first does, whose base is kMInit).  SUMS: whether
 // the lane's sum of a column does, which is formed anyway, and moves the base no later.
-template <bool SUMS, typename T, int D, int NB>
-__device__ __forceinline__ bool form_weights(const State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, float (&x)[NB][8],
+template <bool SUMS, typename T, int D, int NB, bool C>
+__device__ __forceinline__ bool form_weights(const State<T, D, NB, C>& st, const f32x4_t (&s)[NB][2], float scale_log2, float (&x)[NB][8],
                                              float (&sum)[NB]) {
   if constexpr (SUMS) {
     float most = 0.0f;
@@ -247,8 +247,8 @@ __device__ __forceinline__ bool form_weights(const State<T, D, NB>& st, const f3
     }
   return most > kWeightLimit;
 }
-template <bool SUMS, typename T, int D, int NB>
-__device__ __forceinline__ void add_weights(State<T, D, NB>& st, const float (&x)[NB][8], const float (&sum)[NB]) {
+template <bool SUMS, typename T, int D, int NB, bool C>
+__device__ __forceinline__ void add_weights(State<T, D, NB, C>& st, const float (&x)[NB][8], const float (&sum)[NB]) {
 #pragma unroll
   for (int c = 0; c < NB; ++c)
     if constexpr (SUMS) st.l[c] += sum[c];
@@ -260,8 +260,8 @@ __device__ __forceinline__ void add_weights(State<T, D, NB>& st, const float (&x
 // LIFT: first is the unit's first key with large V (INT32_MAX: none); the bases of the
 // columns that see it are lifted.  They lie kHeadroom below the largest score so far, or
 // up to 8 log2 units more (the limit), so they come to lie kLift to kLift + 8 above.
-template <bool LIFT, bool SUMS, typename T, int D, int NB>
-__device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_t (&s)[NB][2], float scale_log2, bool big,
+template <bool LIFT, bool SUMS, typename T, int D, int NB, bool C>
+__device__ __forceinline__ void settle_weights(State<T, D, NB, C>& st, const f32x4_t (&s)[NB][2], float scale_log2, bool big,
                                                float (&x)[NB][8], float (&sum)[NB], int first = INT32_MAX) {
   float up[NB] = {};
   if constexpr (LIFT) {
@@ -300,8 +300,8 @@ __device__ __forceinline__ void settle_weights(State<T, D, NB>& st, const f32x4_
 }
 
 // The lane's eight consecutive outputs of block j (dims 32 j + 8 (lane / 16) ..).
-template <typename T, int D, int NB>
-__device__ __forceinline__ void eight_out(const State<T, D, NB>& st, int c, int j, float (&o)[8]) {
+template <typename T, int D, int NB, bool C>
+__device__ __forceinline__ void eight_out(const State<T, D, NB, C>& st, int c, int j, float (&o)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     o[2 * i] = st.acc[c][2 * j][i];
