@@ -4,13 +4,13 @@
 // (query row, head of the group) of one sequence and KV head, 32 each, and step through
 // the units together.  Each wave loads a quarter of a unit (of one page): of V it makes fp16
 // operands and stages those, 8 KiB per unit at head_dim 128, read back with no bank
-// conflict; of K the codes, which are operands already, 4 KiB.  K of a unit as every wave
-// would load it takes 16 registers from its load on, too many beside 32 columns' queries
-// and outputs: the queries moved to scratch memory, whose loads wait behind K's (eight chunks
-// of 2,048 rows on 0-2,048 tokens 3,480 us).  Loaded into LDS directly it takes none, but
-// every read of LDS then waits for those loads (750); through the registers of a quarter,
-// 690.  One barrier per unit: unit k is multiplied while V of unit k + 1 is converted and
-// K of unit k + 2 put into the other buffers.
+// conflict; of K bf16 operands, 8 KiB.  (Measured with K's codes as e4m3 operands, eight
+// chunks of 2,048 rows on 0-2,048 tokens: loaded by every wave, K takes 16 registers from its
+// load on, too many beside 32 columns' queries and outputs, which then move to scratch
+// memory, whose loads wait behind K's, 3,480 us; loaded into LDS directly it takes none, but
+// every read of LDS then waits for those loads, 750; through the registers of a quarter,
+// 690.)  One barrier per unit: unit k is multiplied while V of unit k + 1 and K of unit
+// k + 2 are converted and put into the other buffers.
 //
 // A unit with a V scale outside fp16's window every wave takes by the general products
 // instead, with V of its own; also one with a NaN among keys that some columns do not see
@@ -234,14 +234,6 @@ void q8_chunk_kernel(QAttnArgs a) {
       for (int c = 0; c < kNB; ++c)
 #pragma unroll
         for (int p = 0; p < 2; ++p) asm volatile("" : "+v"(sn[c][p]));
-      // (that order of issue: 644 us instead of 650)
-      __builtin_amdgcn_sched_group_barrier(0x100, D / 16 + 1, 0);  // K from LDS
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);                // a product
-        __builtin_amdgcn_sched_group_barrier(0x2, 2 * 128 / D, 0);      // vector instructions
-        __builtin_amdgcn_sched_group_barrier(0x400, 128 / D, 0);        // exponentials
-      }
       q::settle_weights<false, true>(st, s, a.scale_log2, big, x, sum);
       convert(k + 1);
       fetch_v(t2);

@@ -54,10 +54,13 @@ __device__ __forceinline__ float scale_of(uint32_t w) {
 // queries scaled so that the largest lies in [128, 256), the first part holds four
 // significant bits of a value and the second the four that a bf16 has left, times
 // 32: exact for values down to 2^-14 of the column's largest, and within 2^-22 of
-// that largest below.  (33 cycles per product against four of 19 for bf16 operands
-// and 16 conversions of 4.)  At head_dim 64 half of such a product would be zeros,
-// and fp32 queries would take six parts: there K becomes bf16, exactly, and the
-// queries their own bits or three bf16 parts, which carry the 24 of an fp32.
+// that largest below.  Such a product adds the dims in eights, of which it keeps the bits
+// down to 2^-13 of the largest alone (measured: a product of 1 beside one of 2^14 in
+// the same eight is lost, in another eight it is not).  (33 cycles per product against
+// four of 19 for bf16 operands and 16 conversions of 4.)  At head_dim 64 half of such a
+// product would be zeros, and fp32 queries would take six parts: there K becomes bf16,
+// exactly, and the queries their own bits or three bf16 parts, which carry the 24 of an
+// fp32.  The 8-bit cache's K always does.
 //
 // Outputs.  For bf16 outputs the weights are rounded once, to fp16 (2^-11 of each, as
 // the chunk kernel of the 16-bit cache rounds them), and V becomes fp16 where its scales

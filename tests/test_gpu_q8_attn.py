@@ -359,6 +359,29 @@ def test_largest_scores(kind, dtype, D, sign):
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("D", [64, 128])
+def test_small_products_beside_a_large_one(kind, dtype, D):
+    """A channel of K that all keys share, up to 2^17 times its neighbours' products: the
+    scores' differences are the neighbours'."""
+    announce(f"q8 {kind} {dtype} D={D}, small products beside a large one")
+    b = Batch(_lens(kind, [40, 90, 33]), 8, 2, D, dtype, seed=4, varlen=kind != "decode")
+    rng = np.random.default_rng(1)
+    for i, c in enumerate((40, 90, 33)):
+        for p in range(-(-c // 16)):
+            x = rng.choice([0, 0, 1, 1.125, -1.875], (2, 16, D)) * (rng.random((2, 16, 1)) < 0.7)
+            x[..., 3], x[..., D - 9] = 1.0, -1.0
+            b.put("k", b.bt[i, p], x, min(16, c - 16 * p))
+    b.q = rng.choice([-1.0, 1.0, 1.25], b.q.shape)
+    for h in range(8):
+        b.q[:, h, 3] = 2.0 ** (6 + h)
+        b.q[:, h, D - 9] = 2.0 ** (17 - 2 * h)
+    b.q = b.round(b.q)
+    b.scale = 1 / 16
+    check(_attend(b, kind), b.expected(), 90, dtype)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
 def test_queries_of_any_size(kind, dtype, D):
     """Queries of zeros, small and large ones, and of very different sizes in one row."""
     announce(f"q8 {kind} {dtype} D={D}, queries of any size")
