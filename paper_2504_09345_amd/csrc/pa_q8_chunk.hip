@@ -49,7 +49,7 @@ void q8_chunk_kernel(QAttnArgs a) {
   const QItem it = q_item(a, blockIdx.x / a.n_split / a.H_kv, kColumns / S, lane);
   if (it.n_pos == 0) return;
   T* out = reinterpret_cast<T*>(a.out);
-  if (it.bad || a.num_pages == 0) {  // (without pages every row sees an entry outside)
+  if (it.bad) {  // (also where there are no pages)
     if (split == 0)
       for (int i = threadIdx.x; i < it.n_pos * S * D; i += 64 * kQWaves)
         store_out<T>(out + ((int64_t)(it.row0 + i / (S * D)) * a.H_q + (int64_t)g * S) * D + i % (S * D), NAN);

@@ -229,8 +229,10 @@ int attend(const void* q, const QCache& c, bool scaled, float scale, void* out, 
     return PA_OK;
   }
   char* ws = static_cast<char*>(workspace);
-  // (without pages nothing of a tile is read, but its scales are: any bytes)
-  const uint8_t* scales = scaled && d->num_pages == 0 ? reinterpret_cast<const uint8_t*>(c.context_lens) : c.scales;
+  // Without pages nothing of a tile is read, but scales are: the decode kernel's of the
+  // first tile (any two bytes), the chunk kernels' none, as a context above the bound.
+  const bool no_scales = scaled && d->num_pages == 0;
+  const uint8_t* scales = no_scales ? reinterpret_cast<const uint8_t*>(c.context_lens) : c.scales;
   const float scale_log2 = scale * 1.4426950408889634f;
   if (p.chunks) {
     QAttnArgs a{};
@@ -252,7 +254,7 @@ int attend(const void* q, const QCache& c, bool scaled, float scale, void* out, 
     a.H_kv = d->num_kv_heads;
     a.rows = p.rows;
     a.num_pages = d->num_pages;
-    a.max_context_len = d->max_context_len;
+    a.max_context_len = no_scales ? -1 : d->max_context_len;
     a.n_slots = p.n_slots;
     a.min_rows = p.min_rows;
     a.max_q_len = d->max_q_len;

@@ -263,15 +263,24 @@ def test_chunks_longer_than_max_q_len():
         check(b.attend(d, b.dims(d, max_q_len=most)).float().cpu(), ref, 64, "bf16")
 
 
-@pytest.mark.parametrize("varlen", [False, True])
-def test_no_pages(varlen):
-    """A pool of none: rows of a context are NaN (every entry lies outside)."""
-    announce(f"q8 attention, a pool without pages varlen={varlen}")
-    b = Batch([(20, 3), (40, 1)], 4, 2, 64, varlen=varlen)
+@pytest.mark.parametrize("kind", KINDS)
+def test_no_pages(kind):
+    """A pool of none: rows of a context are NaN (every entry lies outside), those of none
+    as ever."""
+    announce(f"q8 attention, a pool without pages, {kind}")
+    b = Batch([(20, 3), (0, 0), (40, 1), (4000, 30)], 40, 40, 64, varlen=kind != "decode")
     d = b.upload()
-    dims = b.dims(d)
+    if kind == "shared":
+        b.widen(d, FAR)
+    dims = b.dims(d, max_context_len=FAR if kind == "shared" else None)
     dims.num_pages = 0
-    assert torch.isnan(b.attend(d, dims, torch.zeros_like(d["q"]))).all()
+    d["k"], d["v"], d["scales"] = d["k"][:1], d["v"][:1], d["scales"][:1]
+    out = b.attend(d, dims, torch.zeros_like(d["q"]))
+    live = torch.ones(b.T, dtype=torch.bool, device="cuda")
+    if kind == "decode":
+        live[1] = False
+        assert (out[1] == 0).all()
+    assert torch.isnan(out[live]).all()
 
 
 # --- sizes -----------------------------------------------------------------------
