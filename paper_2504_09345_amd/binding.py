@@ -651,7 +651,10 @@ def pa_rope(q, k, context_lens, inv_freq, q_out, k_out, dims: PaDims, interleave
     if rot_dim is None:
         rot_dim = 2 * inv_freq.numel()
     kind, D, i32 = torch.bfloat16 if dims.dtype == PA_BF16 else torch.float32, dims.head_dim, torch.int32
-    rows = dims.num_q_rows if query_start_loc is not None or (positions is not None and dims.num_q_rows) else dims.num_seqs
+    if positions is not None:
+        rows = dims.num_q_rows or dims.num_seqs
+    else:
+        rows = dims.num_seqs if query_start_loc is None else dims.num_q_rows
     H_q, H_kv = dims.num_q_heads, dims.num_kv_heads
     qa, qs = _rows_rope(q, kind, rows, H_q, D, dev)
     qo, qos = _rows_rope(q_out, kind, rows, H_q, D, dev)

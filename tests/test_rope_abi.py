@@ -95,6 +95,20 @@ def test_binding(monkeypatch):
         pb.pa_rope(q, None, P, w, P, None, d, rot_dim=130, stream=S)
 
 
+@host_only
+def test_rows_with_positions(monkeypatch):
+    """With positions and no number of rows the rows are num_seqs, though
+    query_start_loc is given too: arrays of fewer are refused."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    d, w, i32 = dims(num_seqs=2, num_q_heads=2, num_kv_heads=1, num_q_rows=0), torch.ones(32, dtype=torch.float64), torch.int32
+    q, two, qsl = torch.zeros(2, 2, 128, dtype=torch.bfloat16), torch.zeros(2, dtype=i32), torch.zeros(3, dtype=i32)
+    for x, positions in ((q[:1], two), (q, two[:1]), (q[:0], two[:0])):
+        for loc in (None, qsl):
+            with pytest.raises(ValueError):
+                pb.pa_rope(x, None, None, w, x, None, d, positions=positions, query_start_loc=loc, stream=S)
+
+
 def test_dims_from_shapes():
     d = pb.make_dims_rope(torch.empty(3, 4, 64), torch.empty(3, 2, 64), 100)
     assert (d.num_seqs, d.num_q_heads, d.num_kv_heads, d.head_dim, d.max_context_len, d.dtype, d.num_q_rows) == (3, 4, 2, 64, 100, pb.PA_FP32, 0)
