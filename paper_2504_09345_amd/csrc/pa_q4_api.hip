@@ -24,7 +24,7 @@ int pa_kv_read_q4(const void* k_pages, const void* v_pages, const int32_t* block
 }
 
 int pa_workspace_size_q4(const pa_dims_t* dims, size_t* bytes) {
-  return pa::workspace_bytes_of(dims, bytes);
+  return pa::workspace_bytes_of<pa::q4::Format>(dims, bytes);
 }
 
 int paged_attn_q4(const void* q, const void* k_pages, const void* v_pages, const int32_t* block_table,

@@ -27,7 +27,7 @@ int pa_kv_read_q8(const void* k_pages, const void* v_pages, const uint8_t* scale
 }
 
 int pa_workspace_size_q8(const pa_dims_t* dims, size_t* bytes) {
-  return pa::workspace_bytes_of(dims, bytes);
+  return pa::workspace_bytes_of<pa::q8::Format>(dims, bytes);
 }
 
 int paged_attn_q8(const void* q, const void* k_pages, const void* v_pages, const uint8_t* scales, const int32_t* block_table,

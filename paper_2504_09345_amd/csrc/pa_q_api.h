@@ -97,12 +97,16 @@ struct Plan {
 // while the GPU still holds all of them at once (256 CUs of 12 waves).  Shared and
 // alone, 32 query heads over 8: a chunk of 16 rows on 200 tokens 7 and 10 us, of 300 9
 // and 11, of 64 on 1,500 14 and 18, 4 of 60 on 3,000 34 and 41, 16 of 8 on 2,000 25
-// and 31.
+// and 31.  (8 bits: 6.4 and 8.5, 7.0 and 10.1, 12.0 and 16.6, 25 and 33, 17 and 24; four
+// times as many waves: one chunk of 1,400 rows 41 us instead of 36, of 700 18 and 15.)
 constexpr int kPartWaves = 3072;
 // Parts beyond those, through the workspace and a second launch: as many as give the
 // GPU 2,048 waves of at least kLeastUnits units, at most 64.  (Parts of 4 units cost one
 // chunk of 64 rows on 1,500 tokens 17 us instead of 14; 8 or 16 are one as good as the
-// other.  Twice the waves: one chunk of 700 rows 31 us instead of 19.)
+// other.  Twice the waves: one chunk of 700 rows 31 us instead of 19.  8 bits: units of
+// at least 4, 8 or 16 are one as good as the other but for 10.0 and 11.3 us, 8 and 4, of
+// one chunk of 64 rows on 1,500 tokens at head_dim 64; with twice the waves one chunk of
+// 2,000 rows 94 us instead of 65, two of 120 on 20,000 121 instead of 110.)
 constexpr int kWavesWanted = 2048, kLeastUnits = 8, kMaxSplit = 64;
 // Bytes of all parts' records, which the host can only reckon for every row of the call:
 // it does not know which are of chunks, nor does the grid.  With bounds of 32, 64, 128 and
@@ -126,12 +130,22 @@ constexpr int64_t kRecordBytes = 64 << 20;
 // 20.6; one of 700 19.0 and 40.7 with any of them; 4 of 64 on 300 10.7, 10.7, 23.5 and
 // 23.6; 16 of 8 on 2,000 17.5 with all; and one of 700 beside a decode row of 32,768
 // tokens 62, where the two alone take 19 and 18.
-constexpr int64_t kAloneUnits = 48 * 2048;
+// The 8-bit kernels share for less (K's conversion to bf16 too is a workgroup's, but one
+// barrier a unit more), and the line is 104.  Alone and together, 32 query heads over 8,
+// head_dim 128: one chunk of 1,400 rows 37 and 48 us, of 2,000 55 and 64, of 2,600 81 and
+// 82, of 2,800 92 and 87, of 4,000 176 and 165; 4 of 1,000 62 and 65; 2 of 256 on 8,000
+// 104 and 116; 4 of 64 on 16,000 108 and 102; 2 of 120 on 20,000 128 and 110; with 8
+// query heads one of 4,000 69 and 94, with 64 one of 1,400 53 and 49; at head_dim 64 one
+// of 2,000 39 and 49, of 2,600 57 and 64, of 4,000 113 and 98.
+template <class F> constexpr int64_t kAloneUnits = 0;
+template <> inline constexpr int64_t kAloneUnits<q4::Format> = 48 * 2048;
+template <> inline constexpr int64_t kAloneUnits<q8::Format> = 104 * 2048;
 constexpr int kAloneColumns = 32;
 // Units of a launch of the stream kernel, at most (its counts are 32-bit).
 constexpr int64_t kStreamUnits = 1 << 30;
 
-inline int plan(const pa_dims_t* d, bool varlen, Plan* p) {
+template <class F>
+int plan(const pa_dims_t* d, bool varlen, Plan* p) {
   const int rc = check_cache(d);
   if (rc != PA_OK) return rc;
   if (d->num_q_heads <= 0 || d->num_q_heads % d->num_kv_heads != 0) return PA_EINVAL;
@@ -170,7 +184,7 @@ inline int plan(const pa_dims_t* d, bool varlen, Plan* p) {
     if (chunk_rows < one) chunk_rows = one;
     const int64_t alone_units = (chunk_rows / q_positions(1, s) + 1) * d->num_kv_heads *
                                 ((d->max_context_len - d->max_q_len / 2) / kQUnit + 1);
-    p->shared = d->dtype == PA_BF16 && d->max_q_len * (int64_t)s > kAloneColumns && alone_units > kAloneUnits;
+    p->shared = d->dtype == PA_BF16 && d->max_q_len * (int64_t)s > kAloneColumns && alone_units > kAloneUnits<F>;
     p->blocks = p->shared ? kQChunkBlocks : 1;
     const int64_t slots = p->rows / q_positions(p->blocks, s) + 1 + (int64_t)d->num_seqs;
     const int64_t items = (chunk_rows / q_positions(p->blocks, s) + 1) * d->num_kv_heads;
@@ -197,11 +211,12 @@ inline int plan(const pa_dims_t* d, bool varlen, Plan* p) {
   return PA_OK;
 }
 
-inline int workspace_bytes_of(const pa_dims_t* d, size_t* bytes) {
+template <class F>
+int workspace_bytes_of(const pa_dims_t* d, size_t* bytes) {
   if (bytes == nullptr) return PA_EINVAL;
   Plan p;
   const bool varlen = d != nullptr && (d->max_q_len > 1 || (d->num_q_rows != 0 && d->num_q_rows != d->num_seqs));
-  const int rc = plan(d, varlen, &p);
+  const int rc = plan<F>(d, varlen, &p);
   if (rc != PA_OK) return rc;
   *bytes = p.bytes();
   return PA_OK;
@@ -212,7 +227,7 @@ template <class F>
 int attend(const void* q, const QCache& c, bool scaled, float scale, void* out, const pa_dims_t* d, void* workspace,
            size_t workspace_bytes, hipStream_t stream, const pa_timing_t* timing, bool varlen) {
   Plan p;
-  const int rc = plan(d, varlen, &p);
+  const int rc = plan<F>(d, varlen, &p);
   if (rc != PA_OK) return rc;
   if (!isfinite(scale) || !(scale > 0.0f)) return PA_EINVAL;
   if (p.rows > 0) {

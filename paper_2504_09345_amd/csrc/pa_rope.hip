@@ -31,9 +31,11 @@ struct RopeArgs {
   int n;  // pairs
   int B, H_q, H_kv, rows, max_context_len;
 };
-constexpr int kRopeWaves = 4;  // rows of a workgroup, at most
-constexpr int kManyRows = 1024;       // from which on a workgroup takes so many
-constexpr int kRopeParts = 8, kWavesWanted = 1024;  // waves that a row's heads are spread over, where rows are few
+// Waves that a row's heads are spread over, at most, while the call has not so many.  (On
+// one wave and over several, 40 heads of 128: 1 row 3.2 and 2.3 us, 256 rows 3.7 and 3.2,
+// 1,024 5.2 and 5.0; fp32 3.5, 4.3, 8.5 and 2.3, 3.5, 8.1.  To 4,096 waves: 1,024 rows
+// 6.1 us, 2,048 10.6 instead of 8.1.)
+constexpr int kRopeParts = 8, kWavesWanted = 1024;
 constexpr int64_t kMostGroups = 1 << 20;
 
 // cos and sin of p w.
@@ -100,20 +102,21 @@ __device__ __forceinline__ typename Piece<T, V>::type rounded(const float (&x)[V
 
 // PAIRED: pair i is dims 2 i and 2 i + 1.  Otherwise V divides the number of pairs.
 template <typename T, int D, int V, bool PAIRED>
-__global__ __launch_bounds__(64 * kRopeWaves) void rope_kernel(RopeArgs a) {
+__global__ __launch_bounds__(64) void rope_kernel(RopeArgs a) {
   using P = typename Piece<T, V>::type;
   constexpr int kLanes = D / 2 / V;      // of a head
   constexpr int kHeads = 64 / kLanes;    // at once
-  constexpr int kBatch = 4;              // loads of so many before the first is used
-  __shared__ float2 s_turn[kRopeWaves][64];
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int waves = blockDim.x >> 6;
+  // Loads of so many heads' pieces before the first is used.  (1, 2, 3, 4, of 40 heads of
+  // 128: 256 rows 3.2, 3.0, 3.1 and 3.2 us, 16,384 64, 60, 60 and 60; fp32 3.7, 3.7, 3.4
+  // and 3.5, 133, 127, 126 and 125.)
+  constexpr int kBatch = 4;
+  __shared__ float2 s_turn[64];
+  const int lane = threadIdx.x;
   const int H = a.H_q + a.H_kv, first = lane % kLanes * V, h_first = blockIdx.y * kHeads + lane / kLanes, h_step = gridDim.y * kHeads;
   // the lane's two pieces of a head: of a pair's first and second dims, or in a row
   const bool apart = !PAIRED && first < a.n;
   const int at0 = apart ? first : 2 * first, at1 = apart ? first + a.n : 2 * first + V;
-  for (int64_t row = (int64_t)blockIdx.x * waves + wave; row < a.rows; row += (int64_t)gridDim.x * waves) {
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     P x[kBatch][2];
     auto in = [&](int h) {
       return h < a.H_q ? reinterpret_cast<const T*>(a.q) + row * a.q_stride + (int64_t)h * D
@@ -143,11 +146,11 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_kernel(RopeArgs a) {
         turn.x *= a.factor;
         turn.y *= a.factor;
       }
-      s_turn[wave][lane] = turn;
+      s_turn[lane] = turn;
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float2 t = s_turn[wave][first + i];
+        const float2 t = s_turn[first + i];
         c[i] = t.x;
         s[i] = t.y;
       }
@@ -190,12 +193,9 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_kernel(RopeArgs a) {
 template <typename T, int D, int V, bool PAIRED>
 hipError_t launch(const RopeArgs& a, hipStream_t st) {
   const int H = a.H_q + a.H_kv, heads = 64 / (D / 2 / V);
-  const int waves = a.rows >= kManyRows ? kRopeWaves : 1;
-  const int64_t groups = ((int64_t)a.rows + waves - 1) / waves;
-  // few rows: a row's heads over several waves
   int parts = 1;
-  while (parts * 2 <= kRopeParts && groups * parts * 2 <= kWavesWanted && parts * heads < H) parts *= 2;
-  rope_kernel<T, D, V, PAIRED><<<dim3((uint32_t)(groups < kMostGroups ? groups : kMostGroups), parts), 64 * waves, 0, st>>>(a);
+  while (parts * 2 <= kRopeParts && (int64_t)a.rows * parts * 2 <= kWavesWanted && parts * heads < H) parts *= 2;
+  rope_kernel<T, D, V, PAIRED><<<dim3((uint32_t)(a.rows < kMostGroups ? a.rows : kMostGroups), parts), 64, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -14,7 +14,7 @@ from parity_util import announce
 
 pytestmark = pytest.mark.gpu
 
-FAR = 1 << 20  # a declared context for which a call's chunks share V's operands (bf16)
+FAR = 1 << 22  # a declared context for which a call's chunks share V's operands (bf16)
 KINDS = ["decode", "chunks", "shared"]
 DECODE = [1, 15, 16, 17, 31, 32, 33, 0, 64, 200, 333, 48]
 

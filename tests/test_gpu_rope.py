@@ -107,6 +107,21 @@ def test_any_number_of_rows(T):
                 check(got, x, pos, w, 1.0, False)
 
 
+def test_more_rows_than_workgroups():
+    T = (1 << 20) + 37
+    announce(f"rope {T} rows")
+    pos = np.random.default_rng(5).integers(0, 1 << 20, T)
+    _, k = rows(T, 0, 1, 64, "bf16", seed=5)
+    w, _ = pb.pa_rope_frequencies(64)
+    out = torch.full_like(k, 9.0)
+    pb.pa_rope(None, k, None, w.cuda(), None, out, pb.make_dims_rope(None, k, 0, T, 1), positions=i32(pos))
+    for part in (slice(0, 300), slice(T // 2, T // 2 + 300), slice(T - 300, T)):
+        check(out[part], k[part], pos[part], w, 1.0, False)
+    # (the others: a rotation keeps each pair's length, to a step of bf16 of the larger)
+    size = lambda x: x.float().view(T, 2, 32).pow(2).sum(1).sqrt()
+    assert ((size(out) - size(k)).abs() <= 2.0 ** -7 * size(k) + 1e-30).all()
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("packed", [False, True])
 @pytest.mark.parametrize("rot", [128, 64, 22])
