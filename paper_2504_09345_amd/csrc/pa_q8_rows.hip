@@ -1,9 +1,16 @@
 // The 8-bit cache's write and read of rows (format in pagedattn_q8.h).
 //
 // Writing: a page's scale is that of its largest value, so a wave takes a page's new rows
-// whole, for 64 / (D / 8) KV heads: D / 8 lanes of 8 dims each to a head.  The largest
-// magnitude over the rows and then the lanes (DPP), the exponent from its bits, v_cvt_pk_fp8_f32
-// to codes (its rounding is the format's).  Where the page holds earlier tokens and their
+// whole, for one KV head (two at head_dim 64), of which a lane has 8 dims of four tokens.
+// (Lanes of 8 dims of all 16 tokens, for four heads, 8 heads of 128: 8 prompts of 500 rows
+// 8.4 us instead of 7.8, of 2,048 24.1 instead of 20.3; fp32 10.6 and 9.3, 29.6 and 26.1;
+// but 256 of 20 rows 9.3 instead of 9.9, 8 of 512 beside 512 single ones 11.9 instead of
+// 12.6, with fewer waves that find no rows.  A decode call's one row a page it does take
+// so, for as many heads as it has lanes: 256 rows 3.8 us.)  What bounds it is a wave's
+// chain of loads (its sequence, the page's entry, the scale) and the rows' load beside it:
+// those 16,384 rows, 67 MB read and 34 written, stream at 5 TB/s.  The largest
+// magnitude over the rows and then the lanes, the exponent from its bits, the scaled
+// conversions to codes (their rounding is the format's).  Where the page holds earlier tokens and their
 // scale is too small, the same lanes round those again: a power of two apart, their values
 // are exact in fp32.  K and V are waves of their own.
 // A lane's eight bytes of a token are eight in a row of the K tile; in the V tile they lie
@@ -114,89 +121,85 @@ __device__ __forceinline__ float finite_most_of(float m, const Raw<T>& r) {
   return m;
 }
 
-template <typename T, int D>
+// Scale byte of a page whose largest new value is m: the exponent's byte less 8, or 7
+// above 1.75 (a carry out of the mantissa).
+__device__ __forceinline__ int scale_byte(float m) {
+  return min(max((int)((__float_as_uint(m) + 0x1fffffu) >> 23) - 8, kLow), kHigh);
+}
+// The page's tokens from .. to - 1 (from: a multiple of four) brought from scale byte
+// `held` to e.
+template <int D>
+__device__ __forceinline__ void rescale(uint8_t* tile, bool k, int c, int from, int to, int held, int e) {
+  const float f = power(127 + max(held - e, -64));  // (2^-64 of any code is 0)
+  if (k) {
+    for (int t = from; t < to; ++t) {
+      u32x2_t* at = reinterpret_cast<u32x2_t*>(tile + Place<D>::k(t, c));
+      const u32x2_t w = *at;
+      *at = u32x2_t{again(w.x, f), again(w.y, f)};
+    }
+  } else {
+    for (int t = from; t < to; t += 4) {
+      const uint32_t early = to - t >= 4 ? ~0u : (1u << 8 * (to - t)) - 1;  // bytes
+#pragma unroll
+      for (int m4 = 0; m4 < 4; ++m4) {
+        u32x2_t* at = reinterpret_cast<u32x2_t*>(tile + Place<D>::v(t >> 2, c, m4));
+        const u32x2_t w = *at;
+        *at = u32x2_t{(again(w.x, f) & early) | (w.x & ~early), (again(w.y, f) & early) | (w.y & ~early)};
+      }
+    }
+  }
+}
+// A token's codes alone.
+template <int D>
+__device__ __forceinline__ void put_token(uint8_t* tile, bool k, int c, int t, u32x2_t w) {
+  if (k) {
+    *reinterpret_cast<u32x2_t*>(tile + Place<D>::k(t, c)) = w;
+    return;
+  }
+#pragma unroll
+  for (int m4 = 0; m4 < 4; ++m4) {
+    uint8_t* at = tile + Place<D>::v(t >> 2, c, m4) + (t & 3);
+    const uint32_t pair = (m4 < 2 ? w.x : w.y) >> 16 * (m4 & 1);
+    at[0] = (uint8_t)pair;
+    at[4] = (uint8_t)(pair >> 8);
+  }
+}
+
+// PAGES: lanes of four tokens of a head each; otherwise every sequence has one row, and a
+// wave takes it for as many heads as it has lanes.
+template <typename T, int D, bool PAGES>
 __global__ __launch_bounds__(64 * kRowsWaves) void q8_append_kernel(QRowsArgs a, int slots) {
-  constexpr int CH = D / 8;
+  constexpr int CH = D / 8, N = PAGES ? 4 : 1, kLanes = PAGES ? 4 * CH : CH;  // tokens of a lane, lanes of a head
   const int lane = threadIdx.x & 63;
   const int slot = blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (slot >= slots) return;
   Group p = group_of<kPage, false>(a, slot, lane);
   if (p.n <= 0 || p.bad) return;
-  const int i = blockIdx.y * 64 + lane, which = blockIdx.z;
-  if (i >= a.H_kv * CH) return;  // (whole heads)
-  const int g = i / CH, c = i % CH;
+  const int i = blockIdx.y * 64 + lane;
+  const bool is_k = blockIdx.z == 0;
+  const int g = i / kLanes, c = i % CH;
+  if (g >= a.H_kv) return;  // (whole heads)
+  const int t0 = PAGES ? i / CH % 4 * 4 : p.token;  // the lane's first token
   const int64_t step = (int64_t)a.H_kv * D;
-  const T* from = reinterpret_cast<const T*>(which == 0 ? a.k_rows : a.v_rows) + (int64_t)p.row * step + (int64_t)i * 8;
-  // all 16 tokens of the page, whichever are new (the others: a new row again, unused),
-  // loaded while the page's entry is
-  Raw<T> raw[kPage];
-  auto load_row = [&](int t, int row) {
+  const T* from = reinterpret_cast<const T*>(is_k ? a.k_rows : a.v_rows) + (int64_t)p.row * step + (int64_t)g * D + c * 8;
+  // loaded while the page's entry is; a token that is not new: a new row again, unused
+  Raw<T> raw[N];
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    const int row = PAGES ? min(max(t0 + t - p.token, 0), p.n - 1) : 0;
 #pragma unroll
     for (int h = 0; h < (int)sizeof(T) / 2; ++h) raw[t].w[h] = *reinterpret_cast<const u32x4*>(from + row * step + h * (16 / (int)sizeof(T)));
-  };
-  const bool one = p.n == 1;
-  if (one) {
-    load_row(0, 0);
-  } else {
-#pragma unroll
-    for (int t = 0; t < kPage; ++t) load_row(t, min(max(t - p.token, 0), p.n - 1));
   }
   checked_page(a, p);
   if (p.bad) return;
   const int64_t head = (int64_t)p.page * a.H_kv + g;
-  uint8_t* tile = (which == 0 ? a.k_pages : a.v_pages) + head * q8_tile_bytes(D);
-  uint8_t* scale = a.scales + head * 2 + which;
+  uint8_t* tile = (is_k ? a.k_pages : a.v_pages) + head * q8_tile_bytes(D);
+  uint8_t* scale = a.scales + head * 2 + blockIdx.z;
   const int held = p.token > 0 ? *scale : 0;  // (no earlier tokens: none that bounds it)
-  // The page's scale byte, given the largest of the lane's new finite values; the earlier
-  // tokens are brought to it.
-  auto settle = [&](float m) {
-    m = fmaxf(m, dpp_xor1(m));
-    m = fmaxf(m, dpp_xor2(m));
-    m = fmaxf(m, dpp_half_mirror(m));
-    if constexpr (CH == 16) m = fmaxf(m, dpp_mirror(m));
-    // the exponent's byte less 8, or 7 above 1.75 (a carry out of the mantissa)
-    const int need = min(max((int)((__float_as_uint(m) + 0x1fffffu) >> 23) - 8, kLow), kHigh);
-    const int e = max(need, held);
-    if (p.token > 0 && e > held) {
-      const float f = power(127 + max(held - e, -64));  // (2^-64 of any code is 0)
-      if (which == 0) {
-        for (int t = 0; t < p.token; ++t) {
-          u32x2_t* at = reinterpret_cast<u32x2_t*>(tile + Place<D>::k(t, c));
-          const u32x2_t w = *at;
-          *at = u32x2_t{again(w.x, f), again(w.y, f)};
-        }
-      } else {
-        for (int t = 0; t * 4 < p.token; ++t) {
-          const uint32_t early = p.token - 4 * t >= 4 ? ~0u : (1u << 8 * (p.token - 4 * t)) - 1;  // bytes
-#pragma unroll
-          for (int m4 = 0; m4 < 4; ++m4) {
-            u32x2_t* at = reinterpret_cast<u32x2_t*>(tile + Place<D>::v(t, c, m4));
-            const u32x2_t w = *at;
-            *at = u32x2_t{(again(w.x, f) & early) | (w.x & ~early), (again(w.y, f) & early) | (w.y & ~early)};
-          }
-        }
-      }
-    }
-    if (c == 0 && (p.token == 0 || e > held)) *scale = (uint8_t)e;
-    return e;
-  };
-  auto put_v = [&](int t, u32x2_t w) {  // a token's bytes alone
-#pragma unroll
-    for (int m4 = 0; m4 < 4; ++m4) {
-      uint8_t* at = tile + Place<D>::v(t >> 2, c, m4) + (t & 3);
-      const uint32_t pair = (m4 < 2 ? w.x : w.y) >> 16 * (m4 & 1);
-      at[0] = (uint8_t)pair;
-      at[4] = (uint8_t)(pair >> 8);
-    }
-  };
 
   float most = 0.0f;
-  if (one) {
-    most = most_of(most, raw[0]);
-  } else {
 #pragma unroll
-    for (int t = 0; t < kPage; ++t) most = most_of(most, raw[t]);
-  }
+  for (int t = 0; t < N; ++t) most = most_of(most, raw[t]);
   // (rare: values that are not finite are left out of the scale, and those beyond the
   // largest scale's are cut)
   bool plain = most <= __FLT_MAX__;
@@ -204,50 +207,44 @@ __global__ __launch_bounds__(64 * kRowsWaves) void q8_append_kernel(QRowsArgs a,
     plain = false;
     most = 0.0f;
 #pragma unroll
-    for (int t = 0; t < kPage; ++t)
-      if (t == 0 || !one) most = finite_most_of(most, raw[t]);
+    for (int t = 0; t < N; ++t) most = finite_most_of(most, raw[t]);
   }
-  const int e = settle(most);
+  most = fmaxf(most, dpp_xor1(most));
+  most = fmaxf(most, dpp_xor2(most));
+  most = fmaxf(most, dpp_half_mirror(most));
+  if constexpr (kLanes >= 16) most = fmaxf(most, dpp_mirror(most));
+  if constexpr (kLanes >= 32) most = fmaxf(most, swz_xor16(most));
+  if constexpr (kLanes >= 64) most = fmaxf(most, xor32(most));
+  const int e = max(scale_byte(most), held);
+  if (p.token > 0 && e > held) {
+    if constexpr (PAGES) rescale<D>(tile, is_k, c, t0, min(p.token, t0 + 4), held, e);
+    else rescale<D>(tile, is_k, c, 0, p.token, held, e);
+  }
+  if (i % kLanes == 0 && (p.token == 0 || e > held)) *scale = (uint8_t)e;
   plain = __builtin_amdgcn_ballot_w64(!plain || e >= kHigh) == 0;
   const float size = power(e), inv = power(254 - e);
-  auto codes = [&](int t) { return plain ? encode(raw[t], size) : encode_any(raw[t], inv); };
+  u32x2_t w[N];
+#pragma unroll
+  for (int t = 0; t < N; ++t) w[t] = plain ? encode(raw[t], size) : encode_any(raw[t], inv);
 
-  if (one) {
-    const u32x2_t w = codes(0);
-    if (which == 0) *reinterpret_cast<u32x2_t*>(tile + Place<D>::k(p.token, c)) = w;
-    else put_v(p.token, w);
-    return;
-  }
-  const int first = p.token, end = p.token + p.n;
-#pragma unroll
-  for (int t4 = 0; t4 < kPage / 4; ++t4) {
-    if (4 * t4 + 4 <= first || 4 * t4 >= end) continue;  // (wave-uniform, as those below)
-    uint32_t lo[4], hi[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const u32x2_t w = codes(4 * t4 + t);
-      lo[t] = w.x;
-      hi[t] = w.y;
-    }
-    const bool whole = 4 * t4 >= first && 4 * t4 + 4 <= end;
-    if (which == 0) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if (4 * t4 + t >= first && 4 * t4 + t < end)
-          *reinterpret_cast<u32x2_t*>(tile + Place<D>::k(4 * t4 + t, c)) = u32x2_t{lo[t], hi[t]};
-    } else if (whole) {
+  if constexpr (PAGES) {
+    const int end = p.token + p.n;
+    if (!is_k && t0 >= p.token && t0 + 4 <= end) {  // words of new tokens alone
+      uint32_t lo[4] = {w[0].x, w[1].x, w[2].x, w[3].x}, hi[4] = {w[0].y, w[1].y, w[2].y, w[3].y};
       transpose4(lo);
       transpose4(hi);
 #pragma unroll
       for (int m4 = 0; m4 < 4; ++m4) {
         const int o = m4 % 2 * 2;
-        *reinterpret_cast<u32x2_t*>(tile + Place<D>::v(t4, c, m4)) = m4 < 2 ? u32x2_t{lo[o], lo[o + 1]} : u32x2_t{hi[o], hi[o + 1]};
+        *reinterpret_cast<u32x2_t*>(tile + Place<D>::v(t0 >> 2, c, m4)) = m4 < 2 ? u32x2_t{lo[o], lo[o + 1]} : u32x2_t{hi[o], hi[o + 1]};
       }
-    } else {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if (4 * t4 + t >= first && 4 * t4 + t < end) put_v(4 * t4 + t, u32x2_t{lo[t], hi[t]});
+      return;
     }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (t0 + t >= p.token && t0 + t < end) put_token<D>(tile, is_k, c, t0 + t, w[t]);
+  } else {
+    put_token<D>(tile, is_k, c, t0, w[0]);
   }
 }
 
@@ -325,9 +322,11 @@ int slots_of(const QRowsArgs& a, int group) { return (int)q_row_slots(a.query_st
 hipError_t launch_q8_append(int dtype, int D, const QRowsArgs& a, hipStream_t st) {
   return by_type(dtype, D, a, [&](auto t, auto d) {
     constexpr int D = decltype(d)::value;
+    const bool pages = a.query_start_loc != nullptr;
     const int slots = slots_of(a, kPage);
-    const dim3 grid((slots + kRowsWaves - 1) / kRowsWaves, (a.H_kv * (D / 8) + 63) / 64, 2);
-    q8_append_kernel<decltype(t), D><<<grid, 64 * kRowsWaves, 0, st>>>(a, slots);
+    const dim3 grid((slots + kRowsWaves - 1) / kRowsWaves, (a.H_kv * (D / (pages ? 2 : 8)) + 63) / 64, 2);
+    const auto fn = pages ? &q8_append_kernel<decltype(t), D, true> : &q8_append_kernel<decltype(t), D, false>;
+    fn<<<grid, 64 * kRowsWaves, 0, st>>>(a, slots);
   });
 }
 
