@@ -110,14 +110,17 @@ constexpr int kQStreamThreads = 512;  // of a workgroup
 // tokens (5 units a wave of both) 18.8 us and 19.0, 4 of 8,192-32,768 (5) 17.3 and 19.8,
 // 128 of 512-2,048 (10) 28.5 and 27.1, 256 (20) 48.8 and 47.6, 512 of 1,024-4,096 (80)
 // 157 and 149; in fp32, 64 heads over 8: 64 of 256-2,048 (4) 23.4 and 24.6, 128 of
-// 512-2,048 (10) 38.0 and 38.0, 256 (20) 61.4 and 62.6.
+// 512-2,048 (10) 38.0 and 38.0, 256 (20) 61.4 and 62.6.  (8 bits, fp32: 4 of
+// 8,192-32,768 23.4 and 25.2.)
 constexpr int kQFewUnits = 8;
 // A workgroup takes an item whole, where there are no more items than CUs, if the longest
 // has at most so many units more than a workgroup's equal share: a wave's 3.5
 // units more are what the join through memory costs.  Whole and shared, 32 query heads
 // over 8 in bf16: 1 sequence of 200 tokens 8.4 us and 9.8, of 1,000 10.8 and 10.4, of
 // 2,000 13.9 and 11.6; 8 of 200-500 9.5 and 10.6, of 512-2,048 14.5 and 13.5; 32 of
-// 100-500 10.6 and 13.3, of 512-2,048 16.4 and 18.5.
+// 100-500 10.6 and 13.3, of 512-2,048 16.4 and 18.5.  (8 bits: 1 of 200 8.6 and 10.4; 32
+// of 100-500 11.3 and 13.8, of 512-2,048 19.1 and 21.7; with 14 or 56 units instead of 28
+// none is shorter.)
 constexpr int kQAloneUnits = 28;
 constexpr int kQCounterStride = 16;   // 128 bytes: atomics on one line follow each other 30 ns apart
 static_assert(kQStreamGroups <= kStreamMaxGrid, "a cut item's groups of records");

@@ -19,7 +19,7 @@
 //
 // What bounds it is issue: a unit takes some 190 vector instructions (96 of them V's
 // conversion) and 12 products, about 1,300 cycles, which two or three waves of a SIMD
-// overlap little.  So large calls share V's conversion (pa_q_chunk.h).  Where a call
+// overlap little.  So large calls share V's conversion (pa_q4_chunk.hip).  Where a call
 // has fewer items than the GPU holds waves, 2 or 4 waves of a workgroup share an item's
 // units and join their sums in LDS.
 #include "pa_q4_tile.h"

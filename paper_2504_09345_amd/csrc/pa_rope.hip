@@ -4,7 +4,12 @@
 // into a cosine and a sine (head dims of 128 have 64 pairs at most), which the lanes
 // exchange through LDS, so that each then holds those of the pairs that it rotates: V in a
 // row, the same in every head that it takes.  64 / (D / 2 / V) heads are read and written
-// at once, 16 bytes a lane and half where the pairs' number allows.
+// at once, 16 bytes a lane and half where the pairs' number allows.  A row's loads are under
+// way before its position is known.
+//
+// HBM bounds it: 8,074 rows of 40 heads of 128 in bf16, 165 MB, in 29 us (5.7 TB/s) where
+// the last-level cache holds a part of them, else in 40 (4.2, a large copy 4.7).  256 rows
+// take 3.2 us of the GPU, one 2.3: launch, and a chain of two loads.
 //
 // The angle is a product of 64 bits, in turns; whole turns and quarters are taken off
 // there, and what is left, at most an eighth of a turn, goes through the Taylor series of
