@@ -99,7 +99,7 @@ struct Plan {
 // and 11, of 64 on 1,500 14 and 18, 4 of 60 on 3,000 34 and 41, 16 of 8 on 2,000 25
 // and 31.  (8 bits: 6.4 and 8.5, 7.0 and 10.1, 12.0 and 16.6, 25 and 33, 17 and 24; four
 // times as many waves: one chunk of 1,400 rows 41 us instead of 36, of 700 18 and 15.)
-constexpr int kPartWaves = 3072;
+constexpr int kPartWaves = 256 * 12;
 // Parts beyond those, through the workspace and a second launch: as many as give the
 // GPU 2,048 waves of at least kLeastUnits units, at most 64.  (Parts of 4 units cost one
 // chunk of 64 rows on 1,500 tokens 17 us instead of 14; 8 or 16 are one as good as the
