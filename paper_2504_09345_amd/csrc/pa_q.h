@@ -42,8 +42,8 @@ hipError_t launch_q8_read(int dtype, int D, const QRowsArgs& a, hipStream_t st);
 
 constexpr int kQUnit = 2 * 16;  // tokens of a step: two pages
 
-// Chunk rows.  An item is a KV head's 16 columns (query row, head of the group) of one
-// sequence, or 128 in a workgroup that shares V, over a part of its keys.
+// Chunk rows.  An item is a KV head's 16 or 32 columns (query row, head of the group) of
+// one sequence, or 128 in a workgroup that shares V, over a part of its keys.
 struct QAttnArgs {
   const void* q;
   const uint8_t* k_pages;
@@ -61,7 +61,8 @@ struct QAttnArgs {
   int min_rows;  // sequences of fewer rows are the stream kernel's
   int max_q_len;
   int n_split, split_units;
-  int wave_parts;  // waves (1, 2 or 4) that share an item's units, where a wave has 16 columns
+  int blocks;      // column blocks of an item
+  int wave_parts;  // waves (1, 2 or 4) that share an item's units, where they do not share V
   const uint8_t* scales;
 };
 constexpr int kQWaves = 4;  // waves of a workgroup: each has an item of its own, 2 or 4 share one, or all share V
@@ -77,7 +78,7 @@ namespace q8 { struct Format; }
 template <class F> hipError_t launch_q_attn(int dtype, int D, const QAttnArgs& a, hipStream_t st, KernelEvents ev);
 template <class F> hipError_t launch_q_chunk(int D, const QAttnArgs& a, hipStream_t st, KernelEvents ev);  // bf16
 hipError_t launch_q_merge(int dtype, int D, const QAttnArgs& a, hipStream_t st);
-template <class F, typename T, int D> const void* q_attn_pick();
+template <class F, typename T, int D> const void* q_attn_pick(int blocks);
 
 // The persistent kernel of decode rows (sequences of one row): (sequence, KV head,
 // unit) triples of the whole batch in equal contiguous ranges, one per wave.

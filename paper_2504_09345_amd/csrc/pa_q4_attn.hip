@@ -27,10 +27,10 @@
 
 namespace pa {
 
-extern template const void* q_attn_pick<q4::Format, uint16_t, 64>();
-extern template const void* q_attn_pick<q4::Format, float, 128>();
-extern template const void* q_attn_pick<q4::Format, float, 64>();
-template const void* q_attn_pick<q4::Format, uint16_t, 128>();
+extern template const void* q_attn_pick<q4::Format, uint16_t, 64>(int);
+extern template const void* q_attn_pick<q4::Format, float, 128>(int);
+extern template const void* q_attn_pick<q4::Format, float, 64>(int);
+template const void* q_attn_pick<q4::Format, uint16_t, 128>(int);
 
 template hipError_t launch_q_attn<q4::Format>(int, int, const QAttnArgs&, hipStream_t, KernelEvents);
 

@@ -4,6 +4,6 @@
 
 namespace pa {
 
-template const void* q_attn_pick<q4::Format, uint16_t, 64>();
+template const void* q_attn_pick<q4::Format, uint16_t, 64>(int);
 
 }  // namespace pa

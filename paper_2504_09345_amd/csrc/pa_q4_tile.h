@@ -272,6 +272,7 @@ __device__ __forceinline__ void fold_pv_edge(State<T, D, NB, C>& st, Unit<D>& u,
 struct Format {
   template <int D> using Unit = q4::Unit<D>;
   template <typename T, int D> static constexpr bool kCodes = kCodeScores<T, D>;
+  template <typename T> static constexpr bool kWide = false;  // waves of 32 columns too
   static constexpr bool kSliced = false;  // K operands in bf16: a lane's dims in a row
   static constexpr bool kSums = false;  // a base moves by sums of weights
   static constexpr int tile_bytes(int D) { return q4_tile_bytes(D); }

@@ -4,6 +4,6 @@
 
 namespace pa {
 
-template const void* q_attn_pick<q8::Format, float, 64>();
+template const void* q_attn_pick<q8::Format, float, 64>(int);
 
 }  // namespace pa

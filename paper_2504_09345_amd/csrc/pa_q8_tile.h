@@ -191,6 +191,7 @@ __device__ __forceinline__ void fold_pv_edge(State<T, D, NB, C>& st, Unit<D>& u,
 struct Format {
   template <int D> using Unit = q8::Unit<D>;
   template <typename T, int D> static constexpr bool kCodes = false;
+  template <typename T> static constexpr bool kWide = sizeof(T) == 2;  // waves of 32 columns too
   static constexpr bool kSliced = true;  // K operands in bf16: 16 dims in a row of each 64
   static constexpr bool kSums = true;  // a base moves by sums of weights (not by the largest)
   static constexpr int tile_bytes(int D) { return q8_tile_bytes(D); }

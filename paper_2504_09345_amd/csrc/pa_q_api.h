@@ -100,6 +100,11 @@ struct Plan {
 // and 31.  (8 bits: 6.4 and 8.5, 7.0 and 10.1, 12.0 and 16.6, 25 and 33, 17 and 24; four
 // times as many waves: one chunk of 1,400 rows 41 us instead of 36, of 700 18 and 15.)
 constexpr int kPartWaves = 256 * 12;
+// Twice as many waves of 32 columns where each keeps so many units: the longest items end
+// sooner.  (Never, from 24 and from 8 on: one chunk of 1,400 rows 36, 36 and 40 us, of 1,700
+// 46, 43 and 43, of 2,000 52, 50 and 50, of 2,800 78, 83 and 82; at head_dim 64 of 1,700 34,
+// 26 and 26, of 2,600 54, 46 and 46; 8 of 230 on 500 26, 26 and 31.)
+constexpr int kLongPart = 24;
 // Parts beyond those, through the workspace and a second launch: as many as give the
 // GPU 2,048 waves of at least kLeastUnits units, at most 64.  (Parts of 4 units cost one
 // chunk of 64 rows on 1,500 tokens 17 us instead of 14; 8 or 16 are one as good as the
@@ -130,16 +135,23 @@ constexpr int64_t kRecordBytes = 64 << 20;
 // 20.6; one of 700 19.0 and 40.7 with any of them; 4 of 64 on 300 10.7, 10.7, 23.5 and
 // 23.6; 16 of 8 on 2,000 17.5 with all; and one of 700 beside a decode row of 32,768
 // tokens 62, where the two alone take 19 and 18.
-// The 8-bit kernels share for less (K's conversion to bf16 too is a workgroup's, but one
-// barrier a unit more), and the line is 104.  Alone and together, 32 query heads over 8,
-// head_dim 128: one chunk of 1,400 rows 37 and 48 us, of 2,000 55 and 64, of 2,600 81 and
-// 82, of 2,800 92 and 87, of 4,000 176 and 165; 4 of 1,000 62 and 65; 2 of 256 on 8,000
-// 104 and 116; 4 of 64 on 16,000 108 and 102; 2 of 120 on 20,000 128 and 110; with 8
-// query heads one of 4,000 69 and 94, with 64 one of 1,400 53 and 49; at head_dim 64 one
-// of 2,000 39 and 49, of 2,600 57 and 64, of 4,000 113 and 98.
 template <class F> constexpr int64_t kAloneUnits = 0;
 template <> inline constexpr int64_t kAloneUnits<q4::Format> = 48 * 2048;
-template <> inline constexpr int64_t kAloneUnits<q8::Format> = 104 * 2048;
+// The 8-bit cache's large calls have waves of 32 columns, each alone: K's and V's
+// conversions are paid once for both halves, with no barrier.  (Workgroups of 128 columns
+// that share the conversions' results through LDS were slower throughout: 8 chunks of
+// 2,048 rows 635 us and 583, at head_dim 64 386 and 353; one of 4,000 167 and 144.)  The line
+// is 15 units for each of 2,048 waves.  Of 16 columns and of 32, 32 query heads over 8,
+// head_dim 128: one chunk of 700 rows 15.6 and 20.5 us, of 1,000 24.9 and 22.3, of 1,400
+// 36.9 and 36.3, of 2,000 56 and 50, of 2,600 80 and 74; 8 of 300 24.4 and 25.1, of 200 on
+// 400 24.8 and 23.4, of 230 on 500 32 and 28; 4 of 128 on 1,000 19.3 and 18.8, of 56 on
+// 3,000 25.7 and 29.3, on 5,000 39 and 37; 2 of 256 on 8,000 104 and 77; at head_dim 64
+// one of 700 10.5 and 11.0, of 1,000 18.3 and 15.5, of 2,000 39 and 31; with 64 query heads
+// one of 700 21.5 and 24.4, of 1,400 53 and 50, with 8 of 2,000 22 and 20, with 48 (12 of 16
+// columns used, or 30 of 32) 8 of 512 on 1,000 153 and 105.
+template <> inline constexpr int64_t kAloneUnits<q8::Format> = 15 * 2048;
+template <class F> constexpr bool kWideWaves = false;
+template <> inline constexpr bool kWideWaves<q8::Format> = true;
 constexpr int kAloneColumns = 32;
 // Units of a launch of the stream kernel, at most (its counts are 32-bit).
 constexpr int64_t kStreamUnits = 1 << 30;
@@ -184,12 +196,15 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
     if (chunk_rows < one) chunk_rows = one;
     const int64_t alone_units = (chunk_rows / q_positions(1, s) + 1) * d->num_kv_heads *
                                 ((d->max_context_len - d->max_q_len / 2) / kQUnit + 1);
-    p->shared = d->dtype == PA_BF16 && d->max_q_len * (int64_t)s > kAloneColumns && alone_units > kAloneUnits<F>;
-    p->blocks = p->shared ? kQChunkBlocks : 1;
+    const bool large = d->dtype == PA_BF16 && d->max_q_len * (int64_t)s > kAloneColumns && alone_units > kAloneUnits<F>;
+    p->shared = large && !kWideWaves<F>;
+    p->blocks = p->shared ? kQChunkBlocks : large ? 2 : 1;
     const int64_t slots = p->rows / q_positions(p->blocks, s) + 1 + (int64_t)d->num_seqs;
     const int64_t items = (chunk_rows / q_positions(p->blocks, s) + 1) * d->num_kv_heads;
     if (!p->shared)
-      while (p->wave_parts < kQWaves && items * p->wave_parts * 2 <= kPartWaves && units >= p->wave_parts * 2) p->wave_parts *= 2;
+      while (p->wave_parts < kQWaves && units >= p->wave_parts * 2 &&
+             items * p->wave_parts * 2 <= (p->blocks == 2 && units >= p->wave_parts * 2 * kLongPart ? 2 : 1) * kPartWaves)
+        p->wave_parts *= 2;
     const int waves = p->shared ? kQWaves : p->wave_parts;  // of an item
     int64_t split = kWavesWanted / (items * waves);
     if (split > units / (kLeastUnits * p->wave_parts)) split = units / (kLeastUnits * p->wave_parts);
@@ -271,6 +286,7 @@ int attend(const void* q, const QCache& c, bool scaled, float scale, void* out, 
     a.num_pages = d->num_pages;
     a.max_context_len = no_scales ? -1 : d->max_context_len;
     a.n_slots = p.n_slots;
+    a.blocks = p.blocks;
     a.min_rows = p.min_rows;
     a.max_q_len = d->max_q_len;
     a.n_split = p.n_split;
@@ -279,9 +295,10 @@ int attend(const void* q, const QCache& c, bool scaled, float scale, void* out, 
     KernelEvents ev;
     ev.start = begin;
     ev.stop = p.stream ? nullptr : end;
-    if ((p.shared ? launch_q_chunk<F>(d->head_dim, a, stream, ev)
-                  : launch_q_attn<F>(d->dtype, d->head_dim, a, stream, ev)) != hipSuccess)
-      return PA_EHIP;
+    hipError_t e;
+    if constexpr (kWideWaves<F>) e = launch_q_attn<F>(d->dtype, d->head_dim, a, stream, ev);
+    else e = p.shared ? launch_q_chunk<F>(d->head_dim, a, stream, ev) : launch_q_attn<F>(d->dtype, d->head_dim, a, stream, ev);
+    if (e != hipSuccess) return PA_EHIP;
     if (p.n_split > 1 && launch_q_merge(d->dtype, d->head_dim, a, stream) != hipSuccess) return PA_EHIP;
   }
   if (p.stream) {

@@ -82,18 +82,18 @@ __device__ __forceinline__ void q_finish(const QAttnArgs& a, const q::State<T, D
 }
 
 // What a wave hands to the one that joins an item's parts.
-template <int D>
+template <int D, int NB>
 struct QPart {
-  q::f32x4_t o[D / 16][64];
-  float m[64], l[64];
+  q::f32x4_t o[NB][D / 16][64];
+  float m[NB][64], l[NB][64];
 };
 
-// (Three waves a SIMD: in fp32 at head_dim 128, whose registers would hold two, four
-// chunks of 1,024 rows take 130 us instead of 144.)
-template <class F, typename T, int D>
-__global__ __launch_bounds__(64 * kQWaves) __attribute__((amdgpu_waves_per_eu(3)))
+// NB: column blocks of the wave.  (Three waves a SIMD: in fp32 at head_dim 128, whose
+// registers would hold two, four chunks of 1,024 rows take 130 us instead of 144.  Two
+// blocks there leave room for two.)
+template <class F, typename T, int D, int NB>
+__global__ __launch_bounds__(64 * kQWaves) __attribute__((amdgpu_waves_per_eu(NB == 2 && D == 128 ? 2 : 3)))
 void q_attn_kernel(QAttnArgs a) {
-  constexpr int NB = 1;  // column blocks of the wave
   const int S = a.s;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -220,29 +220,35 @@ void q_attn_kernel(QAttnArgs a) {
     }
   }
   if (sharers > 1) {  // join the parts that have units: the first one's wave takes the others'
-    __shared__ QPart<D> parts[kQWaves];
+    __shared__ QPart<D, NB> parts[kQWaves];
     if (part > 0 && u0 < u1) {
 #pragma unroll
-      for (int j = 0; j < D / 16; ++j) parts[wave].o[j][lane] = st.acc[0][j];
-      parts[wave].m[lane] = st.m[0];
-      parts[wave].l[lane] = st.l[0];
+      for (int c = 0; c < NB; ++c) {
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) parts[wave].o[c][j][lane] = st.acc[c][j];
+        parts[wave].m[c][lane] = st.m[c];
+        parts[wave].l[c][lane] = st.l[c];
+      }
     }
     __syncthreads();
     if (part > 0 || u0 >= u1) return;
     const int n_parts = (s1 - s0 + per - 1) / per;
-    float M = st.m[0];
-    for (int i = 1; i < n_parts; ++i) M = fmaxf(M, parts[wave + i].m[lane]);
-    const float c0 = fast_exp2(st.m[0] - M);
-    st.m[0] = M;
-    st.l[0] *= c0;
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j) st.acc[0][j] *= c0;
-    for (int i = 1; i < n_parts; ++i) {
-      const auto& other = parts[wave + i];
-      const float ci = fast_exp2(other.m[lane] - M);
-      st.l[0] = fmaf(other.l[lane], ci, st.l[0]);
+    for (int c = 0; c < NB; ++c) {
+      float M = st.m[c];
+      for (int i = 1; i < n_parts; ++i) M = fmaxf(M, parts[wave + i].m[c][lane]);
+      const float c0 = fast_exp2(st.m[c] - M);
+      st.m[c] = M;
+      st.l[c] *= c0;
 #pragma unroll
-      for (int j = 0; j < D / 16; ++j) st.acc[0][j] = other.o[j][lane] * ci + st.acc[0][j];
+      for (int j = 0; j < D / 16; ++j) st.acc[c][j] *= c0;
+      for (int i = 1; i < n_parts; ++i) {
+        const auto& other = parts[wave + i];
+        const float ci = fast_exp2(other.m[c][lane] - M);
+        st.l[c] = fmaf(other.l[c][lane], ci, st.l[c]);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) st.acc[c][j] = other.o[c][j][lane] * ci + st.acc[c][j];
+      }
     }
   }
   q_finish<T, D, NB>(a, st, at, split, lane);
@@ -285,22 +291,24 @@ __global__ __launch_bounds__(256) void q_merge_kernel(QAttnArgs a) {
 }
 
 template <class F, typename T, int D>
-const void* q_attn_pick() {
-  return reinterpret_cast<const void*>(&q_attn_kernel<F, T, D>);
+const void* q_attn_pick(int blocks) {
+  if constexpr (F::template kWide<T>)
+    if (blocks == 2) return reinterpret_cast<const void*>(&q_attn_kernel<F, T, D, 2>);
+  return blocks == 1 ? reinterpret_cast<const void*>(&q_attn_kernel<F, T, D, 1>) : nullptr;
 }
 
 template <class F>
-const void* q_attn_fn(int dtype, int D) {
-  if (dtype == 0 && D == 128) return q_attn_pick<F, uint16_t, 128>();
-  if (dtype == 0 && D == 64) return q_attn_pick<F, uint16_t, 64>();
-  if (dtype == 1 && D == 128) return q_attn_pick<F, float, 128>();
-  if (dtype == 1 && D == 64) return q_attn_pick<F, float, 64>();
+const void* q_attn_fn(int dtype, int D, int blocks) {
+  if (dtype == 0 && D == 128) return q_attn_pick<F, uint16_t, 128>(blocks);
+  if (dtype == 0 && D == 64) return q_attn_pick<F, uint16_t, 64>(blocks);
+  if (dtype == 1 && D == 128) return q_attn_pick<F, float, 128>(blocks);
+  if (dtype == 1 && D == 64) return q_attn_pick<F, float, 64>(blocks);
   return nullptr;
 }
 
 template <class F>
 hipError_t launch_q_attn(int dtype, int D, const QAttnArgs& a, hipStream_t st, KernelEvents ev) {
-  const void* fn = q_attn_fn<F>(dtype, D);
+  const void* fn = q_attn_fn<F>(dtype, D, a.blocks);
   if (fn == nullptr) return hipErrorInvalidValue;
   const int64_t parts = (int64_t)a.H_kv * a.n_split;
   const int items = kQWaves / a.wave_parts;  // of a workgroup

@@ -14,8 +14,8 @@ from parity_util import announce
 
 pytestmark = pytest.mark.gpu
 
-FAR = 1 << 22  # a declared context for which a call's chunks share V's operands (bf16)
-KINDS = ["decode", "chunks", "shared"]
+FAR = 1 << 22  # a declared context for which a call's waves have 32 columns (bf16)
+KINDS = ["decode", "chunks", "wide"]
 DECODE = [1, 15, 16, 17, 31, 32, 33, 0, 64, 200, 333, 48]
 
 
@@ -28,7 +28,7 @@ def _lens(kind, ctx):
 def _attend(b, kind, d=None):
     """The call's output on the host, its chunks by the kernel that `kind` names."""
     d = b.upload() if d is None else d
-    if kind != "shared":
+    if kind != "wide":
         return b.attend(d).float().cpu()
     b.widen(d, FAR)
     return b.attend(d, b.dims(d, max_context_len=FAR)).float().cpu()
@@ -64,11 +64,11 @@ def test_varlen(dtype, D, H_q, H_kv, lens):
     [(130, 130), (150, 65)],
     [(300, 40)],
 ], ids=["mixed", "chunks", "one"])
-def test_shared(D, H_q, H_kv, lens):
-    """Workgroups that share V, chosen by a declared context far above the real ones."""
-    announce(f"q8 shared D={D} heads={H_q}/{H_kv} {lens}")
+def test_wide(D, H_q, H_kv, lens):
+    """Waves of 32 columns, chosen by a declared context far above the real ones."""
+    announce(f"q8 wide D={D} heads={H_q}/{H_kv} {lens}")
     b = Batch(lens, H_q, H_kv, D, seed=len(lens))
-    check(_attend(b, "shared"), b.expected(), max(c for c, _ in lens), "bf16")
+    check(_attend(b, "wide"), b.expected(), max(c for c, _ in lens), "bf16")
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -78,8 +78,8 @@ def test_shared(D, H_q, H_kv, lens):
     [(5000, 100), (4700, 120), (33, 2)],          # items in parts
     [(2600, 2600)],
 ], ids=["items", "parts", "prompt"])
-def test_shared_at_size(D, H_q, H_kv, lens):
-    announce(f"q8 shared at size D={D} heads={H_q}/{H_kv} {lens[0]}")
+def test_wide_at_size(D, H_q, H_kv, lens):
+    announce(f"q8 wide at size D={D} heads={H_q}/{H_kv} {lens[0]}")
     b = Batch(lens, H_q, H_kv, D, seed=9)
     check(b.attend(b.upload()).float().cpu(), b.expected(), max(c for c, _ in lens), "bf16")
 
@@ -197,7 +197,7 @@ def test_many_sequences_share_their_pages(B, ctx):
 
 # --- NaN and what the contract does not allow ----------------------------------
 
-@pytest.mark.parametrize("kind", ["chunks", "shared"])
+@pytest.mark.parametrize("kind", ["chunks", "wide"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("D", [64, 128])
 def test_nan_reaches_the_rows_that_see_it(kind, dtype, D):
@@ -222,7 +222,7 @@ def test_rows_outside_the_contract(kind, D):
     ref = b.expected()
     d = b.upload()
     ctx, bt = b.ctx.copy(), b.bt.copy()
-    ctx[0] = 5000 if kind != "shared" else 2 * FAR  # above max_context_len
+    ctx[0] = 5000 if kind != "wide" else 2 * FAR  # above max_context_len
     bt[2, 1] = b.num_pages + 7    # outside the pool
     bt[3, 0] = -5
     d["cl"], d["bt"] = b.cuda(ctx), b.cuda(bt)
@@ -236,7 +236,7 @@ def test_rows_outside_the_contract(kind, D):
         ctx[1] = 2
         d["cl"] = b.cuda(ctx)
         ref[0][q0[1]:q0[2]] = np.nan
-    if kind == "shared":
+    if kind == "wide":
         check(_attend(b, kind, d), ref, 64, "bf16")
     else:
         check(b.attend(d, b.dims(d, max_context_len=64)).float().cpu(), ref, 64, "bf16")
@@ -270,9 +270,9 @@ def test_no_pages(kind):
     announce(f"q8 attention, a pool without pages, {kind}")
     b = Batch([(20, 3), (0, 0), (40, 1), (4000, 30)], 40, 40, 64, varlen=kind != "decode")
     d = b.upload()
-    if kind == "shared":
+    if kind == "wide":
         b.widen(d, FAR)
-    dims = b.dims(d, max_context_len=FAR if kind == "shared" else None)
+    dims = b.dims(d, max_context_len=FAR if kind == "wide" else None)
     dims.num_pages = 0
     d["k"], d["v"], d["scales"] = d["k"][:1], d["v"][:1], d["scales"][:1]
     out = b.attend(d, dims, torch.zeros_like(d["q"]))
@@ -461,7 +461,7 @@ def test_scores_of_every_code_and_scale(kind, dtype, D):
     q = torch.zeros(D, rows, H_q, D, dtype=kind_t, device="cuda")
     q[torch.arange(D), :, :, torch.arange(D)] = 2.0 ** -6
     q = q.view(D * rows, H_q, D)
-    far = FAR if kind == "shared" else 32
+    far = FAR if kind == "wide" else 32
     bt = torch.full((D, far // 16), -1, dtype=torch.int32, device="cuda")
     bt[:, :pages] = torch.arange(pages, device="cuda")
     cl = torch.full((D,), 16 + extra, dtype=torch.int32, device="cuda")
