@@ -148,7 +148,8 @@ template <> inline constexpr int64_t kAloneUnits<q4::Format> = 48 * 2048;
 // 3,000 25.7 and 29.3, on 5,000 39 and 37; 2 of 256 on 8,000 104 and 77; at head_dim 64
 // one of 700 10.5 and 11.0, of 1,000 18.3 and 15.5, of 2,000 39 and 31; with 64 query heads
 // one of 700 21.5 and 24.4, of 1,400 53 and 50, with 8 of 2,000 22 and 20, with 48 (12 of 16
-// columns used, or 30 of 32) 8 of 512 on 1,000 153 and 105.
+// columns used, or 30 of 32) 8 of 512 on 1,000 153 and 105.  (fp32 keeps to 16: a third part
+// of each query leaves no room; one of 2,000 95 and 100 us, at head_dim 64 64 and 62.)
 template <> inline constexpr int64_t kAloneUnits<q8::Format> = 15 * 2048;
 template <class F> constexpr bool kWideWaves = false;
 template <> inline constexpr bool kWideWaves<q8::Format> = true;
