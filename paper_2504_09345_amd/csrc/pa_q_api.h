@@ -108,11 +108,13 @@ constexpr int kLongPart = 24;
 // Parts beyond those, through the workspace and a second launch: as many as give the
 // GPU 2,048 waves of at least kLeastUnits units, at most 64.  (Parts of 4 units cost one
 // chunk of 64 rows on 1,500 tokens 17 us instead of 14; 8 or 16 are one as good as the
-// other.  Twice the waves: one chunk of 700 rows 31 us instead of 19.  8 bits: units of
-// at least 4, 8 or 16 are one as good as the other but for 10.0 and 11.3 us, 8 and 4, of
-// one chunk of 64 rows on 1,500 tokens at head_dim 64; with twice the waves one chunk of
-// 2,000 rows 94 us instead of 65, two of 120 on 20,000 121 instead of 110.)
-constexpr int kWavesWanted = 2048, kLeastUnits = 8, kMaxSplit = 64;
+// other.  Twice the waves: one chunk of 700 rows 31 us instead of 19.)  (8 bits: units of
+// at least 4, 8 or 16 are one as good as the other but for 11.3, 10.0 and 10.0 us of one
+// chunk of 64 rows on 1,500 tokens at head_dim 64.)  Of 32 columns, which two fit a SIMD of,
+// 2,560, so that a division's rest leaves no half of the GPU idle: with 1,024, 2,048, 2,560
+// and 4,096 4 chunks of 64 rows on 16,000 tokens 98, 98, 83 and 88 us, one on 30,000 68, 55,
+// 50 and 62, 2 of 120 on 20,000 118, 98, 98 and 106, 4 of 56 on 5,000 37, 35, 35 and 42.
+constexpr int kWavesWanted = 2048, kWideWavesWanted = 2560, kLeastUnits = 8, kMaxSplit = 64;
 // Bytes of all parts' records, which the host can only reckon for every row of the call:
 // it does not know which are of chunks, nor does the grid.  With bounds of 32, 64, 128 and
 // 4,096 MiB, 32 query heads over 8: two rows on 65,536 tokens beside 512 decode rows of
@@ -207,7 +209,7 @@ int plan(const pa_dims_t* d, bool varlen, Plan* p) {
              items * p->wave_parts * 2 <= (p->blocks == 2 && units >= p->wave_parts * 2 * kLongPart ? 2 : 1) * kPartWaves)
         p->wave_parts *= 2;
     const int waves = p->shared ? kQWaves : p->wave_parts;  // of an item
-    int64_t split = kWavesWanted / (items * waves);
+    int64_t split = (p->blocks == 2 ? kWideWavesWanted : kWavesWanted) / (items * waves);
     if (split > units / (kLeastUnits * p->wave_parts)) split = units / (kLeastUnits * p->wave_parts);
     if (split > kMaxSplit) split = kMaxSplit;
     const int64_t record = (int64_t)p->rows * d->num_q_heads * (d->head_dim + 2) * (int64_t)sizeof(float);  // of one part
