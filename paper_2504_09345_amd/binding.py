@@ -634,8 +634,12 @@ def _rows_rope(t, kind, rows, heads, D, device):
     strides = t.stride()
     if strides[2] != 1 or (heads > 1 and strides[1] != D):
         raise ValueError(f"a tensor of strides {strides}, whose rows' heads do not lie one after the other")
-    # (a lone row's stride is any number: none is used)
-    return t.data_ptr() or None, strides[0] if rows > 1 else 0
+    if rows <= 1:  # (a lone row's stride is any number: none is used)
+        return t.data_ptr() or None, 0
+    # (0, as broadcast rows have it, means packed rows to the library)
+    if strides[0] < heads * D:
+        raise ValueError(f"rows {strides[0]} elements apart, of {heads * D} each")
+    return t.data_ptr() or None, strides[0]
 
 
 def pa_rope(q, k, context_lens, inv_freq, q_out, k_out, dims: PaDims, interleaved=False, factor=1.0, positions=None, query_start_loc=None,

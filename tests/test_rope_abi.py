@@ -96,6 +96,44 @@ def test_binding(monkeypatch):
 
 
 @host_only
+def test_binding_refuses_rows_that_share_memory(monkeypatch):
+    """Rows 0 elements apart (a broadcast tensor), which the library would take as packed
+    ones, or fewer than a row's: 50 rows of 256 elements and fewer stored ones.  A lone row
+    lies on no other, whatever its tensor's stride."""
+    taken = []
+
+    class Lib:
+        def pa_rope(self, q, k, positions, cl, qsl, q_out, k_out, rope, d, stream):
+            taken.append((rope._obj.q_stride, rope._obj.k_stride, rope._obj.q_out_stride, rope._obj.k_out_stride))
+            return pb.PA_OK
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    monkeypatch.setattr(pb, "load", lambda: Lib())
+    w = torch.ones(64, dtype=torch.float64)
+
+    def call(x, out, key, rows=50):
+        d = dims(num_seqs=rows, num_q_heads=2, num_kv_heads=2)
+        q, k, q_out, k_out = (None, x, None, out) if key else (x, None, out, None)
+        for positions, cl in ((torch.zeros(rows, dtype=torch.int32), None), (None, torch.zeros(rows, dtype=torch.int32))):
+            pb.pa_rope(q, k, cl, w, q_out, k_out, d, positions=positions, stream=S)
+
+    rows = torch.zeros(50, 2, 128, dtype=torch.bfloat16)
+    joint = torch.zeros(50, 3, 128, dtype=torch.bfloat16)[:, :2]
+    flat = torch.zeros(50 * 256, dtype=torch.bfloat16)
+    for key in (False, True):
+        call(rows, joint, key)
+        assert taken[-2:] == [(0, 0, 0, 384) if key else (0, 0, 384, 0)] * 2
+        for bad in (rows[:1].expand(50, 2, 128), flat.as_strided((50, 2, 128), (128, 128, 1)), flat.as_strided((50, 2, 128), (248, 128, 1))):
+            with pytest.raises(ValueError, match="rows"):
+                call(bad, rows, key)
+            with pytest.raises(ValueError, match="rows"):
+                call(rows, bad, key)
+        call(rows[:1].expand(50, 2, 128), rows, key, rows=1)  # (the first of them alone)
+        assert taken[-1] == (0, 0, 0, 0)
+
+
+@host_only
 def test_rows_with_positions(monkeypatch):
     """With positions and no number of rows the rows are num_seqs, though
     query_start_loc is given too: arrays of fewer are refused."""
