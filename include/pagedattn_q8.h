@@ -41,9 +41,11 @@
  * max_pages_per_seq and max_context_len describe the cache as in pagedattn.h;
  * dtype (PA_BF16 or PA_FP32) is the type of the dense arrays: k_new, v_new,
  * k_out, v_out, q and out.  pages_per_split must be 0.  Arrays that a call writes
- * overlap none that it reads.  Calls of more work than a launch can have threads
- * (appends and reads from 2^26 single rows or 2^28 rows of chunks on) are refused:
- * PA_ENOTSUP.
+ * overlap none that it reads.  Calls of more work than a launch can have threads are
+ * refused, PA_ENOTSUP: appends and reads from 2^26 - 4 groups of rows on, where a single
+ * row of a decode call is a group, of a call with query_start_loc 16 appended rows or 4
+ * read ones are, and each sequence counts two more (so somewhat below 2^30 appended or
+ * 2^28 read rows).
  */
 #ifndef PAGEDATTN_Q8_H
 #define PAGEDATTN_Q8_H

@@ -136,6 +136,21 @@ def test_binding_raises():
         pb.paged_attn_q8(P, P, P, P, P, P, 0.1, P, dims(), stream=S)
 
 
+@host_only
+@pytest.mark.parametrize("name,group", [("pa_kv_append_q8", 16), ("pa_kv_read_q8", 4)])
+@pytest.mark.parametrize("seqs", [1, 1000])
+def test_most_rows_of_a_call(name, group, seqs):
+    """The header's bound: 2^26 - 4 groups of rows, 16 rows of chunks that are appended and
+    4 that are read, single rows one by one, and two more for each sequence of a call with
+    chunks.  (Without arrays: PA_EINVAL where the size is not refused.)"""
+    none, most = dict(ptrs=(None,) * 4, pools=(None,) * 3), (1 << 26) - 4
+    rows = (most - 2 * seqs) * group
+    for n, code in ((rows, pb.PA_ENOTSUP), (rows - 1, pb.PA_EINVAL), (1 << 30, pb.PA_ENOTSUP), (rows // 2, pb.PA_EINVAL)):
+        assert rows_call(name, dims(num_seqs=seqs, num_q_rows=n), qsl=P, **none) == code, n
+    assert rows_call(name, dims(num_seqs=most), **none) == pb.PA_ENOTSUP
+    assert rows_call(name, dims(num_seqs=most - 1), **none) == pb.PA_EINVAL
+
+
 def test_calls_without_rows_touch_nothing():
     assert pb.pa_workspace_size_q8(dims(num_seqs=0)) == 0
     if not torch.cuda.is_available():
