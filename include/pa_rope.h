@@ -10,7 +10,8 @@
  *
  * inv_freq is in 64 bits, and so are the angles until whole turns are taken off them: a
  * frequency or a product rounded to 32 bits is off by 2^-24 of itself, at position 2^20
- * 1/16 of a radian.  The angles' error is 2^-52 of a; cosine and sine are in 32 bits, the
+ * 1/16 of a radian.  The angles' error is at most 1.3 2^-52 of a (three roundings to 2^-53,
+ * that of 1 / 2 pi among them); cosine and sine are in 32 bits, the
  * products and sums too, and a result is rounded once to the type.
  */
 #ifndef PA_ROPE_H

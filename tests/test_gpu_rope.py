@@ -1,4 +1,7 @@
 """Rotary positions on the GPU against the formula in float64."""
+import random
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -187,6 +190,28 @@ def test_far_positions(p):
     out = torch.zeros_like(q)
     pb.pa_rope(q, None, None, w.cuda(), out, None, pb.make_dims_rope(q, None, 0), positions=i32([p]))
     check(out, q, [p], w, 1.0, False)
+
+
+def test_angles_of_the_documented_error():
+    """Angles so large that their own error shows, against whole turns taken off in rational
+    numbers.  The position times the frequency and that times 1 / 2 pi are rounded to
+    2^-53 each, and so is 1 / 2 pi (0.56 of it): 2.56 2^-53, the header's 1.3 2^-52 of the angle.
+    Besides, as in check: 7 half steps of 32 bits."""
+    announce("rope, the error of large angles")
+    turn = 2 * Fraction(31415926535897932384626433832795028841971693993751, 10 ** 49)
+    rng = random.Random(7)
+    pos = [35717, 960004123, 9922563, 1382648186] + [rng.randrange(1, 1 << 31) for _ in range(28)]
+    w = [0.05750390125848659, 1.1535627085714872, 1.7005355340814332, 1.5563251066324473] + [rng.uniform(1, 2) for _ in range(60)]
+    q = torch.zeros(len(pos), 1, 128, device="cuda")
+    q[..., :64] = 1.0  # (so that the outputs are the cosines and the sines)
+    for size in (2.0 ** -20, 1.0, 2.0 ** 10):
+        out, scaled = torch.zeros_like(q), [x * size for x in w]
+        pb.pa_rope(q, None, None, torch.tensor(scaled, dtype=torch.float64, device="cuda"), out, None, pb.make_dims_rope(q, None, 0), positions=i32(pos))
+        angle = [[p * Fraction(x) for x in scaled] for p in pos]
+        part = np.array([[float(a % turn) for a in row] for row in angle])
+        tol = 1.3 * 2.0 ** -52 * np.array([[float(a) for a in row] for row in angle]) + 7 * 2.0 ** -24
+        got = out[:, 0].double().cpu().numpy()
+        assert (np.abs(got[:, :64] - np.cos(part)) <= tol).all() and (np.abs(got[:, 64:] - np.sin(part)) <= tol).all(), size
 
 
 def test_a_rotation_and_back():
