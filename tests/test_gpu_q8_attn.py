@@ -438,6 +438,60 @@ def test_queries_that_are_not_finite(kind, dtype, D, value):
     check(_attend(b, kind), ref, 90, dtype)
 
 
+# --- waves of 32 columns in small calls ----------------------------------------
+
+def _wide_only(b):
+    """Of a batch whose far declared bound does give its waves 32 columns: bf16, and more
+    columns in the longest chunk than one such wave has."""
+    assert b.dtype == "bf16" and max(b.n_rows) * b.H_q // b.H_kv > 32
+    return b
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H_q,H_kv", [(40, 40), (12, 2)])
+def test_wide_without_pages(D, H_q, H_kv):
+    """A pool of none: rows of a context are NaN (every entry lies outside)."""
+    announce(f"q8 wide D={D} heads={H_q}/{H_kv}, a pool without pages")
+    b = _wide_only(Batch([(20, 3), (0, 0), (40, 1), (4000, 40)], H_q, H_kv, D))
+    d = b.upload()
+    b.widen(d, FAR)
+    dims = b.dims(d, max_context_len=FAR)
+    dims.num_pages = 0
+    d["k"], d["v"], d["scales"] = d["k"][:1], d["v"][:1], d["scales"][:1]
+    assert torch.isnan(b.attend(d, dims, torch.zeros_like(d["q"]))).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows", [9, 60])
+def test_wide_queries_of_any_size(D, rows):
+    """Queries of zeros, small and large ones, and of very different sizes in one row."""
+    announce(f"q8 wide D={D}, {rows} queries of any size")
+    b = _wide_only(Batch([(100, rows)] * 8, 8, 2, D, seed=2))
+    q = b.q.reshape(8, rows, 8, D)
+    for i, f in enumerate([0.0, 2.0 ** -130, 2.0 ** -60, 2.0 ** -10, 1.0, 30.0, 1.0, 1.0]):
+        q[i] *= f
+    q[6] *= np.exp2(-np.arange(D) / 4.0).astype(np.float32)
+    q[7, ..., ::2] *= 2.0 ** -20
+    b.q = b.round(q.reshape(-1, 8, D))
+    check(_attend(b, "wide"), b.expected(), 100, "bf16")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_wide_rows_of_no_sequence_and_too_many(D):
+    """Rows behind the last sequence stay, those of a chunk longer than max_q_len are NaN."""
+    announce(f"q8 wide D={D}, rows of no sequence and of too long a chunk")
+    b = _wide_only(Batch([(64, 40), (70, 41), (40, 1), (9, 2)], 4, 2, D))
+    d = b.upload()
+    b.widen(d, FAR)
+    d["q"] = torch.cat([d["q"], d["q"][:3]])
+    dims = b.dims(d, max_context_len=FAR, num_q_rows=b.T + 3, max_q_len=40)
+    out = b.attend(d, dims, torch.full_like(d["q"], 7.0))
+    assert (out[b.T:] == 7.0).all()
+    ref = b.expected()
+    ref[0][40:81] = np.nan
+    check(out[:b.T].float().cpu(), ref, 70, "bf16")
+
+
 # --- every code and scale byte -----------------------------------------------------
 
 @pytest.mark.parametrize("kind", KINDS)
