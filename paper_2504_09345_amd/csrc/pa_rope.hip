@@ -105,6 +105,25 @@ __device__ __forceinline__ typename Piece<T, V>::type rounded(const float (&x)[V
   }
 }
 
+// a's words that turned(word) says, the others as they are in x: dims that are not
+// rotated keep their bits (a conversion to fp32 and back would make a signalling NaN a
+// quiet one).
+template <typename P, typename F>
+__device__ __forceinline__ P turned_words(const P& a, const P& x, F turned) {
+  if constexpr (sizeof(P) == 2) {
+    return turned(0) ? a : x;
+  } else {
+    struct Words {
+      uint32_t w[sizeof(P) / 4];
+    };
+    Words v = __builtin_bit_cast(Words, a);
+    const Words o = __builtin_bit_cast(Words, x);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(P) / 4; ++i) v.w[i] = turned(i) ? v.w[i] : o.w[i];
+    return __builtin_bit_cast(P, v);
+  }
+}
+
 // PAIRED: pair i is dims 2 i and 2 i + 1.  Otherwise V divides the number of pairs.
 template <typename T, int D, int V, bool PAIRED>
 __global__ __launch_bounds__(64) void rope_kernel(RopeArgs a) {
@@ -169,27 +188,30 @@ __global__ __launch_bounds__(64) void rope_kernel(RopeArgs a) {
         const int h = h0 + b * h_step;
         if (h >= H) break;
         float u[V], w[V];
+        P o[2];
         if constexpr (PAIRED) {  // pieces of pairs first .. in a row: elements 2 i, 2 i + 1
 #pragma unroll
           for (int i = 0; i < V; ++i) {
             const float f = element<T, V>(x[b][2 * i / V], 2 * i % V), g = element<T, V>(x[b][(2 * i + 1) / V], (2 * i + 1) % V);
-            const bool turned = bad || first + i < a.n;
-            const float f1 = turned ? fmaf(f, c[i], -g * s[i]) : f, g1 = turned ? fmaf(g, c[i], f * s[i]) : g;
-            (2 * i / V == 0 ? u : w)[2 * i % V] = f1;
-            ((2 * i + 1) / V == 0 ? u : w)[(2 * i + 1) % V] = g1;
+            (2 * i / V == 0 ? u : w)[2 * i % V] = fmaf(f, c[i], -g * s[i]);
+            ((2 * i + 1) / V == 0 ? u : w)[(2 * i + 1) % V] = fmaf(g, c[i], f * s[i]);
           }
+          constexpr int kWord = 4 / sizeof(T);  // elements
+          o[0] = turned_words(rounded<T, V>(u), x[b][0], [&](int j) { return bad || first + j * kWord / 2 < a.n; });
+          o[1] = turned_words(rounded<T, V>(w), x[b][1], [&](int j) { return bad || first + (V + j * kWord) / 2 < a.n; });
         } else {
-          const bool turned = bad || apart;
 #pragma unroll
           for (int i = 0; i < V; ++i) {
             const float f = element<T, V>(x[b][0], i), g = element<T, V>(x[b][1], i);
-            u[i] = turned ? fmaf(f, c[i], -g * s[i]) : f;
-            w[i] = turned ? fmaf(g, c[i], f * s[i]) : g;
+            u[i] = fmaf(f, c[i], -g * s[i]);
+            w[i] = fmaf(g, c[i], f * s[i]);
           }
+          o[0] = turned_words(rounded<T, V>(u), x[b][0], [&](int) { return bad || apart; });
+          o[1] = turned_words(rounded<T, V>(w), x[b][1], [&](int) { return bad || apart; });
         }
         T* p = out(h);
-        *reinterpret_cast<P*>(p + at0) = rounded<T, V>(u);
-        *reinterpret_cast<P*>(p + at1) = rounded<T, V>(w);
+        *reinterpret_cast<P*>(p + at0) = o[0];
+        *reinterpret_cast<P*>(p + at1) = o[1];
       }
     }
   }

@@ -180,6 +180,29 @@ def test_values_that_are_not_finite_stay_in_their_pairs():
         assert bad == sorted([4, other]) and not out[2, 1].isnan().any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rot", [2, 6, 8, 20, 48])
+def test_dims_behind_rot_dim_keep_their_bits(dtype, D, interleaved, rot):
+    """Of every value that 16 bits have: zeros' signs, the smallest, NaN of either kind."""
+    announce(f"rope {dtype} D={D} rot={rot} interleaved={interleaved}, bits of the other dims")
+    bits = torch.arange(1 << 16, dtype=torch.int32, device="cuda")
+    if dtype == "bf16":
+        x = bits.to(torch.int16).view(torch.bfloat16)
+    else:
+        x = ((bits << 16) | (bits * 40503 & 0xffff)).view(torch.float32)
+    x = x.view(-1, 4, D)
+    x = torch.cat([x, x.flip(-1)])  # (each value in two places)
+    out = torch.zeros_like(x)
+    w, _ = pb.pa_rope_frequencies(rot)
+    same = torch.int16 if dtype == "bf16" else torch.int32
+    for to in (out, x.clone()):
+        src = x if to is out else to
+        pb.pa_rope(src, None, None, w.cuda(), to, None, pb.make_dims_rope(x, None, 0), interleaved, positions=i32(range(len(x))))
+        assert torch.equal(to[..., rot:].contiguous().view(same), x[..., rot:].contiguous().view(same))
+
+
 @pytest.mark.parametrize("p", [0, 1, 2 ** 20 - 1, 2 ** 24 + 1, 2 ** 31 - 1, -(2 ** 31), -12345])
 def test_far_positions(p):
     """Frequencies whose angles fall on every eighth of a turn, and arbitrary ones."""
