@@ -4,8 +4,8 @@
 // A unit is 8 KiB of K and V at head_dim 128, two 16-byte loads a lane and page of each,
 // which become operands by conversions alone: K as bf16, V as fp16 where its scales allow.
 // A page's two scale bytes are loaded beside K, a unit ahead too, and stay in the caches.
-// With twice the 4-bit cache's bytes a unit and four fifths of its vector instructions (158
-// and 202, set-up included: no query in parts, one scale a page) HBM is the bound sooner:
+// With twice the 4-bit cache's bytes a unit and four fifths of its vector and matrix
+// instructions (158 and 202, set-up included: no query in parts, one scale a page) HBM is the bound sooner:
 // 256 sequences of 512-2,048 tokens, 32 query heads over 8, 683 MB in 110 us, 6.2 TB/s,
 // where loads of this pattern alone reach 6.4 (the 4-bit cache's 361 MB take 69); 512 of
 // 256-4,096 beside chunks 2.28 GB in 357, 6.4.

@@ -97,7 +97,7 @@ struct Plan {
 // while the GPU still holds all of them at once (256 CUs of 12 waves).  Shared and
 // alone, 32 query heads over 8: a chunk of 16 rows on 200 tokens 7 and 10 us, of 300 9
 // and 11, of 64 on 1,500 14 and 18, 4 of 60 on 3,000 34 and 41, 16 of 8 on 2,000 25
-// and 31.  (8 bits: 6.4 and 8.5, 7.0 and 10.1, 12.0 and 16.6, 25 and 33, 17 and 24; four
+// and 31.  (8 bits: 6.4 and 8.5, 7.0 and 10.1, 12.0 and 16.6, 25 and 33 with waves of 16 columns, 17 and 24; four
 // times as many waves: one chunk of 1,400 rows 41 us instead of 36, of 700 18 and 15.)
 constexpr int kPartWaves = 256 * 12;
 // Twice as many waves of 32 columns where each keeps so many units: the longest items end
@@ -136,18 +136,22 @@ constexpr int64_t kRecordBytes = 64 << 20;
 // they are and as 4,096, 32,768 and 131,072: one of 16 rows on 200 8.4, 11.0, 11.2 and
 // 20.6; one of 700 19.0 and 40.7 with any of them; 4 of 64 on 300 10.7, 10.7, 23.5 and
 // 23.6; 16 of 8 on 2,000 17.5 with all; and one of 700 beside a decode row of 32,768
-// tokens 62, where the two alone take 19 and 18.
+// tokens 62, where the two alone take 19 and 18.  (8 bits: 6.3, 9.1, 11.3 and 11.4; 14.7 and
+// 19.5 with any; 9.2 and 19.0 with any; 17.7 with all; one of 2,000 48 with all; 4 of 60 on
+// 3,000 38, 44, 57 and 57.)
 template <class F> constexpr int64_t kAloneUnits = 0;
 template <> inline constexpr int64_t kAloneUnits<q4::Format> = 48 * 2048;
 // The 8-bit cache's large calls have waves of 32 columns, each alone: K's and V's
 // conversions are paid once for both halves, with no barrier.  (Workgroups of 128 columns
 // that share the conversions' results through LDS were slower throughout: 8 chunks of
-// 2,048 rows 635 us and 583, at head_dim 64 386 and 353; one of 4,000 167 and 144.)  The line
+// 2,048 rows on 0, 290, .. 2,030 tokens 635 us and 583, at head_dim 64 386 and 353; one of
+// 4,000 167 and 144.)  The line
 // is 15 units for each of 2,048 waves.  Of 16 columns and of 32, 32 query heads over 8,
 // head_dim 128: one chunk of 700 rows 15.6 and 20.5 us, of 1,000 24.9 and 22.3, of 1,400
 // 36.9 and 36.3, of 2,000 56 and 50, of 2,600 80 and 74; 8 of 300 24.4 and 25.1, of 200 on
 // 400 24.8 and 23.4, of 230 on 500 32 and 28; 4 of 128 on 1,000 19.3 and 18.8, of 56 on
-// 3,000 25.7 and 29.3, on 5,000 39 and 37; 2 of 256 on 8,000 104 and 77; at head_dim 64
+// 3,000 25.7 and 29.3, on 5,000 39 and 37; but of 60, of whose items the last are half
+// empty, on 3,000 25.3 and 39, on 5,000 39 and 50; 2 of 256 on 8,000 104 and 77; at head_dim 64
 // one of 700 10.5 and 11.0, of 1,000 18.3 and 15.5, of 2,000 39 and 31; with 64 query heads
 // one of 700 21.5 and 24.4, of 1,400 53 and 50, with 8 of 2,000 22 and 20, with 48 (12 of 16
 // columns used, or 30 of 32) 8 of 512 on 1,000 153 and 105.  (fp32 keeps to 16: a third part
